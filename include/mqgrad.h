@@ -338,6 +338,101 @@ mqg_status mqg_server_step_segments(const uint32_t* const* codes, const float* c
                                     float* acc_out, void* cuda_stream);
 
 /*
+ * ---- Around the codec: the global gradient norm, clipping, and the table of a model over tokens ----
+ *
+ * What a trainer needs right before and after the calls above: a worker clips its gradient before Quantize (Algorithm 1,
+ * WorkerIterate), the server clips the sum before it applies it, and a model over tokens pulls rows of the shared
+ * parameters and pushes their gradient.  The paper leaves both to the system it runs in.
+ *
+ * A list of gradient tensors is three HOST arrays of `count` entries, read during the call only: device pointers, element
+ * counts, types.  A tensor needs its type's own alignment only (4 or 2 bytes); 16 bytes are faster.  An empty tensor's
+ * pointer is not looked at, and count may be 0.  Tensors that are written must not overlap each other or anything else.
+ *
+ *     N = sqrt(sum over all elements of all tensors of x^2)
+ *     c = 1 where N <= max_norm, else max_norm / N
+ *
+ * N is right for every finite gradient (sums in 64 bits beyond a thread's first 32 elements; no square overflows or
+ * vanishes) and rounded to fp32 once (infinity above its range), after c was formed; the order of the sums is fixed, so N
+ * and c are reproducible bit for bit on one device model.  A NaN among the elements makes N and c NaN; an infinity makes N
+ * infinite and c zero (where max_norm is infinite too: c = 1).  max_norm may be 0 or infinite, not negative or NaN
+ * (MQG_ERR_INVALID).
+ *   result     [out] 2 floats: N, c.  They stay on the device: no call here waits for them.
+ *   workspace  [scratch] DEVICE memory of at least mqg_norm_workspace_floats(count) floats, 8-byte aligned.  Contents on
+ *              entry do not matter and are undefined on return; calls that may run concurrently (graphs captured apart
+ *              among them) need separate workspaces.
+ * Errors: MQG_ERR_INVALID (null pointers, unknown types, workspace too small), MQG_ERR_ALIGN.
+ */
+size_t mqg_norm_workspace_floats(int count);
+
+/* Measures N and c; the tensors stay as they are. */
+mqg_status mqg_grad_norm(const void* const* grads, const uint64_t* sizes, const mqg_dtype* dtypes, int count, float max_norm,
+                         float* result, float* workspace, size_t workspace_floats, void* cuda_stream);
+
+/*
+ * Measures N and c, and scales every tensor in place: x <- c * x, rounded once to the tensor's type.  Where c is 1 nothing
+ * is written.
+ */
+mqg_status mqg_clip_grad_norm(void* const* grads, const uint64_t* sizes, const mqg_dtype* dtypes, int count, float max_norm,
+                              float* result, float* workspace, size_t workspace_floats, void* cuda_stream);
+
+/*
+ * Measures N and c, and writes c * x of all tensors one after another into `flat` (sum of sizes elements of flat_dtype, each
+ * rounded once): the flat gradient that mqg_quantize takes.  The tensors stay as they are; with max_norm infinite it is
+ * their concatenation.
+ *   flat  [out] needs its type's own alignment (4 or 2 bytes)
+ */
+mqg_status mqg_clip_flatten(const void* const* grads, const uint64_t* sizes, const mqg_dtype* dtypes, int count,
+                            float max_norm, void* flat, mqg_dtype flat_dtype, float* result, float* workspace,
+                            size_t workspace_floats, void* cuda_stream);
+
+/*
+ * x <- *factor * x for every tensor of a list, in place, rounded once to its type; where *factor is 1 nothing is written.
+ * For a factor that comes from elsewhere (the norm of gradients that are spread over several devices), and for clipping a
+ * gradient that is encoded already: scaling its `scales` (of mqg_quantize and the L2-norm variant) or `ranges` scales what
+ * it decodes to.
+ *   factor  [in] one float in DEVICE memory, e.g. result + 1 of the calls above
+ */
+mqg_status mqg_scale_grads(void* const* grads, const uint64_t* sizes, const mqg_dtype* dtypes, int count, const float* factor,
+                           void* cuda_stream);
+
+/*
+ * mqg_apply of the clipped sum: params[i] = fma(-lr, fl(*factor * acc[i]), params[i]), exactly mqg_scale_grads on acc
+ * followed by mqg_apply, in one pass that leaves acc as it is.  params and acc as in mqg_apply (16-byte aligned).
+ */
+mqg_status mqg_apply_clipped(float* params, const float* acc, float lr, const float* factor, uint64_t n, void* cuda_stream);
+
+typedef enum { MQG_I32 = 0, MQG_I64 = 1 } mqg_index;
+
+/*
+ * Rows of a table for a batch of token ids: out[t] = scale * table[ids[t]], one rounding to fp32 for the product and, for a
+ * bf16 `out`, one to bf16.  An id outside 0..rows-1 marks an empty place (of a padded batch): its row of `out` is zero.
+ *   table  [in] rows x dim elements, row after row; a slice of the flat parameters, for instance
+ *   ids    [in] `tokens` integers;  out [out] tokens x dim elements
+ * All buffers need their types' own alignment only; rows whose bytes are a multiple of 16 on 16-byte boundaries are fastest.
+ * Errors: MQG_ERR_INVALID (null pointers, unknown types; rows or tokens above 2^31 - 1, dim above 2^22), MQG_ERR_ALIGN.
+ */
+mqg_status mqg_embedding(const void* table, mqg_dtype table_dtype, uint64_t rows, uint64_t dim, const void* ids,
+                         mqg_index ids_type, uint64_t tokens, float scale, void* out, mqg_dtype out_dtype,
+                         void* cuda_stream);
+
+/*
+ * The gradient of that table from the gradient of `out`:
+ *     grad[v] = scale * sum over t with ids[t] = v of dout[t]            (0 for a row without tokens), or with add_into_grad
+ *     grad[v] = grad[v] + scale * that sum                               (rows without tokens are not touched)
+ * The tokens are sorted by id and a row's summed in ascending order of t in fp32, from runs of 32 sorted tokens; the scale
+ * and the addition are one rounding each, and a bf16 `grad` is rounded once at the end.  No atomics: the result is
+ * reproducible bit for bit.  What stands in `dout` at empty places is not used, NaN included.
+ *   grad       [out] rows x dim elements; with add_into_grad [in/out]
+ *   workspace  [scratch] DEVICE memory of at least mqg_embedding_workspace_floats(tokens, rows, dim) floats, 16-byte
+ *              aligned; otherwise as for the norm above
+ * Other arguments and errors as mqg_embedding.
+ */
+size_t mqg_embedding_workspace_floats(uint64_t tokens, uint64_t rows, uint64_t dim);
+mqg_status mqg_embedding_grad(const void* dout, mqg_dtype dout_dtype, const void* ids, mqg_index ids_type, uint64_t tokens,
+                              uint64_t rows, uint64_t dim, float scale, void* grad, mqg_dtype grad_dtype, int add_into_grad,
+                              float* workspace, size_t workspace_floats, void* cuda_stream);
+
+/*
  * Kernels stage data through shared memory with asynchronous bulk copies and wait for them on
  * barriers with a bounded number of polls; a wait that runs out makes the kernel record it in a
  * per-device counter, abandon its work and return (its outputs are then incomplete) instead of

@@ -13,6 +13,9 @@ Function names and argument order follow the C ABI:
   mqg_l2_workspace_floats, mqg_quantize_segments_l2_static, mqg_quantize_1bit_ef, mqg_code_words, mqg_num_buckets,
   mqg_wire_bytes, mqg_last_error, mqg_version, mqg_device_timeouts, mqg_check_timeouts,
   mqg_test_wait_override.
+Around the codec (the global gradient norm, clipping, the table of a model over tokens):
+  mqg_norm_workspace_floats, mqg_grad_norm, mqg_clip_grad_norm, mqg_clip_flatten, mqg_scale_grads, mqg_apply_clipped,
+  mqg_embedding, mqg_embedding_workspace_floats, mqg_embedding_grad.
 """
 from __future__ import annotations
 
@@ -31,6 +34,7 @@ MQG_ERR_TOO_MANY_WORKERS = -4
 MQG_ERR_CUDA = -5
 MQG_ERR_TIMEOUT = -6
 MQG_F32, MQG_BF16 = 0, 1
+MQG_I32, MQG_I64 = 0, 1
 MQG_MAX_WORKERS = 32
 
 
@@ -74,6 +78,15 @@ def _load() -> C.CDLL:
         "mqg_quantize_segments_l2": (i32, [vp, i32, vp, vp, i32, u64, vp, vp, i32, u32, u32, u64, vp,
                                            C.c_size_t, vp]),
         "mqg_quantize_segments_l2_static": (i32, [vp, i32, vp, vp, i32, u64, vp, vp, i32, u32, u32, u64, vp]),
+        "mqg_norm_workspace_floats": (C.c_size_t, [i32]),
+        "mqg_grad_norm": (i32, [vp, vp, vp, i32, f32, vp, vp, C.c_size_t, vp]),
+        "mqg_clip_grad_norm": (i32, [vp, vp, vp, i32, f32, vp, vp, C.c_size_t, vp]),
+        "mqg_clip_flatten": (i32, [vp, vp, vp, i32, f32, vp, i32, vp, vp, C.c_size_t, vp]),
+        "mqg_scale_grads": (i32, [vp, vp, vp, i32, vp, vp]),
+        "mqg_apply_clipped": (i32, [vp, vp, f32, vp, u64, vp]),
+        "mqg_embedding": (i32, [vp, i32, u64, u64, vp, i32, u64, f32, vp, i32, vp]),
+        "mqg_embedding_workspace_floats": (C.c_size_t, [u64, u64, u64]),
+        "mqg_embedding_grad": (i32, [vp, i32, vp, i32, u64, u64, u64, f32, vp, i32, i32, vp, C.c_size_t, vp]),
     }
     for name, (res, args) in sigs.items():
         fn = getattr(lib, name)
@@ -115,6 +128,10 @@ _NATIVE = frozenset((
     "mqg_quantize_minmax", "mqg_quantize_workers_minmax", "mqg_dequant_accumulate_minmax", "mqg_server_step_minmax",
     "mqg_quantize_l2", "mqg_quantize_workers_l2", "mqg_quantize_segments_l2", "mqg_quantize_segments_l2_static",
     "mqg_quantize_1bit_ef"))
+# those around the codec
+_NATIVE_AROUND = frozenset((
+    "mqg_grad_norm", "mqg_clip_grad_norm", "mqg_clip_flatten", "mqg_scale_grads", "mqg_apply_clipped", "mqg_embedding",
+    "mqg_embedding_grad"))
 
 
 def _native(name):
@@ -131,7 +148,7 @@ def _native(name):
         native = importlib.util.module_from_spec(spec)
         spec.loader.exec_module(native)
         native._set_error_class(MqgError)
-        for fn in _NATIVE:
+        for fn in _NATIVE | _NATIVE_AROUND:
             getattr(native, fn).__module__ = __name__      # found here when a pickle names it
             globals()[fn] = getattr(native, fn)
     return globals()[name]
@@ -139,7 +156,7 @@ def _native(name):
 
 def __getattr__(name):
     """Loads the native functions when the first of them is asked for, not at import (as _LazyLibrary)."""
-    if name not in _NATIVE:
+    if name not in _NATIVE and name not in _NATIVE_AROUND:
         raise AttributeError("module %r has no attribute %r" % (__name__, name))
     try:
         return _native(name)
@@ -151,7 +168,7 @@ def __getattr__(name):
 
 
 def __dir__():
-    return sorted({*globals(), *_NATIVE})
+    return sorted({*globals(), *_NATIVE, *_NATIVE_AROUND})
 
 
 def mqg_code_words(n: int, bits: int) -> int:
@@ -197,6 +214,14 @@ def mqg_test_wait_override(poll_limit: int = 0, arm_only: bool = False) -> None:
 
 def mqg_l2_workspace_floats(seg_off) -> int:
     return int(_lib.mqg_l2_workspace_floats(len(seg_off) - 1, _u64_table(seg_off)))
+
+
+def mqg_norm_workspace_floats(count: int) -> int:
+    return int(_lib.mqg_norm_workspace_floats(count))
+
+
+def mqg_embedding_workspace_floats(tokens: int, rows: int, dim: int) -> int:
+    return int(_lib.mqg_embedding_workspace_floats(tokens, rows, dim))
 
 
 MQG_L2_STATIC_WORKSPACE_FLOATS = 65536

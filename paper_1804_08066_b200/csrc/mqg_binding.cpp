@@ -8,9 +8,11 @@
 // device waited for the host.
 #include <Python.h>
 
+#include <c10/cuda/CUDAGuard.h>
 #include <c10/cuda/CUDAStream.h>
 #include <torch/csrc/autograd/python_variable.h>
 
+#include <algorithm>
 #include <cstring>
 #include <vector>
 
@@ -533,6 +535,226 @@ MQG_ENTRY(mqg_server_step_segments, 1, 9, "codes", "scales", "W", "bits", "seg_o
                                                            seg.data, code.data, params, lr, acc, s); });
 }
 
+// ---- around the codec: the global norm, clipping, and the table of a model over tokens ----
+// These calls check types and sizes of every tensor, and run on the tensors' device, on its current stream.
+
+struct Operands {
+    int device = -1;
+
+    // A contiguous CUDA tensor of at least `least` elements; all of a call's are on one device.
+    const at::Tensor& tensor(PyObject* o, const char* what, uint64_t least, Py_ssize_t index = -1)
+    {
+        device_ptr(o, what, index);
+        const at::Tensor& t = THPVariable_Unpack(o);
+        if ((uint64_t)t.numel() < least) {
+            PyErr_Format(PyExc_ValueError, "%s holds %lld elements, %llu are needed", what, (long long)t.numel(),
+                         (unsigned long long)least);
+            throw PythonError();
+        }
+        const int on = t.get_device();
+        if (device >= 0 && on != device) {
+            PyErr_Format(PyExc_ValueError, "%s is on cuda:%d, the tensors before it on cuda:%d", what, on, device);
+            throw PythonError();
+        }
+        device = on;
+        return t;
+    }
+    float* floats(PyObject* o, const char* what, uint64_t least, uint64_t* count = nullptr)
+    {
+        const at::Tensor& t = tensor(o, what, least);
+        if (t.scalar_type() != at::kFloat) {
+            PyErr_Format(PyExc_TypeError, "%s must be float32, got %s", what, c10::toString(t.scalar_type()));
+            throw PythonError();
+        }
+        if (count) *count = (uint64_t)t.numel();
+        return static_cast<float*>(t.data_ptr());
+    }
+    void* values(PyObject* o, const char* what, uint64_t least, mqg_dtype* dtype, Py_ssize_t index = -1)
+    {
+        const at::Tensor& t = tensor(o, what, least, index);
+        const at::ScalarType s = t.scalar_type();
+        if (s != at::kFloat && s != at::kBFloat16) {
+            PyErr_Format(PyExc_TypeError, "%s must be float32 or bfloat16, got %s", what, c10::toString(s));
+            throw PythonError();
+        }
+        *dtype = s == at::kFloat ? MQG_F32 : MQG_BF16;
+        return t.data_ptr();
+    }
+    const void* ids(PyObject* o, uint64_t least, mqg_index* type)
+    {
+        const at::Tensor& t = tensor(o, "ids", least);
+        const at::ScalarType s = t.scalar_type();
+        if (s != at::kInt && s != at::kLong) {
+            PyErr_Format(PyExc_TypeError, "ids must be int32 or int64, got %s", c10::toString(s));
+            throw PythonError();
+        }
+        *type = s == at::kLong ? MQG_I64 : MQG_I32;
+        return t.data_ptr();
+    }
+};
+
+template <typename Fn> PyObject* enqueue_on(const Operands& on, Fn&& fn)
+{
+    const c10::cuda::CUDAGuard guard((c10::DeviceIndex)on.device);
+    void* s = c10::cuda::getCurrentCUDAStream((c10::DeviceIndex)on.device).stream();
+    return enqueue([&] { return fn(s); });
+}
+
+// The product of two sizes, with what does not fit 64 bits as the largest value (which no tensor holds).
+uint64_t area(uint64_t a, uint64_t b)
+{
+    uint64_t r;
+    return __builtin_mul_overflow(a, b, &r) ? ~0ull : r;
+}
+
+// A list of gradient tensors of any sizes.
+struct TensorTable {
+    std::vector<void*> ptr;
+    std::vector<uint64_t> size;
+    std::vector<mqg_dtype> dtype;
+    uint64_t total = 0;
+
+    void read(PyObject* o, Operands& on)
+    {
+        const Reference items = {PySequence_Tuple(o)};
+        if (!items.object) throw PythonError();
+        const Py_ssize_t n = PyTuple_GET_SIZE(items.object);
+        ptr.resize((size_t)n), size.resize((size_t)n), dtype.resize((size_t)n);
+        for (Py_ssize_t i = 0; i < n; ++i) {
+            PyObject* item = PyTuple_GET_ITEM(items.object, i);
+            ptr[i] = on.values(item, "grads", 0, &dtype[i], i);
+            size[i] = (uint64_t)THPVariable_Unpack(item).numel();
+            total += size[i];
+        }
+    }
+    uint64_t bytes(size_t i) const { return size[i] * (dtype[i] == MQG_F32 ? 4 : 2); }
+    // Tensors that are written: no two of them share memory.
+    void check_apart() const
+    {
+        bool ascending = true;
+        for (size_t i = 1; i < ptr.size() && ascending; ++i)
+            ascending = static_cast<char*>(ptr[i - 1]) + bytes(i - 1) <= ptr[i];
+        if (ascending) return;
+        std::vector<size_t> order;
+        for (size_t i = 0; i < ptr.size(); ++i)
+            if (size[i] != 0) order.push_back(i);
+        std::sort(order.begin(), order.end(), [&](size_t a, size_t b) { return ptr[a] < ptr[b]; });
+        for (size_t k = 1; k < order.size(); ++k)
+            if (static_cast<char*>(ptr[order[k - 1]]) + bytes(order[k - 1]) > ptr[order[k]]) {
+                PyErr_Format(PyExc_ValueError, "grads[%zu] and grads[%zu] share memory", std::min(order[k - 1], order[k]),
+                             std::max(order[k - 1], order[k]));
+                throw PythonError();
+            }
+    }
+    int count() const { return (int)ptr.size(); }
+};
+
+struct NormArgs {
+    float max_norm, *result, *workspace;
+    uint64_t floats;
+    void read(PyObject* limit, PyObject* res, PyObject* work, Operands& on)
+    {
+        max_norm = to_float(limit);
+        result = on.floats(res, "result", 2);
+        workspace = on.floats(work, "workspace", 0, &floats);
+    }
+};
+
+MQG_ENTRY(mqg_grad_norm, 0, 4, "grads", "max_norm", "result", "workspace")
+{
+    Operands on;
+    TensorTable g;
+    NormArgs a;
+    a.read(v[1], v[2], v[3], on);
+    g.read(v[0], on);
+    return enqueue_on(on, [&](void* s) { return ::mqg_grad_norm(g.ptr.data(), g.size.data(), g.dtype.data(), g.count(), a.max_norm,
+                                                                a.result, a.workspace, a.floats, s); });
+}
+
+MQG_ENTRY(mqg_clip_grad_norm, 0, 4, "grads", "max_norm", "result", "workspace")
+{
+    Operands on;
+    TensorTable g;
+    NormArgs a;
+    a.read(v[1], v[2], v[3], on);
+    g.read(v[0], on);
+    g.check_apart();
+    return enqueue_on(on, [&](void* s) { return ::mqg_clip_grad_norm(g.ptr.data(), g.size.data(), g.dtype.data(), g.count(),
+                                                                     a.max_norm, a.result, a.workspace, a.floats, s); });
+}
+
+MQG_ENTRY(mqg_clip_flatten, 0, 5, "grads", "max_norm", "flat", "result", "workspace")
+{
+    Operands on;
+    TensorTable g;
+    NormArgs a;
+    mqg_dtype type;
+    a.read(v[1], v[3], v[4], on);
+    g.read(v[0], on);
+    char* flat = static_cast<char*>(on.values(v[2], "flat", g.total, &type));
+    const char* end = flat + g.total * (type == MQG_F32 ? 4 : 2);
+    for (size_t i = 0; i < g.ptr.size(); ++i)
+        if (g.ptr[i] < end && static_cast<char*>(g.ptr[i]) + g.bytes(i) > flat) {
+            PyErr_Format(PyExc_ValueError, "grads[%zu] and flat share memory", i);
+            return nullptr;
+        }
+    return enqueue_on(on, [&](void* s) { return ::mqg_clip_flatten(g.ptr.data(), g.size.data(), g.dtype.data(), g.count(),
+                                                                   a.max_norm, flat, type, a.result, a.workspace, a.floats, s); });
+}
+
+MQG_ENTRY(mqg_scale_grads, 0, 2, "grads", "factor")
+{
+    Operands on;
+    TensorTable g;
+    const float* factor = on.floats(v[1], "factor", 1);
+    g.read(v[0], on);
+    g.check_apart();
+    return enqueue_on(on, [&](void* s) { return ::mqg_scale_grads(g.ptr.data(), g.size.data(), g.dtype.data(), g.count(),
+                                                                  factor, s); });
+}
+
+MQG_ENTRY(mqg_apply_clipped, 0, 5, "params", "acc", "lr", "factor", "n")
+{
+    Operands on;
+    const uint64_t n = to_u64(v[4]);
+    const float lr = to_float(v[2]);
+    float* params = on.floats(v[0], "params", n);
+    const float* acc = on.floats(v[1], "acc", n);
+    const float* factor = on.floats(v[3], "factor", 1);
+    return enqueue_on(on, [&](void* s) { return ::mqg_apply_clipped(params, acc, lr, factor, n, s); });
+}
+
+MQG_ENTRY(mqg_embedding, 0, 7, "table", "rows", "dim", "ids", "tokens", "scale", "out")
+{
+    Operands on;
+    const uint64_t rows = to_u64(v[1]), dim = to_u64(v[2]), tokens = to_u64(v[4]);
+    const float scale = to_float(v[5]);
+    mqg_dtype table_type, out_type;
+    mqg_index ids_type;
+    const void* table = on.values(v[0], "table", area(rows, dim), &table_type);
+    const void* ids = on.ids(v[3], tokens, &ids_type);
+    void* out = on.values(v[6], "out", area(tokens, dim), &out_type);
+    return enqueue_on(on, [&](void* s) { return ::mqg_embedding(table, table_type, rows, dim, ids, ids_type, tokens, scale, out,
+                                                                out_type, s); });
+}
+
+MQG_ENTRY(mqg_embedding_grad, 1, 9, "dout", "ids", "tokens", "rows", "dim", "scale", "grad", "workspace", "add_into_grad")
+{
+    Operands on;
+    const uint64_t tokens = to_u64(v[2]), rows = to_u64(v[3]), dim = to_u64(v[4]);
+    const float scale = to_float(v[5]);
+    const int add = to_bool(v[8]) ? 1 : 0;
+    mqg_dtype dout_type, grad_type;
+    mqg_index ids_type;
+    uint64_t floats;
+    const void* dout = on.values(v[0], "dout", area(tokens, dim), &dout_type);
+    const void* ids = on.ids(v[1], tokens, &ids_type);
+    void* grad = on.values(v[6], "grad", area(rows, dim), &grad_type);
+    float* workspace = on.floats(v[7], "workspace", 0, &floats);
+    return enqueue_on(on, [&](void* s) { return ::mqg_embedding_grad(dout, dout_type, ids, ids_type, tokens, rows, dim, scale,
+                                                                     grad, grad_type, add, workspace, floats, s); });
+}
+
 PyObject* set_error_class(PyObject*, PyObject* cls)
 {
     Py_XSETREF(g_error_class, Py_NewRef(cls));
@@ -587,6 +809,22 @@ PyMethodDef kMethods[] = {
                "mqg_quantize_segments_l2 for callers that cannot supply a workspace: the partial sums use an array\n"
                "inside the library (at most MQG_L2_STATIC_WORKSPACE_FLOATS of them); calls that may overlap on the\n"
                "device must be ordered by the caller."),
+    MQG_METHOD(mqg_grad_norm, "(grads, max_norm, result, workspace)",
+               "The norm of a list of gradient tensors and the factor that clips it to max_norm: `result` (float32, 2).\n"
+               "`workspace`: float32 CUDA tensor of at least mqg_norm_workspace_floats(len(grads)) elements."),
+    MQG_METHOD(mqg_clip_grad_norm, "(grads, max_norm, result, workspace)",
+               "mqg_grad_norm, and the tensors scaled by the factor in place."),
+    MQG_METHOD(mqg_clip_flatten, "(grads, max_norm, flat, result, workspace)",
+               "mqg_grad_norm, and the tensors, times the factor, one after another in `flat` (float32 or bfloat16)."),
+    MQG_METHOD(mqg_scale_grads, "(grads, factor)",
+               "Scales a list of tensors in place by a float32 that is on the device."),
+    MQG_METHOD(mqg_apply_clipped, "(params, acc, lr, factor, n)", "params <- params - lr * (factor * acc)."),
+    MQG_METHOD(mqg_embedding, "(table, rows, dim, ids, tokens, scale, out)",
+               "out[t] = scale * table[ids[t]]; zeros where an id is outside 0..rows-1."),
+    MQG_METHOD(mqg_embedding_grad,
+               "(dout, ids, tokens, rows, dim, scale, grad, workspace, add_into_grad=False)",
+               "The gradient of mqg_embedding's table, written to `grad` or added to it; `workspace`: float32 CUDA tensor\n"
+               "of at least mqg_embedding_workspace_floats(tokens, rows, dim) elements."),
     {"_set_error_class", set_error_class, METH_O, nullptr},
     {nullptr, nullptr, 0, nullptr},
 };
@@ -597,7 +835,8 @@ Signature* const kSignatures[] = {
     &sig_mqg_dequant_accumulate_minmax, &sig_mqg_server_step_minmax, &sig_mqg_server_requantize,
     &sig_mqg_quantize_segments, &sig_mqg_quantize_segments_workers, &sig_mqg_server_step_segments,
     &sig_mqg_quantize_1bit_ef, &sig_mqg_quantize_l2, &sig_mqg_quantize_segments_l2,
-    &sig_mqg_quantize_segments_l2_static,
+    &sig_mqg_quantize_segments_l2_static, &sig_mqg_grad_norm, &sig_mqg_clip_grad_norm, &sig_mqg_clip_flatten,
+    &sig_mqg_scale_grads, &sig_mqg_apply_clipped, &sig_mqg_embedding, &sig_mqg_embedding_grad,
 };
 
 PyModuleDef kModule = {PyModuleDef_HEAD_INIT, "_binding", "Native entry points of libmqgrad.", -1, kMethods,

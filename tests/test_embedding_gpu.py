@@ -1,0 +1,233 @@
+"""Rows of a table looked up for token ids, and the gradient of the table from sorted tokens.
+
+The lookup has one rounding of the product (and one to bf16): compared bit for bit.  The gradient of a row with k tokens is a
+sum in fp32 over runs of at most 32 sorted tokens, whose sums are added up in turn: no term goes through more than 32 + (k / 32
++ 1) additions, or k in all where that is less, each off by at most 2^-24 of what it adds to, which is at most the sum of the
+magnitudes.  Then the product with the scale and, with add_into_grad, the sum with what was there (2^-24 each), and the
+rounding to the output's type (half a step)."""
+import math
+
+import pytest
+import torch
+
+import paper_1804_08066_b200 as mqg
+from tests.buffers import Buffer, same_bits
+
+pytestmark = pytest.mark.gpu
+F32, BF16, I32, I64 = torch.float32, torch.bfloat16, torch.int32, torch.int64
+
+
+def _ids(tokens, rows, kind, dtype, seed=0):
+    gen = torch.Generator().manual_seed(seed)
+    if kind == "uniform":
+        ids = torch.randint(0, max(1, rows), (tokens,), generator=gen)
+    elif kind == "zipf":
+        ids = (rows ** torch.rand(tokens, generator=gen, dtype=torch.float64)).long() - 1
+    elif kind == "same":
+        ids = torch.full((tokens,), rows - 1)
+    elif kind == "empty":
+        ids = torch.full((tokens,), -1)
+    elif kind == "ascending":
+        ids = torch.arange(tokens) * rows // max(1, tokens)
+    else:                                    # outside the table on both sides
+        ids = torch.randint(-rows - 1, 2 * rows + 1, (tokens,), generator=gen)
+        ids[::7] = 2 ** 31 - 1 if dtype == I32 else 2 ** 32 + 1
+        ids[3::7] = -2 ** 31 if dtype == I32 else -2 ** 63
+    return ids.to(dtype)
+
+
+def _held(ids, rows):
+    return (ids.long() >= 0) & (ids.long() < rows)
+
+
+def _lookup(table, ids, scale, out):
+    held = _held(ids, table.shape[0])
+    y = torch.zeros(ids.numel(), table.shape[1])
+    y[held] = table[ids.long()[held]].float() * torch.tensor(scale, dtype=F32)
+    return y.to(out)
+
+
+SHAPES = [(1, 1, 1), (5, 7, 3), (3, 8, 1), (1000, 64, 500), (17, 257, 100), (300, 1024, 33), (9, 4100, 65), (50_021, 36, 4099)]
+
+
+@pytest.mark.parametrize("types", [(F32, F32), (F32, BF16), (BF16, F32), (BF16, BF16)])
+@pytest.mark.parametrize("shift", [0, 1, 4])
+@pytest.mark.parametrize("shape", SHAPES)
+def test_lookup(shape, shift, types):
+    rows, dim, tokens = shape
+    gen = torch.Generator().manual_seed(rows + dim)
+    table = torch.randn(rows, dim, generator=gen).to(types[0])
+    t = Buffer(rows * dim, types[0], shift, table.flatten())
+    for kind, dtype in (("uniform", I64), ("zipf", I32), ("outside", I64), ("outside", I32)):
+        ids = _ids(tokens, rows, kind, dtype)
+        out = Buffer(tokens * dim, types[1], (3 * shift) % 5)
+        mqg.mqg_embedding(t.view, rows, dim, Buffer(tokens, dtype, shift, ids).view, tokens, 1.7, out.view)
+        assert same_bits(out.cpu(), _lookup(table, ids, 1.7, types[1]).flatten())
+    t.check()
+
+
+def test_lookup_of_nothing_and_from_nothing():
+    ids, out = torch.zeros(4, dtype=I64, device="cuda"), Buffer(12, F32)
+    mqg.mqg_embedding(torch.empty(0, device="cuda"), 0, 3, ids, 4, 1.0, out.view)
+    assert (out.cpu() == 0).all()
+    out = Buffer(12, F32)
+    before = out.raw.clone()
+    mqg.mqg_embedding(torch.ones(15, device="cuda"), 5, 3, ids, 0, 1.0, out.view)
+    mqg.mqg_embedding(torch.ones(15, device="cuda"), 5, 0, ids, 4, 1.0, out.view)
+    assert (out.raw == before).all()
+
+
+def test_rows_behind_the_last_token_stay():
+    out = Buffer(100 * 8, BF16)
+    mqg.mqg_embedding(torch.ones(40, device="cuda"), 5, 8, torch.zeros(64, dtype=I64, device="cuda"), 33, 1.0, out.view)
+    got = out.cpu()
+    assert (got[:33 * 8] == 1).all() and (got[33 * 8:].view(torch.int16) == 0x5A5A).all()
+
+
+def _gradient(dout, ids, rows, scale, old):
+    """The formula in 64 bits, and how far fp32 may be off it before the last rounding."""
+    held = _held(ids, rows)
+    at, d = ids.long()[held], dout.double()[held]
+    total = torch.zeros(rows, dout.shape[1], dtype=torch.float64).index_add_(0, at, d) * scale
+    size = torch.zeros(rows, dout.shape[1], dtype=torch.float64).index_add_(0, at, d.abs()) * abs(scale)
+    k = torch.zeros(rows, dtype=torch.float64).index_add_(0, at, torch.ones(at.numel(), dtype=torch.float64))
+    depth = torch.minimum(k, 33 + k / 32)
+    off = (depth[:, None] * size + total.abs()) * 2.0 ** -24
+    if old is not None:
+        total = total + old.double()
+        off = off + total.abs() * 2.0 ** -24
+    return total, off * 1.001, k > 0
+
+
+def _check_gradient(shape, kind, id_type, types, add, shift=0, scale=1.3, seed=0):
+    rows, dim, tokens = shape
+    gen = torch.Generator().manual_seed(seed + tokens)
+    ids = _ids(tokens, rows, kind, id_type, seed)
+    dout = torch.randn(tokens, dim, generator=gen).to(types[0])
+    if tokens:
+        dout[~_held(ids, rows)] = math.nan                            # empty places hold what they like
+    old = torch.randn(rows, dim, generator=gen).to(types[1])
+    scale = float(torch.tensor(scale, dtype=F32))
+    want, off, used = _gradient(dout, ids, rows, scale, old if add else None)
+    floats = mqg.mqg_embedding_workspace_floats(tokens, rows, dim)
+    d = Buffer(tokens * dim, types[0], shift, dout.flatten())
+    i = Buffer(tokens, id_type, shift, ids)
+    got = []
+    for fill in (float("nan"), 0.0):
+        g = Buffer(rows * dim, types[1], (3 * shift) % 5, old.flatten())
+        w = Buffer(floats, F32, values=torch.full((floats,), fill))
+        mqg.mqg_embedding_grad(d.view, i.view, tokens, rows, dim, scale, g.view, w.view, add_into_grad=add)
+        got.append(g.cpu().view(rows, dim))
+        w.check()
+    assert same_bits(got[0], got[1])                                  # reproducible, whatever the workspace held
+    y = got[0].double()
+    half_step = torch.finfo(types[1]).eps / 2 if types[1] == BF16 else 0.0   # fp32: counted in `off`
+    assert ((y - want).abs() <= off + half_step * (want.abs() + off)).all()
+    if add:
+        assert same_bits(got[0][~used], old[~used])
+    else:
+        assert (got[0][~used] == 0).all()
+
+
+GRAD_SHAPES = [(1, 1, 1), (5, 7, 3), (3, 8, 40), (1000, 64, 2048), (17, 257, 100), (300, 1024, 33), (9, 4100, 65),
+               (40_000, 36, 4099), (70_001, 4, 20_000), (3, 130, 9000)]
+
+
+@pytest.mark.parametrize("add", [False, True])
+@pytest.mark.parametrize("kind", ["uniform", "zipf", "outside"])
+@pytest.mark.parametrize("shape", GRAD_SHAPES)
+def test_gradient(shape, kind, add):
+    _check_gradient(shape, kind, I64, (F32, F32), add)
+    _check_gradient(shape, kind, I32, (BF16, F32), add, shift=1)
+
+
+@pytest.mark.parametrize("add", [False, True])
+@pytest.mark.parametrize("shift", [0, 1, 4])
+@pytest.mark.parametrize("types", [(F32, F32), (F32, BF16), (BF16, F32), (BF16, BF16)])
+def test_gradient_of_each_type_and_alignment(types, shift, add):
+    for shape in ((50, 24, 300), (50, 20, 300), (50, 18, 300), (50, 17, 300), (50, 520, 70)):
+        _check_gradient(shape, "zipf", I64, types, add, shift)
+
+
+@pytest.mark.parametrize("add", [False, True])
+@pytest.mark.parametrize("tokens", [0, 1, 31, 32, 33, 64, 65, 96, 1000, 8192, 8193, 30_000])
+@pytest.mark.parametrize("kind", ["same", "empty", "ascending"])
+def test_gradient_of_long_and_of_missing_runs(kind, tokens, add):
+    _check_gradient((40, 12, tokens), kind, I64, (F32, F32), add)
+    _check_gradient((40, 12, tokens), kind, I32, (BF16, BF16), add)
+
+
+@pytest.mark.parametrize("rows", [1, 2, 255, 256, 257, 65_535, 65_536, 65_537, 1 << 20, (1 << 24) + 3])
+def test_gradient_of_tables_at_the_digits_edges(rows):
+    _check_gradient((rows, 2, 10_000), "uniform", I64, (F32, F32), False)
+    _check_gradient((rows, 1, 300), "outside", I32, (F32, F32), True)
+
+
+def test_gradient_by_differences():
+    """<R, lookup(table)> is linear in the table: its central difference is the gradient of R."""
+    rows, dim, tokens, scale, h = 6, 5, 40, 0.75, 0.5
+    gen = torch.Generator().manual_seed(1)
+    ids = _ids(tokens, rows, "zipf", I64).cuda()
+    r = torch.randn(tokens, dim, generator=gen).cuda()
+    table = torch.randn(rows, dim, generator=gen).cuda()
+    grad = torch.zeros(rows, dim, device="cuda")
+    w = torch.zeros(mqg.mqg_embedding_workspace_floats(tokens, rows, dim), device="cuda")
+    mqg.mqg_embedding_grad(r, ids, tokens, rows, dim, scale, grad, w)
+
+    def value(t):
+        out = torch.zeros(tokens, dim, device="cuda")
+        mqg.mqg_embedding(t, rows, dim, ids, tokens, scale, out)
+        return float((out.double() * r.double()).sum())
+
+    for v in range(rows):
+        for c in range(dim):
+            up, down = table.clone(), table.clone()
+            up[v, c] += h
+            down[v, c] -= h
+            # at most 40 products, each off by 2^-24 of |table +- h| < 8 and |r| < 8, twice over 2 h
+            assert abs((value(up) - value(down)) / (2 * h) - float(grad[v, c])) < 40 * 64 * 2.0 ** -23
+
+
+def test_gradient_captured_replayed_and_on_another_stream():
+    rows, dim, tokens = 500, 64, 3000
+    ids = [_ids(tokens, rows, "zipf", I64, seed).cuda() for seed in (0, 1)]
+    dout = torch.randn(tokens, dim, generator=torch.Generator().manual_seed(2)).cuda()
+    floats = mqg.mqg_embedding_workspace_floats(tokens, rows, dim)
+    want = []
+    for i in ids:
+        g = torch.empty(rows, dim, device="cuda")
+        mqg.mqg_embedding_grad(dout, i, tokens, rows, dim, 2.0, g, torch.empty(floats, device="cuda"))
+        want.append(g.cpu())
+    side, held, g, out = torch.cuda.Stream(), ids[0].clone(), torch.empty(rows, dim, device="cuda"), torch.empty(tokens, dim, device="cuda")
+    w = torch.empty(floats, device="cuda")
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        mqg.mqg_embedding_grad(dout, held, tokens, rows, dim, 2.0, g, w)
+    torch.cuda.synchronize()
+    assert same_bits(g.cpu(), want[0])
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        mqg.mqg_embedding_grad(dout, held, tokens, rows, dim, 2.0, g, w)
+        mqg.mqg_embedding(g, rows, dim, held, tokens, 1.0, out)
+    for k in (1, 0, 1):
+        held.copy_(ids[k])
+        g.fill_(math.nan)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert same_bits(g.cpu(), want[k])
+        assert same_bits(out.cpu(), _lookup(want[k], ids[k].cpu(), 1.0, F32))
+
+
+def test_a_table_beyond_32_bit_offsets():
+    rows, dim = 70_000, 1 << 16                      # 4.6 * 10^9 elements of bf16
+    table = torch.zeros(rows, dim, dtype=BF16, device="cuda")
+    ids = torch.tensor([rows - 1, 0, 65_536, rows, rows - 1, -1], device="cuda")
+    table[rows - 1], table[65_536] = 3, 5
+    out = torch.empty(6, dim, dtype=F32, device="cuda")
+    mqg.mqg_embedding(table, rows, dim, ids, 6, 2.0, out)
+    assert [float(x) for x in out[:, -1]] == [6, 0, 10, 0, 6, 0] and [float(x) for x in out[:, 0]] == [6, 0, 10, 0, 6, 0]
+    w = torch.empty(mqg.mqg_embedding_workspace_floats(6, rows, dim), device="cuda")
+    mqg.mqg_embedding_grad(out, ids, 6, rows, dim, 1.0, table, w, add_into_grad=True)
+    assert [float(table[r, c]) for r in (rows - 1, 65_536, 0, 1) for c in (0, dim - 1)] == [15, 15, 15, 15, 0, 0, 0, 0]
+    mqg.mqg_embedding_grad(out, ids, 6, rows, dim, 1.0, table, w)
+    assert [float(table[r, c]) for r in (rows - 1, 65_536, 0, 1) for c in (0, dim - 1)] == [12, 12, 10, 10, 0, 0, 0, 0]
