@@ -419,9 +419,10 @@ mqg_status mqg_embedding(const void* table, mqg_dtype table_dtype, uint64_t rows
  * The gradient of that table from the gradient of `out`:
  *     grad[v] = scale * sum over t with ids[t] = v of dout[t]            (0 for a row without tokens), or with add_into_grad
  *     grad[v] = grad[v] + scale * that sum                               (rows without tokens are not touched)
- * The tokens are sorted by id and a row's summed in ascending order of t in fp32, from runs of 32 sorted tokens; the scale
- * and the addition are one rounding each, and a bf16 `grad` is rounded once at the end.  No atomics: the result is
- * reproducible bit for bit.  What stands in `dout` at empty places is not used, NaN included.
+ * The tokens are sorted by id and a row's summed in ascending order of t in fp32: one after the other, a row of many tokens
+ * from sums of at most 32 each, in their order.  The scale and the addition are one rounding each, and a bf16 `grad` is
+ * rounded once at the end.  The order of every sum is fixed by the arguments' sizes and the ids: the result is reproducible
+ * bit for bit.  What stands in `dout` at empty places is not used, NaN included.
  *   grad       [out] rows x dim elements; with add_into_grad [in/out]
  *   workspace  [scratch] DEVICE memory of at least mqg_embedding_workspace_floats(tokens, rows, dim) floats, 16-byte
  *              aligned; otherwise as for the norm above

@@ -2,277 +2,193 @@
 //
 //   grad[v] = fl((grad[v] +) scale * sum over t with ids[t] = v of dout[t])
 //
-// in fp32, tokens in ascending order.  Three steps:
-//   1. the tokens are sorted by id (stable, least significant digit first; ids outside 0..rows-1 go behind all others), so
-//      that the tokens of one row are neighbours and no atomic is needed: the order of every sum is fixed;
-//   2. the sorted tokens are cut into chunks of kChunk; a thread takes V columns of a chunk and adds up its runs of equal
-//      ids.  A run inside the chunk goes to its row; one that crosses the chunk's edge leaves a partial sum;
-//   3. the partial sums of such a run are added up in the order of the chunks.
-// Rows that no token uses are set to zero unless the gradient is added to what is there.
+// in fp32, tokens in ascending order.  Three launches:
+//   1. the tokens are sorted by id (mqg_token_sort.cu), so that the tokens of a row are neighbours (a run) and no atomic is
+//      needed: the order of every sum is fixed.  Unless the gradient is added to what is there, the same launch sets it to
+//      zero;
+//   2. the sorted tokens are cut into chunks of C; a thread takes V columns of a chunk and adds up its runs.  A run that
+//      crosses chunks belongs to the chunk it begins in, which follows it, as long as it covers no chunk as a whole (less
+//      than 2 C tokens); of a longer one every chunk leaves its part's sum in the workspace;
+//   3. the parts of the long runs are added up in the order of the chunks.
 #include "mqg_tma.cuh"
-#include "mqg_training.h"
+#include "mqg_token_sort.h"
 #include "mqg_vector.cuh"
 
 namespace mqg {
 namespace {
 
-// ---- the sort ----
-constexpr int kSortThreads = 1024, kSortWarps = kSortThreads / 32;
-constexpr int kKeysPerThread = 8, kSortTile = kSortThreads * kKeysPerThread;
-constexpr int kDigitBits = 8, kBins = 1 << kDigitBits;
-
-// An id as the key it is sorted by.
-template <typename ID> __device__ __forceinline__ uint32_t key_of(ID id, uint32_t rows)
-{
-    return id >= 0 && (uint64_t)id < rows ? (uint32_t)id : rows;
-}
-
-// Where a pass reads its keys and tokens: the caller's ids (tokens = positions), or the pass before.
-template <typename ID> struct SortInput {
-    const ID* ids;
-    const uint2* pairs;      // (key, token); used where ids is null
-    uint32_t count, rows;
-    __device__ __forceinline__ uint2 get(uint32_t i) const
-    {
-        return ids != nullptr ? make_uint2(key_of(__ldg(ids + i), rows), i) : __ldcg(pairs + i);
-    }
-};
-
-// Ranks the tile's keys by digit, stably: rank[r] = how many keys of the warp before this one have its digit;
-// warp_count[w][d] = how many of warp w's keys have digit d.  A warp takes 256 consecutive keys, 32 at a time.
-template <typename ID>
-__device__ __forceinline__ void rank_tile(const SortInput<ID>& in, int shift, uint16_t (*warp_count)[kBins],
-                                          uint2 (&pair)[kKeysPerThread], uint32_t (&rank)[kKeysPerThread])
-{
-    const uint32_t lane = threadIdx.x & 31, w = threadIdx.x >> 5;
-    for (int d = lane; d < kBins; d += 32) warp_count[w][d] = 0;
-    const uint32_t first = blockIdx.x * (uint32_t)kSortTile + w * (32 * kKeysPerThread) + lane;
-#pragma unroll
-    for (int r = 0; r < kKeysPerThread; ++r)
-        pair[r] = first + r * 32 < in.count ? in.get(first + r * 32) : make_uint2(0, 0);
-    __syncwarp();
-#pragma unroll
-    for (int r = 0; r < kKeysPerThread; ++r) {
-        const bool held = first + r * 32 < in.count;
-        const uint32_t d = held ? (pair[r].x >> shift) & (kBins - 1) : kBins;
-        const uint32_t same = __match_any_sync(0xFFFFFFFFu, d);
-        const uint32_t before = held ? warp_count[w][d] : 0;
-        __syncwarp();
-        if (held && (same >> lane) == 1u) warp_count[w][d] = (uint16_t)(before + __popc(same));
-        __syncwarp();
-        rank[r] = before + __popc(same & ((1u << lane) - 1));
-    }
-}
-
-template <typename ID>
-__global__ void __launch_bounds__(kSortThreads)
-sort_count_kernel(const SortInput<ID> in, int shift, uint32_t* __restrict__ counts)
-{
-    __shared__ uint16_t warp_count[kSortWarps][kBins];
-    uint2 pair[kKeysPerThread];
-    uint32_t rank[kKeysPerThread];
-    grid_dependency_wait();
-    rank_tile(in, shift, warp_count, pair, rank);
-    __syncthreads();
-    if (threadIdx.x < kBins) {
-        uint32_t sum = 0;
-        for (int w = 0; w < kSortWarps; ++w) sum += warp_count[w][threadIdx.x];
-        counts[(uint64_t)blockIdx.x * kBins + threadIdx.x] = sum;
-    }
-}
-
-// counts[block][digit] becomes the first place of the block's keys of that digit.
-__global__ void __launch_bounds__(kBins)
-sort_scan_kernel(uint32_t* __restrict__ counts, uint32_t blocks)
-{
-    __shared__ uint32_t total[kBins];
-    const uint32_t d = threadIdx.x;
-    grid_dependency_wait();
-    uint32_t sum = 0;
-#pragma unroll 8
-    for (uint32_t b = 0; b < blocks; ++b) sum += __ldcg(counts + (uint64_t)b * kBins + d);
-    total[d] = sum;
-    __syncthreads();
-    for (int step = 1; step < kBins; step *= 2) {
-        const uint32_t v = d >= (uint32_t)step ? total[d - step] : 0;
-        __syncthreads();
-        total[d] += v;
-        __syncthreads();
-    }
-    uint32_t at = total[d] - sum;
-#pragma unroll 8
-    for (uint32_t b = 0; b < blocks; ++b) {
-        const uint32_t c = __ldcg(counts + (uint64_t)b * kBins + d);
-        counts[(uint64_t)b * kBins + d] = at;
-        at += c;
-    }
-}
-
-template <typename ID>
-__global__ void __launch_bounds__(kSortThreads)
-sort_place_kernel(const SortInput<ID> in, int shift, const uint32_t* __restrict__ counts, uint2* __restrict__ out)
-{
-    __shared__ uint16_t warp_count[kSortWarps][kBins];
-    __shared__ uint32_t warp_first[kSortWarps][kBins];
-    uint2 pair[kKeysPerThread];
-    uint32_t rank[kKeysPerThread];
-    grid_dependency_wait();
-    rank_tile(in, shift, warp_count, pair, rank);
-    __syncthreads();
-    if (threadIdx.x < kBins) {
-        uint32_t at = __ldcg(counts + (uint64_t)blockIdx.x * kBins + threadIdx.x);
-        for (int w = 0; w < kSortWarps; ++w) {
-            warp_first[w][threadIdx.x] = at;
-            at += warp_count[w][threadIdx.x];
-        }
-    }
-    __syncthreads();
-    const uint32_t lane = threadIdx.x & 31, w = threadIdx.x >> 5;
-    const uint32_t first = blockIdx.x * (uint32_t)kSortTile + w * (32 * kKeysPerThread) + lane;
-#pragma unroll
-    for (int r = 0; r < kKeysPerThread; ++r)
-        if (first + r * 32 < in.count) out[warp_first[w][(pair[r].x >> shift) & (kBins - 1)] + rank[r]] = pair[r];
-}
-
-// ---- the sums ----
-constexpr int kChunk = 32;                              // sorted tokens of one thread
-constexpr int kSumThreads = 128;
-constexpr int kAhead = 8;                               // rows whose loads are in flight together
+constexpr int kThreads = 128;
 
 struct GradArgs {
-    const uint2* sorted;     // (row, token), rows ascending; a row of `rows` = none
+    const uint2* sorted;     // (row, token), rows ascending; the row `rows` = none
     const void* dout;
     void* grad;
-    float* partial;          // [chunk][2][dim]: the sum of the run that enters the chunk, and of the one that begins there
-                             // and leaves it
+    float* parts;            // [chunk][2][dim]: the sum of the long run that enters the chunk, and of the one that begins in it
+    uint32_t* long_runs;     // how many there are, then the chunks that they begin in
     uint64_t dim;
     uint32_t tokens, rows, chunks;
+    int chunk_bits;
     float scale;
 };
 
-template <int DST, int V, bool ADD>
-__device__ __forceinline__ void write_row(const GradArgs& a, uint32_t row, uint64_t col, const float (&sum)[V])
+__device__ __forceinline__ uint32_t row_at(const GradArgs& a, uint32_t i) { return __ldg(&a.sorted[i].x); }
+
+template <int V> __device__ __forceinline__ float* part_at(const GradArgs& a, uint32_t chunk, bool begins, uint64_t col)
 {
-    auto* p = static_cast<typename Element<DST>::type*>(a.grad) + (uint64_t)row * a.dim + col;
-    Packed<DST, V> y;
-    if (ADD) y.load(p);
+    return a.parts + ((uint64_t)chunk * 2 + (begins ? 1 : 0)) * a.dim + col;
+}
+
+// grad's row from the sum and, with ADD, what was there.
+template <int DST, int V, bool ADD>
+__device__ __forceinline__ void finish_row(typename Element<DST>::type* p, Packed<DST, V>& y, float scale, const float (&sum)[V])
+{
 #pragma unroll
-    for (int e = 0; e < V; ++e) y.set(e, ADD ? __fadd_rn(y.get(e), __fmul_rn(a.scale, sum[e])) : __fmul_rn(a.scale, sum[e]));
+    for (int e = 0; e < V; ++e) y.set(e, ADD ? __fadd_rn(y.get(e), __fmul_rn(scale, sum[e])) : __fmul_rn(scale, sum[e]));
     y.store(p);
 }
 
-template <int V> __device__ __forceinline__ float* partial_at(const GradArgs& a, uint32_t chunk, int leaves, uint64_t col)
+template <int V> __device__ __forceinline__ void store_part(float* p, const float (&sum)[V])
 {
-    return a.partial + ((uint64_t)chunk * 2 + leaves) * a.dim + col;
+    Packed<kF32, V> y;
+#pragma unroll
+    for (int e = 0; e < V; ++e) y.set(e, sum[e]);
+    y.store(p);
 }
 
 // Threads: x = columns, V of them each; y = chunks.
 template <int SRC, int DST, int V, bool ADD>
-__global__ void __launch_bounds__(kSumThreads) grad_sum_kernel(const GradArgs a)
+__global__ void __launch_bounds__(kThreads) grad_sum_kernel(const GradArgs a)
 {
+    constexpr int kAhead = ADD ? 4 : 8;                 // tokens whose loads are in flight together
     const uint64_t col = ((uint64_t)blockIdx.y * blockDim.x + threadIdx.x) * V;
     const uint32_t chunk = blockIdx.x * blockDim.y + threadIdx.y;
     grid_dependency_wait();
     if (col >= a.dim || chunk >= a.chunks) return;
-    const uint32_t first = chunk * kChunk, last = min(first + kChunk, a.tokens);
-    uint32_t row = __ldcg(&a.sorted[first]).x;
-    if (row == a.rows) return;
-    bool enters = first > 0 && __ldcg(&a.sorted[first - 1]).x == row;
+    const uint32_t size = 1u << a.chunk_bits, first = chunk << a.chunk_bits, end = min(first + size, a.tokens);
+    const uint32_t row0 = row_at(a, first), row1 = row_at(a, end - 1);
+    if (row0 == a.rows) return;
+    const bool enters = first != 0 && row_at(a, first - 1) == row0;
+    const bool leaves = row1 != a.rows && end < a.tokens && row_at(a, end) == row1;
+    // long: covers this chunk, the one before or the one behind as a whole
+    const bool long_in = enters && (row0 == row1 || row_at(a, first - size) == row0);
+    const bool long_out = leaves && (row0 == row1 || row_at(a, min(end + size, a.tokens) - 1) == row1);
+    const uint32_t limit = leaves && !long_out ? min(end + size, a.tokens) - 1 : end;
+    if (long_out && !(long_in && row0 == row1) && col == 0) a.long_runs[1 + atomicAdd(a.long_runs, 1u)] = chunk;
+
+    const auto* dout = static_cast<const typename Element<SRC>::type*>(a.dout) + col;
+    auto* grad = static_cast<typename Element<DST>::type*>(a.grad) + col;
     float sum[V];
 #pragma unroll
     for (int e = 0; e < V; ++e) sum[e] = 0.0f;
-    const auto* dout = static_cast<const typename Element<SRC>::type*>(a.dout) + col;
-    for (uint32_t p = first; p < last && row != a.rows; p += kAhead) {
-        uint2 k[kAhead];
-        Packed<SRC, V> x[kAhead];
+    for (uint32_t p = first; p < limit; p += kAhead) {
+        uint2 k[kAhead + 1];
 #pragma unroll
-        for (int u = 0; u < kAhead; ++u) k[u] = p + u < last ? __ldcg(&a.sorted[p + u]) : make_uint2(row, ~0u);
+        for (int u = 0; u <= kAhead; ++u) k[u] = p + u < a.tokens ? __ldg(a.sorted + p + u) : make_uint2(a.rows, 0);
+        if (p >= end && k[0].x != row1) break;
+        Packed<SRC, V> x[kAhead];
+        Packed<DST, V> y[kAhead];
+        bool used[kAhead], ends[kAhead];
 #pragma unroll
         for (int u = 0; u < kAhead; ++u) {
-            if (p + u < last && k[u].x != a.rows) x[u].load(dout + (uint64_t)k[u].y * a.dim);
+            // what stands before a short run's end belongs to the chunk before; what stands behind this chunk's to its run
+            used[u] = p + u < limit && k[u].x != a.rows && (p + u < end || k[u].x == row1) && !(enters && !long_in && k[u].x == row0);
+            ends[u] = used[u] && k[u + 1].x != k[u].x;
+            if (used[u]) x[u].load(dout + (uint64_t)k[u].y * a.dim);
+            if (ADD && ends[u] && !(long_in && k[u].x == row0)) y[u].load(grad + (uint64_t)k[u].x * a.dim);
         }
 #pragma unroll
         for (int u = 0; u < kAhead; ++u) {
-            if (p + u >= last || row == a.rows) break;
-            if (k[u].x != row) {
-                if (enters) {
-#pragma unroll
-                    for (int e = 0; e < V; ++e) partial_at<V>(a, chunk, 0, col)[e] = sum[e];
-                } else {
-                    write_row<DST, V, ADD>(a, row, col, sum);
-                }
-                row = k[u].x;
-                enters = false;
-#pragma unroll
-                for (int e = 0; e < V; ++e) sum[e] = 0.0f;
-                if (row == a.rows) break;
-            }
+            if (!used[u]) continue;
 #pragma unroll
             for (int e = 0; e < V; ++e) sum[e] = __fadd_rn(sum[e], x[u].get(e));
+            if (!ends[u]) continue;
+            if (long_in && k[u].x == row0) store_part<V>(part_at<V>(a, chunk, false, col), sum);
+            else finish_row<DST, V, ADD>(grad + (uint64_t)k[u].x * a.dim, y[u], a.scale, sum);
+#pragma unroll
+            for (int e = 0; e < V; ++e) sum[e] = 0.0f;
         }
     }
-    if (row == a.rows) return;
-    const bool leaves = last < a.tokens && __ldcg(&a.sorted[last]).x == row;
-    if (enters || leaves) {
-#pragma unroll
-        for (int e = 0; e < V; ++e) partial_at<V>(a, chunk, enters ? 0 : 1, col)[e] = sum[e];
-    } else {
-        write_row<DST, V, ADD>(a, row, col, sum);
-    }
+    if (long_out) store_part<V>(part_at<V>(a, chunk, !(long_in && row0 == row1), col), sum);
 }
 
-// The rows whose runs cross chunks: by the chunk where the run begins.
+// The long runs: a CTA takes the columns of kThreads / kSplits vectors of one run after another, kSplits groups of threads
+// equal shares of its parts.
+constexpr int kSplits = 8, kColumns = kThreads / kSplits;
+
 template <int DST, int V, bool ADD>
-__global__ void __launch_bounds__(kSumThreads) grad_join_kernel(const GradArgs a)
+__global__ void __launch_bounds__(kThreads) grad_join_kernel(const GradArgs a, uint32_t column_tiles)
 {
-    const uint64_t col = ((uint64_t)blockIdx.y * blockDim.x + threadIdx.x) * V;
-    uint32_t chunk = blockIdx.x * blockDim.y + threadIdx.y;
+    __shared__ float share[kSplits][V][kColumns];
     grid_dependency_wait();
-    if (col >= a.dim || chunk + 1 >= a.chunks) return;
-    const uint32_t first = chunk * kChunk, end = first + kChunk;
-    const uint32_t row = __ldcg(&a.sorted[end - 1]).x;
-    if (row == a.rows || __ldcg(&a.sorted[end]).x != row) return;                     // nothing leaves the chunk
-    if (first > 0 && __ldcg(&a.sorted[first - 1]).x == row) return;                   // it began before
-    float sum[V];
-#pragma unroll
-    for (int e = 0; e < V; ++e) sum[e] = __ldcg(partial_at<V>(a, chunk, 1, col) + e);
-    do {
-        ++chunk;
-#pragma unroll
-        for (int e = 0; e < V; ++e) sum[e] = __fadd_rn(sum[e], __ldcg(partial_at<V>(a, chunk, 0, col) + e));
-    } while (chunk + 1 < a.chunks && __ldcg(&a.sorted[(chunk + 1) * kChunk]).x == row);
-    write_row<DST, V, ADD>(a, row, col, sum);
-}
-
-// Zeros in the rows that no token uses: 32 rows for each block, whose first warp looks each up among the sorted tokens.
-template <int DST, int V>
-__global__ void __launch_bounds__(kSumThreads) grad_zero_kernel(const GradArgs a)
-{
-    __shared__ uint32_t used;
-    const uint32_t row0 = blockIdx.x * 32u, rows = min(32u, a.rows - row0);
-    grid_dependency_wait();
-    if (threadIdx.x < 32) {
-        const uint32_t row = row0 + threadIdx.x;
-        uint32_t lo = 0, hi = a.tokens;                 // the first sorted token whose row is not below
-        while (lo < hi) {
-            const uint32_t mid = lo + (hi - lo) / 2;
-            if (__ldcg(&a.sorted[mid]).x < row) lo = mid + 1; else hi = mid;
+    const uint64_t items = (uint64_t)__ldcg(a.long_runs) * column_tiles;
+    const uint32_t x = threadIdx.x % kColumns, s = threadIdx.x / kColumns, lane = threadIdx.x & 31;
+    for (uint64_t item = blockIdx.x; item < items; item += gridDim.x) {
+        const uint32_t begin = __ldcg(a.long_runs + 1 + item / column_tiles);
+        const uint64_t col = ((uint64_t)(item % column_tiles) * kColumns + x) * V;
+        const uint32_t row = row_at(a, ((begin + 1) << a.chunk_bits) - 1);
+        uint32_t n = 1;                                 // chunks that the run has a part in
+        for (bool more = true; more;) {
+            const uint64_t next = ((uint64_t)(begin + n + lane)) << a.chunk_bits;
+            const uint32_t on = __ballot_sync(0xFFFFFFFFu, next < a.tokens && row_at(a, (uint32_t)next) == row);
+            n += on == 0xFFFFFFFFu ? 32 : __ffs(~on) - 1;
+            more = on == 0xFFFFFFFFu;
         }
-        const uint32_t u = __ballot_sync(0xFFFFFFFFu, lo < a.tokens && __ldcg(&a.sorted[lo]).x == row);
-        if (threadIdx.x == 0) used = u;
-    }
-    __syncthreads();
-    Packed<DST, V> zero;
+        const uint32_t per = (n + kSplits - 1) / kSplits, from = min(s * per, n), to = min(from + per, n);
+        float sum[V];
 #pragma unroll
-    for (int e = 0; e < V; ++e) zero.set(e, 0.0f);
-    auto* p = static_cast<typename Element<DST>::type*>(a.grad) + (uint64_t)row0 * a.dim;
-    for (uint32_t r = 0; r < rows; ++r)
-        if (!((used >> r) & 1u))
-            for (uint64_t c = (uint64_t)threadIdx.x * V; c < a.dim; c += kSumThreads * V) zero.store(p + r * a.dim + c);
+        for (int e = 0; e < V; ++e) sum[e] = 0.0f;
+        if (col < a.dim) {
+#pragma unroll 8
+            for (uint32_t i = from; i < to; ++i) {
+                Packed<kF32, V> y;
+                y.load(part_at<V>(a, begin + i, i == 0, col));
+#pragma unroll
+                for (int e = 0; e < V; ++e) sum[e] = __fadd_rn(sum[e], y.get(e));
+            }
+        }
+#pragma unroll
+        for (int e = 0; e < V; ++e) share[s][e][x] = sum[e];
+        __syncthreads();
+        if (s == 0 && col < a.dim) {
+#pragma unroll
+            for (int t = 1; t < kSplits; ++t)
+#pragma unroll
+                for (int e = 0; e < V; ++e) sum[e] = __fadd_rn(sum[e], share[t][e][x]);
+            auto* p = static_cast<typename Element<DST>::type*>(a.grad) + (uint64_t)row * a.dim + col;
+            Packed<DST, V> y;
+            if (ADD) y.load(p);
+            finish_row<DST, V, ADD>(p, y, a.scale, sum);
+        }
+        __syncthreads();
+    }
 }
 
 // ---- host ----
 constexpr uint64_t round4(uint64_t words) { return (words + 3) & ~3ull; }
+
+// Tokens of a chunk: as many as leave the sums' launch a few CTAs for each SM.
+int chunk_bits_of(uint64_t tokens, uint64_t dim)
+{
+    int bits = 5;
+    while (bits > 3 && ((tokens * dim) >> bits) < 1024 * 1024) --bits;
+    return bits;
+}
+
+struct Layout {
+    int chunk_bits;
+    uint32_t chunks;
+    uint64_t sorted, runs, scratch, parts, total;       // sizes in words
+    Layout(uint64_t tokens, uint64_t dim)
+    {
+        chunk_bits = chunk_bits_of(tokens, dim);
+        chunks = (uint32_t)((tokens + (1u << chunk_bits) - 1) >> chunk_bits);
+        sorted = round4(2 * tokens);
+        runs = round4(1 + (uint64_t)chunks);
+        scratch = round4(token_sort_words(tokens));
+        parts = 2 * (uint64_t)chunks * round4(dim);
+        total = sorted + runs + scratch + parts;
+    }
+};
 
 template <typename... KArgs, typename... Args>
 cudaError_t launch_pdl_block(void (*kernel)(KArgs...), dim3 grid, dim3 block, cudaStream_t stream, Args&&... args)
@@ -289,55 +205,18 @@ cudaError_t launch_pdl_block(void (*kernel)(KArgs...), dim3 grid, dim3 block, cu
     return cudaLaunchKernelEx(&cfg, kernel, static_cast<KArgs>(args)...);
 }
 
-struct Layout {
-    uint32_t chunks, sort_blocks;
-    uint64_t pairs, counts, partial, total;             // sizes in words
-    Layout(uint64_t tokens, uint64_t dim)
-    {
-        chunks = (uint32_t)((tokens + kChunk - 1) / kChunk);
-        sort_blocks = (uint32_t)((tokens + kSortTile - 1) / kSortTile);
-        pairs = round4(2 * tokens);
-        counts = round4((uint64_t)sort_blocks * kBins);
-        partial = 2 * (uint64_t)chunks * dim;
-        total = 2 * pairs + counts + partial;
-    }
-};
-
-template <typename ID>
-cudaError_t sort_tokens(const ID* ids, uint32_t tokens, uint32_t rows, uint2* a, uint2* b, uint32_t* counts, const Layout& lay,
-                        cudaStream_t stream, const uint2** sorted)
-{
-    int bits = 1;
-    while (bits < 32 && ((uint64_t)rows >> bits) != 0) ++bits;                        // of the largest key, `rows`
-    SortInput<ID> in = {ids, nullptr, tokens, rows};
-    for (int shift = 0; shift < bits; shift += kDigitBits) {
-        cudaError_t err = launch_pdl(sort_count_kernel<ID>, lay.sort_blocks, kSortThreads, stream, in, shift, counts);
-        if (err == cudaSuccess) err = launch_pdl(sort_scan_kernel, 1, kBins, stream, counts, lay.sort_blocks);
-        if (err == cudaSuccess) err = launch_pdl(sort_place_kernel<ID>, lay.sort_blocks, kSortThreads, stream, in, shift, counts, a);
-        if (err != cudaSuccess) return err;
-        in.ids = nullptr;
-        in.pairs = a;
-        *sorted = a;
-        uint2* t = a; a = b; b = t;
-    }
-    return cudaSuccess;
-}
-
 template <int SRC, int DST, int V, bool ADD> cudaError_t launch_sums(const GradArgs& a, cudaStream_t stream)
 {
-    if (!ADD) {
-        const cudaError_t err = launch_pdl(grad_zero_kernel<DST, V>, (a.rows + 31) / 32, kSumThreads, stream, a);
-        if (err != cudaSuccess) return err;
-    }
-    if (a.chunks == 0) return cudaSuccess;
     const uint64_t cols = a.dim / V;
     unsigned bx = 1;
-    while (bx < (unsigned)kSumThreads && bx < cols) bx *= 2;
-    const unsigned by = kSumThreads / bx;
+    while (bx < (unsigned)kThreads && bx < cols) bx *= 2;
+    const unsigned by = kThreads / bx;
     const dim3 grid((a.chunks + by - 1) / by, (unsigned)((cols + bx - 1) / bx));
     cudaError_t err = launch_pdl_block(grad_sum_kernel<SRC, DST, V, ADD>, grid, dim3(bx, by), stream, a);
-    if (err == cudaSuccess && a.chunks > 1) err = launch_pdl_block(grad_join_kernel<DST, V, ADD>, grid, dim3(bx, by), stream, a);
-    return err;
+    if (err != cudaSuccess || a.chunks < 2) return err;
+    const uint32_t tiles = (uint32_t)((cols + kColumns - 1) / kColumns);
+    const uint64_t most = (uint64_t)(a.chunks - 1) * tiles;
+    return launch_pdl(grad_join_kernel<DST, V, ADD>, (unsigned)(most < 592 ? most : 592), kThreads, stream, a, tiles);
 }
 
 template <int SRC, int DST, int V> cudaError_t by_add(const GradArgs& a, bool add, cudaStream_t stream)
@@ -367,16 +246,14 @@ cudaError_t launch_embedding_grad(const void* dout, int dout_dtype, const TokenI
                                   float scale, void* grad, int grad_dtype, bool add, float* workspace, cudaStream_t stream)
 {
     const Layout lay(ids.count, dim);
-    const uint32_t tokens = (uint32_t)ids.count;
-    uint2* first = reinterpret_cast<uint2*>(workspace);
-    uint2* second = reinterpret_cast<uint2*>(workspace + lay.pairs);
-    uint32_t* counts = reinterpret_cast<uint32_t*>(workspace + 2 * lay.pairs);
-    GradArgs a = {nullptr, dout, grad, workspace + 2 * lay.pairs + lay.counts, dim, tokens, (uint32_t)rows, lay.chunks, scale};
-    cudaError_t err = cudaSuccess;
-    if (tokens != 0)
-        err = ids.wide ? sort_tokens(static_cast<const int64_t*>(ids.ptr), tokens, a.rows, first, second, counts, lay, stream, &a.sorted)
-                       : sort_tokens(static_cast<const int32_t*>(ids.ptr), tokens, a.rows, first, second, counts, lay, stream, &a.sorted);
-    if (err != cudaSuccess) return err;
+    uint2* sorted = reinterpret_cast<uint2*>(workspace);
+    uint32_t* runs = reinterpret_cast<uint32_t*>(workspace + lay.sorted);
+    uint32_t* scratch = runs + lay.runs;
+    const GradArgs a = {sorted, dout, grad, workspace + lay.sorted + lay.runs + lay.scratch, runs, dim, (uint32_t)ids.count,
+                        (uint32_t)rows, lay.chunks, lay.chunk_bits, scale};
+    const uint64_t zero_bytes = add ? 0 : rows * dim * (grad_dtype == kF32 ? 4 : 2);
+    const cudaError_t err = launch_token_sort(ids, a.rows, sorted, runs, scratch, grad, zero_bytes, stream);
+    if (err != cudaSuccess || a.chunks == 0) return err;
     if (dout_dtype == kF32)
         return grad_dtype == kF32 ? by_vector<kF32, kF32>(a, add, stream) : by_vector<kF32, kBf16>(a, add, stream);
     return grad_dtype == kF32 ? by_vector<kBf16, kF32>(a, add, stream) : by_vector<kBf16, kBf16>(a, add, stream);

@@ -1,9 +1,9 @@
 """Rows of a table looked up for token ids, and the gradient of the table from sorted tokens.
 
 The lookup has one rounding of the product (and one to bf16): compared bit for bit.  The gradient of a row with k tokens is a
-sum in fp32 over runs of at most 32 sorted tokens, whose sums are added up in turn: no term goes through more than 32 + (k / 32
-+ 1) additions, or k in all where that is less, each off by at most 2^-24 of what it adds to, which is at most the sum of the
-magnitudes.  Then the product with the scale and, with add_into_grad, the sum with what was there (2^-24 each), and the
+sum in fp32: one after the other, or (some of those with 9 tokens and more, all with 64 and more) sums of at most 32 each, which are
+added up in turn: with at least 8 tokens to each of them but two, no term goes through more than 64 + k / 8 additions, or k in
+all where that is less, each off by at most 2^-24 of what it adds to, which is at most the sum of the magnitudes.  Then the product with the scale and, with add_into_grad, the sum with what was there (2^-24 each), and the
 rounding to the output's type (half a step)."""
 import math
 
@@ -91,7 +91,7 @@ def _gradient(dout, ids, rows, scale, old):
     total = torch.zeros(rows, dout.shape[1], dtype=torch.float64).index_add_(0, at, d) * scale
     size = torch.zeros(rows, dout.shape[1], dtype=torch.float64).index_add_(0, at, d.abs()) * abs(scale)
     k = torch.zeros(rows, dtype=torch.float64).index_add_(0, at, torch.ones(at.numel(), dtype=torch.float64))
-    depth = torch.minimum(k, 33 + k / 32)
+    depth = torch.minimum(k, 64 + k / 8)
     off = (depth[:, None] * size + total.abs()) * 2.0 ** -24
     if old is not None:
         total = total + old.double()
