@@ -2,11 +2,10 @@
 //
 //   grad[v] = fl((grad[v] +) scale * sum over t with ids[t] = v of dout[t])
 //
-// in fp32, tokens in ascending order.  Three launches:
+// in fp32, tokens in ascending order:
 //   1. the tokens are sorted by id (mqg_token_sort.cu), so that the tokens of a row are neighbours (a run) and no atomic is
-//      needed: the order of every sum is fixed.  Unless the gradient is added to what is there, the same launch sets it to
-//      zero;
-//   2. the sorted tokens are cut into chunks of C; a thread takes V columns of a chunk and adds up its runs.  A run that
+//      needed: the order of every sum is fixed.  Unless the gradient is added to what is there, it is set to zero meanwhile;
+//   2. the sorted tokens are cut into chunks of C; a thread takes eight columns of a chunk and adds up its runs.  A run that
 //      crosses chunks belongs to the chunk it begins in, which follows it, as long as it covers no chunk as a whole (less
 //      than 2 C tokens); of a longer one every chunk leaves its part's sum in the workspace;
 //   3. the parts of the long runs are added up in the order of the chunks.
@@ -18,146 +17,295 @@ namespace mqg {
 namespace {
 
 constexpr int kThreads = 128;
+constexpr int kColumns = 8;                             // of a thread, in groups of W neighbours
+constexpr int kMaxChunkBits = 5, kLeastThreadBits = 3;
+constexpr int kMaxDown = kThreads >> kLeastThreadBits;  // chunks of a CTA
 
 struct GradArgs {
     const uint2* sorted;     // (row, token), rows ascending; the row `rows` = none
     const void* dout;
     void* grad;
-    float* parts;            // [chunk][2][dim]: the sum of the long run that enters the chunk, and of the one that begins in it
-    uint32_t* long_runs;     // how many there are, then the chunks that they begin in
-    uint64_t dim;
-    uint32_t tokens, rows, chunks;
+    float4* parts;           // [chunk][2][words]: the sums of the long run that enters the chunk, and of the one that begins in it
+    uint32_t* run_count;
+    uint4* long_runs;        // (chunk that it begins in, chunks that it has parts in, row, 0)
+    uint32_t dim, tokens, rows, chunks;
     int chunk_bits;
+    uint32_t tiles;          // CTAs side by side over the columns
+    int thread_bits;         // 2^this threads of a CTA over the columns, the others over chunks
     float scale;
 };
 
-__device__ __forceinline__ uint32_t row_at(const GradArgs& a, uint32_t i) { return __ldg(&a.sorted[i].x); }
-
-template <int V> __device__ __forceinline__ float* part_at(const GradArgs& a, uint32_t chunk, bool begins, uint64_t col)
+// The sums of a thread's eight columns are two words of a part: word j of thread t of tile i is word (2 i + j) * threads + t.
+__device__ __forceinline__ uint32_t part_words(const GradArgs& a) { return a.tiles * 2 << a.thread_bits; }
+__device__ __forceinline__ float4* part_at(const GradArgs& a, uint32_t chunk, bool begins)
 {
-    return a.parts + ((uint64_t)chunk * 2 + (begins ? 1 : 0)) * a.dim + col;
+    return a.parts + ((uint64_t)chunk * 2 + (begins ? 1 : 0)) * part_words(a);
 }
 
-// grad's row from the sum and, with ADD, what was there.
-template <int DST, int V, bool ADD>
-__device__ __forceinline__ void finish_row(typename Element<DST>::type* p, Packed<DST, V>& y, float scale, const float (&sum)[V])
-{
-#pragma unroll
-    for (int e = 0; e < V; ++e) y.set(e, ADD ? __fadd_rn(y.get(e), __fmul_rn(scale, sum[e])) : __fmul_rn(scale, sum[e]));
-    y.store(p);
-}
+// The sorted tokens that a CTA's chunks look at, in shared memory: its chunks', and a chunk more on both sides.
+struct Window {
+    uint2 token[(kMaxDown + 2) << kMaxChunkBits];
+    uint32_t begin;                                     // token[0] is sorted token `begin`, modulo 2^32
 
-template <int V> __device__ __forceinline__ void store_part(float* p, const float (&sum)[V])
-{
-    Packed<kF32, V> y;
-#pragma unroll
-    for (int e = 0; e < V; ++e) y.set(e, sum[e]);
-    y.store(p);
-}
-
-// Threads: x = columns, V of them each; y = chunks.
-template <int SRC, int DST, int V, bool ADD>
-__global__ void __launch_bounds__(kThreads) grad_sum_kernel(const GradArgs a)
-{
-    constexpr int kAhead = ADD ? 4 : 8;                 // tokens whose loads are in flight together
-    const uint64_t col = ((uint64_t)blockIdx.y * blockDim.x + threadIdx.x) * V;
-    const uint32_t chunk = blockIdx.x * blockDim.y + threadIdx.y;
-    grid_dependency_wait();
-    if (col >= a.dim || chunk >= a.chunks) return;
-    const uint32_t size = 1u << a.chunk_bits, first = chunk << a.chunk_bits, end = min(first + size, a.tokens);
-    const uint32_t row0 = row_at(a, first), row1 = row_at(a, end - 1);
-    if (row0 == a.rows) return;
-    const bool enters = first != 0 && row_at(a, first - 1) == row0;
-    const bool leaves = row1 != a.rows && end < a.tokens && row_at(a, end) == row1;
-    // long: covers this chunk, the one before or the one behind as a whole
-    const bool long_in = enters && (row0 == row1 || row_at(a, first - size) == row0);
-    const bool long_out = leaves && (row0 == row1 || row_at(a, min(end + size, a.tokens) - 1) == row1);
-    const uint32_t limit = leaves && !long_out ? min(end + size, a.tokens) - 1 : end;
-    if (long_out && !(long_in && row0 == row1) && col == 0) a.long_runs[1 + atomicAdd(a.long_runs, 1u)] = chunk;
-
-    const auto* dout = static_cast<const typename Element<SRC>::type*>(a.dout) + col;
-    auto* grad = static_cast<typename Element<DST>::type*>(a.grad) + col;
-    float sum[V];
-#pragma unroll
-    for (int e = 0; e < V; ++e) sum[e] = 0.0f;
-    for (uint32_t p = first; p < limit; p += kAhead) {
-        uint2 k[kAhead + 1];
-#pragma unroll
-        for (int u = 0; u <= kAhead; ++u) k[u] = p + u < a.tokens ? __ldg(a.sorted + p + u) : make_uint2(a.rows, 0);
-        if (p >= end && k[0].x != row1) break;
-        Packed<SRC, V> x[kAhead];
-        Packed<DST, V> y[kAhead];
-        bool used[kAhead], ends[kAhead];
-#pragma unroll
-        for (int u = 0; u < kAhead; ++u) {
-            // what stands before a short run's end belongs to the chunk before; what stands behind this chunk's to its run
-            used[u] = p + u < limit && k[u].x != a.rows && (p + u < end || k[u].x == row1) && !(enters && !long_in && k[u].x == row0);
-            ends[u] = used[u] && k[u + 1].x != k[u].x;
-            if (used[u]) x[u].load(dout + (uint64_t)k[u].y * a.dim);
-            if (ADD && ends[u] && !(long_in && k[u].x == row0)) y[u].load(grad + (uint64_t)k[u].x * a.dim);
+    __device__ __forceinline__ void load(const GradArgs& a, uint32_t first_chunk, uint32_t chunks)
+    {
+        const uint32_t from = (first_chunk - 1) << a.chunk_bits, n = (chunks + 2) << a.chunk_bits;
+        for (uint32_t i = threadIdx.x; i < n; i += kThreads) {
+            const uint32_t p = from + i;                // wraps in the chunk before the first
+            token[i] = p < a.tokens ? __ldg(a.sorted + p) : make_uint2(a.rows, 0);
         }
-#pragma unroll
-        for (int u = 0; u < kAhead; ++u) {
-            if (!used[u]) continue;
-#pragma unroll
-            for (int e = 0; e < V; ++e) sum[e] = __fadd_rn(sum[e], x[u].get(e));
-            if (!ends[u]) continue;
-            if (long_in && k[u].x == row0) store_part<V>(part_at<V>(a, chunk, false, col), sum);
-            else finish_row<DST, V, ADD>(grad + (uint64_t)k[u].x * a.dim, y[u], a.scale, sum);
-#pragma unroll
-            for (int e = 0; e < V; ++e) sum[e] = 0.0f;
+        if (threadIdx.x == 0) begin = from;
+        __syncthreads();
+    }
+    __device__ __forceinline__ uint2 at(uint32_t p) const { return token[p - begin]; }
+    __device__ __forceinline__ uint32_t row(uint32_t p) const { return token[p - begin].x; }
+};
+
+// What a thread has to do in its chunk: sorted tokens begin..end - 1.
+struct ChunkWork {
+    uint32_t begin, end;
+    uint32_t entering;       // the row of a long run that enters the chunk, or `rows`
+    uint32_t leaving;        // the row of a long run that leaves it, or `rows`
+    bool begins;             // the one that leaves it begins here
+
+    __device__ __forceinline__ ChunkWork(const GradArgs& a, const Window& s, uint32_t chunk)
+    {
+        const uint32_t size = 1u << a.chunk_bits, first = chunk << a.chunk_bits;
+        begin = first;
+        end = min(first + size, a.tokens);
+        const uint32_t row0 = s.row(first), row1 = s.row(end - 1);
+        const bool enters = first != 0 && s.row(first - 1) == row0;
+        const bool crosses = row1 != a.rows && end < a.tokens && s.row(end) == row1;
+        // long: covers this chunk, the one before or the one behind as a whole
+        const bool long_in = enters && row0 != a.rows && (row0 == row1 || s.row(first - size) == row0);
+        const bool long_out = crosses && (row0 == row1 || s.row(min(end + size, a.tokens) - 1) == row1);
+        begins = long_out && !(long_in && row0 == row1);
+        entering = long_in ? row0 : a.rows;
+        leaving = long_out ? row1 : a.rows;
+        if (enters && !long_in) {                       // a short run's end, which belongs to the chunk before
+            for (uint32_t step = size / 2; step != 0; step /= 2)
+                if (begin + step < end && s.row(begin + step - 1) == row0) begin += step;
+            while (begin < end && s.row(begin) == row0) ++begin;
+        }
+        if (crosses && !long_out) {                     // a short run's end in the chunk behind
+            while (s.row(end) == row1) ++end;
+        } else if (row1 == a.rows) {                    // ids outside the table
+            while (end > begin && s.row(end - 1) == a.rows) --end;
         }
     }
-    if (long_out) store_part<V>(part_at<V>(a, chunk, !(long_in && row0 == row1), col), sum);
+};
+
+// A copy of 4, 8 or 16 bytes to shared memory that only the copying thread reads.
+template <int BYTES> __device__ __forceinline__ void copy_async(void* smem, const void* p)
+{
+    if constexpr (BYTES == 16)
+        asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem_u32(smem)), "l"(p) : "memory");
+    else
+        asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" ::"r"(smem_u32(smem)), "l"(p), "n"(BYTES) : "memory");
+}
+__device__ __forceinline__ void copies_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N> __device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+
+// A thread's columns of DEPTH rows under way: in slots of shared memory that the thread alone writes and reads, or, for groups
+// of less than the 4 bytes that asynchronous copies take (bf16 rows of an odd length), in registers.
+template <int DTYPE, int W, int DEPTH> struct Flight {
+    static constexpr int kGroups = kColumns / W;
+    static constexpr bool kAsync = W * kElemBytes<DTYPE> >= 4;
+    using Group = Packed<DTYPE, W>;
+    static_assert(Group::kWords == 1, "a group is one access");
+    struct Shared { typename Group::word slot[kAsync ? DEPTH : 1][kGroups][kAsync ? kThreads : 1]; };
+    Group held[kAsync ? 1 : DEPTH][kGroups];
+
+    // The groups whose bit is set, `apart` elements from one to the next.
+    __device__ __forceinline__ void fetch(Shared& s, int i, const typename Element<DTYPE>::type* p, uint32_t apart, uint32_t groups)
+    {
+#pragma unroll
+        for (int g = 0; g < kGroups; ++g) {
+            if (!((groups >> g) & 1u)) continue;
+            if constexpr (kAsync) copy_async<Group::kBytes>(&s.slot[i][g][threadIdx.x], p + g * apart);
+            else held[i][g].load(p + g * apart);
+        }
+    }
+    __device__ __forceinline__ Group get(const Shared& s, int i, int g) const
+    {
+        if constexpr (kAsync) {
+            Group x;
+            x.w[0] = s.slot[i][g][threadIdx.x];
+            return x;
+        } else {
+            return held[i][g];
+        }
+    }
+};
+
+// One group of a row of grad: the sum times the scale and, with ADD, what was there.
+template <int DST, int W, bool ADD>
+__device__ __forceinline__ void finish(typename Element<DST>::type* p, Packed<DST, W> y, float scale, const float* sum)
+{
+#pragma unroll
+    for (int e = 0; e < W; ++e) y.set(e, ADD ? __fadd_rn(y.get(e), __fmul_rn(scale, sum[e])) : __fmul_rn(scale, sum[e]));
+    y.store(p);
 }
 
-// The long runs: a CTA takes the columns of kThreads / kSplits vectors of one run after another, kSplits groups of threads
-// equal shares of its parts.
-constexpr int kSplits = 8, kColumns = kThreads / kSplits;
-
-template <int DST, int V, bool ADD>
-__global__ void __launch_bounds__(kThreads) grad_join_kernel(const GradArgs a, uint32_t column_tiles)
+// How many chunks the long run that begins in `chunk` has parts in: 32 looks at a time, 32 chunks apart and then one.
+__device__ __forceinline__ uint32_t chunks_of_run(const GradArgs& a, uint32_t chunk, uint32_t row)
 {
-    __shared__ float share[kSplits][V][kColumns];
+    uint32_t n = 1;
+#pragma unroll
+    for (int bits = 5; bits >= 0; bits -= 5) {
+        uint32_t on;
+        do {
+            on = 0;
+#pragma unroll
+            for (uint32_t k = 1; k <= 32; ++k) {        // the run covers a first part of the chunks: as many as are on
+                const uint64_t p = ((uint64_t)chunk + n + (k << bits) - 1) << a.chunk_bits;
+                on += p < a.tokens && __ldg(&a.sorted[p].x) == row ? 1 : 0;
+            }
+            n += on << bits;
+        } while (on == 32);
+    }
+    return n;
+}
+
+// CTAs that read the same rows are neighbours in the grid.  Lanes take neighbouring groups, so that every access of a warp
+// covers whole sectors (two 16-byte stores per thread, 32 bytes apart from lane to lane, made the fp32 sums write half
+// sectors).  kDepth rows are under way for each thread: four with 23 KB of shared memory to a CTA did as well as six, and
+// left room for more CTAs whose beginnings and ends overlap; eight were 10 % slower.
+template <int SRC, int DST, int W, bool ADD>
+__global__ void __launch_bounds__(kThreads) grad_sum_kernel(const GradArgs a)
+{
+    constexpr int kDepth = 4, kGroups = kColumns / W;
+    using X = Flight<SRC, W, kDepth>;
+    using Y = Flight<DST, W, ADD ? kDepth : 1>;
+    __shared__ typename X::Shared xs;
+    __shared__ typename Y::Shared ys;
+    __shared__ Window tokens;
+    const uint32_t across = 1u << a.thread_bits, down = blockIdx.x / a.tiles, tile = blockIdx.x - down * a.tiles;
+    const uint32_t t = threadIdx.x & (across - 1), first_chunk = down * (kThreads >> a.thread_bits);
+    const uint32_t chunk = first_chunk + (threadIdx.x >> a.thread_bits);
+    const uint32_t col = (tile * across * kGroups + t) * W, apart = across * W;
     grid_dependency_wait();
-    const uint64_t items = (uint64_t)__ldcg(a.long_runs) * column_tiles;
-    const uint32_t x = threadIdx.x % kColumns, s = threadIdx.x / kColumns, lane = threadIdx.x & 31;
-    for (uint64_t item = blockIdx.x; item < items; item += gridDim.x) {
-        const uint32_t begin = __ldcg(a.long_runs + 1 + item / column_tiles);
-        const uint64_t col = ((uint64_t)(item % column_tiles) * kColumns + x) * V;
-        const uint32_t row = row_at(a, ((begin + 1) << a.chunk_bits) - 1);
-        uint32_t n = 1;                                 // chunks that the run has a part in
-        for (bool more = true; more;) {
-            const uint64_t next = ((uint64_t)(begin + n + lane)) << a.chunk_bits;
-            const uint32_t on = __ballot_sync(0xFFFFFFFFu, next < a.tokens && row_at(a, (uint32_t)next) == row);
-            n += on == 0xFFFFFFFFu ? 32 : __ffs(~on) - 1;
-            more = on == 0xFFFFFFFFu;
-        }
-        const uint32_t per = (n + kSplits - 1) / kSplits, from = min(s * per, n), to = min(from + per, n);
-        float sum[V];
+    tokens.load(a, first_chunk, kThreads >> a.thread_bits);
+    if (col >= a.dim || chunk >= a.chunks) return;
+    uint32_t groups = 0;
 #pragma unroll
-        for (int e = 0; e < V; ++e) sum[e] = 0.0f;
-        if (col < a.dim) {
-#pragma unroll 8
-            for (uint32_t i = from; i < to; ++i) {
-                Packed<kF32, V> y;
-                y.load(part_at<V>(a, begin + i, i == 0, col));
-#pragma unroll
-                for (int e = 0; e < V; ++e) sum[e] = __fadd_rn(sum[e], y.get(e));
+    for (int g = 0; g < kGroups; ++g) groups |= col + g * apart < a.dim ? 1u << g : 0u;
+
+    const ChunkWork w(a, tokens, chunk);
+    if (w.begins && col == 0) a.long_runs[atomicAdd(a.run_count, 1u)] = make_uint4(chunk, chunks_of_run(a, chunk, w.leaving), w.leaving, 0);
+    const auto* dout = static_cast<const typename Element<SRC>::type*>(a.dout) + col;
+    auto* grad = static_cast<typename Element<DST>::type*>(a.grad) + col;
+    X x;
+    Y y;
+    uint2 next = tokens.at(w.begin);
+    uint32_t row[kDepth], ends = 0;                     // of the tokens under way; bits: those that end a run
+    const auto fetch = [&](uint32_t p, int i) {         // called for one token after the other
+        if (p < w.end) {
+            const uint2 k = next;
+            next = tokens.at(p + 1);
+            row[i] = k.x;
+            x.fetch(xs, i, dout + (uint64_t)k.y * a.dim, apart, groups);
+            if (next.x != k.x) {
+                ends |= 1u << i;
+                if (ADD && k.x != w.entering) y.fetch(ys, i, grad + (uint64_t)k.x * a.dim, apart, groups);
             }
         }
+        copies_commit();
+    };
+    float sum[kColumns];
 #pragma unroll
-        for (int e = 0; e < V; ++e) share[s][e][x] = sum[e];
+    for (int e = 0; e < kColumns; ++e) sum[e] = 0.0f;
+    const auto store_part = [&](bool begins) {
+        float4* p = part_at(a, chunk, begins) + (tile * 2 << a.thread_bits) + t;
+        p[0] = make_float4(sum[0], sum[1], sum[2], sum[3]);
+        p[across] = make_float4(sum[4], sum[5], sum[6], sum[7]);
+    };
+#pragma unroll
+    for (int i = 0; i < kDepth; ++i) fetch(w.begin + i, i);
+    for (uint32_t p = w.begin; p < w.end; p += kDepth) {
+#pragma unroll
+        for (int i = 0; i < kDepth; ++i) {
+            if (p + i >= w.end) break;
+            copies_wait<kDepth - 1>();
+#pragma unroll
+            for (int g = 0; g < kGroups; ++g) {
+                const auto v = x.get(xs, i, g);
+#pragma unroll
+                for (int e = 0; e < W; ++e) sum[g * W + e] = __fadd_rn(sum[g * W + e], v.get(e));
+            }
+            if ((ends >> i) & 1u) {
+                ends &= ~(1u << i);
+                if (row[i] == w.entering) {
+                    store_part(false);
+                } else {
+#pragma unroll
+                    for (int g = 0; g < kGroups; ++g) {
+                        if (!((groups >> g) & 1u)) continue;
+                        Packed<DST, W> old;
+                        if (ADD) old = y.get(ys, ADD ? i : 0, g);
+                        finish<DST, W, ADD>(grad + (uint64_t)row[i] * a.dim + g * apart, old, a.scale, sum + g * W);
+                    }
+                }
+#pragma unroll
+                for (int e = 0; e < kColumns; ++e) sum[e] = 0.0f;
+            }
+            fetch(p + kDepth + i, i);
+        }
+    }
+    if (w.leaving != a.rows) store_part(w.begins);
+}
+
+// The long runs: a CTA takes kJoinWords words of one run after another, kSplits groups of threads equal shares of its parts.
+// What bounds it is the chain of dependent loads: the run, its length, its parts, in that order.
+constexpr int kJoinThreads = 256, kSplits = 8, kJoinWords = kJoinThreads / kSplits;
+
+template <int DST, int W, bool ADD>
+__global__ void __launch_bounds__(kJoinThreads) grad_join_kernel(const GradArgs a)
+{
+    __shared__ float4 share[kSplits][kJoinWords];
+    grid_dependency_wait();
+    const uint32_t words = part_words(a), tiles = (words + kJoinWords - 1) / kJoinWords;
+    const uint64_t items = (uint64_t)__ldcg(a.run_count) * tiles;
+    const uint32_t s = threadIdx.x / kJoinWords;
+    for (uint64_t item = blockIdx.x; item < items; item += gridDim.x) {
+        const uint32_t run = (uint32_t)(item / tiles), word = (uint32_t)(item - (uint64_t)run * tiles) * kJoinWords + threadIdx.x % kJoinWords;
+        const uint4 r = __ldcg(a.long_runs + run);
+        const uint32_t n = word < words ? r.y : 0;
+        const uint32_t per = (n + kSplits - 1) / kSplits, from = min(s * per, n), to = min(from + per, n);
+        float4 sum = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll 8
+        for (uint32_t i = from; i < to; ++i) {
+            const float4 v = __ldcg(part_at(a, r.x + i, i == 0) + word);
+            sum.x = __fadd_rn(sum.x, v.x);
+            sum.y = __fadd_rn(sum.y, v.y);
+            sum.z = __fadd_rn(sum.z, v.z);
+            sum.w = __fadd_rn(sum.w, v.w);
+        }
+        share[s][threadIdx.x % kJoinWords] = sum;
         __syncthreads();
-        if (s == 0 && col < a.dim) {
+        if (s == 0 && word < words) {
 #pragma unroll
-            for (int t = 1; t < kSplits; ++t)
+            for (int k = 1; k < kSplits; ++k) {
+                const float4 v = share[k][threadIdx.x];
+                sum.x = __fadd_rn(sum.x, v.x);
+                sum.y = __fadd_rn(sum.y, v.y);
+                sum.z = __fadd_rn(sum.z, v.z);
+                sum.w = __fadd_rn(sum.w, v.w);
+            }
+            // the word's columns: a group of four, half a group of eight, or several smaller groups
+            constexpr int G = W < 4 ? W : 4;
+            const uint32_t across = 1u << a.thread_bits, tile = word / (2 * across), half = (word / across) & 1, t = word & (across - 1);
+            const float v[4] = {sum.x, sum.y, sum.z, sum.w};
 #pragma unroll
-                for (int e = 0; e < V; ++e) sum[e] = __fadd_rn(sum[e], share[t][e][x]);
-            auto* p = static_cast<typename Element<DST>::type*>(a.grad) + (uint64_t)row * a.dim + col;
-            Packed<DST, V> y;
-            if (ADD) y.load(p);
-            finish_row<DST, V, ADD>(p, y, a.scale, sum);
+            for (int g = 0; g < 4 / G; ++g) {
+                const uint32_t group = W == 8 ? 0 : half * (4 / G) + g;
+                const uint32_t col = ((tile * (kColumns / W) + group) * across + t) * W + (W == 8 ? half * 4 : 0);
+                if (col >= a.dim) continue;
+                auto* p = static_cast<typename Element<DST>::type*>(a.grad) + (uint64_t)r.z * a.dim + col;
+                Packed<DST, G> old;
+                if (ADD) old.load(p);
+                finish<DST, G, ADD>(p, old, a.scale, v + g * G);
+            }
         }
         __syncthreads();
     }
@@ -166,67 +314,46 @@ __global__ void __launch_bounds__(kThreads) grad_join_kernel(const GradArgs a, u
 // ---- host ----
 constexpr uint64_t round4(uint64_t words) { return (words + 3) & ~3ull; }
 
-// Tokens of a chunk: as many as leave the sums' launch a few CTAs for each SM.
-int chunk_bits_of(uint64_t tokens, uint64_t dim)
-{
-    int bits = 5;
-    while (bits > 3 && ((tokens * dim) >> bits) < 1024 * 1024) --bits;
-    return bits;
-}
-
 struct Layout {
-    int chunk_bits;
-    uint32_t chunks;
+    int chunk_bits, thread_bits;
+    uint32_t chunks, tiles;
     uint64_t sorted, runs, scratch, parts, total;       // sizes in words
-    Layout(uint64_t tokens, uint64_t dim)
+    Layout(uint64_t tokens, uint64_t rows, uint64_t dim)
     {
-        chunk_bits = chunk_bits_of(tokens, dim);
+        // 32 tokens to a chunk, down to 8 where that leaves less than a CTA for each of 1024 x 1024 elements
+        chunk_bits = kMaxChunkBits;
+        while (chunk_bits > 3 && ((tokens * dim) >> chunk_bits) < 1024 * 1024) --chunk_bits;
         chunks = (uint32_t)((tokens + (1u << chunk_bits) - 1) >> chunk_bits);
+        thread_bits = kLeastThreadBits;
+        while ((1 << thread_bits) < kThreads && (uint64_t)kColumns << thread_bits < dim) ++thread_bits;
+        const uint64_t tile = (uint64_t)kColumns << thread_bits;
+        tiles = (uint32_t)((dim + tile - 1) / tile);
         sorted = round4(2 * tokens);
-        runs = round4(1 + (uint64_t)chunks);
-        scratch = round4(token_sort_words(tokens));
-        parts = 2 * (uint64_t)chunks * round4(dim);
+        runs = 4 + 4 * (uint64_t)chunks;
+        scratch = round4(token_sort_words(tokens, rows));
+        parts = 2 * (uint64_t)chunks * tiles * tile;
         total = sorted + runs + scratch + parts;
     }
 };
 
-template <typename... KArgs, typename... Args>
-cudaError_t launch_pdl_block(void (*kernel)(KArgs...), dim3 grid, dim3 block, cudaStream_t stream, Args&&... args)
+template <int SRC, int DST, int W, bool ADD> cudaError_t launch_sums(const GradArgs& a, cudaStream_t stream)
 {
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = grid;
-    cfg.blockDim = block;
-    cfg.stream = stream;
-    cudaLaunchAttribute attr[1];
-    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr[0].val.programmaticStreamSerializationAllowed = 1;
-    cfg.attrs = attr;
-    cfg.numAttrs = 1;
-    return cudaLaunchKernelEx(&cfg, kernel, static_cast<KArgs>(args)...);
+    const uint32_t down = kThreads >> a.thread_bits;
+    const cudaError_t err = launch_pdl(grad_sum_kernel<SRC, DST, W, ADD>, (a.chunks + down - 1) / down * a.tiles, kThreads, stream, a);
+    if (err != cudaSuccess || a.chunks < 2) return err;                              // a long run is in two chunks at least
+    const uint64_t most = (uint64_t)(a.chunks - 1) * (((a.tiles * 2 << a.thread_bits) + kJoinWords - 1) / kJoinWords);
+    return launch_pdl(grad_join_kernel<DST, W, ADD>, (unsigned)(most < 1184 ? most : 1184), kJoinThreads, stream, a);
 }
 
-template <int SRC, int DST, int V, bool ADD> cudaError_t launch_sums(const GradArgs& a, cudaStream_t stream)
+template <int SRC, int DST, int W> cudaError_t by_add(const GradArgs& a, bool add, cudaStream_t stream)
 {
-    const uint64_t cols = a.dim / V;
-    unsigned bx = 1;
-    while (bx < (unsigned)kThreads && bx < cols) bx *= 2;
-    const unsigned by = kThreads / bx;
-    const dim3 grid((a.chunks + by - 1) / by, (unsigned)((cols + bx - 1) / bx));
-    cudaError_t err = launch_pdl_block(grad_sum_kernel<SRC, DST, V, ADD>, grid, dim3(bx, by), stream, a);
-    if (err != cudaSuccess || a.chunks < 2) return err;
-    const uint32_t tiles = (uint32_t)((cols + kColumns - 1) / kColumns);
-    const uint64_t most = (uint64_t)(a.chunks - 1) * tiles;
-    return launch_pdl(grad_join_kernel<DST, V, ADD>, (unsigned)(most < 592 ? most : 592), kThreads, stream, a, tiles);
+    return add ? launch_sums<SRC, DST, W, true>(a, stream) : launch_sums<SRC, DST, W, false>(a, stream);
 }
 
-template <int SRC, int DST, int V> cudaError_t by_add(const GradArgs& a, bool add, cudaStream_t stream)
+// Groups of up to 16 bytes of the wider type, as long as they divide the rows and start on their boundaries.
+template <int SRC, int DST> cudaError_t by_group(const GradArgs& a, bool add, cudaStream_t stream)
 {
-    return add ? launch_sums<SRC, DST, V, true>(a, stream) : launch_sums<SRC, DST, V, false>(a, stream);
-}
-
-template <int SRC, int DST> cudaError_t by_vector(const GradArgs& a, bool add, cudaStream_t stream)
-{
-    constexpr int most = SRC == kF32 && DST == kF32 ? 4 : 8;
+    constexpr int most = SRC == kF32 || DST == kF32 ? 4 : 8;
     switch (row_vector(most, a.dim, a.dout, kElemBytes<SRC>, a.grad, kElemBytes<DST>)) {
         case 8: if constexpr (most == 8) return by_add<SRC, DST, 8>(a, add, stream);
         case 4: return by_add<SRC, DST, 4>(a, add, stream);
@@ -239,24 +366,25 @@ template <int SRC, int DST> cudaError_t by_vector(const GradArgs& a, bool add, c
 
 size_t embedding_workspace_floats(uint64_t tokens, uint64_t rows, uint64_t dim)
 {
-    return tokens == 0 || rows == 0 || dim == 0 ? 0 : (size_t)Layout(tokens, dim).total;
+    return tokens == 0 || rows == 0 || dim == 0 ? 0 : (size_t)Layout(tokens, rows, dim).total;
 }
 
 cudaError_t launch_embedding_grad(const void* dout, int dout_dtype, const TokenIds& ids, uint64_t rows, uint64_t dim,
                                   float scale, void* grad, int grad_dtype, bool add, float* workspace, cudaStream_t stream)
 {
-    const Layout lay(ids.count, dim);
+    const Layout lay(ids.count, rows, dim);
     uint2* sorted = reinterpret_cast<uint2*>(workspace);
     uint32_t* runs = reinterpret_cast<uint32_t*>(workspace + lay.sorted);
     uint32_t* scratch = runs + lay.runs;
-    const GradArgs a = {sorted, dout, grad, workspace + lay.sorted + lay.runs + lay.scratch, runs, dim, (uint32_t)ids.count,
-                        (uint32_t)rows, lay.chunks, lay.chunk_bits, scale};
-    const uint64_t zero_bytes = add ? 0 : rows * dim * (grad_dtype == kF32 ? 4 : 2);
-    const cudaError_t err = launch_token_sort(ids, a.rows, sorted, runs, scratch, grad, zero_bytes, stream);
+    const GradArgs a = {sorted, dout, grad, reinterpret_cast<float4*>(scratch + lay.scratch), runs,
+                        reinterpret_cast<uint4*>(runs + 4), (uint32_t)dim, (uint32_t)ids.count, (uint32_t)rows, lay.chunks,
+                        lay.chunk_bits, lay.tiles, lay.thread_bits, scale};
+    const cudaError_t err = launch_token_sort(ids, a.rows, sorted, runs, scratch, add ? nullptr : grad,
+                                              dim * (grad_dtype == kF32 ? 4 : 2), stream);
     if (err != cudaSuccess || a.chunks == 0) return err;
     if (dout_dtype == kF32)
-        return grad_dtype == kF32 ? by_vector<kF32, kF32>(a, add, stream) : by_vector<kF32, kBf16>(a, add, stream);
-    return grad_dtype == kF32 ? by_vector<kBf16, kF32>(a, add, stream) : by_vector<kBf16, kBf16>(a, add, stream);
+        return grad_dtype == kF32 ? by_group<kF32, kF32>(a, add, stream) : by_group<kF32, kBf16>(a, add, stream);
+    return grad_dtype == kF32 ? by_group<kBf16, kF32>(a, add, stream) : by_group<kBf16, kBf16>(a, add, stream);
 }
 
 }  // namespace mqg

@@ -1,11 +1,11 @@
 // Token ids sorted by id, stably, with the tokens' positions: least significant digit first, up to ten bits to a pass.
 //
-// Up to 65,536 tokens one thread-block cluster sorts in one launch.  A CTA holds K x 1024 pairs (key, token) of the order so
-// far, K to a thread; a warp ranks its 32 K consecutive pairs by ballots, 32 at a time, the warps' digit counts are added up
-// in shared memory and the CTAs' through distributed shared memory, and every pair is stored to its place in the CTA that
-// holds it in the next pass (after the last one: to memory).  What bounds it is latency: two cluster barriers and about five
-// dependent turns through shared memory for each pass.
-// The launch's other CTAs set the buffer that the sums go to to zero meanwhile, which depends on nothing.
+// Up to 131,072 tokens one thread-block cluster sorts in one launch.  A thread takes K pairs (key, token) of the order so far,
+// a warp 32 K consecutive ones; it ranks them by ballots, the warps' digit counts are added up in shared memory and the CTAs'
+// through distributed shared memory, and every pair is stored to its place in memory, where the next pass reads it from L2.
+// (Stores to the shared memory of the CTA that holds the place took 10,000 cycles for 8192 pairs to a CTA, stores to memory
+// 2,900.)  What bounds it is latency: two cluster barriers and about five dependent turns through shared memory a pass.
+// Rows that no token uses are set to zero by a kernel that runs beside the sort: the sort first marks the rows that are used.
 //
 // More tokens take three launches a pass: count, scan, place.
 #include <atomic>
@@ -22,12 +22,16 @@ template <typename ID> __device__ __forceinline__ uint32_t key_of(ID id, uint32_
     return id >= 0 && (uint64_t)id < rows ? (uint32_t)id : rows;
 }
 
+constexpr int kMaxDigitBits = 10;
+
 // The lanes of the warp that hold the same digit, among those that hold a key at all.
 __device__ __forceinline__ uint32_t same_digit(uint32_t digit, int bits, uint32_t held)
 {
     uint32_t same = held;
-    for (int b = 0; b < bits; ++b) {
-        const bool one = (digit >> b) & 1u;
+#pragma unroll
+    for (int b = 0; b < kMaxDigitBits; ++b) {
+        if (b >= bits) break;
+        const bool one = (digit & (1u << b)) != 0;
         const uint32_t ones = __ballot_sync(0xFFFFFFFFu, one);
         same &= one ? ones : ~ones;
     }
@@ -36,17 +40,17 @@ __device__ __forceinline__ uint32_t same_digit(uint32_t digit, int bits, uint32_
 
 // ---- one launch ----
 constexpr int kThreads = 1024, kWarps = kThreads / 32;
-constexpr int kMaxDigitBits = 10;
+constexpr unsigned kMaxCluster = 16;
 
 struct SortArgs {
     const void* ids;
     uint2* sorted;
+    uint2* spare;            // of the passes but the last
     uint32_t* counter;       // set to zero for the kernels that follow
-    void* zero;              // bytes to set to zero
-    uint64_t zero_bytes;
+    uint32_t* used;          // a bit for each row: whether a token has it; null: not wanted
     uint32_t tokens, rows;
     int bits, digit_bits;
-    unsigned ctas;           // of the sort: the grid's first ones, one cluster
+    unsigned ctas;           // one cluster
 };
 
 __device__ __forceinline__ uint32_t cluster_rank()
@@ -60,105 +64,118 @@ __device__ __forceinline__ void cluster_sync()
     asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
     asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
-__device__ __forceinline__ uint32_t peer_address(const void* p, uint32_t rank)
-{
-    uint32_t at;
-    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"(smem_u32(p)), "r"(rank));
-    return at;
-}
 __device__ __forceinline__ uint32_t peer_load(const uint32_t* p, uint32_t rank)
 {
-    uint32_t v;
-    asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(v) : "r"(peer_address(p, rank)) : "memory");
+    uint32_t at, v;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"(smem_u32(p)), "r"(rank));
+    asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(v) : "r"(at));
     return v;
 }
-__device__ __forceinline__ void peer_store(uint2* p, uint32_t rank, uint2 v)
+
+__host__ __device__ constexpr size_t sort_smem(int bins)
 {
-    asm volatile("st.shared::cluster.v2.u32 [%0], {%1, %2};" ::"r"(peer_address(p, rank)), "r"(v.x), "r"(v.y) : "memory");
+    return (size_t)bins * (kWarps * sizeof(uint16_t) + 2 * sizeof(uint32_t)) + kWarps * sizeof(uint32_t);
 }
 
-__host__ __device__ constexpr size_t sort_smem(int per_thread, int bins)
+// Marks the rows that the cluster's ids use, first each CTA's in shared memory: a frequent row is one access to L2 for each CTA
+// instead of one for each token.
+constexpr uint32_t kMaxMarkedRows = 32768 * 8;
+template <typename ID> __device__ __forceinline__ void mark_used(const SortArgs& a, uint32_t* mine, uint32_t rank)
 {
-    return (size_t)per_thread * kThreads * sizeof(uint2) + (size_t)bins * (kWarps * sizeof(uint16_t) + 2 * sizeof(uint32_t)) +
-           kWarps * sizeof(uint32_t);
+    const uint32_t words = (a.rows + 31) / 32, threads = a.ctas * kThreads;
+    for (uint32_t i = threadIdx.x; i < words; i += kThreads) mine[i] = 0;
+    for (uint32_t i = rank * kThreads + threadIdx.x; i < words; i += threads) a.used[i] = 0;
+    cluster_sync();
+#pragma unroll 4
+    for (uint32_t i = rank * kThreads + threadIdx.x; i < a.tokens; i += threads) {
+        const uint32_t row = key_of(__ldg(static_cast<const ID*>(a.ids) + i), a.rows);
+        if (row < a.rows) atomicOr(mine + row / 32, 1u << (row & 31));
+    }
+    __syncthreads();
+    for (uint32_t i = threadIdx.x; i < words; i += kThreads)
+        if (mine[i] != 0) atomicOr(a.used + i, mine[i]);
+    __threadfence();                                    // before the launch that reads them is released
+    cluster_sync();
 }
 
-__device__ void set_zero(void* p, uint64_t bytes, unsigned cta, unsigned ctas)
-{
-    char* c = static_cast<char*>(p);
-    const uint64_t to_boundary = (16 - (reinterpret_cast<uintptr_t>(c) & 15)) & 15;
-    const uint64_t head = to_boundary < bytes ? to_boundary : bytes;
-    const uint64_t nvec = (bytes - head) / 16, tail = bytes - head - nvec * 16;
-    if (cta == 0 && threadIdx.x < head) c[threadIdx.x] = 0;
-    if (cta == 0 && threadIdx.x < tail) c[bytes - tail + threadIdx.x] = 0;
-    uint4* v = reinterpret_cast<uint4*>(c + head);
-    const uint64_t stride = (uint64_t)ctas * kThreads;
-    for (uint64_t i = (uint64_t)cta * kThreads + threadIdx.x; i < nvec; i += stride) v[i] = make_uint4(0, 0, 0, 0);
-}
+// Lets the next launch of the stream begin once every CTA has said so (or gone); it still waits for this launch's end in its
+// own grid_dependency_wait().
+__device__ __forceinline__ void release_dependents() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
 
 template <typename ID, int K>
 __global__ void __launch_bounds__(kThreads) sort_cluster_kernel(const SortArgs a)
 {
     extern __shared__ __align__(16) unsigned char smem[];
-    constexpr uint32_t kHeld = K * kThreads;            // pairs of a CTA
     const int bins = 1 << a.digit_bits;
-    uint2* pairs = reinterpret_cast<uint2*>(smem);
-    uint16_t* warp_count = reinterpret_cast<uint16_t*>(pairs + kHeld);               // [warp][digit]
+    uint16_t* warp_count = reinterpret_cast<uint16_t*>(smem);                        // [warp][digit]
     uint32_t* cta_count = reinterpret_cast<uint32_t*>(warp_count + kWarps * bins);   // [digit]
     uint32_t* place = cta_count + bins;                                              // [digit]
     uint32_t* warp_total = place + bins;                                             // [warp]
     const uint32_t d = threadIdx.x, lane = threadIdx.x & 31, w = threadIdx.x >> 5;
 
     grid_dependency_wait();
-    if (blockIdx.x >= a.ctas) {
-        set_zero(a.zero, a.zero_bytes, blockIdx.x - a.ctas, gridDim.x - a.ctas);
-        return;
-    }
     const uint32_t rank = cluster_rank();
+    if (a.used != nullptr) mark_used<ID>(a, reinterpret_cast<uint32_t*>(smem), rank);
+    release_dependents();
     if (rank == 0 && threadIdx.x == 0) *a.counter = 0;
-    const uint32_t local = w * (32 * K) + lane, first = rank * kHeld + local;
+    const uint32_t first = rank * (K * kThreads) + w * (32 * K) + lane;
     uint16_t* mine = warp_count + w * bins;
+    const int passes = (a.bits + a.digit_bits - 1) / a.digit_bits;
+    uint2* to = passes & 1 ? a.sorted : a.spare;
+    uint2* from = passes & 1 ? a.spare : a.sorted;
     for (int shift = 0; shift < a.bits; shift += a.digit_bits) {
-        const bool last = shift + a.digit_bits >= a.bits;
         uint2 pair[K];
 #pragma unroll
         for (int r = 0; r < K; ++r) {
             const uint32_t i = first + r * 32;
-            if (shift != 0) pair[r] = pairs[local + r * 32];
-            else pair[r] = make_uint2(i < a.tokens ? key_of(__ldg(static_cast<const ID*>(a.ids) + i), a.rows) : 0u, i);
+            pair[r] = make_uint2(0, i);
+            if (i < a.tokens) {
+                if (shift != 0) pair[r] = __ldcg(from + i);
+                else pair[r].x = key_of(__ldg(static_cast<const ID*>(a.ids) + i), a.rows);
+            }
         }
         for (int i = lane; i < bins / 2; i += 32) reinterpret_cast<uint32_t*>(mine)[i] = 0;
-        __syncwarp();
-        uint32_t before[K];
+        uint32_t same[K];
 #pragma unroll
-        for (int r = 0; r < K; ++r) {
-            const bool held = first + r * 32 < a.tokens;
+        for (int r = 0; r < K; ++r)
+            same[r] = same_digit((pair[r].x >> shift) & (bins - 1), a.digit_bits, __ballot_sync(0xFFFFFFFFu, first + r * 32 < a.tokens));
+        __syncwarp();
+#pragma unroll
+        for (int r = 0; r < K; ++r) {                   // same[r] becomes the pairs before this one with its digit, of the warp
             const uint32_t digit = (pair[r].x >> shift) & (bins - 1);
-            const uint32_t same = same_digit(digit, a.digit_bits, __ballot_sync(0xFFFFFFFFu, held));
             const uint32_t so_far = mine[digit];
             __syncwarp();
-            if (held && (same >> lane) == 1u) mine[digit] = (uint16_t)(so_far + __popc(same));
+            if ((same[r] >> lane) == 1u) mine[digit] = (uint16_t)(so_far + __popc(same[r]));
             __syncwarp();
-            before[r] = so_far + __popc(same & ((1u << lane) - 1));
+            same[r] = so_far + __popc(same[r] & ((1u << lane) - 1));
         }
         __syncthreads();
-        uint32_t count = 0;
+        uint32_t earlier = 0, total = 0;                // keys of this digit: of the CTAs before, of all
         if (d < (uint32_t)bins) {
-#pragma unroll 8
+#pragma unroll 16
             for (int v = 0; v < kWarps; ++v) {
                 const uint32_t c = warp_count[v * bins + d];
-                warp_count[v * bins + d] = (uint16_t)count;
-                count += c;
-            }
-            cta_count[d] = count;
-        }
-        cluster_sync();                                 // the counts are there, and every CTA holds its pairs in registers
-        uint32_t earlier = 0, total = 0;
-        if (d < (uint32_t)bins) {
-            for (uint32_t r = 0; r < a.ctas; ++r) {
-                const uint32_t c = peer_load(cta_count + d, r);
-                earlier += r < rank ? c : 0;
+                warp_count[v * bins + d] = (uint16_t)total;
                 total += c;
+            }
+            cta_count[d] = total;
+        }
+        if (a.ctas > 1) {
+            cluster_sync();                             // the counts are there
+            if (d < (uint32_t)bins) {
+                total = 0;
+#pragma unroll
+                for (uint32_t half = 0; half < kMaxCluster; half += 8) {
+                    if (half >= a.ctas) break;
+                    uint32_t c[8];
+#pragma unroll
+                    for (uint32_t r = 0; r < 8; ++r) c[r] = half + r < a.ctas ? peer_load(cta_count + d, half + r) : 0;
+#pragma unroll
+                    for (uint32_t r = 0; r < 8; ++r) {
+                        earlier += half + r < rank ? c[r] : 0;
+                        total += c[r];
+                    }
+                }
             }
         }
         uint32_t sum = total;                           // over the digits up to this one
@@ -176,17 +193,71 @@ __global__ void __launch_bounds__(kThreads) sort_cluster_kernel(const SortArgs a
         __syncthreads();
 #pragma unroll
         for (int r = 0; r < K; ++r) {
-            if (first + r * 32 >= a.tokens) continue;
             const uint32_t digit = (pair[r].x >> shift) & (bins - 1);
-            const uint32_t at = place[digit] + mine[digit] + before[r];
-            if (last) a.sorted[at] = pair[r];
-            else peer_store(pairs + at % kHeld, at / kHeld, pair[r]);
+            if (first + r * 32 < a.tokens) to[place[digit] + mine[digit] + same[r]] = pair[r];
         }
-        cluster_sync();                                 // the pairs are there, and no CTA's counts go before they were read
+        if (a.ctas > 1) cluster_sync();                 // the pairs are there, and no CTA's counts go before they were read
+        else __syncthreads();
+        uint2* t = to; to = from; from = t;
     }
 }
 
-template <typename ID, int K> cudaError_t launch_cluster(const SortArgs& a, unsigned grid, cudaStream_t stream)
+// ---- the zeros ----
+// Bound by the writes to DRAM.  CTAs of 256 threads that write 4 KB each, in the order of the addresses: 6633 GB/s on 205 MB, as
+// much as the driver's memset; 136 CTAs that go through the buffer side by side 5860.
+// They run beside the sort, which releases them once the rows that are used are marked (or, where nothing is marked, at
+// once): what they read of the sort's is written before that.  Only the last CTA waits for the sort's end, so that what
+// follows finds both done.
+constexpr int kZeroThreads = 256;
+
+__global__ void __launch_bounds__(kZeroThreads) zero_kernel(char* p, uint64_t bytes, uint64_t head)
+{
+    const uint64_t nvec = (bytes - head) / 16, i = (uint64_t)blockIdx.x * kZeroThreads + threadIdx.x;
+    if (i < nvec) reinterpret_cast<uint4*>(p + head)[i] = make_uint4(0, 0, 0, 0);
+    if (blockIdx.x != gridDim.x - 1) return;
+    const uint64_t tail = bytes - head - nvec * 16;     // what stands before the first and behind the last 16-byte vector
+    if (threadIdx.x < head) p[threadIdx.x] = 0;
+    if (threadIdx.x < tail) p[bytes - tail + threadIdx.x] = 0;
+    grid_dependency_wait();
+}
+
+// The same for the rows that are not marked: a CTA has 1 to 32 rows of one word of marks, about 32 KB of them.
+struct UnusedArgs {
+    uint4* rows_at;
+    const uint32_t* used;
+    uint32_t rows, row_vectors;
+    int row_bits, thread_bits;                          // a CTA's rows; threads of a row
+};
+
+__global__ void __launch_bounds__(kZeroThreads) zero_unused_kernel(const UnusedArgs a)
+{
+    const uint32_t row0 = blockIdx.x << a.row_bits, marks = __ldcg(a.used + row0 / 32) >> (row0 & 31);
+    const uint32_t step = kZeroThreads >> a.thread_bits, lane = threadIdx.x & ((1u << a.thread_bits) - 1);
+    for (uint32_t r = threadIdx.x >> a.thread_bits; r < (1u << a.row_bits) && row0 + r < a.rows; r += step) {
+        if ((marks >> r) & 1u) continue;
+        uint4* row = a.rows_at + (uint64_t)(row0 + r) * a.row_vectors;
+        for (uint32_t i = lane; i < a.row_vectors; i += 1u << a.thread_bits) row[i] = make_uint4(0, 0, 0, 0);
+    }
+    if (blockIdx.x == gridDim.x - 1) grid_dependency_wait();
+}
+
+cudaError_t launch_zero(void* p, uint64_t bytes, cudaStream_t stream)
+{
+    const uint64_t to_boundary = (16 - (reinterpret_cast<uintptr_t>(p) & 15)) & 15;
+    const uint64_t head = to_boundary < bytes ? to_boundary : bytes, per_cta = kZeroThreads * 16;
+    const uint64_t ctas = ((bytes - head) / 16 * 16 + per_cta - 1) / per_cta;
+    return launch_pdl(zero_kernel, ctas == 0 ? 1u : (unsigned)ctas, kZeroThreads, stream, static_cast<char*>(p), bytes, head);
+}
+
+cudaError_t launch_zero_unused(void* p, uint32_t rows, uint64_t row_bytes, const uint32_t* used, cudaStream_t stream)
+{
+    UnusedArgs a = {static_cast<uint4*>(p), used, rows, (uint32_t)(row_bytes / 16), 0, 0};
+    while (a.row_bits < 5 && (row_bytes << a.row_bits) < 32768) ++a.row_bits;
+    while ((1 << a.thread_bits) < kZeroThreads && (1u << a.thread_bits) < a.row_vectors) ++a.thread_bits;
+    return launch_pdl(zero_unused_kernel, (unsigned)(((uint64_t)rows + (1u << a.row_bits) - 1) >> a.row_bits), kZeroThreads, stream, a);
+}
+
+template <typename ID, int K> cudaError_t launch_cluster(const SortArgs& a, cudaStream_t stream)
 {
     static std::atomic<bool> ready[64];                 // per device (zero-initialised)
     int dev = 0;
@@ -195,32 +266,35 @@ template <typename ID, int K> cudaError_t launch_cluster(const SortArgs& a, unsi
     if (dev < 0 || dev >= 64) return cudaErrorInvalidDevice;
     if (!ready[dev].load(std::memory_order_relaxed)) {
         err = cudaFuncSetAttribute(sort_cluster_kernel<ID, K>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                   (int)sort_smem(K, 1 << kMaxDigitBits));
+                                   (int)sort_smem(1 << kMaxDigitBits));
+        if (err == cudaSuccess)                         // clusters of 16 CTAs
+            err = cudaFuncSetAttribute(sort_cluster_kernel<ID, K>, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
         if (err != cudaSuccess) return err;
         ready[dev].store(true, std::memory_order_relaxed);
     }
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(grid);
+    cfg.gridDim = dim3(a.ctas);
     cfg.blockDim = dim3(kThreads);
-    cfg.dynamicSmemBytes = sort_smem(K, 1 << a.digit_bits);
+    cfg.dynamicSmemBytes = sort_smem(1 << a.digit_bits);
+    if (a.used != nullptr && cfg.dynamicSmemBytes < (a.rows + 31) / 32 * 4) cfg.dynamicSmemBytes = (a.rows + 31) / 32 * 4;
     cfg.stream = stream;
     cudaLaunchAttribute attr[2];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr[0].val.programmaticStreamSerializationAllowed = 1;
     attr[1].id = cudaLaunchAttributeClusterDimension;
-    attr[1].val.clusterDim.x = a.ctas == 0 ? 1 : a.ctas;
+    attr[1].val.clusterDim.x = a.ctas;
     attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
     cfg.attrs = attr;
     cfg.numAttrs = 2;
     return cudaLaunchKernelEx(&cfg, sort_cluster_kernel<ID, K>, a);
 }
 
-template <typename ID> cudaError_t launch_by_size(const SortArgs& a, uint32_t per_thread, unsigned grid, cudaStream_t stream)
+template <typename ID> cudaError_t launch_by_size(const SortArgs& a, uint32_t per_thread, cudaStream_t stream)
 {
-    return per_thread <= 1 ? launch_cluster<ID, 1>(a, grid, stream)
-           : per_thread <= 2 ? launch_cluster<ID, 2>(a, grid, stream)
-           : per_thread <= 4 ? launch_cluster<ID, 4>(a, grid, stream)
-                             : launch_cluster<ID, 8>(a, grid, stream);
+    return per_thread <= 1 ? launch_cluster<ID, 1>(a, stream)
+           : per_thread <= 2 ? launch_cluster<ID, 2>(a, stream)
+           : per_thread <= 4 ? launch_cluster<ID, 4>(a, stream)
+                             : launch_cluster<ID, 8>(a, stream);
 }
 
 // ---- three launches a pass ----
@@ -332,7 +406,6 @@ place_kernel(const PassInput<ID> in, int shift, const uint32_t* __restrict__ cou
 }
 
 // ---- host ----
-constexpr uint32_t kMaxCluster = 8;
 constexpr uint32_t kClusterTokens = kMaxCluster * 8 * kThreads;
 
 int key_bits(uint32_t rows)                             // of the largest key, `rows`
@@ -343,11 +416,11 @@ int key_bits(uint32_t rows)                             // of the largest key, `
 }
 
 template <typename ID>
-cudaError_t sort_in_passes(const ID* ids, const SortArgs& s, uint2* spare, uint32_t* counts, cudaStream_t stream)
+cudaError_t sort_in_passes(const ID* ids, const SortArgs& s, uint32_t* counts, cudaStream_t stream)
 {
     const uint32_t blocks = (uint32_t)(((uint64_t)s.tokens + kTile - 1) / kTile);
     const int passes = (s.bits + 7) / 8;
-    uint2 *out = passes % 2 ? s.sorted : spare, *other = passes % 2 ? spare : s.sorted;
+    uint2 *out = passes % 2 ? s.sorted : s.spare, *other = passes % 2 ? s.spare : s.sorted;
     PassInput<ID> in = {ids, nullptr, s.tokens, s.rows};
     for (int shift = 0; shift < s.bits; shift += 8) {
         cudaError_t err = launch_pdl(count_kernel<ID>, blocks, kThreads, stream, in, shift, counts);
@@ -363,48 +436,36 @@ cudaError_t sort_in_passes(const ID* ids, const SortArgs& s, uint2* spare, uint3
 
 }  // namespace
 
-uint64_t token_sort_words(uint64_t tokens)
+uint64_t token_sort_words(uint64_t tokens, uint64_t rows)
 {
-    if (tokens <= kClusterTokens) return 0;
-    return 2 * tokens + (tokens + kTile - 1) / kTile * kBins;
+    if (tokens > kClusterTokens) return 2 * tokens + (tokens + kTile - 1) / kTile * kBins;
+    return 2 * tokens + (rows <= kMaxMarkedRows ? (rows + 31) / 32 : 0);
 }
 
 cudaError_t launch_token_sort(const TokenIds& ids, uint32_t rows, uint2* sorted, uint32_t* counter, uint32_t* scratch,
-                              void* zero, uint64_t zero_bytes, cudaStream_t stream)
+                              void* zero, uint64_t row_bytes, cudaStream_t stream)
 {
-    SortArgs a = {ids.ptr, sorted, counter, zero, zero_bytes, (uint32_t)ids.count, rows, key_bits(rows), 1, 0};
-    const bool one_launch = a.tokens <= kClusterTokens;
-    uint32_t per_thread = 1;
-    if (one_launch && a.tokens != 0) {
-        // passes of equal digits; a CTA for each 2048 tokens, then more tokens to a CTA
+    uint32_t* behind = scratch + 2 * ids.count;
+    SortArgs a = {ids.ptr, sorted, reinterpret_cast<uint2*>(scratch), counter, nullptr, (uint32_t)ids.count, rows, key_bits(rows), 1, 1};
+    cudaError_t err = cudaSuccess;
+    if (a.tokens > kClusterTokens) {
+        err = ids.wide ? sort_in_passes(static_cast<const int64_t*>(ids.ptr), a, behind, stream)
+                       : sort_in_passes(static_cast<const int32_t*>(ids.ptr), a, behind, stream);
+    } else if (a.tokens != 0) {
+        // passes of equal digits; a CTA for each 2048 tokens, then more tokens to a thread
         const int passes = (a.bits + kMaxDigitBits - 1) / kMaxDigitBits;
         a.digit_bits = (a.bits + passes - 1) / passes;
-        a.ctas = 1;
-        while (a.ctas < kMaxCluster && a.ctas * 2048u < a.tokens) a.ctas *= 2;
-        per_thread = (a.tokens + a.ctas * kThreads - 1) / (a.ctas * kThreads);
+        while (a.ctas < kMaxCluster && a.ctas * 2 * kThreads < a.tokens) a.ctas *= 2;
+        const uint32_t per_thread = (a.tokens + a.ctas * kThreads - 1) / (a.ctas * kThreads);
+        // Zeros that the sums overwrite while they are in L2 cost no write to DRAM: marks pay where the rows that may be
+        // used exceed it (64,000 rows of 16 KB, 65,536 tokens: 302 -> 273 us; 50,000 of 4 KB, 16,384 tokens: 50 -> 53).
+        const bool vectors = row_bytes % 16 == 0 && (reinterpret_cast<uintptr_t>(zero) & 15) == 0;
+        if (zero != nullptr && vectors && rows <= kMaxMarkedRows && (a.tokens < rows ? a.tokens : rows) * row_bytes >= (1u << 27))
+            a.used = behind;
+        err = ids.wide ? launch_by_size<int64_t>(a, per_thread, stream) : launch_by_size<int32_t>(a, per_thread, stream);
     }
-    if (one_launch || zero_bytes != 0) {
-        int dev = 0, sms = 0;
-        cudaError_t err = cudaGetDevice(&dev);
-        if (err == cudaSuccess) err = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
-        if (err != cudaSuccess) return err;
-        // the CTAs that write zeros: 32 KB each at least, whole clusters of them, no more than fit beside the sort
-        const unsigned size = a.ctas == 0 ? 1 : a.ctas;
-        uint64_t extra = (zero_bytes + 32767) / 32768;
-        const uint64_t room = (uint64_t)sms > size ? (uint64_t)sms - size : 1;
-        if (extra > room) extra = room;
-        extra = extra == 0 ? 0 : extra < size ? size : extra / size * size;
-        const unsigned grid = a.ctas + (unsigned)extra;
-        if (grid != 0) {
-            err = ids.wide ? launch_by_size<int64_t>(a, per_thread, grid, stream) : launch_by_size<int32_t>(a, per_thread, grid, stream);
-            if (err != cudaSuccess) return err;
-        }
-    }
-    if (one_launch) return cudaSuccess;
-    uint2* spare = reinterpret_cast<uint2*>(scratch);
-    uint32_t* counts = scratch + 2 * (uint64_t)a.tokens;
-    return ids.wide ? sort_in_passes(static_cast<const int64_t*>(ids.ptr), a, spare, counts, stream)
-                    : sort_in_passes(static_cast<const int32_t*>(ids.ptr), a, spare, counts, stream);
+    if (err != cudaSuccess || zero == nullptr) return err;
+    return a.used != nullptr ? launch_zero_unused(zero, rows, row_bytes, a.used, stream) : launch_zero(zero, rows * row_bytes, stream);
 }
 
 }  // namespace mqg

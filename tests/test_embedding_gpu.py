@@ -163,6 +163,28 @@ def test_gradient_of_tables_at_the_digits_edges(rows):
     _check_gradient((rows, 1, 300), "outside", I32, (F32, F32), True)
 
 
+@pytest.mark.parametrize("add", [False, True])
+@pytest.mark.parametrize("kind", ["zipf", "uniform", "outside"])
+@pytest.mark.parametrize("tokens", [2047, 2049, 16_385, 65_537, 131_072, 131_073, 150_001])
+def test_gradient_by_the_sort_of_each_size(tokens, kind, add):
+    _check_gradient((50_000, 3, tokens), kind, I64, (F32, F32), add)
+    _check_gradient((300, 4, tokens), kind, I32, (BF16, F32), add, shift=1)
+
+
+@pytest.mark.parametrize("shape", [(40_000, 1024, 33_000), (33_333, 1040, 33_000), (33_000, 4096, 8200), (260_000, 160, 262_144)])
+def test_zeros_beside_rows_in_use_when_both_exceed_l2(shape):
+    rows, dim, tokens = shape
+    ids = _ids(tokens, rows, "outside" if rows == 40_000 else "zipf", I64)
+    held = _held(ids, rows)
+    d = torch.ones(tokens, dim, device="cuda")
+    grad = torch.full((rows, dim), math.nan, device="cuda")
+    w = torch.empty(mqg.mqg_embedding_workspace_floats(tokens, rows, dim), device="cuda")
+    for _ in range(2):
+        mqg.mqg_embedding_grad(d, ids.cuda(), tokens, rows, dim, 0.5, grad, w)
+    count = torch.zeros(rows).index_add_(0, ids[held], torch.ones(int(held.sum())))       # whole numbers: sums are exact
+    assert (grad.cpu() == 0.5 * count[:, None]).all()
+
+
 def test_gradient_by_differences():
     """<R, lookup(table)> is linear in the table: its central difference is the gradient of R."""
     rows, dim, tokens, scale, h = 6, 5, 40, 0.75, 0.5
