@@ -3,12 +3,15 @@
 //   N = sqrt(sum over all elements of x^2)        c = 1 where N <= max_norm, else max_norm / N
 //   y = fl(c * x)
 //
-// The tensors are cut into tiles of 16 KB.  The measuring kernel's CTAs take the tiles in turn and leave one partial sum
-// each; every CTA of the kernel that scales then adds up the partial sums itself (at most 1184 of them for each launch of
-// the first kernel, from L2), so that there is no launch between the two, no atomic, and a fixed order of every sum.
-// Squares are summed in fp32 inside a thread's share of a tile (at most 32 of them) and in 64 bits from there on.  A share
+// The tensors are cut into tiles of 16 KB.  Up to eight of them are one launch, a cluster whose CTAs have a tile each.  Above that
+// the measuring kernel's CTAs take the tiles in turn and leave one partial sum each, in a fixed order and without atomics, and
+// every CTA of the kernel that scales adds them up itself (740 at most for each launch of the first kernel, from L2), so that
+// no launch stands between the two, or, for long lists, a third kernel does.  The second reading comes from DRAM all the same where the tensors and what is written exceed
+// about a quarter of L2: of 100 MB read twice, the second time backwards, 27 MB came from L2, whatever the eviction priorities.
+// Squares are summed in fp32 inside a thread's share of a tile (at most 33 of them) and in 64 bits from there on.  A share
 // whose sum of squares leaves the range where fp32 holds it is summed again in 64 bits: the norm is right for every finite
 // gradient, also where single squares overflow or vanish in fp32.
+#include <atomic>
 #include <cmath>
 
 #include "mqg_tma.cuh"
@@ -20,7 +23,13 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kTileBytes = 16384;
-constexpr int kMaxBlocks = 1184;                        // 8 CTAs for each of 148 SMs
+// CTAs that are there at once, for 148 SMs: 5 to an SM of the measuring kernel (eight spill their vectors), 4 of the one that
+// scales.
+constexpr int kNormBlocks = 740, kScaleBlocks = 592;
+// Above so many tiles a kernel of its own adds up the partial sums, and the one that scales has a CTA to a tile, which go
+// through memory in the order of its addresses: 122 MB of bf16 into 245 of fp32 in 54 us where CTAs that take tiles in turn need
+// 61.
+constexpr uint64_t kApartTiles = 2 * kScaleBlocks;
 
 // Tensors of one launch, passed by value: a kernel's parameters hold 32,764 bytes.
 template <int CAP> struct TensorTable {
@@ -30,63 +39,98 @@ template <int CAP> struct TensorTable {
     const void* ptr[CAP];
     uint8_t dtype[CAP];
 };
-constexpr int kSmallTable = 64, kLargeTable = 1024;
+constexpr int kLargeTable = 1024;
 
+// Where a tile lies.
+struct Tile {
+    const void* ptr;         // its first element
+    uint64_t at;             // elements before it in the whole list
+    uint32_t count;          // its elements
+    uint32_t before, behind; // elements of the tensor around it, as far as 16 bytes reach
+    int dtype;
+};
+
+// The tensor that a tile is in: the last one that starts at or before it.  All lanes of a warp look at once, at every k-th tensor
+// and then at k neighbours, with ordinary loads: a search by halves is ten dependent misses of the constant cache, which a
+// launch begins without its parameters.
 template <int CAP> __device__ __forceinline__ int find_tensor(const TensorTable<CAP>& tab, uint32_t tile)
 {
-    int lo = 0, hi = tab.count - 1;                     // the last tensor that starts at or before the tile
-    while (lo < hi) {
-        const int mid = (lo + hi + 1) >> 1;
-        if (tab.tile_start[mid] <= tile) lo = mid; else hi = mid - 1;
+    const uint32_t* start = tab.tile_start;
+    asm volatile("" : "+l"(start));                     // an address like any other
+    const int lane = threadIdx.x & 31, k = (tab.count + 31) / 32;
+    int base = 0;
+    if (CAP > 32 && k > 1) {
+        const uint32_t first = lane * k < tab.count ? start[lane * k] : ~0u;
+        base = (31 - __clz(__ballot_sync(0xFFFFFFFFu, first <= tile))) * k;
     }
-    return lo;
+    const uint32_t first = lane < k * (k == 1 ? 32 : 1) && base + lane < tab.count ? start[base + lane] : ~0u;
+    return base + 31 - __clz(__ballot_sync(0xFFFFFFFFu, first <= tile));
 }
 
-__device__ __forceinline__ double block_sum(double v)
+template <int CAP> __device__ __forceinline__ Tile tile_of(const TensorTable<CAP>& tab, int tensor, uint32_t tile)
 {
-    __shared__ double warp_sum[kThreads / 32];
+    Tile t;
+    t.dtype = tab.dtype[tensor];
+    const int shift = t.dtype == kF32 ? 2 : 1;
+    const uint64_t n = tab.first[tensor + 1] - tab.first[tensor];
+    const uint64_t e0 = (uint64_t)(tile - tab.tile_start[tensor]) * (kTileBytes >> shift);
+    t.ptr = static_cast<const char*>(tab.ptr[tensor]) + (e0 << shift);
+    t.at = tab.first[tensor] + e0;
+    t.count = (uint32_t)min((uint64_t)(kTileBytes >> shift), n - e0);
+    t.before = (uint32_t)min(e0, (uint64_t)8);
+    t.behind = (uint32_t)min(n - e0 - t.count, (uint64_t)8);
+    return t;
+}
+
+// A tile's elements before its first 16-byte boundary, its vectors and what is left behind them.
+template <int DTYPE> struct Parts {
+    static constexpr int V = 16 / kElemBytes<DTYPE>;
+    uint32_t head, nvec, tail, count;
+    __device__ __forceinline__ Parts(const void* p, uint32_t m) : count(m)
+    {
+        const uint32_t to_boundary = (uint32_t)((16 - (reinterpret_cast<uintptr_t>(p) & 15)) & 15) / kElemBytes<DTYPE>;
+        head = to_boundary < m ? to_boundary : m;
+        nvec = (m - head) / V;
+        tail = m - head - nvec * V;
+    }
+    // The element outside the vectors that thread i takes care of, if there is one.
+    __device__ __forceinline__ bool edge(uint32_t i, uint32_t& at) const
+    {
+        at = i < head ? i : count - tail + (i - head);
+        return i < head + tail;
+    }
+};
+
+template <int THREADS> __device__ __forceinline__ double block_sum(double v)
+{
+    __shared__ double warp_sum[THREADS / 32];
 #pragma unroll
     for (int d = 16; d > 0; d >>= 1) v += __shfl_xor_sync(0xFFFFFFFFu, v, d);
     if ((threadIdx.x & 31) == 0) warp_sum[threadIdx.x >> 5] = v;
     __syncthreads();
     double t = 0.0;
 #pragma unroll
-    for (int w = 0; w < kThreads / 32; ++w) t += warp_sum[w];
+    for (int w = 0; w < THREADS / 32; ++w) t += warp_sum[w];
     return t;
 }
 
-// What fp32 holds a sum of at most 32 squares in without loss: none overflows, and what vanishes of the smallest is below
+// What fp32 holds a sum of at most 33 squares in without loss: none overflows, and what vanishes of the smallest is below
 // 2^-40 of the sum.
 __device__ __forceinline__ bool squares_in_range(float s) { return s >= 0x1p-100f && s <= 0x1p120f; }
 
-// Sum of squares of m <= a tile's elements from p on, this thread's share.
-template <int DTYPE>
-__device__ __forceinline__ double tile_squares(const typename Element<DTYPE>::type* p, uint32_t m)
+// Sum of the squares of K vectors and an edge element.
+template <int DTYPE, int K>
+__device__ __forceinline__ double squares(const Packed<DTYPE, 16 / kElemBytes<DTYPE>> (&x)[K], float edge)
 {
-    constexpr int V = 16 / kElemBytes<DTYPE>, K = kTileBytes / 16 / kThreads;
-    const uint32_t to_boundary = (uint32_t)((16 - (reinterpret_cast<uintptr_t>(p) & 15)) & 15) / kElemBytes<DTYPE>;
-    const uint32_t head = to_boundary < m ? to_boundary : m;
-    const uint32_t nvec = (m - head) / V, tail = m - head - nvec * V;
-    Packed<DTYPE, V> x[K];
-#pragma unroll
-    for (int k = 0; k < K; ++k) {
-        const uint32_t i = threadIdx.x + k * kThreads;
-        if (i < nvec) x[k].load(p + head + i * V);
-        else x[k].w[0] = make_uint4(0, 0, 0, 0);
-    }
-    float edge = 0.0f;                                  // the elements before the first and behind the last vector
-    if (threadIdx.x < head) edge = widen(p[threadIdx.x]);
-    else if (threadIdx.x < head + tail) edge = widen(p[m - tail + (threadIdx.x - head)]);
-    float s[K];
-#pragma unroll
-    for (int k = 0; k < K; ++k) {
-        s[k] = x[k].get(0) * x[k].get(0);
-#pragma unroll
-        for (int e = 1; e < V; ++e) s[k] = __fmaf_rn(x[k].get(e), x[k].get(e), s[k]);
-    }
+    constexpr int V = 16 / kElemBytes<DTYPE>;
     float t = edge * edge;
 #pragma unroll
-    for (int k = 0; k < K; ++k) t += s[k];
+    for (int k = 0; k < K; ++k) {
+        float s = x[k].get(0) * x[k].get(0);
+#pragma unroll
+        for (int e = 1; e < V; ++e) s = __fmaf_rn(x[k].get(e), x[k].get(e), s);
+        t += s;
+    }
     if (squares_in_range(t)) return (double)t;
     double d = (double)edge * (double)edge;
 #pragma unroll
@@ -96,45 +140,68 @@ __device__ __forceinline__ double tile_squares(const typename Element<DTYPE>::ty
     return d;
 }
 
+// This thread's share of a tile's sum of squares.
+template <int DTYPE> __device__ __forceinline__ double tile_squares(const Tile& t)
+{
+    constexpr int V = 16 / kElemBytes<DTYPE>, K = kTileBytes / 16 / kThreads;
+    const auto* p = static_cast<const typename Element<DTYPE>::type*>(t.ptr);
+    const Parts<DTYPE> parts(p, t.count);
+    Packed<DTYPE, V> x[K];
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+        const uint32_t i = threadIdx.x + k * kThreads;
+        if (i < parts.nvec) x[k].load(p + parts.head + i * V);
+        else x[k].w[0] = make_uint4(0, 0, 0, 0);
+    }
+    uint32_t at;
+    const float edge = parts.edge(threadIdx.x, at) ? widen(p[at]) : 0.0f;
+    return squares<DTYPE, K>(x, edge);
+}
+
+// Bound by reading the tensors.  (CTAs of eight neighbouring tiles each, in the order of the addresses: 78.9 us on 500 MB against
+// 79.6, and a turn of a few CTAs more on shorter lists.)
 template <int CAP>
-__global__ void __launch_bounds__(kThreads)
+__global__ void __launch_bounds__(kThreads, kNormBlocks / 148)
 norm_kernel(const __grid_constant__ TensorTable<CAP> tab, double* __restrict__ partial)
 {
     const uint32_t ntiles = tab.tile_start[tab.count];
     double sum = 0.0;
+    Tile t = tile_of(tab, find_tensor(tab, blockIdx.x), blockIdx.x);
     grid_dependency_wait();
-    for (uint32_t tile = blockIdx.x; tile < ntiles; tile += gridDim.x) {
-        const int j = find_tensor(tab, tile);
-        const uint64_t n = tab.first[j + 1] - tab.first[j];
-        const uint32_t at = tile - tab.tile_start[j];
-        if (tab.dtype[j] == kF32) {
-            constexpr uint32_t E = kTileBytes / 4;
-            const uint64_t e0 = (uint64_t)at * E;
-            sum += tile_squares<kF32>(static_cast<const float*>(tab.ptr[j]) + e0, (uint32_t)min((uint64_t)E, n - e0));
-        } else {
-            constexpr uint32_t E = kTileBytes / 2;
-            const uint64_t e0 = (uint64_t)at * E;
-            sum += tile_squares<kBf16>(static_cast<const __nv_bfloat16*>(tab.ptr[j]) + e0, (uint32_t)min((uint64_t)E, n - e0));
-        }
+    for (uint32_t tile = blockIdx.x; tile < ntiles;) {
+        sum += t.dtype == kF32 ? tile_squares<kF32>(t) : tile_squares<kBf16>(t);
+        tile += gridDim.x;
+        if (tile < ntiles) t = tile_of(tab, find_tensor(tab, tile), tile);
     }
-    sum = block_sum(sum);
+    sum = block_sum<kThreads>(sum);
     if (threadIdx.x == 0) partial[blockIdx.x] = sum;
 }
 
-// The clipping factor from the partial sums, the same in every CTA.  The norm is compared and divided in 64 bits; a NaN
-// among the elements makes the norm and the factor NaN, an infinity makes the factor 0.
-__device__ __forceinline__ float factor_of(const double* partial, int npartial, float max_norm, float* norm)
+// The factor for a sum of squares S, and the norm, in 64 bits: 1 / sqrt(S) by one step of Newton's iteration from fp32's
+// reciprocal root of S scaled to 1 .. 4 (an error of 2^-21 becomes 2^-41).  A division and a square root in 64 bits took every CTA
+// that scales longer than adding up the partial sums.  A NaN among the elements makes norm and factor NaN, an infinity makes
+// the factor 0.
+__device__ __forceinline__ float factor_of(double s, float max_norm, float* norm)
 {
-    double s = 0.0;
-    for (int i = threadIdx.x; i < npartial; i += kThreads) s += __ldcg(partial + i);
-    const double n = sqrt(block_sum(s));
+    const int high = __double2hiint(s), even = ((high >> 20) - 1023) & ~1;          // exponent of the scale 2^even <= S
+    if (!(s > 0.0) || (high >> 20) == 0x7FF) {          // zero, infinity, NaN
+        *norm = (float)s;
+        return s <= (double)max_norm ? 1.0f : s > 0.0 ? 0.0f : (float)s;
+    }
+    const double m = __hiloint2double(high - (even << 20), __double2loint(s)), y0 = (double)rsqrtf((float)m);
+    const double y = fma(y0, fma(-0.5 * m * y0, y0, 0.5), y0);
+    const double up = __hiloint2double((even / 2 + 1023) << 20, 0), down = __hiloint2double((1023 - even / 2) << 20, 0);
+    const double n = m * y * up;
     *norm = (float)n;
-    return n <= (double)max_norm ? 1.0f : (float)((double)max_norm / n);
+    return n <= (double)max_norm ? 1.0f : (float)((double)max_norm * (y * down));
 }
 
-__device__ __forceinline__ void write_result(float* result, float norm, float factor)
+__device__ __forceinline__ double sum_of_partials(const double* partial, int count)
 {
-    if (blockIdx.x == 0 && threadIdx.x == 0) { result[0] = norm; result[1] = factor; }
+    double s = 0.0;
+#pragma unroll 4
+    for (int i = threadIdx.x; i < count; i += kThreads) s += __ldcg(partial + i);
+    return block_sum<kThreads>(s);
 }
 
 __global__ void __launch_bounds__(kThreads)
@@ -142,65 +209,98 @@ norm_result_kernel(const double* __restrict__ partial, int npartial, float max_n
 {
     grid_dependency_wait();
     float norm;
-    const float c = factor_of(partial, npartial, max_norm, &norm);
-    write_result(result, norm, c);
+    const float c = factor_of(sum_of_partials(partial, npartial), max_norm, &norm);
+    if (threadIdx.x == 0) { result[0] = norm; result[1] = c; }
 }
 
-// y[i] = c * x[i] for m <= a tile's elements, in place.
-template <int DTYPE>
-__device__ __forceinline__ void scale_tile(typename Element<DTYPE>::type* p, uint32_t m, float c)
+// y = c * x in place.
+template <int DTYPE> __device__ __forceinline__ void scale_tile(const Tile& t, float c)
 {
     constexpr int V = 16 / kElemBytes<DTYPE>, K = kTileBytes / 16 / kThreads;
-    const uint32_t to_boundary = (uint32_t)((16 - (reinterpret_cast<uintptr_t>(p) & 15)) & 15) / kElemBytes<DTYPE>;
-    const uint32_t head = to_boundary < m ? to_boundary : m;
-    const uint32_t nvec = (m - head) / V, tail = m - head - nvec * V;
+    auto* p = static_cast<typename Element<DTYPE>::type*>(const_cast<void*>(t.ptr));
+    const Parts<DTYPE> parts(p, t.count);
     Packed<DTYPE, V> x[K];
 #pragma unroll
     for (int k = 0; k < K; ++k) {
         const uint32_t i = threadIdx.x + k * kThreads;
-        if (i < nvec) x[k].load(p + head + i * V);
+        if (i < parts.nvec) x[k].load(p + parts.head + i * V);
+    }
+    uint32_t at;
+    if (parts.edge(threadIdx.x, at)) narrow(c * widen(p[at]), p[at]);
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+        const uint32_t i = threadIdx.x + k * kThreads;
+        if (i >= parts.nvec) continue;
+#pragma unroll
+        for (int e = 0; e < V; ++e) x[k].set(e, c * x[k].get(e));
+        x[k].store(p + parts.head + i * V);
+    }
+}
+
+// W elements of x from the aligned word that holds the first of them and the next word; `bytes` lie before it in the word.
+template <int DTYPE, int W>
+__device__ __forceinline__ Packed<DTYPE, W> load_across(const typename Element<DTYPE>::type* x, uint32_t bytes)
+{
+    constexpr int N = W * kElemBytes<DTYPE> / 4;         // 32-bit words of a word
+    const auto* aligned = reinterpret_cast<const typename Element<DTYPE>::type*>(reinterpret_cast<const char*>(x) - bytes);
+    union { Packed<DTYPE, W> p[2]; uint32_t w[2 * N]; } in;
+    union { Packed<DTYPE, W> p; uint32_t w[N]; } out;
+#pragma unroll
+    for (int k = 0; k < 2; ++k) in.p[k].w[0] = reinterpret_cast<const typename Packed<DTYPE, W>::word*>(aligned)[k];
+    const uint32_t words = bytes / 4, bits = bytes % 4 * 8;
+#pragma unroll
+    for (int k = 0; k < N; ++k) {
+        uint32_t lo = in.w[k], hi = in.w[k + 1];
+#pragma unroll
+        for (int q = 1; q < N; ++q)
+            if (words == (uint32_t)q) { lo = in.w[k + q]; hi = k + q + 1 < 2 * N ? in.w[k + q + 1] : 0; }
+        out.w[k] = __funnelshift_r(lo, hi, bits);
+    }
+    return out.p;
+}
+
+// y = c * x into another buffer, by words of W elements from y's first 16-byte boundary on: 16 bytes of the wider type, so that
+// every access of a warp covers whole sectors.  Where x does not lie on its words' boundaries there, a word is put together from
+// the two that hold it.
+template <int SRC, int DST>
+__device__ __forceinline__ void copy_tile(const Tile& t, typename Element<DST>::type* y, float c)
+{
+    constexpr int W = 16 / (kElemBytes<SRC> > kElemBytes<DST> ? kElemBytes<SRC> : kElemBytes<DST>);
+    constexpr int K = kTileBytes / kElemBytes<SRC> / W / kThreads;
+    constexpr uint32_t kWord = W * kElemBytes<SRC>;
+    const auto* x = static_cast<const typename Element<SRC>::type*>(t.ptr);
+    const uint32_t to_boundary = (uint32_t)((16 - (reinterpret_cast<uintptr_t>(y) & 15)) & 15) / kElemBytes<DST>;
+    const uint32_t head = to_boundary < t.count ? to_boundary : t.count;
+    const uint32_t nvec = (t.count - head) / W, tail = t.count - head - nvec * W;
+    const uint32_t off = (uint32_t)(reinterpret_cast<uintptr_t>(x + head) & (kWord - 1));
+    // words that lie in the tensor with all that is read for them
+    const uint32_t lead = off / kElemBytes<SRC>, from = lead <= head + t.before ? 0u : 1u;
+    const uint32_t to = off == 0 || tail + t.behind + lead >= (uint32_t)W ? nvec : nvec == 0 ? 0u : nvec - 1;
+    Packed<SRC, W> in[K];
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+        const uint32_t i = threadIdx.x + k * kThreads;
+        if (off == 0) {
+            if (i < nvec) in[k].load(x + head + i * W);
+        } else if (i >= from && i < to) {
+            in[k] = load_across<SRC, W>(x + head + i * W, off);
+        } else if (i < nvec) {
+#pragma unroll
+            for (int e = 0; e < W; ++e) in[k].e[e] = x[head + i * W + e];
+        }
     }
     if (threadIdx.x < head + tail) {
-        const uint32_t i = threadIdx.x < head ? threadIdx.x : m - tail + (threadIdx.x - head);
-        narrow(c * widen(p[i]), p[i]);
+        const uint32_t i = threadIdx.x < head ? threadIdx.x : t.count - tail + (threadIdx.x - head);
+        narrow(c * widen(x[i]), y[i]);
     }
 #pragma unroll
     for (int k = 0; k < K; ++k) {
         const uint32_t i = threadIdx.x + k * kThreads;
         if (i >= nvec) continue;
+        Packed<DST, W> out;
 #pragma unroll
-        for (int e = 0; e < V; ++e) x[k].set(e, c * x[k].get(e));
-        x[k].store(p + head + i * V);
-    }
-}
-
-// y[i] = c * x[i] for m elements, x and y of different buffers: vectors from y's first 16-byte boundary on; x is read by
-// vectors where it is on a boundary there, else element by element.
-template <int SRC, int DST>
-__device__ __forceinline__ void copy_tile(const typename Element<SRC>::type* x, typename Element<DST>::type* y, uint32_t m, float c)
-{
-    constexpr int V = 16 / (kElemBytes<SRC> > kElemBytes<DST> ? kElemBytes<DST> : kElemBytes<SRC>);
-    constexpr int W = Packed<SRC, V>::kWordBytes;
-    const uint32_t to_boundary = (uint32_t)((16 - (reinterpret_cast<uintptr_t>(y) & 15)) & 15) / kElemBytes<DST>;
-    const uint32_t head = to_boundary < m ? to_boundary : m;
-    const uint32_t nvec = (m - head) / V, tail = m - head - nvec * V;
-    const bool together = (reinterpret_cast<uintptr_t>(x + head) & (W - 1)) == 0;
-    if (threadIdx.x < head + tail) {
-        const uint32_t i = threadIdx.x < head ? threadIdx.x : m - tail + (threadIdx.x - head);
-        narrow(c * widen(x[i]), y[i]);
-    }
-    for (uint32_t i = threadIdx.x; i < nvec; i += kThreads) {
-        const uint32_t at = head + i * V;
-        Packed<SRC, V> in;
-        if (together) in.load(x + at);
-        else {
-#pragma unroll
-            for (int e = 0; e < V; ++e) in.e[e] = x[at + e];
-        }
-        Packed<DST, V> out;
-#pragma unroll
-        for (int e = 0; e < V; ++e) out.set(e, c * in.get(e));
-        out.store(y + at);
+        for (int e = 0; e < W; ++e) out.set(e, c * in[k].get(e));
+        out.store(y + head + i * W);
     }
 }
 
@@ -211,52 +311,165 @@ __global__ void __launch_bounds__(kThreads)
 scale_kernel(const __grid_constant__ TensorTable<CAP> tab, const double* __restrict__ partial, int npartial, float max_norm,
              const float* __restrict__ factor, void* __restrict__ flat, float* __restrict__ result)
 {
-    const uint32_t ntiles = tab.tile_start[tab.count];
+    uint32_t tile = tab.tile_start[tab.count] - 1 - blockIdx.x;
+    Tile t = tile_of(tab, find_tensor(tab, tile), tile);
     grid_dependency_wait();
     float c;
     if (partial != nullptr) {
         float norm;
-        c = factor_of(partial, npartial, max_norm, &norm);
-        if (result != nullptr) write_result(result, norm, c);
+        c = factor_of(sum_of_partials(partial, npartial), max_norm, &norm);
+        if (result != nullptr && blockIdx.x == 0 && threadIdx.x == 0) { result[0] = norm; result[1] = c; }
     } else {
         c = __ldcg(factor);
     }
     if (DST < 0 && c == 1.0f) return;                   // every product would be its own factor
-    for (uint32_t i = blockIdx.x; i < ntiles; i += gridDim.x) {
-        const uint32_t tile = ntiles - 1 - i;
-        const int j = find_tensor(tab, tile);
-        const uint64_t n = tab.first[j + 1] - tab.first[j];
-        const uint32_t at = tile - tab.tile_start[j];
-        const uint32_t E = tab.dtype[j] == kF32 ? kTileBytes / 4 : kTileBytes / 2;
-        const uint64_t e0 = (uint64_t)at * E;
-        const uint32_t m = (uint32_t)min((uint64_t)E, n - e0);
+    for (;;) {
         if constexpr (DST < 0) {
-            if (tab.dtype[j] == kF32) scale_tile<kF32>(static_cast<float*>(const_cast<void*>(tab.ptr[j])) + e0, m, c);
-            else scale_tile<kBf16>(static_cast<__nv_bfloat16*>(const_cast<void*>(tab.ptr[j])) + e0, m, c);
+            if (t.dtype == kF32) scale_tile<kF32>(t, c);
+            else scale_tile<kBf16>(t, c);
         } else {
-            auto* y = static_cast<typename Element<DST>::type*>(flat) + tab.first[j] + e0;
-            if (tab.dtype[j] == kF32) copy_tile<kF32, DST>(static_cast<const float*>(tab.ptr[j]) + e0, y, m, c);
-            else copy_tile<kBf16, DST>(static_cast<const __nv_bfloat16*>(tab.ptr[j]) + e0, y, m, c);
+            auto* y = static_cast<typename Element<DST>::type*>(flat) + t.at;
+            if (t.dtype == kF32) copy_tile<kF32, DST>(t, y, c);
+            else copy_tile<kBf16, DST>(t, y, c);
         }
+        if (tile < gridDim.x) return;
+        tile -= gridDim.x;
+        t = tile_of(tab, find_tensor(tab, tile), tile);
     }
 }
 
-// params[i] <- fma(-lr, fl(c * acc[i]), params[i])
+// ---- one launch ----
+constexpr int kClusterThreads = kTileBytes / 16;        // a vector of the tile to each
+constexpr int kClusterTensors = 32;
+constexpr unsigned kClusterTiles = 8;
+
+__device__ __forceinline__ uint32_t cluster_rank()
+{
+    uint32_t rank;
+    asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank));
+    return rank;
+}
+__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
+__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
+__device__ __forceinline__ double peer_load(const double* p, uint32_t rank)
+{
+    uint32_t at;
+    double v;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"(smem_u32(p)), "r"(rank));
+    asm volatile("ld.shared::cluster.f64 %0, [%1];" : "=d"(v) : "r"(at) : "memory");
+    return v;
+}
+
+// The sum of squares of a cluster's CTAs.
+__device__ __forceinline__ double cluster_sum(double v)
+{
+    __shared__ double cta_sum;
+    v = block_sum<kClusterThreads>(v);
+    if (threadIdx.x == 0) cta_sum = v;
+    cluster_arrive();
+    cluster_wait();
+    double all = 0.0;
+    for (uint32_t r = 0; r < gridDim.x; ++r) all += peer_load(&cta_sum, r);
+    cluster_arrive();                                   // no CTA's sum goes before all have read it
+    return all;
+}
+
+// One tile: measured, and scaled as it is held.
+template <int SRC, int DST>
+__device__ __forceinline__ void clip_tile(const Tile& t, float max_norm, void* flat, float* result)
+{
+    constexpr int V = 16 / kElemBytes<SRC>;
+    const auto* p = static_cast<const typename Element<SRC>::type*>(t.ptr);
+    const Parts<SRC> parts(p, t.count);
+    const bool has_vector = threadIdx.x < parts.nvec;
+    Packed<SRC, V> x[1];
+    x[0].w[0] = make_uint4(0, 0, 0, 0);
+    if (has_vector) x[0].load(p + parts.head + threadIdx.x * V);
+    uint32_t at;
+    const bool has_edge = parts.edge(threadIdx.x, at);
+    const float edge = has_edge ? widen(p[at]) : 0.0f;
+    float norm;
+    const float c = factor_of(cluster_sum(squares<SRC, 1>(x, edge)), max_norm, &norm);
+    if (cluster_rank() == 0 && threadIdx.x == 0) { result[0] = norm; result[1] = c; }
+    if (DST == -2 || (DST == -1 && c == 1.0f)) return;
+    constexpr int D = DST < 0 ? SRC : DST;
+    using Out = typename Element<D>::type;
+    Out* y = DST < 0 ? static_cast<Out*>(const_cast<void*>(t.ptr)) : static_cast<Out*>(flat) + t.at;
+    if (has_edge) narrow(c * edge, y[at]);
+    if (!has_vector) return;
+    y += parts.head + threadIdx.x * V;
+    Packed<D, V> out;
+#pragma unroll
+    for (int e = 0; e < V; ++e) out.set(e, c * x[0].get(e));
+    if ((reinterpret_cast<uintptr_t>(y) & (Packed<D, V>::kWordBytes - 1)) == 0) {
+        out.store(y);
+    } else {
+#pragma unroll
+        for (int e = 0; e < V; ++e) y[e] = out.e[e];
+    }
+}
+
+// Bound by latency: the launch, one turn to memory, the barrier.  8 tiles: 3.5 us a call where two launches take 4.6; 25 tiles
+// in the same cluster 5.8, and clusters of 16 CTAs take 5.2 for whatever they hold.  DST: -1 in place, -2 only the norm.
+template <int DST>
+__global__ void __launch_bounds__(kClusterThreads)
+clip_cluster_kernel(const __grid_constant__ TensorTable<kClusterTensors> tab, float max_norm, void* __restrict__ flat,
+                    float* __restrict__ result)
+{
+    const uint32_t tile = cluster_rank();
+    if (tile >= tab.tile_start[tab.count]) {            // fills the cluster up, or there are no elements at all
+        grid_dependency_wait();
+        float norm;
+        const float c = factor_of(cluster_sum(0.0), max_norm, &norm);
+        if (tile == 0 && threadIdx.x == 0) { result[0] = norm; result[1] = c; }
+    } else {
+        const Tile t = tile_of(tab, find_tensor(tab, tile), tile);
+        grid_dependency_wait();
+        if (t.dtype == kF32) clip_tile<kF32, DST>(t, max_norm, flat, result);
+        else clip_tile<kBf16, DST>(t, max_norm, flat, result);
+    }
+    cluster_wait();
+}
+
+template <int DST>
+cudaError_t launch_cluster(const TensorTable<kClusterTensors>& tab, float max_norm, void* flat, float* result, cudaStream_t stream)
+{
+    unsigned ctas = 1;
+    while (ctas < tab.tile_start[tab.count]) ctas *= 2;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(ctas);
+    cfg.blockDim = dim3(kClusterThreads);
+    cfg.stream = stream;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = ctas;
+    attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 2;
+    return cudaLaunchKernelEx(&cfg, clip_cluster_kernel<DST>, tab, max_norm, flat, result);
+}
+
+// params[i] <- fma(-lr, fl(c * acc[i]), params[i]), the last elements first: acc has mostly just been read, from the front on,
+// by the call that measured it, and its end is what L2 still holds.  params pass through (evict-first), so that they do not
+// displace it.
 __global__ void __launch_bounds__(kThreads)
 apply_clipped_kernel(float* __restrict__ params, const float* __restrict__ acc, float lr, const float* __restrict__ factor,
                      uint64_t n)
 {
-    const uint64_t n4 = n / 4, stride = (uint64_t)gridDim.x * blockDim.x;
+    const uint64_t n4 = n / 4, stride = (uint64_t)gridDim.x * kThreads;
     grid_dependency_wait();
     const float c = __ldcg(factor);
-    for (uint64_t i = (uint64_t)blockIdx.x * blockDim.x + threadIdx.x; i < n4; i += stride) {
-        float4 p = __ldcg(reinterpret_cast<const float4*>(params) + i);
+    for (uint64_t k = (uint64_t)blockIdx.x * kThreads + threadIdx.x; k < n4; k += stride) {
+        const uint64_t i = n4 - 1 - k;
+        float4 p = __ldcs(reinterpret_cast<const float4*>(params) + i);
         const float4 g = __ldcg(reinterpret_cast<const float4*>(acc) + i);
         p.x = __fmaf_rn(-lr, __fmul_rn(c, g.x), p.x);
         p.y = __fmaf_rn(-lr, __fmul_rn(c, g.y), p.y);
         p.z = __fmaf_rn(-lr, __fmul_rn(c, g.z), p.z);
         p.w = __fmaf_rn(-lr, __fmul_rn(c, g.w), p.w);
-        reinterpret_cast<float4*>(params)[i] = p;
+        __stcs(reinterpret_cast<float4*>(params) + i, p);
     }
     if (blockIdx.x == 0 && threadIdx.x < (n & 3)) {
         const uint64_t i = n4 * 4 + threadIdx.x;
@@ -264,18 +477,22 @@ apply_clipped_kernel(float* __restrict__ params, const float* __restrict__ acc, 
     }
 }
 
-// Fills `tab` with the tensors of the list from *next on, as many as fit; false if there are none left.
+uint64_t tiles_of(const TensorList& list, int j)
+{
+    const uint64_t per_tile = list.dtype[j] == kF32 ? kTileBytes / 4 : kTileBytes / 2;
+    return (list.size[j] + per_tile - 1) / per_tile;
+}
+
 template <int CAP> void fill_table(const TensorList& list, int first, int last, uint64_t before, TensorTable<CAP>& tab)
 {
     uint64_t tiles = 0;
     int k = 0;
     for (int j = first; j < last; ++j, ++k) {
-        const uint64_t per_tile = list.dtype[j] == kF32 ? kTileBytes / 4 : kTileBytes / 2;
         tab.tile_start[k] = (uint32_t)tiles;
         tab.first[k] = before;
         tab.ptr[k] = list.ptr[j];
         tab.dtype[k] = (uint8_t)list.dtype[j];
-        tiles += (list.size[j] + per_tile - 1) / per_tile;
+        tiles += tiles_of(list, j);
         before += list.size[j];
     }
     tab.tile_start[k] = (uint32_t)tiles;
@@ -283,41 +500,41 @@ template <int CAP> void fill_table(const TensorList& list, int first, int last, 
     tab.count = k;
 }
 
-// Calls fn(table, elements before it) for the list in tables of at most kLargeTable tensors.
+template <int CAP, typename Fn> cudaError_t with_table(const TensorList& list, int first, int last, uint64_t& before, Fn& fn)
+{
+    TensorTable<CAP> tab;
+    fill_table(list, first, last, before, tab);
+    before = tab.first[tab.count];
+    return fn(tab);
+}
+
+// Calls fn(table) for the list in tables of at most kLargeTable tensors, each as small as its tensors allow: a launch costs
+// 0.25 us more for every 4 KB of parameters.
 template <typename Fn> cudaError_t for_each_table(const TensorList& list, Fn&& fn)
 {
     uint64_t before = 0;
-    for (int first = 0; first < list.count;) {
-        const int last = list.count - first > kLargeTable ? first + kLargeTable : list.count;
-        cudaError_t err;
-        if (last - first <= kSmallTable) {
-            TensorTable<kSmallTable> tab;
-            fill_table(list, first, last, before, tab);
-            before = tab.first[tab.count];
-            err = fn(tab);
-        } else {
-            TensorTable<kLargeTable> tab;
-            fill_table(list, first, last, before, tab);
-            before = tab.first[tab.count];
-            err = fn(tab);
-        }
-        if (err != cudaSuccess) return err;
-        first = last;
+    cudaError_t err = cudaSuccess;
+    for (int first = 0; first < list.count && err == cudaSuccess; first += kLargeTable) {
+        const int last = list.count - first > kLargeTable ? first + kLargeTable : list.count, n = last - first;
+        err = n <= 32    ? with_table<32>(list, first, last, before, fn)
+              : n <= 384 ? with_table<384>(list, first, last, before, fn)
+                         : with_table<kLargeTable>(list, first, last, before, fn);
     }
-    return cudaSuccess;
+    return err;
 }
 
-template <int CAP> unsigned blocks_of(const TensorTable<CAP>& tab)
+template <int CAP> unsigned blocks_of(const TensorTable<CAP>& tab, int most)
 {
     const uint32_t tiles = tab.tile_start[tab.count];
-    return tiles < (uint32_t)kMaxBlocks ? tiles : (unsigned)kMaxBlocks;
+    return tiles < (uint32_t)most ? tiles : (unsigned)most;
 }
 
 template <int DST, int CAP>
 cudaError_t scale_table(const TensorTable<CAP>& tab, const double* partial, int npartial, float max_norm, const float* factor,
                         void* flat, float* result, cudaStream_t stream)
 {
-    const unsigned blocks = blocks_of(tab);
+    // A CTA to a tile where the factor is there already and every tile is written; in place most calls write nothing.
+    const unsigned blocks = blocks_of(tab, DST >= 0 && partial == nullptr ? 0x7FFFFFFF : kScaleBlocks);
     if (blocks == 0) return cudaSuccess;
     return launch_pdl(scale_kernel<CAP, DST>, blocks, kThreads, stream, tab, partial, npartial, max_norm, factor, flat, result);
 }
@@ -327,34 +544,45 @@ cudaError_t scale_table(const TensorTable<CAP>& tab, const double* partial, int 
 size_t norm_workspace_floats(int count)
 {
     const size_t tables = count <= 0 ? 1 : ((size_t)count + kLargeTable - 1) / kLargeTable;
-    return tables * kMaxBlocks * 2;                     // a 64-bit sum for each CTA
+    return tables * kNormBlocks * 2;                    // a 64-bit sum for each CTA
 }
 
 cudaError_t launch_clip(const TensorList& list, float max_norm, ClipForm form, void* flat, int flat_dtype, float* result,
                         float* workspace, cudaStream_t stream)
 {
+    uint64_t tiles = 0;
+    for (int j = 0; j < list.count; ++j) tiles += tiles_of(list, j);
+    if (list.count <= kClusterTensors && tiles <= kClusterTiles) {
+        TensorTable<kClusterTensors> tab;
+        fill_table(list, 0, list.count, 0, tab);
+        return form == kMeasureOnly ? launch_cluster<-2>(tab, max_norm, nullptr, result, stream)
+               : form == kInPlace   ? launch_cluster<-1>(tab, max_norm, nullptr, result, stream)
+               : flat_dtype == kF32 ? launch_cluster<kF32>(tab, max_norm, flat, result, stream)
+                                    : launch_cluster<kBf16>(tab, max_norm, flat, result, stream);
+    }
     double* partial = reinterpret_cast<double*>(workspace);
     int npartial = 0;
     cudaError_t err = for_each_table(list, [&](const auto& tab) {
-        const unsigned blocks = blocks_of(tab);
+        const unsigned blocks = blocks_of(tab, kNormBlocks);
         if (blocks == 0) return cudaSuccess;
-        using Tab = std::decay_t<decltype(tab)>;
-        constexpr int CAP = sizeof(tab.dtype);
-        static_assert(std::is_same_v<Tab, TensorTable<CAP>>, "one byte for each tensor");
+        constexpr int CAP = sizeof(tab.dtype);          // a byte for each tensor
         const cudaError_t e = launch_pdl(norm_kernel<CAP>, blocks, kThreads, stream, tab, partial + npartial);
         npartial += (int)blocks;
         return e;
     });
     if (err != cudaSuccess) return err;
-    if (form == kMeasureOnly || npartial == 0)
-        return launch_pdl(norm_result_kernel, 1, kThreads, stream, partial, npartial, max_norm, result);
+    if (form == kMeasureOnly || tiles > kApartTiles) {
+        err = launch_pdl(norm_result_kernel, 1, kThreads, stream, partial, npartial, max_norm, result);
+        if (err != cudaSuccess || form == kMeasureOnly) return err;
+        partial = nullptr;
+    }
     float* to = result;                                 // the first launch writes the result
     return for_each_table(list, [&](const auto& tab) {
         if (tab.tile_start[tab.count] == 0) return cudaSuccess;
         const cudaError_t e =
-            form == kInPlace ? scale_table<-1>(tab, partial, npartial, max_norm, nullptr, nullptr, to, stream)
-            : flat_dtype == kF32 ? scale_table<kF32>(tab, partial, npartial, max_norm, nullptr, flat, to, stream)
-                                 : scale_table<kBf16>(tab, partial, npartial, max_norm, nullptr, flat, to, stream);
+            form == kInPlace ? scale_table<-1>(tab, partial, npartial, max_norm, result + 1, nullptr, to, stream)
+            : flat_dtype == kF32 ? scale_table<kF32>(tab, partial, npartial, max_norm, result + 1, flat, to, stream)
+                                 : scale_table<kBf16>(tab, partial, npartial, max_norm, result + 1, flat, to, stream);
         to = nullptr;
         return e;
     });
@@ -372,7 +600,7 @@ cudaError_t launch_apply_clipped(float* params, const float* acc, float lr, cons
 {
     uint64_t blocks = (n / 4 + kThreads - 1) / kThreads;
     if (blocks < 1) blocks = 1;
-    if (blocks > 2 * kMaxBlocks) blocks = 2 * kMaxBlocks;
+    if (blocks > 2 * kNormBlocks) blocks = 2 * kNormBlocks;
     return launch_pdl(apply_clipped_kernel, (unsigned)blocks, kThreads, stream, params, acc, lr, factor, n);
 }
 

@@ -35,7 +35,6 @@ template <int DTYPE, int V> struct Packed {
         word w[kWords];
         typename Element<DTYPE>::type e[V];
     };
-    __device__ __forceinline__ Packed() {}
     // `p` is aligned to kWordBytes.  Read once: the lines need not stay in L1.
     __device__ __forceinline__ void load(const typename Element<DTYPE>::type* p)
     {
