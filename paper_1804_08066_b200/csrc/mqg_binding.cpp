@@ -544,8 +544,9 @@ struct Operands {
     // A contiguous CUDA tensor of at least `least` elements; all of a call's are on one device.
     const at::Tensor& tensor(PyObject* o, const char* what, uint64_t least, Py_ssize_t index = -1)
     {
-        device_ptr(o, what, index);
+        if (!is_tensor(o)) device_ptr(o, what, index);  // (says so)
         const at::Tensor& t = THPVariable_Unpack(o);
+        if (!t.is_cuda() || !t.is_contiguous()) device_ptr(o, what, index);
         if ((uint64_t)t.numel() < least) {
             PyErr_Format(PyExc_ValueError, "%s holds %lld elements, %llu are needed", what, (long long)t.numel(),
                          (unsigned long long)least);
@@ -569,7 +570,7 @@ struct Operands {
         if (count) *count = (uint64_t)t.numel();
         return static_cast<float*>(t.data_ptr());
     }
-    void* values(PyObject* o, const char* what, uint64_t least, mqg_dtype* dtype, Py_ssize_t index = -1)
+    void* values(PyObject* o, const char* what, uint64_t least, mqg_dtype* dtype, Py_ssize_t index = -1, uint64_t* count = nullptr)
     {
         const at::Tensor& t = tensor(o, what, least, index);
         const at::ScalarType s = t.scalar_type();
@@ -578,6 +579,7 @@ struct Operands {
             throw PythonError();
         }
         *dtype = s == at::kFloat ? MQG_F32 : MQG_BF16;
+        if (count) *count = (uint64_t)t.numel();
         return t.data_ptr();
     }
     const void* ids(PyObject* o, uint64_t least, mqg_index* type)
@@ -595,8 +597,12 @@ struct Operands {
 
 template <typename Fn> PyObject* enqueue_on(const Operands& on, Fn&& fn)
 {
+    if (c10::cuda::current_device() == on.device) {
+        void* s = stream();
+        return enqueue([&] { return fn(s); });
+    }
     const c10::cuda::CUDAGuard guard((c10::DeviceIndex)on.device);
-    void* s = c10::cuda::getCurrentCUDAStream((c10::DeviceIndex)on.device).stream();
+    void* s = stream();
     return enqueue([&] { return fn(s); });
 }
 
@@ -607,46 +613,56 @@ uint64_t area(uint64_t a, uint64_t b)
     return __builtin_mul_overflow(a, b, &r) ? ~0ull : r;
 }
 
-// A list of gradient tensors of any sizes.
+// A list of gradient tensors of any sizes.  Everything that is wanted of the items is read at once, and no Python code runs
+// meanwhile.
 struct TensorTable {
-    std::vector<void*> ptr;
-    std::vector<uint64_t> size;
-    std::vector<mqg_dtype> dtype;
+    static constexpr size_t kInline = 64;
+    void* inline_ptr[kInline];
+    uint64_t inline_size[kInline];
+    mqg_dtype inline_dtype[kInline];
+    std::vector<char> store;
+    void** ptr = inline_ptr;
+    uint64_t* size = inline_size;
+    mqg_dtype* dtype = inline_dtype;
+    size_t n = 0;
     uint64_t total = 0;
 
     void read(PyObject* o, Operands& on)
     {
-        const Reference items = {PySequence_Tuple(o)};
+        const Reference items = {PySequence_Fast(o, "a list of tensors is expected")};
         if (!items.object) throw PythonError();
-        const Py_ssize_t n = PyTuple_GET_SIZE(items.object);
-        ptr.resize((size_t)n), size.resize((size_t)n), dtype.resize((size_t)n);
-        for (Py_ssize_t i = 0; i < n; ++i) {
-            PyObject* item = PyTuple_GET_ITEM(items.object, i);
-            ptr[i] = on.values(item, "grads", 0, &dtype[i], i);
-            size[i] = (uint64_t)THPVariable_Unpack(item).numel();
+        n = (size_t)PySequence_Fast_GET_SIZE(items.object);
+        if (n > kInline) {
+            store.resize(n * (sizeof(void*) + sizeof(uint64_t) + sizeof(mqg_dtype)));
+            ptr = reinterpret_cast<void**>(store.data());
+            size = reinterpret_cast<uint64_t*>(ptr + n);
+            dtype = reinterpret_cast<mqg_dtype*>(size + n);
+        }
+        PyObject** item = PySequence_Fast_ITEMS(items.object);
+        for (size_t i = 0; i < n; ++i) {
+            ptr[i] = on.values(item[i], "grads", 0, &dtype[i], (Py_ssize_t)i, &size[i]);
             total += size[i];
         }
     }
-    uint64_t bytes(size_t i) const { return size[i] * (dtype[i] == MQG_F32 ? 4 : 2); }
+    const char* end(size_t i) const { return static_cast<const char*>(ptr[i]) + size[i] * (dtype[i] == MQG_F32 ? 4 : 2); }
     // Tensors that are written: no two of them share memory.
     void check_apart() const
     {
         bool ascending = true;
-        for (size_t i = 1; i < ptr.size() && ascending; ++i)
-            ascending = static_cast<char*>(ptr[i - 1]) + bytes(i - 1) <= ptr[i];
+        for (size_t i = 1; i < n && ascending; ++i) ascending = end(i - 1) <= ptr[i];
         if (ascending) return;
         std::vector<size_t> order;
-        for (size_t i = 0; i < ptr.size(); ++i)
+        for (size_t i = 0; i < n; ++i)
             if (size[i] != 0) order.push_back(i);
         std::sort(order.begin(), order.end(), [&](size_t a, size_t b) { return ptr[a] < ptr[b]; });
         for (size_t k = 1; k < order.size(); ++k)
-            if (static_cast<char*>(ptr[order[k - 1]]) + bytes(order[k - 1]) > ptr[order[k]]) {
+            if (end(order[k - 1]) > ptr[order[k]]) {
                 PyErr_Format(PyExc_ValueError, "grads[%zu] and grads[%zu] share memory", std::min(order[k - 1], order[k]),
                              std::max(order[k - 1], order[k]));
                 throw PythonError();
             }
     }
-    int count() const { return (int)ptr.size(); }
+    int count() const { return (int)n; }
 };
 
 struct NormArgs {
@@ -667,7 +683,7 @@ MQG_ENTRY(mqg_grad_norm, 0, 4, "grads", "max_norm", "result", "workspace")
     NormArgs a;
     a.read(v[1], v[2], v[3], on);
     g.read(v[0], on);
-    return enqueue_on(on, [&](void* s) { return ::mqg_grad_norm(g.ptr.data(), g.size.data(), g.dtype.data(), g.count(), a.max_norm,
+    return enqueue_on(on, [&](void* s) { return ::mqg_grad_norm(g.ptr, g.size, g.dtype, g.count(), a.max_norm,
                                                                 a.result, a.workspace, a.floats, s); });
 }
 
@@ -679,7 +695,7 @@ MQG_ENTRY(mqg_clip_grad_norm, 0, 4, "grads", "max_norm", "result", "workspace")
     a.read(v[1], v[2], v[3], on);
     g.read(v[0], on);
     g.check_apart();
-    return enqueue_on(on, [&](void* s) { return ::mqg_clip_grad_norm(g.ptr.data(), g.size.data(), g.dtype.data(), g.count(),
+    return enqueue_on(on, [&](void* s) { return ::mqg_clip_grad_norm(g.ptr, g.size, g.dtype, g.count(),
                                                                      a.max_norm, a.result, a.workspace, a.floats, s); });
 }
 
@@ -693,12 +709,12 @@ MQG_ENTRY(mqg_clip_flatten, 0, 5, "grads", "max_norm", "flat", "result", "worksp
     g.read(v[0], on);
     char* flat = static_cast<char*>(on.values(v[2], "flat", g.total, &type));
     const char* end = flat + g.total * (type == MQG_F32 ? 4 : 2);
-    for (size_t i = 0; i < g.ptr.size(); ++i)
-        if (g.ptr[i] < end && static_cast<char*>(g.ptr[i]) + g.bytes(i) > flat) {
+    for (size_t i = 0; i < g.n; ++i)
+        if (g.ptr[i] < end && g.end(i) > flat && g.size[i] != 0) {
             PyErr_Format(PyExc_ValueError, "grads[%zu] and flat share memory", i);
             return nullptr;
         }
-    return enqueue_on(on, [&](void* s) { return ::mqg_clip_flatten(g.ptr.data(), g.size.data(), g.dtype.data(), g.count(),
+    return enqueue_on(on, [&](void* s) { return ::mqg_clip_flatten(g.ptr, g.size, g.dtype, g.count(),
                                                                    a.max_norm, flat, type, a.result, a.workspace, a.floats, s); });
 }
 
@@ -709,7 +725,7 @@ MQG_ENTRY(mqg_scale_grads, 0, 2, "grads", "factor")
     const float* factor = on.floats(v[1], "factor", 1);
     g.read(v[0], on);
     g.check_apart();
-    return enqueue_on(on, [&](void* s) { return ::mqg_scale_grads(g.ptr.data(), g.size.data(), g.dtype.data(), g.count(),
+    return enqueue_on(on, [&](void* s) { return ::mqg_scale_grads(g.ptr, g.size, g.dtype, g.count(),
                                                                   factor, s); });
 }
 

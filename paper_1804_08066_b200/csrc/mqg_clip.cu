@@ -101,16 +101,16 @@ template <int DTYPE> struct Parts {
     }
 };
 
-template <int THREADS> __device__ __forceinline__ double block_sum(double v)
+__device__ __forceinline__ double block_sum(double v)
 {
-    __shared__ double warp_sum[THREADS / 32];
+    __shared__ double warp_sum[kThreads / 32];
 #pragma unroll
     for (int d = 16; d > 0; d >>= 1) v += __shfl_xor_sync(0xFFFFFFFFu, v, d);
     if ((threadIdx.x & 31) == 0) warp_sum[threadIdx.x >> 5] = v;
     __syncthreads();
     double t = 0.0;
 #pragma unroll
-    for (int w = 0; w < THREADS / 32; ++w) t += warp_sum[w];
+    for (int w = 0; w < kThreads / 32; ++w) t += warp_sum[w];
     return t;
 }
 
@@ -140,23 +140,31 @@ __device__ __forceinline__ double squares(const Packed<DTYPE, 16 / kElemBytes<DT
     return d;
 }
 
-// This thread's share of a tile's sum of squares.
-template <int DTYPE> __device__ __forceinline__ double tile_squares(const Tile& t)
-{
-    constexpr int V = 16 / kElemBytes<DTYPE>, K = kTileBytes / 16 / kThreads;
-    const auto* p = static_cast<const typename Element<DTYPE>::type*>(t.ptr);
-    const Parts<DTYPE> parts(p, t.count);
-    Packed<DTYPE, V> x[K];
+// This thread's vectors of a tile, zeros where there are none, and its element outside them.
+constexpr int kVectors = kTileBytes / 16 / kThreads;
+template <int DTYPE> struct Share {
+    static constexpr int V = 16 / kElemBytes<DTYPE>;
+    const typename Element<DTYPE>::type* p;
+    Parts<DTYPE> parts;
+    Packed<DTYPE, V> x[kVectors];
+    float edge;
+    uint32_t edge_at;
+    bool has_edge;
+
+    __device__ __forceinline__ Share(const Tile& t) : p(static_cast<const typename Element<DTYPE>::type*>(t.ptr)), parts(p, t.count)
+    {
 #pragma unroll
-    for (int k = 0; k < K; ++k) {
-        const uint32_t i = threadIdx.x + k * kThreads;
-        if (i < parts.nvec) x[k].load(p + parts.head + i * V);
-        else x[k].w[0] = make_uint4(0, 0, 0, 0);
+        for (int k = 0; k < kVectors; ++k) {
+            if (has(k)) x[k].load(p + at(k));
+            else x[k].w[0] = make_uint4(0, 0, 0, 0);
+        }
+        has_edge = parts.edge(threadIdx.x, edge_at);
+        edge = has_edge ? widen(p[edge_at]) : 0.0f;
     }
-    uint32_t at;
-    const float edge = parts.edge(threadIdx.x, at) ? widen(p[at]) : 0.0f;
-    return squares<DTYPE, K>(x, edge);
-}
+    __device__ __forceinline__ bool has(int k) const { return threadIdx.x + k * kThreads < parts.nvec; }
+    __device__ __forceinline__ uint32_t at(int k) const { return parts.head + (threadIdx.x + k * kThreads) * V; }
+    __device__ __forceinline__ double sum() const { return squares<DTYPE, kVectors>(x, edge); }
+};
 
 // Bound by reading the tensors.  (CTAs of eight neighbouring tiles each, in the order of the addresses: 78.9 us on 500 MB against
 // 79.6, and a turn of a few CTAs more on shorter lists.)
@@ -169,11 +177,11 @@ norm_kernel(const __grid_constant__ TensorTable<CAP> tab, double* __restrict__ p
     Tile t = tile_of(tab, find_tensor(tab, blockIdx.x), blockIdx.x);
     grid_dependency_wait();
     for (uint32_t tile = blockIdx.x; tile < ntiles;) {
-        sum += t.dtype == kF32 ? tile_squares<kF32>(t) : tile_squares<kBf16>(t);
+        sum += t.dtype == kF32 ? Share<kF32>(t).sum() : Share<kBf16>(t).sum();
         tile += gridDim.x;
         if (tile < ntiles) t = tile_of(tab, find_tensor(tab, tile), tile);
     }
-    sum = block_sum<kThreads>(sum);
+    sum = block_sum(sum);
     if (threadIdx.x == 0) partial[blockIdx.x] = sum;
 }
 
@@ -201,7 +209,7 @@ __device__ __forceinline__ double sum_of_partials(const double* partial, int cou
     double s = 0.0;
 #pragma unroll 4
     for (int i = threadIdx.x; i < count; i += kThreads) s += __ldcg(partial + i);
-    return block_sum<kThreads>(s);
+    return block_sum(s);
 }
 
 __global__ void __launch_bounds__(kThreads)
@@ -216,47 +224,16 @@ norm_result_kernel(const double* __restrict__ partial, int npartial, float max_n
 // y = c * x in place.
 template <int DTYPE> __device__ __forceinline__ void scale_tile(const Tile& t, float c)
 {
-    constexpr int V = 16 / kElemBytes<DTYPE>, K = kTileBytes / 16 / kThreads;
     auto* p = static_cast<typename Element<DTYPE>::type*>(const_cast<void*>(t.ptr));
-    const Parts<DTYPE> parts(p, t.count);
-    Packed<DTYPE, V> x[K];
+    Share<DTYPE> s(t);
+    if (s.has_edge) narrow(c * s.edge, p[s.edge_at]);
 #pragma unroll
-    for (int k = 0; k < K; ++k) {
-        const uint32_t i = threadIdx.x + k * kThreads;
-        if (i < parts.nvec) x[k].load(p + parts.head + i * V);
+    for (int k = 0; k < kVectors; ++k) {
+        if (!s.has(k)) continue;
+#pragma unroll
+        for (int e = 0; e < Share<DTYPE>::V; ++e) s.x[k].set(e, c * s.x[k].get(e));
+        s.x[k].store(p + s.at(k));
     }
-    uint32_t at;
-    if (parts.edge(threadIdx.x, at)) narrow(c * widen(p[at]), p[at]);
-#pragma unroll
-    for (int k = 0; k < K; ++k) {
-        const uint32_t i = threadIdx.x + k * kThreads;
-        if (i >= parts.nvec) continue;
-#pragma unroll
-        for (int e = 0; e < V; ++e) x[k].set(e, c * x[k].get(e));
-        x[k].store(p + parts.head + i * V);
-    }
-}
-
-// W elements of x from the aligned word that holds the first of them and the next word; `bytes` lie before it in the word.
-template <int DTYPE, int W>
-__device__ __forceinline__ Packed<DTYPE, W> load_across(const typename Element<DTYPE>::type* x, uint32_t bytes)
-{
-    constexpr int N = W * kElemBytes<DTYPE> / 4;         // 32-bit words of a word
-    const auto* aligned = reinterpret_cast<const typename Element<DTYPE>::type*>(reinterpret_cast<const char*>(x) - bytes);
-    union { Packed<DTYPE, W> p[2]; uint32_t w[2 * N]; } in;
-    union { Packed<DTYPE, W> p; uint32_t w[N]; } out;
-#pragma unroll
-    for (int k = 0; k < 2; ++k) in.p[k].w[0] = reinterpret_cast<const typename Packed<DTYPE, W>::word*>(aligned)[k];
-    const uint32_t words = bytes / 4, bits = bytes % 4 * 8;
-#pragma unroll
-    for (int k = 0; k < N; ++k) {
-        uint32_t lo = in.w[k], hi = in.w[k + 1];
-#pragma unroll
-        for (int q = 1; q < N; ++q)
-            if (words == (uint32_t)q) { lo = in.w[k + q]; hi = k + q + 1 < 2 * N ? in.w[k + q + 1] : 0; }
-        out.w[k] = __funnelshift_r(lo, hi, bits);
-    }
-    return out.p;
 }
 
 // y = c * x into another buffer, by words of W elements from y's first 16-byte boundary on: 16 bytes of the wider type, so that
@@ -339,7 +316,6 @@ scale_kernel(const __grid_constant__ TensorTable<CAP> tab, const double* __restr
 }
 
 // ---- one launch ----
-constexpr int kClusterThreads = kTileBytes / 16;        // a vector of the tile to each
 constexpr int kClusterTensors = 32;
 constexpr unsigned kClusterTiles = 8;
 
@@ -364,7 +340,7 @@ __device__ __forceinline__ double peer_load(const double* p, uint32_t rank)
 __device__ __forceinline__ double cluster_sum(double v)
 {
     __shared__ double cta_sum;
-    v = block_sum<kClusterThreads>(v);
+    v = block_sum(v);
     if (threadIdx.x == 0) cta_sum = v;
     cluster_arrive();
     cluster_wait();
@@ -378,41 +354,36 @@ __device__ __forceinline__ double cluster_sum(double v)
 template <int SRC, int DST>
 __device__ __forceinline__ void clip_tile(const Tile& t, float max_norm, void* flat, float* result)
 {
-    constexpr int V = 16 / kElemBytes<SRC>;
-    const auto* p = static_cast<const typename Element<SRC>::type*>(t.ptr);
-    const Parts<SRC> parts(p, t.count);
-    const bool has_vector = threadIdx.x < parts.nvec;
-    Packed<SRC, V> x[1];
-    x[0].w[0] = make_uint4(0, 0, 0, 0);
-    if (has_vector) x[0].load(p + parts.head + threadIdx.x * V);
-    uint32_t at;
-    const bool has_edge = parts.edge(threadIdx.x, at);
-    const float edge = has_edge ? widen(p[at]) : 0.0f;
+    constexpr int V = Share<SRC>::V;
+    const Share<SRC> s(t);
     float norm;
-    const float c = factor_of(cluster_sum(squares<SRC, 1>(x, edge)), max_norm, &norm);
+    const float c = factor_of(cluster_sum(s.sum()), max_norm, &norm);
     if (cluster_rank() == 0 && threadIdx.x == 0) { result[0] = norm; result[1] = c; }
     if (DST == -2 || (DST == -1 && c == 1.0f)) return;
     constexpr int D = DST < 0 ? SRC : DST;
     using Out = typename Element<D>::type;
     Out* y = DST < 0 ? static_cast<Out*>(const_cast<void*>(t.ptr)) : static_cast<Out*>(flat) + t.at;
-    if (has_edge) narrow(c * edge, y[at]);
-    if (!has_vector) return;
-    y += parts.head + threadIdx.x * V;
-    Packed<D, V> out;
+    if (s.has_edge) narrow(c * s.edge, y[s.edge_at]);
+    const bool aligned = (reinterpret_cast<uintptr_t>(y + s.parts.head) & (Packed<D, V>::kWordBytes - 1)) == 0;
 #pragma unroll
-    for (int e = 0; e < V; ++e) out.set(e, c * x[0].get(e));
-    if ((reinterpret_cast<uintptr_t>(y) & (Packed<D, V>::kWordBytes - 1)) == 0) {
-        out.store(y);
-    } else {
+    for (int k = 0; k < kVectors; ++k) {
+        if (!s.has(k)) continue;
+        Packed<D, V> out;
 #pragma unroll
-        for (int e = 0; e < V; ++e) y[e] = out.e[e];
+        for (int e = 0; e < V; ++e) out.set(e, c * s.x[k].get(e));
+        if (aligned) {
+            out.store(y + s.at(k));
+        } else {
+#pragma unroll
+            for (int e = 0; e < V; ++e) y[s.at(k) + e] = out.e[e];
+        }
     }
 }
 
 // Bound by latency: the launch, one turn to memory, the barrier.  8 tiles: 3.5 us a call where two launches take 4.6; 25 tiles
 // in the same cluster 5.8, and clusters of 16 CTAs take 5.2 for whatever they hold.  DST: -1 in place, -2 only the norm.
 template <int DST>
-__global__ void __launch_bounds__(kClusterThreads)
+__global__ void __launch_bounds__(kThreads)
 clip_cluster_kernel(const __grid_constant__ TensorTable<kClusterTensors> tab, float max_norm, void* __restrict__ flat,
                     float* __restrict__ result)
 {
@@ -438,7 +409,7 @@ cudaError_t launch_cluster(const TensorTable<kClusterTensors>& tab, float max_no
     while (ctas < tab.tile_start[tab.count]) ctas *= 2;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(ctas);
-    cfg.blockDim = dim3(kClusterThreads);
+    cfg.blockDim = dim3(kThreads);
     cfg.stream = stream;
     cudaLaunchAttribute attr[2];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
@@ -447,7 +418,7 @@ cudaError_t launch_cluster(const TensorTable<kClusterTensors>& tab, float max_no
     attr[1].val.clusterDim.x = ctas;
     attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
     cfg.attrs = attr;
-    cfg.numAttrs = 2;
+    cfg.numAttrs = ctas == 1 ? 1 : 2;
     return cudaLaunchKernelEx(&cfg, clip_cluster_kernel<DST>, tab, max_norm, flat, result);
 }
 
