@@ -1,13 +1,19 @@
 """The whole MQGrad loop on one GPU with simulated workers (Algorithm 1 end to end):
 
     python -m paper_1804_08066_b200.train_loop [--iters 60] [--workers 4] [--selector window|sarsa]
+                                               [--model cnn|tokens] [--clip C] [--clip-at worker|server]
 
 A small CNN (3x3 convolutions 3-32-64-128, two fully connected layers) is trained on synthetic
 32x32x3 images (ten fixed Gaussian class means plus unit noise), batch 128 per worker.  Every
 iteration each worker's flat gradient goes through mqg_quantize, the server pass
 mqg_server_step updates the shared flat parameter vector, and the host selector picks the next
 bit width from the losses.  The model and its autograd belong to this harness; the library is
-only the codec.  Prints one JSON line with the share of iteration time spent inside libmqgrad
+the codec and what stands around it: with `--model tokens` the model is a classifier of token
+sequences (synthetic too: every class prefers some tokens, lengths vary) whose table is looked up
+by mqg_embedding and gets its gradient from mqg_embedding_grad; with `--clip C` a worker's
+gradients are clipped to norm C on their way into the flat vector (mqg_clip_flatten), or the
+server measures the mean of the decoded gradients and applies it clipped (mqg_grad_norm,
+mqg_apply_clipped).  Prints one JSON line with the share of iteration time spent inside libmqgrad
 (the paper's Table 3 reports 4.1-13.3 % for quantize + de-quantize + MDP on its CPU clusters).
 """
 from __future__ import annotations
@@ -45,6 +51,51 @@ class SmallCnn(nn.Module):
         return self.f2(F.relu(self.f1(x.flatten(1))))
 
 
+VOCABULARY, WIDTH, LENGTH = 1000, 64, 16         # tokens, elements of a table's row, places of a sequence
+
+
+class TokenClassifier(nn.Module):
+    """The mean of a sequence's table rows (times sqrt(WIDTH)), and two fully connected layers."""
+
+    scale = WIDTH ** 0.5
+
+    def __init__(self):
+        super().__init__()
+        self.table = nn.Parameter(torch.randn(VOCABULARY, WIDTH) / WIDTH)
+        self.f1 = nn.Linear(WIDTH, 128)
+        self.f2 = nn.Linear(128, 10)
+
+    def forward(self, rows, held):
+        """`rows`: the scaled table rows of [batch, LENGTH] places, zero in the empty ones; `held`: which are not empty."""
+        mean = rows.sum(1) / held.sum(1, keepdim=True).clamp(min=1)
+        return self.f2(F.relu(self.f1(mean)))
+
+
+def token_batch(gen, batch):
+    """Ids [batch, LENGTH] with -1 behind a sequence's end, and labels; a class draws every second token from its own tenth of
+    the vocabulary."""
+    y = torch.randint(0, 10, (batch,), generator=gen, device="cuda")
+    own = y[:, None] + 10 * torch.randint(0, VOCABULARY // 10, (batch, LENGTH), generator=gen, device="cuda")
+    ids = torch.randint(0, VOCABULARY, (batch, LENGTH), generator=gen, device="cuda")
+    ids = torch.where(torch.rand(batch, LENGTH, generator=gen, device="cuda") < 0.5, own, ids)
+    length = torch.randint(1, LENGTH + 1, (batch, 1), generator=gen, device="cuda")
+    return torch.where(torch.arange(LENGTH, device="cuda") < length, ids, -1), y
+
+
+def token_gradients(model, ids, y, workspace):
+    """Loss of a batch and the gradient of every parameter, in their order."""
+    n = ids.numel()
+    rows = torch.empty(*ids.shape, WIDTH, device="cuda")
+    mqg.mqg_embedding(model.table.data, VOCABULARY, WIDTH, ids, n, model.scale, rows)
+    rows.requires_grad_()
+    model.zero_grad(set_to_none=True)
+    loss = F.cross_entropy(model(rows, ids >= 0), y)
+    loss.backward()
+    table = torch.empty_like(model.table.data)
+    mqg.mqg_embedding_grad(rows.grad.contiguous(), ids, n, VOCABULARY, WIDTH, model.scale, table, workspace)
+    return loss, [table, *(p.grad for p in model.parameters() if p is not model.table)]
+
+
 def flatten_parameters(model):
     """Re-seat every parameter as a view into one flat fp32 vector (the shared parameters w)."""
     n = sum(p.numel() for p in model.parameters())
@@ -57,13 +108,19 @@ def flatten_parameters(model):
     return flat
 
 
-def run(iters=60, workers=4, batch=128, lr=0.05, selector="window", seed=0):
+def run(iters=60, workers=4, batch=128, lr=0.05, selector="window", seed=0, model="cnn", clip=None, clip_at="worker"):
     torch.manual_seed(seed)
-    model = SmallCnn().cuda()
+    kind, model = model, (SmallCnn() if model == "cnn" else TokenClassifier()).cuda()
     flat = flatten_parameters(model)
     n = flat.numel()
     gen = torch.Generator(device="cuda").manual_seed(seed + 1)
-    means = torch.randn(10, 3, 32, 32, generator=gen, device="cuda")
+    if kind == "cnn":
+        means = torch.randn(10, 3, 32, 32, generator=gen, device="cuda")
+    else:
+        sums = torch.empty(mqg.mqg_embedding_workspace_floats(batch * LENGTH, VOCABULARY, WIDTH), device="cuda")
+    norms = torch.zeros(iters, workers if clip_at == "worker" else 1, 2, device="cuda")       # norm and factor
+    norm_workspace = torch.empty(mqg.mqg_norm_workspace_floats(len(list(model.parameters()))), device="cuda")
+    acc = torch.empty(n, device="cuda") if clip is not None and clip_at == "server" else None
     sel = WindowQSelector(seed=seed) if selector == "window" else SarsaBitSelector(seed=seed)
     codes = [torch.zeros(mqg.mqg_code_words(n, 8), dtype=torch.int32, device="cuda") for _ in range(workers)]
     scales = [torch.zeros(mqg.mqg_num_buckets(n, BUCKET), dtype=torch.float32, device="cuda") for _ in range(workers)]
@@ -75,12 +132,20 @@ def run(iters=60, workers=4, batch=128, lr=0.05, selector="window", seed=0):
         torch.cuda.synchronize()
         grads, loss_sum = [], 0.0
         for w in range(workers):
-            y = torch.randint(0, 10, (batch,), generator=gen, device="cuda")
-            x = means[y] + torch.randn(batch, 3, 32, 32, generator=gen, device="cuda")
-            model.zero_grad(set_to_none=True)
-            loss = F.cross_entropy(model(x), y)
-            loss.backward()
-            grads.append(torch.cat([p.grad.reshape(-1) for p in model.parameters()]))
+            if kind == "cnn":
+                y = torch.randint(0, 10, (batch,), generator=gen, device="cuda")
+                x = means[y] + torch.randn(batch, 3, 32, 32, generator=gen, device="cuda")
+                model.zero_grad(set_to_none=True)
+                loss = F.cross_entropy(model(x), y)
+                loss.backward()
+                parts = [p.grad for p in model.parameters()]
+            else:
+                loss, parts = token_gradients(model, *token_batch(gen, batch), sums)
+            if clip is not None and clip_at == "worker":
+                grads.append(torch.empty(n, device="cuda"))
+                mqg.mqg_clip_flatten([g.contiguous() for g in parts], clip, grads[w], norms[m, w], norm_workspace)
+            else:
+                grads.append(torch.cat([g.reshape(-1) for g in parts]))
             loss_sum += float(loss.detach())
         loss_m = loss_sum / workers
         bits = sel.step(m, loss_m, last_ms)                       # server MDP: loss in, width out
@@ -88,7 +153,12 @@ def run(iters=60, workers=4, batch=128, lr=0.05, selector="window", seed=0):
         e0.record()
         for w in range(workers):
             mqg.mqg_quantize(grads[w], n, bits, BUCKET, seed, codes[w], scales[w], worker=w, step=m)
-        mqg.mqg_server_step(codes, scales, workers, bits, n, BUCKET, flat, lr / workers)
+        if acc is None:
+            mqg.mqg_server_step(codes, scales, workers, bits, n, BUCKET, flat, lr / workers)
+        else:                                                     # the mean's norm is the sum's / workers
+            mqg.mqg_dequant_accumulate(codes, scales, workers, bits, n, acc, BUCKET)
+            mqg.mqg_grad_norm([acc], clip * workers, norms[m, 0], norm_workspace)
+            mqg.mqg_apply_clipped(flat, acc, lr / workers, norms[m, 0, 1:], n)
         e1.record()
         torch.cuda.synchronize()
         lib_ms += e0.elapsed_time(e1)
@@ -97,7 +167,8 @@ def run(iters=60, workers=4, batch=128, lr=0.05, selector="window", seed=0):
         wire += workers * mqg.mqg_wire_bytes(n, bits, BUCKET)
         losses.append(loss_m), chosen.append(bits)
     assert mqg.mqg_device_timeouts() == 0
-    return {"iters": iters, "workers": workers, "parameters": n, "selector": selector,
+    return {"iters": iters, "workers": workers, "parameters": n, "selector": selector, "model": kind,
+            "clip_norm": clip, "clip_factors": None if clip is None else norms[..., 1].mean(1).tolist(),
             "first_loss": losses[0], "last_loss": losses[-1], "bits_chosen": chosen,
             "libmqgrad_ms_per_iter": lib_ms / iters, "iteration_ms": total_ms / iters,
             "libmqgrad_share_pct": 100.0 * lib_ms / total_ms,
@@ -111,5 +182,8 @@ if __name__ == "__main__":
     ap.add_argument("--iters", type=int, default=60)
     ap.add_argument("--workers", type=int, default=4)
     ap.add_argument("--selector", default="window", choices=["window", "sarsa"])
+    ap.add_argument("--model", default="cnn", choices=["cnn", "tokens"])
+    ap.add_argument("--clip", type=float, default=None, help="largest norm of a gradient")
+    ap.add_argument("--clip-at", default="worker", choices=["worker", "server"])
     a = ap.parse_args()
-    print(json.dumps(run(a.iters, a.workers, selector=a.selector)))
+    print(json.dumps(run(a.iters, a.workers, selector=a.selector, model=a.model, clip=a.clip, clip_at=a.clip_at)))
