@@ -1,45 +1,25 @@
 // Token ids sorted by id, stably, with the tokens' positions: least significant digit first, up to ten bits to a pass.
 //
-// Up to 131,072 tokens one thread-block cluster sorts in one launch.  A thread takes K pairs (key, token) of the order so far,
-// a warp 32 K consecutive ones; it ranks them by ballots, the warps' digit counts are added up in shared memory and the CTAs'
-// through distributed shared memory, and every pair is stored to its place in memory, where the next pass reads it from L2.
-// (Stores to the shared memory of the CTA that holds the place took 10,000 cycles for 8192 pairs to a CTA, stores to memory
-// 2,900.)  What bounds it is latency: two cluster barriers and about five dependent turns through shared memory a pass.
-// Rows that no token uses are set to zero by a kernel that runs beside the sort: the sort first marks the rows that are used.
+// Up to 4096 tokens one CTA sorts, in shared memory, by digits of at most eight bits: a pass costs little more than ranking.
+// (8192 tokens of 16-bit ids: 20.6 us in one CTA, 11 in a cluster; 2048: 7.6 and 8.5.)
+// Up to 131,072 a thread-block cluster does in one launch, by digits of up to ten bits, since every pass has two cluster
+// barriers.  In both a thread takes K pairs (key, token) of the order so far, a warp 32 K consecutive ones; it ranks them by
+// ballots, the warps' digit counts are added up in shared memory (and the CTAs' through distributed shared memory), and every
+// pair goes to its place: in shared memory, or, for the cluster, in memory, where the next pass reads it from L2.  (Stores to
+// the shared memory of the CTA that holds the place took 10,000 cycles for 8192 pairs to a CTA, stores to memory 2,900.)  What
+// bounds both is latency.  Rows that no token uses are set to zero by a kernel that runs beside the sort: the sort first marks
+// the rows that are used.
 //
 // More tokens take three launches a pass: count, scan, place.
 #include <atomic>
 
-#include "mqg_tma.cuh"
-#include "mqg_token_sort.h"
+#include "mqg_token_sort.cuh"
 
 namespace mqg {
 namespace {
 
-// An id as the key it is sorted by: those outside 0..rows-1 go behind all others.
-template <typename ID> __device__ __forceinline__ uint32_t key_of(ID id, uint32_t rows)
-{
-    return id >= 0 && (uint64_t)id < rows ? (uint32_t)id : rows;
-}
-
-constexpr int kMaxDigitBits = 10;
-
-// The lanes of the warp that hold the same digit, among those that hold a key at all.
-__device__ __forceinline__ uint32_t same_digit(uint32_t digit, int bits, uint32_t held)
-{
-    uint32_t same = held;
-#pragma unroll
-    for (int b = 0; b < kMaxDigitBits; ++b) {
-        if (b >= bits) break;
-        const bool one = (digit & (1u << b)) != 0;
-        const uint32_t ones = __ballot_sync(0xFFFFFFFFu, one);
-        same &= one ? ones : ~ones;
-    }
-    return same;
-}
-
 // ---- one launch ----
-constexpr int kThreads = 1024, kWarps = kThreads / 32;
+constexpr int kThreads = kSortThreads, kWarps = kSortWarps;
 constexpr unsigned kMaxCluster = 16;
 
 struct SortArgs {
@@ -102,8 +82,25 @@ template <typename ID> __device__ __forceinline__ void mark_used(const SortArgs&
 // own grid_dependency_wait().
 __device__ __forceinline__ void release_dependents() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
 
+// ---- one CTA ----
 template <typename ID, int K>
-__global__ void __launch_bounds__(kThreads) sort_cluster_kernel(const SortArgs a)
+__global__ void __launch_bounds__(kThreads, 1) sort_small_kernel(const SortArgs a)
+{
+    extern __shared__ __align__(16) unsigned char smem[];
+    __shared__ SmallSort s;
+    uint2* pairs = reinterpret_cast<uint2*>(smem);
+    grid_dependency_wait();
+    if (threadIdx.x == 0) *a.counter = 0;
+    release_dependents();
+    uint2 pair[K];
+    const uint32_t held = load_pairs<ID, K>(static_cast<const ID*>(a.ids), a.tokens, a.rows, (threadIdx.x >> 5) * (32 * K) + (threadIdx.x & 31), pair);
+    sort_in_cta<K>(pair, held, a.bits, s, pairs);
+    for (uint32_t i = threadIdx.x; i < a.tokens; i += kThreads) a.sorted[i] = pairs[i];
+}
+
+// ---- one cluster ----
+template <typename ID, int K>
+__global__ void __launch_bounds__(kThreads, 1) sort_cluster_kernel(const SortArgs a)
 {
     extern __shared__ __align__(16) unsigned char smem[];
     const int bins = 1 << a.digit_bits;
@@ -123,32 +120,18 @@ __global__ void __launch_bounds__(kThreads) sort_cluster_kernel(const SortArgs a
     const int passes = (a.bits + a.digit_bits - 1) / a.digit_bits;
     uint2* to = passes & 1 ? a.sorted : a.spare;
     uint2* from = passes & 1 ? a.spare : a.sorted;
+    uint2 pair[K];
+    const uint32_t held = load_pairs<ID, K>(static_cast<const ID*>(a.ids), a.tokens, a.rows, first, pair);
     for (int shift = 0; shift < a.bits; shift += a.digit_bits) {
-        uint2 pair[K];
+        if (shift != 0) {
 #pragma unroll
-        for (int r = 0; r < K; ++r) {
-            const uint32_t i = first + r * 32;
-            pair[r] = make_uint2(0, i);
-            if (i < a.tokens) {
-                if (shift != 0) pair[r] = __ldcg(from + i);
-                else pair[r].x = key_of(__ldg(static_cast<const ID*>(a.ids) + i), a.rows);
-            }
+            for (int r = 0; r < K; ++r)
+                if ((held >> r) & 1u) pair[r] = __ldcg(from + first + r * 32);
         }
         for (int i = lane; i < bins / 2; i += 32) reinterpret_cast<uint32_t*>(mine)[i] = 0;
-        uint32_t same[K];
-#pragma unroll
-        for (int r = 0; r < K; ++r)
-            same[r] = same_digit((pair[r].x >> shift) & (bins - 1), a.digit_bits, __ballot_sync(0xFFFFFFFFu, first + r * 32 < a.tokens));
         __syncwarp();
-#pragma unroll
-        for (int r = 0; r < K; ++r) {                   // same[r] becomes the pairs before this one with its digit, of the warp
-            const uint32_t digit = (pair[r].x >> shift) & (bins - 1);
-            const uint32_t so_far = mine[digit];
-            __syncwarp();
-            if ((same[r] >> lane) == 1u) mine[digit] = (uint16_t)(so_far + __popc(same[r]));
-            __syncwarp();
-            same[r] = so_far + __popc(same[r] & ((1u << lane) - 1));
-        }
+        uint32_t rank_in_warp[K];
+        rank_pairs<K>(pair, held, shift, a.digit_bits, mine, rank_in_warp);
         __syncthreads();
         uint32_t earlier = 0, total = 0;                // keys of this digit: of the CTAs before, of all
         if (d < (uint32_t)bins) {
@@ -160,21 +143,19 @@ __global__ void __launch_bounds__(kThreads) sort_cluster_kernel(const SortArgs a
             }
             cta_count[d] = total;
         }
-        if (a.ctas > 1) {
-            cluster_sync();                             // the counts are there
-            if (d < (uint32_t)bins) {
-                total = 0;
+        cluster_sync();                                 // the counts are there
+        if (d < (uint32_t)bins) {
+            total = 0;
 #pragma unroll
-                for (uint32_t half = 0; half < kMaxCluster; half += 8) {
-                    if (half >= a.ctas) break;
-                    uint32_t c[8];
+            for (uint32_t half = 0; half < kMaxCluster; half += 8) {
+                if (half >= a.ctas) break;
+                uint32_t c[8];
 #pragma unroll
-                    for (uint32_t r = 0; r < 8; ++r) c[r] = half + r < a.ctas ? peer_load(cta_count + d, half + r) : 0;
+                for (uint32_t r = 0; r < 8; ++r) c[r] = half + r < a.ctas ? peer_load(cta_count + d, half + r) : 0;
 #pragma unroll
-                    for (uint32_t r = 0; r < 8; ++r) {
-                        earlier += half + r < rank ? c[r] : 0;
-                        total += c[r];
-                    }
+                for (uint32_t r = 0; r < 8; ++r) {
+                    earlier += half + r < rank ? c[r] : 0;
+                    total += c[r];
                 }
             }
         }
@@ -194,10 +175,9 @@ __global__ void __launch_bounds__(kThreads) sort_cluster_kernel(const SortArgs a
 #pragma unroll
         for (int r = 0; r < K; ++r) {
             const uint32_t digit = (pair[r].x >> shift) & (bins - 1);
-            if (first + r * 32 < a.tokens) to[place[digit] + mine[digit] + same[r]] = pair[r];
+            if ((held >> r) & 1u) to[place[digit] + mine[digit] + rank_in_warp[r]] = pair[r];
         }
-        if (a.ctas > 1) cluster_sync();                 // the pairs are there, and no CTA's counts go before they were read
-        else __syncthreads();
+        cluster_sync();                                 // the pairs are there, and no CTA's counts go before they were read
         uint2* t = to; to = from; from = t;
     }
 }
@@ -289,8 +269,28 @@ template <typename ID, int K> cudaError_t launch_cluster(const SortArgs& a, cuda
     return cudaLaunchKernelEx(&cfg, sort_cluster_kernel<ID, K>, a);
 }
 
+template <typename ID, int K> cudaError_t launch_small(const SortArgs& a, cudaStream_t stream)
+{
+    static std::atomic<bool> ready[64];                 // per device (zero-initialised)
+    constexpr int kSmem = K * kThreads * (int)sizeof(uint2);
+    int dev = 0;
+    cudaError_t err = cudaGetDevice(&dev);
+    if (err != cudaSuccess) return err;
+    if (dev < 0 || dev >= 64) return cudaErrorInvalidDevice;
+    if (!ready[dev].load(std::memory_order_relaxed)) {
+        err = cudaFuncSetAttribute(sort_small_kernel<ID, K>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem);
+        if (err != cudaSuccess) return err;
+        ready[dev].store(true, std::memory_order_relaxed);
+    }
+    return launch_pdl_smem(sort_small_kernel<ID, K>, 1, kThreads, kSmem, stream, a);
+}
+
 template <typename ID> cudaError_t launch_by_size(const SortArgs& a, uint32_t per_thread, cudaStream_t stream)
 {
+    if (a.ctas == 1)
+        return per_thread <= 1 ? launch_small<ID, 1>(a, stream)
+               : per_thread <= 2 ? launch_small<ID, 2>(a, stream)
+                                 : launch_small<ID, 4>(a, stream);
     return per_thread <= 1 ? launch_cluster<ID, 1>(a, stream)
            : per_thread <= 2 ? launch_cluster<ID, 2>(a, stream)
            : per_thread <= 4 ? launch_cluster<ID, 4>(a, stream)
@@ -406,14 +406,7 @@ place_kernel(const PassInput<ID> in, int shift, const uint32_t* __restrict__ cou
 }
 
 // ---- host ----
-constexpr uint32_t kClusterTokens = kMaxCluster * 8 * kThreads;
-
-int key_bits(uint32_t rows)                             // of the largest key, `rows`
-{
-    int bits = 1;
-    while (bits < 32 && ((uint64_t)rows >> bits) != 0) ++bits;
-    return bits;
-}
+constexpr uint32_t kClusterTokens = kMaxCluster * 8 * kThreads, kSmallTokens = 4 * kThreads;
 
 template <typename ID>
 cudaError_t sort_in_passes(const ID* ids, const SortArgs& s, uint32_t* counts, cudaStream_t stream)
@@ -436,6 +429,13 @@ cudaError_t sort_in_passes(const ID* ids, const SortArgs& s, uint32_t* counts, c
 
 }  // namespace
 
+int token_key_bits(uint32_t rows)
+{
+    int bits = 1;
+    while (bits < 32 && ((uint64_t)rows >> bits) != 0) ++bits;
+    return bits;
+}
+
 uint64_t token_sort_words(uint64_t tokens, uint64_t rows)
 {
     if (tokens > kClusterTokens) return 2 * tokens + (tokens + kTile - 1) / kTile * kBins;
@@ -446,21 +446,21 @@ cudaError_t launch_token_sort(const TokenIds& ids, uint32_t rows, uint2* sorted,
                               void* zero, uint64_t row_bytes, cudaStream_t stream)
 {
     uint32_t* behind = scratch + 2 * ids.count;
-    SortArgs a = {ids.ptr, sorted, reinterpret_cast<uint2*>(scratch), counter, nullptr, (uint32_t)ids.count, rows, key_bits(rows), 1, 1};
+    SortArgs a = {ids.ptr, sorted, reinterpret_cast<uint2*>(scratch), counter, nullptr, (uint32_t)ids.count, rows, token_key_bits(rows), 1, 1};
     cudaError_t err = cudaSuccess;
     if (a.tokens > kClusterTokens) {
         err = ids.wide ? sort_in_passes(static_cast<const int64_t*>(ids.ptr), a, behind, stream)
                        : sort_in_passes(static_cast<const int32_t*>(ids.ptr), a, behind, stream);
     } else if (a.tokens != 0) {
-        // passes of equal digits; a CTA for each 2048 tokens, then more tokens to a thread
+        // the cluster: passes of equal digits; a CTA for each 2048 tokens, then more tokens to a thread
         const int passes = (a.bits + kMaxDigitBits - 1) / kMaxDigitBits;
         a.digit_bits = (a.bits + passes - 1) / passes;
-        while (a.ctas < kMaxCluster && a.ctas * 2 * kThreads < a.tokens) a.ctas *= 2;
+        while (a.tokens > kSmallTokens && a.ctas < kMaxCluster && a.ctas * 2 * kThreads < a.tokens) a.ctas *= 2;
         const uint32_t per_thread = (a.tokens + a.ctas * kThreads - 1) / (a.ctas * kThreads);
         // Zeros that the sums overwrite while they are in L2 cost no write to DRAM: marks pay where the rows that may be
         // used exceed it (64,000 rows of 16 KB, 65,536 tokens: 302 -> 273 us; 50,000 of 4 KB, 16,384 tokens: 50 -> 53).
         const bool vectors = row_bytes % 16 == 0 && (reinterpret_cast<uintptr_t>(zero) & 15) == 0;
-        if (zero != nullptr && vectors && rows <= kMaxMarkedRows && (a.tokens < rows ? a.tokens : rows) * row_bytes >= (1u << 27))
+        if (a.ctas > 1 && zero != nullptr && vectors && rows <= kMaxMarkedRows && (a.tokens < rows ? a.tokens : rows) * row_bytes >= (1u << 27))
             a.used = behind;
         err = ids.wide ? launch_by_size<int64_t>(a, per_thread, stream) : launch_by_size<int32_t>(a, per_thread, stream);
     }

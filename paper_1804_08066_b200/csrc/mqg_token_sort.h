@@ -5,6 +5,9 @@
 
 namespace mqg {
 
+// Bits of the largest key, `rows`.
+int token_key_bits(uint32_t rows);
+
 // 32-bit words of scratch memory (8-byte aligned) that the sort needs beside its output.
 uint64_t token_sort_words(uint64_t tokens, uint64_t rows);
 
