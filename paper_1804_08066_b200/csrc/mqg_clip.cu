@@ -46,7 +46,6 @@ struct Tile {
     const void* ptr;         // its first element
     uint64_t at;             // elements before it in the whole list
     uint32_t count;          // its elements
-    uint32_t before, behind; // elements of the tensor around it, as far as 16 bytes reach
     int dtype;
 };
 
@@ -77,8 +76,6 @@ template <int CAP> __device__ __forceinline__ Tile tile_of(const TensorTable<CAP
     t.ptr = static_cast<const char*>(tab.ptr[tensor]) + (e0 << shift);
     t.at = tab.first[tensor] + e0;
     t.count = (uint32_t)min((uint64_t)(kTileBytes >> shift), n - e0);
-    t.before = (uint32_t)min(e0, (uint64_t)8);
-    t.behind = (uint32_t)min(n - e0 - t.count, (uint64_t)8);
     return t;
 }
 
@@ -237,34 +234,35 @@ template <int DTYPE> __device__ __forceinline__ void scale_tile(const Tile& t, f
 }
 
 // y = c * x into another buffer, by words of W elements from y's first 16-byte boundary on: 16 bytes of the wider type, so that
-// every access of a warp covers whole sectors.  Where x does not lie on its words' boundaries there, a word is put together from
-// the two that hold it.
+// every access of a warp covers whole sectors.  Where x does not lie on its words' boundaries there, element by element, lanes
+// side by side.  (Words put together from the two that hold them took twice as long: ten times the instructions.)
 template <int SRC, int DST>
 __device__ __forceinline__ void copy_tile(const Tile& t, typename Element<DST>::type* y, float c)
 {
     constexpr int W = 16 / (kElemBytes<SRC> > kElemBytes<DST> ? kElemBytes<SRC> : kElemBytes<DST>);
     constexpr int K = kTileBytes / kElemBytes<SRC> / W / kThreads;
-    constexpr uint32_t kWord = W * kElemBytes<SRC>;
     const auto* x = static_cast<const typename Element<SRC>::type*>(t.ptr);
     const uint32_t to_boundary = (uint32_t)((16 - (reinterpret_cast<uintptr_t>(y) & 15)) & 15) / kElemBytes<DST>;
     const uint32_t head = to_boundary < t.count ? to_boundary : t.count;
+    if ((reinterpret_cast<uintptr_t>(x + head) & (W * kElemBytes<SRC> - 1)) != 0) {
+        constexpr int kAhead = 8;
+        for (uint32_t i0 = threadIdx.x; i0 < t.count; i0 += kAhead * kThreads) {
+            typename Element<SRC>::type v[kAhead];
+#pragma unroll
+            for (int k = 0; k < kAhead; ++k)
+                if (i0 + k * kThreads < t.count) v[k] = __ldcg(x + i0 + k * kThreads);
+#pragma unroll
+            for (int k = 0; k < kAhead; ++k)
+                if (i0 + k * kThreads < t.count) narrow(c * widen(v[k]), y[i0 + k * kThreads]);
+        }
+        return;
+    }
     const uint32_t nvec = (t.count - head) / W, tail = t.count - head - nvec * W;
-    const uint32_t off = (uint32_t)(reinterpret_cast<uintptr_t>(x + head) & (kWord - 1));
-    // words that lie in the tensor with all that is read for them
-    const uint32_t lead = off / kElemBytes<SRC>, from = lead <= head + t.before ? 0u : 1u;
-    const uint32_t to = off == 0 || tail + t.behind + lead >= (uint32_t)W ? nvec : nvec == 0 ? 0u : nvec - 1;
     Packed<SRC, W> in[K];
 #pragma unroll
     for (int k = 0; k < K; ++k) {
         const uint32_t i = threadIdx.x + k * kThreads;
-        if (off == 0) {
-            if (i < nvec) in[k].load(x + head + i * W);
-        } else if (i >= from && i < to) {
-            in[k] = load_across<SRC, W>(x + head + i * W, off);
-        } else if (i < nvec) {
-#pragma unroll
-            for (int e = 0; e < W; ++e) in[k].e[e] = x[head + i * W + e];
-        }
+        if (i < nvec) in[k].load(x + head + i * W);
     }
     if (threadIdx.x < head + tail) {
         const uint32_t i = threadIdx.x < head ? threadIdx.x : t.count - tail + (threadIdx.x - head);

@@ -50,29 +50,6 @@ template <int DTYPE, int V> struct Packed {
     __device__ __forceinline__ void set(int i, float x) { narrow(x, e[i]); }
 };
 
-// W elements from x on, put together from the aligned word that holds the first of them and the word behind it; `bytes` of the
-// first word lie before x.  Words of 4 to 16 bytes.
-template <int DTYPE, int W>
-__device__ __forceinline__ Packed<DTYPE, W> load_across(const typename Element<DTYPE>::type* x, uint32_t bytes)
-{
-    constexpr int N = W * kElemBytes<DTYPE> / 4;         // 32-bit words of a word
-    const auto* aligned = reinterpret_cast<const typename Packed<DTYPE, W>::word*>(reinterpret_cast<const char*>(x) - bytes);
-    union { Packed<DTYPE, W> p[2]; uint32_t w[2 * N]; } in;
-    union { Packed<DTYPE, W> p; uint32_t w[N]; } out;
-    in.p[0].w[0] = aligned[0];
-    in.p[1].w[0] = aligned[1];
-    const uint32_t words = bytes / 4, bits = bytes % 4 * 8;
-#pragma unroll
-    for (int k = 0; k < N; ++k) {
-        uint32_t lo = in.w[k], hi = in.w[k + 1];
-#pragma unroll
-        for (int q = 1; q < N; ++q)
-            if (words == (uint32_t)q) { lo = in.w[k + q]; hi = k + q + 1 < 2 * N ? in.w[k + q + 1] : 0; }
-        out.w[k] = __funnelshift_r(lo, hi, bits);
-    }
-    return out.p;
-}
-
 // The longest vector of at most `most` elements that divides rows of `dim` elements and starts on its accesses' boundaries
 // in both buffers (a null buffer fits all).
 inline int row_vector(int most, uint64_t dim, const void* a, int a_bytes, const void* b, int b_bytes)
