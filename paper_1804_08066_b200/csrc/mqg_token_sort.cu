@@ -1,7 +1,7 @@
 // Token ids sorted by id, stably, with the tokens' positions: least significant digit first, up to ten bits to a pass.
 //
-// Up to 4096 tokens one CTA sorts, in shared memory, by digits of at most eight bits: a pass costs little more than ranking.
-// (8192 tokens of 16-bit ids: 20.6 us in one CTA, 11 in a cluster; 2048: 7.6 and 8.5.)
+// Up to 2048 tokens one CTA sorts, in shared memory, by digits of at most six bits: a pass costs little more than ranking.
+// (2048 tokens of 16-bit ids: 8.5 us a launch; 4096: 13.0 in one CTA, 8.6 in a cluster.)
 // Up to 131,072 a thread-block cluster does in one launch, by digits of up to ten bits, since every pass has two cluster
 // barriers.  In both a thread takes K pairs (key, token) of the order so far, a warp 32 K consecutive ones; it ranks them by
 // ballots, the warps' digit counts are added up in shared memory (and the CTAs' through distributed shared memory), and every
@@ -289,8 +289,7 @@ template <typename ID> cudaError_t launch_by_size(const SortArgs& a, uint32_t pe
 {
     if (a.ctas == 1)
         return per_thread <= 1 ? launch_small<ID, 1>(a, stream)
-               : per_thread <= 2 ? launch_small<ID, 2>(a, stream)
-                                 : launch_small<ID, 4>(a, stream);
+                               : launch_small<ID, 2>(a, stream);
     return per_thread <= 1 ? launch_cluster<ID, 1>(a, stream)
            : per_thread <= 2 ? launch_cluster<ID, 2>(a, stream)
            : per_thread <= 4 ? launch_cluster<ID, 4>(a, stream)
@@ -406,7 +405,7 @@ place_kernel(const PassInput<ID> in, int shift, const uint32_t* __restrict__ cou
 }
 
 // ---- host ----
-constexpr uint32_t kClusterTokens = kMaxCluster * 8 * kThreads, kSmallTokens = 4 * kThreads;
+constexpr uint32_t kClusterTokens = kMaxCluster * 8 * kThreads, kSmallTokens = 2 * kThreads;
 
 template <typename ID>
 cudaError_t sort_in_passes(const ID* ids, const SortArgs& s, uint32_t* counts, cudaStream_t stream)
@@ -452,10 +451,11 @@ cudaError_t launch_token_sort(const TokenIds& ids, uint32_t rows, uint2* sorted,
         err = ids.wide ? sort_in_passes(static_cast<const int64_t*>(ids.ptr), a, behind, stream)
                        : sort_in_passes(static_cast<const int32_t*>(ids.ptr), a, behind, stream);
     } else if (a.tokens != 0) {
-        // the cluster: passes of equal digits; a CTA for each 2048 tokens, then more tokens to a thread
+        // the cluster: passes of equal digits; a CTA for each 1024 tokens, then more tokens to a thread (4096 tokens: 8.6 us a
+        // launch with four CTAs, 10.5 with two)
         const int passes = (a.bits + kMaxDigitBits - 1) / kMaxDigitBits;
         a.digit_bits = (a.bits + passes - 1) / passes;
-        while (a.tokens > kSmallTokens && a.ctas < kMaxCluster && a.ctas * 2 * kThreads < a.tokens) a.ctas *= 2;
+        while (a.tokens > kSmallTokens && a.ctas < kMaxCluster && a.ctas * kThreads < a.tokens) a.ctas *= 2;
         const uint32_t per_thread = (a.tokens + a.ctas * kThreads - 1) / (a.ctas * kThreads);
         // Zeros that the sums overwrite while they are in L2 cost no write to DRAM: marks pay where the rows that may be
         // used exceed it (64,000 rows of 16 KB, 65,536 tokens: 302 -> 273 us; 50,000 of 4 KB, 16,384 tokens: 50 -> 53).
