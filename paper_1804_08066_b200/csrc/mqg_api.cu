@@ -173,7 +173,7 @@ size_t mqg_wire_bytes(uint64_t n, int bits, uint64_t bucket)
 
 const char* mqg_last_error(void) { return g_err; }
 
-int mqg_version(void) { return 100; }
+int mqg_version(void) { return 200; }
 
 mqg_status mqg_device_timeouts(unsigned int* count)
 {

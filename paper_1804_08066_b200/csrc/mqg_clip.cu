@@ -193,7 +193,7 @@ __device__ __forceinline__ float factor_of(double s, float max_norm, float* norm
         *norm = (float)s;
         return s <= (double)max_norm ? 1.0f : s > 0.0 ? 0.0f : (float)s;
     }
-    const double m = __hiloint2double(high - (even << 20), __double2loint(s)), y0 = (double)rsqrtf((float)m);
+    const double m = __hiloint2double(high - even * (1 << 20), __double2loint(s)), y0 = (double)rsqrtf((float)m);
     const double y = fma(y0, fma(-0.5 * m * y0, y0, 0.5), y0);
     const double up = __hiloint2double((even / 2 + 1023) << 20, 0), down = __hiloint2double((1023 - even / 2) << 20, 0);
     const double n = m * y * up;

@@ -51,7 +51,8 @@ struct Window {
         const uint32_t from = (first_chunk - 1) << a.chunk_bits, n = (chunks + 2) << a.chunk_bits;
         for (uint32_t i = threadIdx.x; i < n; i += kThreads) {
             const uint32_t p = from + i;                // wraps in the chunk before the first
-            token[i] = p < a.tokens ? __ldg(a.sorted + p) : make_uint2(a.rows, 0);
+            // (not by way of L1: this launch may have begun before the sort was done)
+            token[i] = p < a.tokens ? __ldcg(a.sorted + p) : make_uint2(a.rows, 0);
         }
         if (threadIdx.x == 0) begin = from;
         __syncthreads();
@@ -159,7 +160,7 @@ __device__ __forceinline__ uint32_t chunks_of_run(const GradArgs& a, uint32_t ch
 #pragma unroll
             for (uint32_t k = 1; k <= 32; ++k) {        // the run covers a first part of the chunks: as many as are on
                 const uint64_t p = ((uint64_t)chunk + n + (k << bits) - 1) << a.chunk_bits;
-                on += p < a.tokens && __ldg(&a.sorted[p].x) == row ? 1 : 0;
+                on += p < a.tokens && __ldcg(&a.sorted[p].x) == row ? 1 : 0;
             }
             n += on << bits;
         } while (on == 32);

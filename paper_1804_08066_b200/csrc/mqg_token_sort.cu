@@ -185,20 +185,22 @@ __global__ void __launch_bounds__(kThreads, 1) sort_cluster_kernel(const SortArg
 // ---- the zeros ----
 // Bound by the writes to DRAM.  CTAs of 256 threads that write 4 KB each, in the order of the addresses: 6633 GB/s on 205 MB, as
 // much as the driver's memset; 136 CTAs that go through the buffer side by side 5860.
-// They run beside the sort, which releases them once the rows that are used are marked (or, where nothing is marked, at
-// once): what they read of the sort's is written before that.  Only the last CTA waits for the sort's end, so that what
-// follows finds both done.
+// They run beside the sort, which has waited for the launches before it when it releases them, once the rows that are used are
+// marked (or, where nothing is marked, at once): what they read of the sort's is in L2 by then.  Only the last CTA waits for
+// the sort's end, so that what follows finds both done.
 constexpr int kZeroThreads = 256;
 
-__global__ void __launch_bounds__(kZeroThreads) zero_kernel(char* p, uint64_t bytes, uint64_t head)
+// `beside`: the launch before this one is the sort, which has waited for those before it; otherwise this one has to.
+__global__ void __launch_bounds__(kZeroThreads) zero_kernel(char* p, uint64_t bytes, uint64_t head, bool beside)
 {
+    if (!beside) grid_dependency_wait();
     const uint64_t nvec = (bytes - head) / 16, i = (uint64_t)blockIdx.x * kZeroThreads + threadIdx.x;
     if (i < nvec) reinterpret_cast<uint4*>(p + head)[i] = make_uint4(0, 0, 0, 0);
     if (blockIdx.x != gridDim.x - 1) return;
     const uint64_t tail = bytes - head - nvec * 16;     // what stands before the first and behind the last 16-byte vector
     if (threadIdx.x < head) p[threadIdx.x] = 0;
     if (threadIdx.x < tail) p[bytes - tail + threadIdx.x] = 0;
-    grid_dependency_wait();
+    if (beside) grid_dependency_wait();
 }
 
 // The same for the rows that are not marked: a CTA has 1 to 32 rows of one word of marks, about 32 KB of them.
@@ -221,12 +223,13 @@ __global__ void __launch_bounds__(kZeroThreads) zero_unused_kernel(const UnusedA
     if (blockIdx.x == gridDim.x - 1) grid_dependency_wait();
 }
 
-cudaError_t launch_zero(void* p, uint64_t bytes, cudaStream_t stream)
+cudaError_t launch_zero(void* p, uint64_t bytes, bool beside, cudaStream_t stream)
 {
     const uint64_t to_boundary = (16 - (reinterpret_cast<uintptr_t>(p) & 15)) & 15;
     const uint64_t head = to_boundary < bytes ? to_boundary : bytes, per_cta = kZeroThreads * 16;
     const uint64_t ctas = ((bytes - head) / 16 * 16 + per_cta - 1) / per_cta;
-    return launch_pdl(zero_kernel, ctas == 0 ? 1u : (unsigned)ctas, kZeroThreads, stream, static_cast<char*>(p), bytes, head);
+    return launch_pdl(zero_kernel, ctas == 0 ? 1u : (unsigned)ctas, kZeroThreads, stream, static_cast<char*>(p), bytes, head,
+                      beside);
 }
 
 cudaError_t launch_zero_unused(void* p, uint32_t rows, uint64_t row_bytes, const uint32_t* used, cudaStream_t stream)
@@ -465,7 +468,8 @@ cudaError_t launch_token_sort(const TokenIds& ids, uint32_t rows, uint2* sorted,
         err = ids.wide ? launch_by_size<int64_t>(a, per_thread, stream) : launch_by_size<int32_t>(a, per_thread, stream);
     }
     if (err != cudaSuccess || zero == nullptr) return err;
-    return a.used != nullptr ? launch_zero_unused(zero, rows, row_bytes, a.used, stream) : launch_zero(zero, rows * row_bytes, stream);
+    return a.used != nullptr ? launch_zero_unused(zero, rows, row_bytes, a.used, stream) 
+                             : launch_zero(zero, rows * row_bytes, a.tokens != 0 && a.tokens <= kClusterTokens, stream);
 }
 
 }  // namespace mqg
