@@ -313,57 +313,94 @@ __global__ void __launch_bounds__(kJoinThreads) grad_join_kernel(const GradArgs 
 }
 
 // ---- one launch, for few tokens ----
-// A CTA has eight columns of the table: it sorts the tokens (every CTA does, in shared memory), adds up its columns of them in
-// chunks of 16, joins the long runs' parts, which stay in shared memory, and has set its columns of all rows to zero before.
-// Bound by latency: of the launch, the sort and two turns to memory.
-constexpr int kSmallPerThread = 2, kSmallColumns = 8, kSmallChunkBits = 4;
-constexpr uint32_t kSmallTokens = kSmallPerThread * kSortThreads, kSmallChunks = kSortThreads / kSmallColumns;
-static_assert(kSmallTokens >> kSmallChunkBits == kSmallChunks, "a thread to each column of a chunk");
+// A CTA has up to 32 columns of every G-th row of the table (every G-th, so that the frequent ids, which often are neighbours, do
+// not meet in one CTA).  It sets them to zero, finds its rows' tokens among all and sorts them in shared memory, adds them up in
+// chunks, a thread to each column of a chunk, and joins the long runs' parts, which stay in shared memory.  Bound by latency: of
+// the launch, the sort (one pass where the CTA has at most 64 rows) and two turns to memory.  (64 columns: 2048 tokens, a
+// seventh of them the same, 1000 rows of 64 take 9.4 us against 8, as many evenly spread 6.2 against 6.4.)
+constexpr int kSmallPerThread = 2, kSmallColumnBits = 5, kLeastColumnBits = 3;
+constexpr uint32_t kSmallTokens = kSmallPerThread * kSortThreads;
+// 4 tokens to a chunk, up to 32 where that makes more than 64 chunks or more than there are threads for
+constexpr uint32_t kSmallChunks = kSmallTokens >> kMaxChunkBits, kSmallParts = kSmallChunks * 2 << kSmallColumnBits;
 
 struct SmallArgs {
     const void* ids;
     const void* dout;
     void* grad;
     uint32_t dim, tokens, rows;
-    int key_bits, chunk_bits, wide;
+    uint32_t groups;         // G
+    int key_bits;            // of a row's number in its group
+    int column_bits;         // 2^this columns of a CTA
+    int wide;
     float scale;
 };
 
+// The CTA's tokens, sorted: (row's number in the group, token).
 struct SmallWindow {
     const uint2* pairs;
     uint32_t tokens, rows;
+    int chunk_bits;
     __device__ __forceinline__ uint2 at(uint32_t p) const { return p < tokens ? pairs[p] : make_uint2(rows, 0); }
     __device__ __forceinline__ uint32_t row(uint32_t p) const { return p < tokens ? pairs[p].x : rows; }
 };
+
+// Zeros into the first `columns` columns at `grad` of every groups-th row.
+template <typename T>
+__device__ __forceinline__ void zero_rows(T* grad, uint32_t rows, uint64_t pitch, uint32_t columns, int column_bits)
+{
+    constexpr uint32_t V = 16 / sizeof(T);
+    if (((reinterpret_cast<uintptr_t>(grad) | pitch * sizeof(T) | columns * sizeof(T)) & 15) == 0) {
+        const int bits = column_bits - (sizeof(T) == 4 ? 2 : 3);
+        const uint32_t at = (threadIdx.x & ((1u << bits) - 1)) * V;
+        if (at >= columns) return;
+        for (uint32_t row = threadIdx.x >> bits; row < rows; row += kSortThreads >> bits)
+            *reinterpret_cast<uint4*>(grad + row * pitch + at) = make_uint4(0, 0, 0, 0);
+    } else {
+        const uint32_t at = threadIdx.x & ((1u << column_bits) - 1);
+        if (at >= columns) return;
+        for (uint32_t row = threadIdx.x >> column_bits; row < rows; row += kSortThreads >> column_bits)
+            narrow(0.0f, grad[row * pitch + at]);
+    }
+}
 
 template <int SRC, int DST, bool ADD>
 __global__ void __launch_bounds__(kSortThreads, 1) grad_small_kernel(const SmallArgs a)
 {
     __shared__ SmallSort sort;
     __shared__ uint2 pairs[kSmallTokens];
-    __shared__ float parts[kSmallChunks][2][kSmallColumns];
+    __shared__ float parts[kSmallParts];                // [chunk][2][column]
     __shared__ uint2 long_runs[kSmallChunks];           // (chunk, row)
     __shared__ uint32_t run_count;
-    const uint32_t c = threadIdx.x % kSmallColumns, chunk = threadIdx.x / kSmallColumns, col = blockIdx.x * kSmallColumns + c;
+    const uint32_t across = 1u << a.column_bits, chunks = kSortThreads >> a.column_bits;
+    const uint32_t c = threadIdx.x & (across - 1), first_chunk = threadIdx.x >> a.column_bits;
+    const uint32_t tile = blockIdx.x / a.groups, group = blockIdx.x - tile * a.groups, col0 = tile * across;
     const uint32_t first = (threadIdx.x >> 5) * (32 * kSmallPerThread) + (threadIdx.x & 31);
-    const auto* dout = static_cast<const typename Element<SRC>::type*>(a.dout) + col;
-    auto* grad = static_cast<typename Element<DST>::type*>(a.grad) + col;
+    const uint32_t rows = (a.rows - 1 - group) / a.groups + 1;
+    const uint64_t pitch = (uint64_t)a.groups * a.dim;
+    const auto* dout = static_cast<const typename Element<SRC>::type*>(a.dout) + col0 + c;
+    auto* grad = static_cast<typename Element<DST>::type*>(a.grad) + (uint64_t)group * a.dim + col0;
     const auto finish_one = [&](uint32_t row, float sum, float old) {
-        narrow(ADD ? __fadd_rn(old, __fmul_rn(a.scale, sum)) : __fmul_rn(a.scale, sum), grad[(uint64_t)row * a.dim]);
+        narrow(ADD ? __fadd_rn(old, __fmul_rn(a.scale, sum)) : __fmul_rn(a.scale, sum), grad[row * pitch + c]);
     };
     if (threadIdx.x == 0) run_count = 0;
     grid_dependency_wait();
     uint2 pair[kSmallPerThread];
-    const uint32_t held = a.wide ? load_pairs<int64_t, kSmallPerThread>(static_cast<const int64_t*>(a.ids), a.tokens, a.rows, first, pair)
-                                 : load_pairs<int32_t, kSmallPerThread>(static_cast<const int32_t*>(a.ids), a.tokens, a.rows, first, pair);
-    if (!ADD && col < a.dim)
-        for (uint32_t row = chunk; row < a.rows; row += kSmallChunks) narrow(0.0f, grad[(uint64_t)row * a.dim]);
-    sort_in_cta<kSmallPerThread>(pair, held, a.key_bits, sort, pairs);               // ends with a barrier
+    uint32_t held = a.wide ? load_pairs<int64_t, kSmallPerThread>(static_cast<const int64_t*>(a.ids), a.tokens, a.rows, first, pair)
+                           : load_pairs<int32_t, kSmallPerThread>(static_cast<const int32_t*>(a.ids), a.tokens, a.rows, first, pair);
+    if (!ADD) zero_rows(grad, rows, pitch, min(across, a.dim - col0), a.column_bits);
+#pragma unroll
+    for (int r = 0; r < kSmallPerThread; ++r) {
+        const uint32_t row = pair[r].x / a.groups;
+        if (pair[r].x >= a.rows || pair[r].x - row * a.groups != group) held &= ~(1u << r);
+        pair[r].x = row;
+    }
+    const uint32_t n = sort_in_cta<kSmallPerThread>(pair, held, a.key_bits, sort, pairs);     // ends with a barrier
 
-    const SmallWindow tokens = {pairs, a.tokens, a.rows};
-    if (col < a.dim && (chunk << kSmallChunkBits) < a.tokens) {
+    SmallWindow tokens = {pairs, n, rows, 2};
+    while (tokens.chunk_bits < kMaxChunkBits && n > min(chunks, kSmallChunks) << tokens.chunk_bits) ++tokens.chunk_bits;
+    for (uint32_t chunk = first_chunk; col0 + c < a.dim && (chunk << tokens.chunk_bits) < n; chunk += chunks) {
         constexpr int kAhead = 16;                      // as a rule, all of a chunk
-        const ChunkWork w(a, tokens, chunk);
+        const ChunkWork w(tokens, tokens, chunk);
         if (w.begins && c == 0) long_runs[atomicAdd(&run_count, 1u)] = make_uint2(chunk, w.leaving);
         float sum = 0.0f;
         for (uint32_t p = w.begin; p < w.end; p += kAhead) {
@@ -374,7 +411,7 @@ __global__ void __launch_bounds__(kSortThreads, 1) grad_small_kernel(const Small
                 const uint2 k = tokens.at(p + u);
                 x[u] = widen(dout[(uint64_t)k.y * a.dim]);
                 if constexpr (ADD)
-                    if (tokens.row(p + u + 1) != k.x && k.x != w.entering) old[u] = widen(grad[(uint64_t)k.x * a.dim]);
+                    if (tokens.row(p + u + 1) != k.x && k.x != w.entering) old[u] = widen(grad[k.x * pitch + c]);
             }
 #pragma unroll
             for (int u = 0; u < kAhead; ++u) {
@@ -382,26 +419,26 @@ __global__ void __launch_bounds__(kSortThreads, 1) grad_small_kernel(const Small
                 sum = __fadd_rn(sum, x[u]);
                 const uint32_t row = tokens.row(p + u);
                 if (tokens.row(p + u + 1) == row) continue;
-                if (row == w.entering) parts[chunk][0][c] = sum;
+                if (row == w.entering) parts[(chunk * 2) * across + c] = sum;
                 else finish_one(row, sum, ADD ? old[ADD ? u : 0] : 0.0f);
                 sum = 0.0f;
             }
         }
-        if (w.leaving != a.rows) parts[chunk][w.begins ? 1 : 0][c] = sum;
+        if (w.leaving != rows) parts[(chunk * 2 + (w.begins ? 1 : 0)) * across + c] = sum;
     }
     __syncthreads();
-    if (col >= a.dim) return;
-    for (uint32_t i = chunk; i < run_count; i += kSmallChunks) {
+    if (col0 + c >= a.dim) return;
+    for (uint32_t i = first_chunk; i < run_count; i += chunks) {
         const uint2 r = long_runs[i];
-        const float old = ADD ? widen(grad[(uint64_t)r.y * a.dim]) : 0.0f;
-        float sum = parts[r.x][1][c];
+        const float old = ADD ? widen(grad[r.y * pitch + c]) : 0.0f;
+        float sum = parts[(r.x * 2 + 1) * across + c];
         for (uint32_t k = r.x + 1;; k += 8) {           // the chunks that the run goes on in, eight looks at a time
             float part[8];
             bool on[8];
 #pragma unroll
             for (int u = 0; u < 8; ++u) {
-                on[u] = tokens.row((k + u) << kSmallChunkBits) == r.y;
-                part[u] = on[u] ? parts[k + u][0][c] : 0.0f;
+                on[u] = tokens.row((k + u) << tokens.chunk_bits) == r.y;
+                part[u] = on[u] ? parts[(k + u) * 2 * across + c] : 0.0f;
             }
 #pragma unroll
             for (int u = 0; u < 8; ++u)
@@ -467,19 +504,27 @@ template <int SRC, int DST> cudaError_t by_group(const GradArgs& a, bool add, cu
 
 namespace {
 
-// One launch instead of four: 2048 tokens, 1000 rows of 64 take 12.5 us against 17, 32 tokens 6.8 against 10.  Every CTA sorts,
-// so there must not be more of them than SMs, and a CTA's columns of a long table are too short to be set to zero fast (100
-// tokens, 4096 rows of 1024: 12 us against 11.3).
-bool small_applies(uint64_t tokens, uint64_t rows, uint64_t dim, bool add)
+// One launch instead of four: 2048 tokens, 1000 rows of 64 take 6.4 us against 12.5, 32 tokens 4.2 against 8.7, 2048 tokens, 4096
+// rows of 515 12.7 against 17.  Not where there is more to add up (64 rows of 1024: 19 us against 16) or where the zeros are
+// what takes the time: the CTAs write a piece of a row at a time, single elements where rows start anywhere (30,000 rows of 1024
+// in bf16: 13 us against 11; of 515: 14 against 8; 100,000 rows of 64 in fp32: 9 against 15).
+bool small_applies(uint64_t tokens, uint64_t rows, uint64_t dim, bool add, const void* grad, uint64_t element)
 {
-    return tokens != 0 && tokens <= kSmallTokens && dim <= 148 * kSmallColumns && (add || rows <= 2048);
+    if (tokens == 0 || tokens > kSmallTokens || tokens * dim > 3 << 19) return false;
+    const bool words = (reinterpret_cast<uintptr_t>(grad) | dim * element) % 16 == 0;
+    return add || rows * dim <= (words ? (32u << 20) / element : 4u << 20);
 }
 
-template <int SRC, int DST> cudaError_t launch_small(const SmallArgs& a, bool add, cudaStream_t stream)
+template <int SRC, int DST> cudaError_t launch_small(SmallArgs a, bool add, cudaStream_t stream)
 {
-    const unsigned grid = (a.dim + kSmallColumns - 1) / kSmallColumns;
-    return add ? launch_pdl(grad_small_kernel<SRC, DST, true>, grid, kSortThreads, stream, a)
-               : launch_pdl(grad_small_kernel<SRC, DST, false>, grid, kSortThreads, stream, a);
+    a.column_bits = kLeastColumnBits;
+    while (a.column_bits < kSmallColumnBits && 1u << a.column_bits < a.dim) ++a.column_bits;
+    const uint32_t tiles = (a.dim + (1u << a.column_bits) - 1) >> a.column_bits;
+    a.groups = tiles < 148 ? 148 / tiles : 1;           // a CTA to each SM
+    if (a.groups > a.rows) a.groups = a.rows;
+    a.key_bits = token_key_bits((a.rows - 1) / a.groups);
+    return add ? launch_pdl(grad_small_kernel<SRC, DST, true>, tiles * a.groups, kSortThreads, stream, a)
+               : launch_pdl(grad_small_kernel<SRC, DST, false>, tiles * a.groups, kSortThreads, stream, a);
 }
 
 }  // namespace
@@ -492,9 +537,10 @@ size_t embedding_workspace_floats(uint64_t tokens, uint64_t rows, uint64_t dim)
 cudaError_t launch_embedding_grad(const void* dout, int dout_dtype, const TokenIds& ids, uint64_t rows, uint64_t dim,
                                   float scale, void* grad, int grad_dtype, bool add, float* workspace, cudaStream_t stream)
 {
-    if (small_applies(ids.count, rows, dim, add)) {
-        const SmallArgs s = {ids.ptr, dout, grad, (uint32_t)dim, (uint32_t)ids.count, (uint32_t)rows, token_key_bits((uint32_t)rows),
-                             kSmallChunkBits, ids.wide, scale};
+    if (small_applies(ids.count, rows, dim, add, grad, grad_dtype == kF32 ? 4 : 2)) {
+        SmallArgs s = {ids.ptr, dout, grad, (uint32_t)dim, (uint32_t)ids.count, (uint32_t)rows};
+        s.wide = ids.wide;
+        s.scale = scale;
         if (dout_dtype == kF32)
             return grad_dtype == kF32 ? launch_small<kF32, kF32>(s, add, stream) : launch_small<kF32, kBf16>(s, add, stream);
         return grad_dtype == kF32 ? launch_small<kBf16, kF32>(s, add, stream) : launch_small<kBf16, kBf16>(s, add, stream);

@@ -97,16 +97,22 @@ struct SmallSort {
     uint32_t total[1 << kSmallBits];
 };
 
-// `pairs`: K x 1024 in shared memory; the sorted pairs are there at the end, `held` of this thread's pairs exist.
+// `pairs`: K x 1024 in shared memory; the sorted pairs are there at the end, `held` of this thread's pairs exist.  Returns how
+// many there are.
 template <int K>
-__device__ __forceinline__ void sort_in_cta(uint2 (&pair)[K], uint32_t held, int bits, SmallSort& s, uint2* pairs)
+__device__ __forceinline__ uint32_t sort_in_cta(uint2 (&pair)[K], uint32_t held, int bits, SmallSort& s, uint2* pairs)
 {
     const uint32_t lane = threadIdx.x & 31, w = threadIdx.x >> 5, local = w * (32 * K) + lane;
     const int passes = (bits + kSmallBits - 1) / kSmallBits, digit_bits = (bits + passes - 1) / passes, bins = 1 << digit_bits;
+    uint32_t n = 0;
     for (int shift = 0; shift < bits; shift += digit_bits) {
-        if (shift != 0) {
+        if (shift != 0) {                               // the first pass left them one behind the other
+            held = 0;
 #pragma unroll
-            for (int r = 0; r < K; ++r) pair[r] = pairs[local + r * 32];
+            for (int r = 0; r < K; ++r) {
+                pair[r] = pairs[local + r * 32];
+                held |= local + r * 32 < n ? 1u << r : 0u;
+            }
         }
         for (int i = lane; i < (bins + 1) / 2; i += 32) reinterpret_cast<uint32_t*>(s.count[w])[i] = 0;
         __syncwarp();
@@ -125,7 +131,9 @@ __device__ __forceinline__ void sort_in_cta(uint2 (&pair)[K], uint32_t held, int
         uint32_t total = 0;
         for (int i = 0; i < per; ++i)
             if ((int)lane * per + i < bins) total += s.total[lane * per + i];
-        uint32_t at = sum_up_to_lane(total) - total;
+        const uint32_t up_to = sum_up_to_lane(total);
+        n = __shfl_sync(0xFFFFFFFFu, up_to, 31);
+        uint32_t at = up_to - total;
         for (int i = 0; i < per; ++i) {
             if ((int)lane * per + i >= bins) break;
             s.count[w][lane * per + i] += (uint16_t)at;
@@ -139,6 +147,7 @@ __device__ __forceinline__ void sort_in_cta(uint2 (&pair)[K], uint32_t held, int
         }
         __syncthreads();
     }
+    return n;
 }
 
 }  // namespace mqg
