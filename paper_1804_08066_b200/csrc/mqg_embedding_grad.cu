@@ -9,6 +9,8 @@
 //      crosses chunks belongs to the chunk it begins in, which follows it, as long as it covers no chunk as a whole (less
 //      than 2 C tokens); of a longer one every chunk leaves its part's sum in the workspace;
 //   3. the parts of the long runs are added up in the order of the chunks.
+#include <atomic>
+
 #include "mqg_token_sort.cuh"
 #include "mqg_vector.cuh"
 
@@ -316,12 +318,17 @@ __global__ void __launch_bounds__(kJoinThreads) grad_join_kernel(const GradArgs 
 // A CTA has up to 32 columns of every G-th row of the table (every G-th, so that the frequent ids, which often are neighbours, do
 // not meet in one CTA).  It sets them to zero, finds its rows' tokens among all and sorts them in shared memory, adds them up in
 // chunks, a thread to each column of a chunk, and joins the long runs' parts, which stay in shared memory.  Bound by latency: of
-// the launch, the sort (one pass where the CTA has at most 64 rows) and two turns to memory.  (64 columns: 2048 tokens, a
-// seventh of them the same, 1000 rows of 64 take 9.4 us against 8, as many evenly spread 6.2 against 6.4.)
-constexpr int kSmallPerThread = 2, kSmallColumnBits = 5, kLeastColumnBits = 3;
+// the launch, the search, the sort (one pass where the CTA has at most 64 rows) and two turns to memory.  (64 columns: 2048
+// tokens, a seventh of them the same, 1000 rows of 64 take 9.4 us against 8, as many evenly spread 6.2 against 6.4.)
+constexpr int kSmallColumnBits = 5, kLeastColumnBits = 3, kSmallPerThread = 8;
 constexpr uint32_t kSmallTokens = kSmallPerThread * kSortThreads;
-// 4 tokens to a chunk, up to 32 where that makes more than 64 chunks or more than there are threads for
-constexpr uint32_t kSmallChunks = kSmallTokens >> kMaxChunkBits, kSmallParts = kSmallChunks * 2 << kSmallColumnBits;
+static_assert(kSmallTokens <= 1u << PairWord::kTokenBits, "a token is part of a word");
+constexpr uint32_t kFewChunks = 64;                     // 4 tokens to a chunk, up to 32 where that makes more chunks than this
+
+__host__ __device__ constexpr uint32_t small_chunks(uint32_t tokens)
+{
+    return tokens >> kMaxChunkBits > kFewChunks ? (tokens + (1u << kMaxChunkBits) - 1) >> kMaxChunkBits : kFewChunks;
+}
 
 struct SmallArgs {
     const void* ids;
@@ -329,20 +336,66 @@ struct SmallArgs {
     void* grad;
     uint32_t dim, tokens, rows;
     uint32_t groups;         // G
-    int key_bits;            // of a row's number in its group
+    uint32_t reciprocal;     // ceil(2^32 / G): a row's number in its group is the high word of the product; 0: G = 1
+    int key_bits;            // of that number
     int column_bits;         // 2^this columns of a CTA
     int wide;
     float scale;
 };
+constexpr uint64_t kSmallRows = 1 << 24;                // what the reciprocal is exact for, up to G = 148
 
-// The CTA's tokens, sorted: (row's number in the group, token).
+// The CTA's tokens, sorted by row.
 struct SmallWindow {
-    const uint2* pairs;
+    const PairWord* pairs;
     uint32_t tokens, rows;
     int chunk_bits;
-    __device__ __forceinline__ uint2 at(uint32_t p) const { return p < tokens ? pairs[p] : make_uint2(rows, 0); }
-    __device__ __forceinline__ uint32_t row(uint32_t p) const { return p < tokens ? pairs[p].x : rows; }
+    __device__ __forceinline__ uint32_t row(uint32_t p) const { return p < tokens ? pairs[p].key() : rows; }
 };
+
+// The tokens of the CTA's rows into `pairs`, in order; returns how many.
+template <typename ID>
+__device__ __forceinline__ uint32_t find_tokens(const SmallArgs& a, uint32_t group, PairWord* pairs, uint32_t* warp_total)
+{
+    const uint32_t lane = threadIdx.x & 31, w = threadIdx.x >> 5, per = (a.tokens + kSortThreads - 1) / kSortThreads;
+    const uint32_t first = w * 32 * per + lane;
+    const ID* ids = static_cast<const ID*>(a.ids);
+    uint32_t row[kSmallPerThread];
+#pragma unroll
+    for (int r = 0; r < kSmallPerThread; ++r) {
+        const uint32_t i = first + r * 32;
+        row[r] = (uint32_t)r < per && i < a.tokens ? key_of(__ldg(ids + i), a.rows) : a.rows;
+    }
+    uint32_t count = 0, held = 0;
+#pragma unroll
+    for (int r = 0; r < kSmallPerThread; ++r) {
+        if ((uint32_t)r >= per) break;
+        const uint32_t k = a.reciprocal != 0 ? __umulhi(row[r], a.reciprocal) : row[r];
+        const bool mine = row[r] < a.rows && row[r] - k * a.groups == group;
+        held |= mine ? 1u << r : 0u;
+        row[r] = k;
+        count += __popc(__ballot_sync(0xFFFFFFFFu, mine));
+    }
+    if (lane == 0) warp_total[w] = count;
+    __syncthreads();
+    const uint32_t total = warp_total[lane], up_to = sum_up_to_lane(total);
+    uint32_t at = __shfl_sync(0xFFFFFFFFu, up_to - total, w);
+#pragma unroll
+    for (int r = 0; r < kSmallPerThread; ++r) {
+        if ((uint32_t)r >= per) break;
+        const bool mine = (held >> r) & 1u;
+        const uint32_t all = __ballot_sync(0xFFFFFFFFu, mine);
+        if (mine) pairs[at + __popc(all & ((1u << lane) - 1))].v = row[r] << PairWord::kTokenBits | (first + r * 32);
+        at += __popc(all);
+    }
+    __syncthreads();
+    return __shfl_sync(0xFFFFFFFFu, up_to, 31);
+}
+
+template <int K> __device__ __forceinline__ void sort_small(PairWord* pairs, uint32_t n, int bits, SmallSort& s)
+{
+    PairWord pair[K];
+    sort_in_cta<K>(pair, take_pairs<K>(pair, pairs, n), n, bits, s, pairs);
+}
 
 // Zeros into the first `columns` columns at `grad` of every groups-th row.
 template <typename T>
@@ -366,15 +419,14 @@ __device__ __forceinline__ void zero_rows(T* grad, uint32_t rows, uint64_t pitch
 template <int SRC, int DST, bool ADD>
 __global__ void __launch_bounds__(kSortThreads, 1) grad_small_kernel(const SmallArgs a)
 {
+    extern __shared__ __align__(16) unsigned char smem[];
     __shared__ SmallSort sort;
-    __shared__ uint2 pairs[kSmallTokens];
-    __shared__ float parts[kSmallParts];                // [chunk][2][column]
-    __shared__ uint2 long_runs[kSmallChunks];           // (chunk, row)
-    __shared__ uint32_t run_count;
+    __shared__ uint32_t warp_total[kSortWarps], long_runs[small_chunks(kSmallTokens)], run_count;
+    float* parts = reinterpret_cast<float*>(smem);      // [chunk][2][column]
+    PairWord* pairs = reinterpret_cast<PairWord*>(parts + (small_chunks(a.tokens) * 2 << a.column_bits));
     const uint32_t across = 1u << a.column_bits, chunks = kSortThreads >> a.column_bits;
     const uint32_t c = threadIdx.x & (across - 1), first_chunk = threadIdx.x >> a.column_bits;
     const uint32_t tile = blockIdx.x / a.groups, group = blockIdx.x - tile * a.groups, col0 = tile * across;
-    const uint32_t first = (threadIdx.x >> 5) * (32 * kSmallPerThread) + (threadIdx.x & 31);
     const uint32_t rows = (a.rows - 1 - group) / a.groups + 1;
     const uint64_t pitch = (uint64_t)a.groups * a.dim;
     const auto* dout = static_cast<const typename Element<SRC>::type*>(a.dout) + col0 + c;
@@ -384,43 +436,44 @@ __global__ void __launch_bounds__(kSortThreads, 1) grad_small_kernel(const Small
     };
     if (threadIdx.x == 0) run_count = 0;
     grid_dependency_wait();
-    uint2 pair[kSmallPerThread];
-    uint32_t held = a.wide ? load_pairs<int64_t, kSmallPerThread>(static_cast<const int64_t*>(a.ids), a.tokens, a.rows, first, pair)
-                           : load_pairs<int32_t, kSmallPerThread>(static_cast<const int32_t*>(a.ids), a.tokens, a.rows, first, pair);
     if (!ADD) zero_rows(grad, rows, pitch, min(across, a.dim - col0), a.column_bits);
-#pragma unroll
-    for (int r = 0; r < kSmallPerThread; ++r) {
-        const uint32_t row = pair[r].x / a.groups;
-        if (pair[r].x >= a.rows || pair[r].x - row * a.groups != group) held &= ~(1u << r);
-        pair[r].x = row;
+    const uint32_t n = a.wide ? find_tokens<int64_t>(a, group, pairs, warp_total) : find_tokens<int32_t>(a, group, pairs, warp_total);
+    if (n > 1 && rows > 1) {
+        if (n <= kSortThreads) sort_small<1>(pairs, n, a.key_bits, sort);
+        else if (n <= 2 * kSortThreads) sort_small<2>(pairs, n, a.key_bits, sort);
+        else if (n <= 4 * kSortThreads) sort_small<4>(pairs, n, a.key_bits, sort);
+        else sort_small<kSmallPerThread>(pairs, n, a.key_bits, sort);
     }
-    const uint32_t n = sort_in_cta<kSmallPerThread>(pair, held, a.key_bits, sort, pairs);     // ends with a barrier
 
     SmallWindow tokens = {pairs, n, rows, 2};
-    while (tokens.chunk_bits < kMaxChunkBits && n > min(chunks, kSmallChunks) << tokens.chunk_bits) ++tokens.chunk_bits;
+    while (tokens.chunk_bits < kMaxChunkBits && n > min(chunks, kFewChunks) << tokens.chunk_bits) ++tokens.chunk_bits;
     for (uint32_t chunk = first_chunk; col0 + c < a.dim && (chunk << tokens.chunk_bits) < n; chunk += chunks) {
         constexpr int kAhead = 16;                      // as a rule, all of a chunk
         const ChunkWork w(tokens, tokens, chunk);
-        if (w.begins && c == 0) long_runs[atomicAdd(&run_count, 1u)] = make_uint2(chunk, w.leaving);
+        if (w.begins && c == 0) long_runs[atomicAdd(&run_count, 1u)] = chunk;
         float sum = 0.0f;
         for (uint32_t p = w.begin; p < w.end; p += kAhead) {
-            float x[kAhead], old[ADD ? kAhead : 1];
+            typename Element<SRC>::type x[kAhead];      // (widened here, every load would be waited for before the next)
+            typename Element<DST>::type old[ADD ? kAhead : 1];
+            uint32_t ends = 0;
 #pragma unroll
             for (int u = 0; u < kAhead; ++u) {
                 if (p + u >= w.end) break;
-                const uint2 k = tokens.at(p + u);
-                x[u] = widen(dout[(uint64_t)k.y * a.dim]);
-                if constexpr (ADD)
-                    if (tokens.row(p + u + 1) != k.x && k.x != w.entering) old[u] = widen(grad[k.x * pitch + c]);
+                const PairWord k = pairs[p + u];
+                x[u] = dout[(uint64_t)k.token() * a.dim];
+                if (tokens.row(p + u + 1) != k.key()) {
+                    ends |= 1u << u;
+                    if (ADD && k.key() != w.entering) old[ADD ? u : 0] = grad[k.key() * pitch + c];
+                }
             }
 #pragma unroll
             for (int u = 0; u < kAhead; ++u) {
                 if (p + u >= w.end) break;
-                sum = __fadd_rn(sum, x[u]);
-                const uint32_t row = tokens.row(p + u);
-                if (tokens.row(p + u + 1) == row) continue;
+                sum = __fadd_rn(sum, widen(x[u]));
+                if (!((ends >> u) & 1u)) continue;
+                const uint32_t row = pairs[p + u].key();
                 if (row == w.entering) parts[(chunk * 2) * across + c] = sum;
-                else finish_one(row, sum, ADD ? old[ADD ? u : 0] : 0.0f);
+                else finish_one(row, sum, ADD ? widen(old[ADD ? u : 0]) : 0.0f);
                 sum = 0.0f;
             }
         }
@@ -429,15 +482,15 @@ __global__ void __launch_bounds__(kSortThreads, 1) grad_small_kernel(const Small
     __syncthreads();
     if (col0 + c >= a.dim) return;
     for (uint32_t i = first_chunk; i < run_count; i += chunks) {
-        const uint2 r = long_runs[i];
-        const float old = ADD ? widen(grad[r.y * pitch + c]) : 0.0f;
-        float sum = parts[(r.x * 2 + 1) * across + c];
-        for (uint32_t k = r.x + 1;; k += 8) {           // the chunks that the run goes on in, eight looks at a time
+        const uint32_t begin = long_runs[i], row = tokens.row(((begin + 1) << tokens.chunk_bits) - 1);
+        const float old = ADD ? widen(grad[row * pitch + c]) : 0.0f;
+        float sum = parts[(begin * 2 + 1) * across + c];
+        for (uint32_t k = begin + 1;; k += 8) {         // the chunks that the run goes on in, eight looks at a time
             float part[8];
             bool on[8];
 #pragma unroll
             for (int u = 0; u < 8; ++u) {
-                on[u] = tokens.row((k + u) << tokens.chunk_bits) == r.y;
+                on[u] = tokens.row((k + u) << tokens.chunk_bits) == row;
                 part[u] = on[u] ? parts[(k + u) * 2 * across + c] : 0.0f;
             }
 #pragma unroll
@@ -445,7 +498,7 @@ __global__ void __launch_bounds__(kSortThreads, 1) grad_small_kernel(const Small
                 if (on[u]) sum = __fadd_rn(sum, part[u]);
             if (!on[7]) break;
         }
-        finish_one(r.y, sum, old);
+        finish_one(row, sum, old);
     }
 }
 
@@ -504,27 +557,59 @@ template <int SRC, int DST> cudaError_t by_group(const GradArgs& a, bool add, cu
 
 namespace {
 
-// One launch instead of four: 2048 tokens, 1000 rows of 64 take 6.4 us against 12.5, 32 tokens 4.2 against 8.7, 2048 tokens, 4096
-// rows of 515 12.7 against 17.  Not where there is more to add up (64 rows of 1024: 19 us against 16) or where the zeros are
-// what takes the time: the CTAs write a piece of a row at a time, single elements where rows start anywhere (30,000 rows of 1024
-// in bf16: 13 us against 11; of 515: 14 against 8; 100,000 rows of 64 in fp32: 9 against 15).
-bool small_applies(uint64_t tokens, uint64_t rows, uint64_t dim, bool add, const void* grad, uint64_t element)
-{
-    if (tokens == 0 || tokens > kSmallTokens || tokens * dim > 3 << 19) return false;
-    const bool words = (reinterpret_cast<uintptr_t>(grad) | dim * element) % 16 == 0;
-    return add || rows * dim <= (words ? (32u << 20) / element : 4u << 20);
-}
+// One launch instead of four: 2048 tokens, 1000 rows of 64 take 6 us against 12 to 15, 64 tokens 4.7 against 9, 8192 tokens, 1000
+// rows of 256 11 against 18, 4096 tokens, 8000 rows of 515 14 to 16 against 19 to 22.  Not where there is more to add up (4096
+// tokens of 1024 take as long either way, 8192 of 1024 24 us against 20) or where the zeros are what takes the time: the CTAs
+// write a piece of a row at a time, single elements where rows start anywhere (30,000 rows of 1024 in bf16, one token: 13 us
+// against 11; of 515: 14 against 8; 100,000 rows of 64 in fp32: 9 against 15).
+constexpr uint64_t kSmallElements = 1 << 22;
 
-template <int SRC, int DST> cudaError_t launch_small(SmallArgs a, bool add, cudaStream_t stream)
+bool small_shape(SmallArgs& a)
 {
     a.column_bits = kLeastColumnBits;
     while (a.column_bits < kSmallColumnBits && 1u << a.column_bits < a.dim) ++a.column_bits;
     const uint32_t tiles = (a.dim + (1u << a.column_bits) - 1) >> a.column_bits;
     a.groups = tiles < 148 ? 148 / tiles : 1;           // a CTA to each SM
     if (a.groups > a.rows) a.groups = a.rows;
+    a.reciprocal = a.groups > 1 ? (uint32_t)(((1ull << 32) + a.groups - 1) / a.groups) : 0;
     a.key_bits = token_key_bits((a.rows - 1) / a.groups);
-    return add ? launch_pdl(grad_small_kernel<SRC, DST, true>, tiles * a.groups, kSortThreads, stream, a)
-               : launch_pdl(grad_small_kernel<SRC, DST, false>, tiles * a.groups, kSortThreads, stream, a);
+    return a.key_bits <= PairWord::kKeyBits;
+}
+
+bool small_applies(const TokenIds& ids, uint64_t rows, uint64_t dim, bool add, const void* grad, uint64_t element, SmallArgs& a)
+{
+    if (ids.count == 0 || ids.count > kSmallTokens || ids.count * dim > kSmallElements || rows > kSmallRows) return false;
+    const bool words = (reinterpret_cast<uintptr_t>(grad) | dim * element) % 16 == 0;
+    if (!add && rows * dim > (words ? (32u << 20) / element : 4u << 20)) return false;
+    a.ids = ids.ptr;
+    a.dim = (uint32_t)dim;
+    a.tokens = (uint32_t)ids.count;
+    a.rows = (uint32_t)rows;
+    a.wide = ids.wide;
+    return small_shape(a);
+}
+
+template <int SRC, int DST, bool ADD> cudaError_t launch_small(const SmallArgs& a, cudaStream_t stream)
+{
+    static std::atomic<bool> ready[64];                 // per device (zero-initialised)
+    const auto bytes = [](uint32_t tokens, int column_bits) { return (small_chunks(tokens) * 2 << column_bits) * 4 + tokens * 4; };
+    int dev = 0;
+    cudaError_t err = cudaGetDevice(&dev);
+    if (err != cudaSuccess) return err;
+    if (dev < 0 || dev >= 64) return cudaErrorInvalidDevice;
+    if (!ready[dev].load(std::memory_order_relaxed)) {
+        err = cudaFuncSetAttribute(grad_small_kernel<SRC, DST, ADD>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                   (int)bytes(kSmallTokens, kSmallColumnBits));
+        if (err != cudaSuccess) return err;
+        ready[dev].store(true, std::memory_order_relaxed);
+    }
+    const uint32_t tiles = (a.dim + (1u << a.column_bits) - 1) >> a.column_bits;
+    return launch_pdl_smem(grad_small_kernel<SRC, DST, ADD>, tiles * a.groups, kSortThreads, bytes(a.tokens, a.column_bits), stream, a);
+}
+
+template <int SRC, int DST> cudaError_t small_by_add(const SmallArgs& a, bool add, cudaStream_t stream)
+{
+    return add ? launch_small<SRC, DST, true>(a, stream) : launch_small<SRC, DST, false>(a, stream);
 }
 
 }  // namespace
@@ -537,13 +622,14 @@ size_t embedding_workspace_floats(uint64_t tokens, uint64_t rows, uint64_t dim)
 cudaError_t launch_embedding_grad(const void* dout, int dout_dtype, const TokenIds& ids, uint64_t rows, uint64_t dim,
                                   float scale, void* grad, int grad_dtype, bool add, float* workspace, cudaStream_t stream)
 {
-    if (small_applies(ids.count, rows, dim, add, grad, grad_dtype == kF32 ? 4 : 2)) {
-        SmallArgs s = {ids.ptr, dout, grad, (uint32_t)dim, (uint32_t)ids.count, (uint32_t)rows};
-        s.wide = ids.wide;
+    SmallArgs s = {};
+    if (small_applies(ids, rows, dim, add, grad, grad_dtype == kF32 ? 4 : 2, s)) {
+        s.dout = dout;
+        s.grad = grad;
         s.scale = scale;
         if (dout_dtype == kF32)
-            return grad_dtype == kF32 ? launch_small<kF32, kF32>(s, add, stream) : launch_small<kF32, kBf16>(s, add, stream);
-        return grad_dtype == kF32 ? launch_small<kBf16, kF32>(s, add, stream) : launch_small<kBf16, kBf16>(s, add, stream);
+            return grad_dtype == kF32 ? small_by_add<kF32, kF32>(s, add, stream) : small_by_add<kF32, kBf16>(s, add, stream);
+        return grad_dtype == kF32 ? small_by_add<kBf16, kF32>(s, add, stream) : small_by_add<kBf16, kBf16>(s, add, stream);
     }
     const Layout lay(ids.count, rows, dim);
     uint2* sorted = reinterpret_cast<uint2*>(workspace);

@@ -94,7 +94,7 @@ __global__ void __launch_bounds__(kThreads, 1) sort_small_kernel(const SortArgs 
     release_dependents();
     uint2 pair[K];
     const uint32_t held = load_pairs<ID, K>(static_cast<const ID*>(a.ids), a.tokens, a.rows, (threadIdx.x >> 5) * (32 * K) + (threadIdx.x & 31), pair);
-    sort_in_cta<K>(pair, held, a.bits, s, pairs);
+    sort_in_cta<K>(pair, held, a.tokens, a.bits, s, pairs);
     for (uint32_t i = threadIdx.x; i < a.tokens; i += kThreads) a.sorted[i] = pairs[i];
 }
 

@@ -16,6 +16,16 @@ template <typename ID> __device__ __forceinline__ uint32_t key_of(ID id, uint32_
 
 constexpr int kMaxDigitBits = 10;
 
+// A key of up to 19 bits and one of 8192 tokens in a word.
+struct PairWord {
+    static constexpr int kTokenBits = 13, kKeyBits = 32 - kTokenBits;
+    uint32_t v;
+    __device__ __forceinline__ uint32_t key() const { return v >> kTokenBits; }
+    __device__ __forceinline__ uint32_t token() const { return v & ((1u << kTokenBits) - 1); }
+};
+__device__ __forceinline__ uint32_t key_in(const uint2& pair) { return pair.x; }
+__device__ __forceinline__ uint32_t key_in(const PairWord& pair) { return pair.key(); }
+
 // The lanes of the warp that hold the same digit, among those that hold a key at all.  (Straight through the digit's bits: with a
 // branch at every bit a round of ballots took half as long again.)
 __device__ __forceinline__ uint32_t same_digit(uint32_t digit, int bits, uint32_t held)
@@ -60,20 +70,20 @@ __device__ __forceinline__ uint32_t load_pairs(const ID* ids, uint32_t tokens, u
 
 // Ranks a warp's pairs, 32 at a time: rank[r] = how many of the warp's pairs with the same digit stand before this one;
 // count[digit] = how many the warp has.  `held`: a bit for each r.
-template <int K>
-__device__ __forceinline__ void rank_pairs(const uint2 (&pair)[K], uint32_t held, int shift, int bits, uint16_t* count, uint32_t (&rank)[K])
+template <int K, typename Pair>
+__device__ __forceinline__ void rank_pairs(const Pair (&pair)[K], uint32_t held, int shift, int bits, uint16_t* count, uint32_t (&rank)[K])
 {
     const uint32_t lane = threadIdx.x & 31, mask = (1u << bits) - 1;
     uint32_t there[K];
 #pragma unroll
     for (int r = 0; r < K; ++r) {
         there[r] = __ballot_sync(0xFFFFFFFFu, (held >> r) & 1u);
-        rank[r] = there[r] == 0 ? 0 : same_digit((pair[r].x >> shift) & mask, bits, there[r]);
+        rank[r] = there[r] == 0 ? 0 : same_digit((key_in(pair[r]) >> shift) & mask, bits, there[r]);
     }
 #pragma unroll
     for (int r = 0; r < K; ++r) {
         if (there[r] == 0) continue;
-        const uint32_t digit = (pair[r].x >> shift) & mask, same = rank[r], so_far = count[digit];
+        const uint32_t digit = (key_in(pair[r]) >> shift) & mask, same = rank[r], so_far = count[digit];
         __syncwarp();
         if (((held >> r) & 1u) && (same >> lane) == 1u) count[digit] = (uint16_t)(so_far + __popc(same));
         __syncwarp();
@@ -97,23 +107,29 @@ struct SmallSort {
     uint32_t total[1 << kSmallBits];
 };
 
-// `pairs`: K x 1024 in shared memory; the sorted pairs are there at the end, `held` of this thread's pairs exist.  Returns how
-// many there are.
-template <int K>
-__device__ __forceinline__ uint32_t sort_in_cta(uint2 (&pair)[K], uint32_t held, int bits, SmallSort& s, uint2* pairs)
+// This thread's pairs of n in shared memory.
+template <int K, typename Pair>
+__device__ __forceinline__ uint32_t take_pairs(Pair (&pair)[K], const Pair* pairs, uint32_t n)
 {
-    const uint32_t lane = threadIdx.x & 31, w = threadIdx.x >> 5, local = w * (32 * K) + lane;
-    const int passes = (bits + kSmallBits - 1) / kSmallBits, digit_bits = (bits + passes - 1) / passes, bins = 1 << digit_bits;
-    uint32_t n = 0;
-    for (int shift = 0; shift < bits; shift += digit_bits) {
-        if (shift != 0) {                               // the first pass left them one behind the other
-            held = 0;
+    const uint32_t local = (threadIdx.x >> 5) * (32 * K) + (threadIdx.x & 31);
+    uint32_t held = 0;
 #pragma unroll
-            for (int r = 0; r < K; ++r) {
-                pair[r] = pairs[local + r * 32];
-                held |= local + r * 32 < n ? 1u << r : 0u;
-            }
-        }
+    for (int r = 0; r < K; ++r) {
+        if (local + r * 32 >= n) continue;
+        pair[r] = pairs[local + r * 32];
+        held |= 1u << r;
+    }
+    return held;
+}
+
+// n pairs, of which `held` are this thread's; the sorted ones are in `pairs`, in shared memory, at the end.
+template <int K, typename Pair>
+__device__ __forceinline__ void sort_in_cta(Pair (&pair)[K], uint32_t held, uint32_t n, int bits, SmallSort& s, Pair* pairs)
+{
+    const uint32_t lane = threadIdx.x & 31, w = threadIdx.x >> 5;
+    const int passes = (bits + kSmallBits - 1) / kSmallBits, digit_bits = (bits + passes - 1) / passes, bins = 1 << digit_bits;
+    for (int shift = 0; shift < bits; shift += digit_bits) {
+        if (shift != 0) held = take_pairs<K>(pair, pairs, n);
         for (int i = lane; i < (bins + 1) / 2; i += 32) reinterpret_cast<uint32_t*>(s.count[w])[i] = 0;
         __syncwarp();
         uint32_t rank[K];
@@ -131,9 +147,7 @@ __device__ __forceinline__ uint32_t sort_in_cta(uint2 (&pair)[K], uint32_t held,
         uint32_t total = 0;
         for (int i = 0; i < per; ++i)
             if ((int)lane * per + i < bins) total += s.total[lane * per + i];
-        const uint32_t up_to = sum_up_to_lane(total);
-        n = __shfl_sync(0xFFFFFFFFu, up_to, 31);
-        uint32_t at = up_to - total;
+        uint32_t at = sum_up_to_lane(total) - total;
         for (int i = 0; i < per; ++i) {
             if ((int)lane * per + i >= bins) break;
             s.count[w][lane * per + i] += (uint16_t)at;
@@ -142,12 +156,11 @@ __device__ __forceinline__ uint32_t sort_in_cta(uint2 (&pair)[K], uint32_t held,
         __syncwarp();
 #pragma unroll
         for (int r = 0; r < K; ++r) {
-            const uint32_t digit = (pair[r].x >> shift) & (bins - 1);
+            const uint32_t digit = (key_in(pair[r]) >> shift) & (bins - 1);
             if ((held >> r) & 1u) pairs[s.count[w][digit] + rank[r]] = pair[r];
         }
         __syncthreads();
     }
-    return n;
 }
 
 }  // namespace mqg

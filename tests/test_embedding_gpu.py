@@ -173,7 +173,7 @@ def test_gradient_by_the_sort_of_each_size(tokens, kind, add):
 
 @pytest.mark.parametrize("add", [False, True])
 @pytest.mark.parametrize("kind", ["same", "zipf", "uniform", "outside"])
-@pytest.mark.parametrize("tokens", [1, 8, 9, 250, 1024, 2048])
+@pytest.mark.parametrize("tokens", [1, 8, 9, 250, 1024, 1025, 2048, 4097, 8191])
 def test_gradient_of_few_tokens(tokens, kind, add):
     for rows, dim in ((1, 9), (2, 33), (147, 32), (149, 31), (1000, 8), (9500, 40)):
         _check_gradient((rows, dim, tokens), kind, I32, (F32, BF16), add, shift=1)
@@ -181,7 +181,7 @@ def test_gradient_of_few_tokens(tokens, kind, add):
 
 
 @pytest.mark.parametrize("add", [False, True])
-@pytest.mark.parametrize("shape", [(50, 768, 2048), (50, 769, 2048), (131_072, 64, 40), (131_073, 64, 40), (64_527, 65, 40), (64_528, 65, 40),
+@pytest.mark.parametrize("shape", [(50, 512, 8192), (50, 513, 8192), (50, 24, 8193), (1 << 24, 1, 100), (131_072, 64, 40), (131_073, 64, 40), (64_527, 65, 40), (64_528, 65, 40),
                                    (2, 200_000, 7), (3, 250_000, 7)])
 def test_gradient_where_one_launch_ends(shape, add):
     _check_gradient(shape, "zipf", I64, (F32, F32), add)
