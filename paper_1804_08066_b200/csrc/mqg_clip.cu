@@ -3,11 +3,12 @@
 //   N = sqrt(sum over all elements of x^2)        c = 1 where N <= max_norm, else max_norm / N
 //   y = fl(c * x)
 //
-// The tensors are cut into tiles of 16 KB.  Up to eight of them are one launch, a cluster whose CTAs have a tile each.  Above that
+// The tensors are cut into tiles of 16 KB.  Up to 32 of them are one launch, a cluster whose CTAs hold one or four each.  Above that
 // the measuring kernel's CTAs take the tiles in turn and leave one partial sum each, in a fixed order and without atomics, and
 // every CTA of the kernel that scales adds them up itself (740 at most for each launch of the first kernel, from L2), so that
-// no launch stands between the two, or, for long lists, a third kernel does.  The second reading comes from DRAM all the same where the tensors and what is written exceed
-// about a quarter of L2: of 100 MB read twice, the second time backwards, 27 MB came from L2, whatever the eviction priorities.
+// no launch stands between the two, or, for long lists, a third kernel does.  The second reading comes from DRAM all the same
+// where the tensors and what is written exceed about a quarter of L2: of 100 MB read twice, the second time backwards, 27 MB
+// came from L2, whatever the eviction priorities.
 // Squares are summed in fp32 inside a thread's share of a tile (at most 33 of them) and in 64 bits from there on.  A share
 // whose sum of squares leaves the range where fp32 holds it is summed again in 64 bits: the norm is right for every finite
 // gradient, also where single squares overflow or vanish in fp32.
@@ -98,16 +99,16 @@ template <int DTYPE> struct Parts {
     }
 };
 
-__device__ __forceinline__ double block_sum(double v)
+template <int BLOCK = kThreads> __device__ __forceinline__ double block_sum(double v)
 {
-    __shared__ double warp_sum[kThreads / 32];
+    __shared__ double warp_sum[BLOCK / 32];
 #pragma unroll
     for (int d = 16; d > 0; d >>= 1) v += __shfl_xor_sync(0xFFFFFFFFu, v, d);
     if ((threadIdx.x & 31) == 0) warp_sum[threadIdx.x >> 5] = v;
     __syncthreads();
     double t = 0.0;
 #pragma unroll
-    for (int w = 0; w < kThreads / 32; ++w) t += warp_sum[w];
+    for (int w = 0; w < BLOCK / 32; ++w) t += warp_sum[w];
     return t;
 }
 
@@ -137,8 +138,12 @@ __device__ __forceinline__ double squares(const Packed<DTYPE, 16 / kElemBytes<DT
     return d;
 }
 
+// The number of this thread among the kThreads that have a tile.
+__device__ __forceinline__ uint32_t tile_thread() { return threadIdx.x % kThreads; }
+
 // This thread's vectors of a tile, zeros where there are none, and its element outside them.
 constexpr int kVectors = kTileBytes / 16 / kThreads;
+struct Held { uint4 x[kVectors]; float edge; };
 template <int DTYPE> struct Share {
     static constexpr int V = 16 / kElemBytes<DTYPE>;
     const typename Element<DTYPE>::type* p;
@@ -155,11 +160,25 @@ template <int DTYPE> struct Share {
             if (has(k)) x[k].load(p + at(k));
             else x[k].w[0] = make_uint4(0, 0, 0, 0);
         }
-        has_edge = parts.edge(threadIdx.x, edge_at);
+        has_edge = parts.edge(tile_thread(), edge_at);
         edge = has_edge ? widen(p[edge_at]) : 0.0f;
     }
-    __device__ __forceinline__ bool has(int k) const { return threadIdx.x + k * kThreads < parts.nvec; }
-    __device__ __forceinline__ uint32_t at(int k) const { return parts.head + (threadIdx.x + k * kThreads) * V; }
+    // as it was held by another of the same tile
+    __device__ __forceinline__ Share(const Tile& t, const Held& h) : p(static_cast<const typename Element<DTYPE>::type*>(t.ptr)), parts(p, t.count)
+    {
+#pragma unroll
+        for (int k = 0; k < kVectors; ++k) x[k].w[0] = h.x[k];
+        has_edge = parts.edge(tile_thread(), edge_at);
+        edge = h.edge;
+    }
+    __device__ __forceinline__ void hold(Held& h) const
+    {
+#pragma unroll
+        for (int k = 0; k < kVectors; ++k) h.x[k] = x[k].w[0];
+        h.edge = edge;
+    }
+    __device__ __forceinline__ bool has(int k) const { return tile_thread() + k * kThreads < parts.nvec; }
+    __device__ __forceinline__ uint32_t at(int k) const { return parts.head + (tile_thread() + k * kThreads) * V; }
     __device__ __forceinline__ double sum() const { return squares<DTYPE, kVectors>(x, edge); }
 };
 
@@ -315,7 +334,7 @@ scale_kernel(const __grid_constant__ TensorTable<CAP> tab, const double* __restr
 
 // ---- one launch ----
 constexpr int kClusterTensors = 32;
-constexpr unsigned kClusterTiles = 8;
+constexpr unsigned kClusterCtas = 8, kClusterTiles = 4 * kClusterCtas;
 
 __device__ __forceinline__ uint32_t cluster_rank()
 {
@@ -335,10 +354,10 @@ __device__ __forceinline__ double peer_load(const double* p, uint32_t rank)
 }
 
 // The sum of squares of a cluster's CTAs.
-__device__ __forceinline__ double cluster_sum(double v)
+template <int BLOCK> __device__ __forceinline__ double cluster_sum(double v)
 {
     __shared__ double cta_sum;
-    v = block_sum(v);
+    v = block_sum<BLOCK>(v);
     if (threadIdx.x == 0) cta_sum = v;
     cluster_arrive();
     cluster_wait();
@@ -348,18 +367,19 @@ __device__ __forceinline__ double cluster_sum(double v)
     return all;
 }
 
-// One tile: measured, and scaled as it is held.
-template <int SRC, int DST>
-__device__ __forceinline__ void clip_tile(const Tile& t, float max_norm, void* flat, float* result)
+template <int SRC> __device__ __forceinline__ double measure_tile(const Tile& t, Held& h)
 {
-    constexpr int V = Share<SRC>::V;
     const Share<SRC> s(t);
-    float norm;
-    const float c = factor_of(cluster_sum(s.sum()), max_norm, &norm);
-    if (cluster_rank() == 0 && threadIdx.x == 0) { result[0] = norm; result[1] = c; }
-    if (DST == -2 || (DST == -1 && c == 1.0f)) return;
-    constexpr int D = DST < 0 ? SRC : DST;
+    s.hold(h);
+    return s.sum();
+}
+
+// c times a tile as it is held.
+template <int SRC, int DST> __device__ __forceinline__ void write_tile(const Tile& t, const Held& h, float c, void* flat)
+{
+    constexpr int V = Share<SRC>::V, D = DST < 0 ? SRC : DST;
     using Out = typename Element<D>::type;
+    const Share<SRC> s(t, h);
     Out* y = DST < 0 ? static_cast<Out*>(const_cast<void*>(t.ptr)) : static_cast<Out*>(flat) + t.at;
     if (s.has_edge) narrow(c * s.edge, y[s.edge_at]);
     const bool aligned = (reinterpret_cast<uintptr_t>(y + s.parts.head) & (Packed<D, V>::kWordBytes - 1)) == 0;
@@ -378,36 +398,41 @@ __device__ __forceinline__ void clip_tile(const Tile& t, float max_norm, void* f
     }
 }
 
-// Bound by latency: the launch, one turn to memory, the barrier.  8 tiles: 3.5 us a call where two launches take 4.6; 25 tiles
-// in the same cluster 5.8, and clusters of 16 CTAs take 5.2 for whatever they hold.  DST: -1 in place, -2 only the norm.
-template <int DST>
-__global__ void __launch_bounds__(kThreads)
+// Bound by latency: the launch, one turn to memory, the barrier.  Up to 8 tiles in CTAs of a tile each, up to 32 in CTAs of four: 9
+// to 32 tiles measured in 3.4 to 3.7 us a call, written in 3.6 to 4.7, where two launches take 5.0 to 6.  (25 tiles in CTAs of 256
+// threads that take them in turn: 5.8; clusters of 16 CTAs take 5.2 for whatever they hold.)  DST: -1 in place, -2 only the norm.
+template <int DST, int BLOCK>
+__global__ void __launch_bounds__(BLOCK)
 clip_cluster_kernel(const __grid_constant__ TensorTable<kClusterTensors> tab, float max_norm, void* __restrict__ flat,
                     float* __restrict__ result)
 {
-    const uint32_t tile = cluster_rank();
-    if (tile >= tab.tile_start[tab.count]) {            // fills the cluster up, or there are no elements at all
-        grid_dependency_wait();
-        float norm;
-        const float c = factor_of(cluster_sum(0.0), max_norm, &norm);
-        if (tile == 0 && threadIdx.x == 0) { result[0] = norm; result[1] = c; }
-    } else {
-        const Tile t = tile_of(tab, find_tensor(tab, tile), tile);
-        grid_dependency_wait();
-        if (t.dtype == kF32) clip_tile<kF32, DST>(t, max_norm, flat, result);
-        else clip_tile<kBf16, DST>(t, max_norm, flat, result);
+    const uint32_t tile = cluster_rank() * (BLOCK / kThreads) + threadIdx.x / kThreads;
+    const bool has_tile = tile < tab.tile_start[tab.count];     // others fill the cluster up, or there are no elements at all
+    Tile t = {};
+    if (has_tile) t = tile_of(tab, find_tensor(tab, tile), tile);
+    grid_dependency_wait();
+    Held h;
+    double sum = 0.0;
+    if (has_tile) sum = t.dtype == kF32 ? measure_tile<kF32>(t, h) : measure_tile<kBf16>(t, h);
+    float norm;
+    const float c = factor_of(cluster_sum<BLOCK>(sum), max_norm, &norm);
+    if (cluster_rank() == 0 && threadIdx.x == 0) { result[0] = norm; result[1] = c; }
+    if (DST != -2 && has_tile && !(DST == -1 && c == 1.0f)) {
+        if (t.dtype == kF32) write_tile<kF32, DST>(t, h, c, flat);
+        else write_tile<kBf16, DST>(t, h, c, flat);
     }
     cluster_wait();
 }
 
-template <int DST>
+template <int DST, int BLOCK>
 cudaError_t launch_cluster(const TensorTable<kClusterTensors>& tab, float max_norm, void* flat, float* result, cudaStream_t stream)
 {
+    constexpr unsigned per = BLOCK / kThreads;
     unsigned ctas = 1;
-    while (ctas < tab.tile_start[tab.count]) ctas *= 2;
+    while (ctas * per < tab.tile_start[tab.count]) ctas *= 2;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(ctas);
-    cfg.blockDim = dim3(kThreads);
+    cfg.blockDim = dim3(BLOCK);
     cfg.stream = stream;
     cudaLaunchAttribute attr[2];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
@@ -417,7 +442,14 @@ cudaError_t launch_cluster(const TensorTable<kClusterTensors>& tab, float max_no
     attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
     cfg.attrs = attr;
     cfg.numAttrs = ctas == 1 ? 1 : 2;
-    return cudaLaunchKernelEx(&cfg, clip_cluster_kernel<DST>, tab, max_norm, flat, result);
+    return cudaLaunchKernelEx(&cfg, clip_cluster_kernel<DST, BLOCK>, tab, max_norm, flat, result);
+}
+
+template <int DST>
+cudaError_t cluster_by_size(const TensorTable<kClusterTensors>& tab, float max_norm, void* flat, float* result, cudaStream_t stream)
+{
+    return tab.tile_start[tab.count] <= kClusterCtas ? launch_cluster<DST, kThreads>(tab, max_norm, flat, result, stream)
+                                                     : launch_cluster<DST, 4 * kThreads>(tab, max_norm, flat, result, stream);
 }
 
 // params[i] <- fma(-lr, fl(c * acc[i]), params[i]), the last elements first: acc has mostly just been read, from the front on,
@@ -524,10 +556,10 @@ cudaError_t launch_clip(const TensorList& list, float max_norm, ClipForm form, v
     if (list.count <= kClusterTensors && tiles <= kClusterTiles) {
         TensorTable<kClusterTensors> tab;
         fill_table(list, 0, list.count, 0, tab);
-        return form == kMeasureOnly ? launch_cluster<-2>(tab, max_norm, nullptr, result, stream)
-               : form == kInPlace   ? launch_cluster<-1>(tab, max_norm, nullptr, result, stream)
-               : flat_dtype == kF32 ? launch_cluster<kF32>(tab, max_norm, flat, result, stream)
-                                    : launch_cluster<kBf16>(tab, max_norm, flat, result, stream);
+        return form == kMeasureOnly ? cluster_by_size<-2>(tab, max_norm, nullptr, result, stream)
+               : form == kInPlace   ? cluster_by_size<-1>(tab, max_norm, nullptr, result, stream)
+               : flat_dtype == kF32 ? cluster_by_size<kF32>(tab, max_norm, flat, result, stream)
+                                    : cluster_by_size<kBf16>(tab, max_norm, flat, result, stream);
     }
     double* partial = reinterpret_cast<double*>(workspace);
     int npartial = 0;

@@ -28,6 +28,12 @@ SIZES = {
     "seventy": [(37 * i) % 501 for i in range(70)],
     "two_tables": [1 + (53 * i) % 97 for i in range(1500)],
     "long": [6_000_011, 7, 3_000_000],
+    "nine_tiles": [8 * 4096 + 1],
+    "32_tiles": [31 * 4096, 4095],
+    "33_tiles": [31 * 4096 + 1, 4096],
+    "32_wide_tiles": [31 * 8192, 8191],
+    "32_tensors": [100 + i for i in range(32)],
+    "33_tensors": [100 + i for i in range(33)],
 }
 
 
