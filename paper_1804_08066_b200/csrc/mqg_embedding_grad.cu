@@ -559,17 +559,19 @@ namespace {
 
 // One launch instead of four: 2048 tokens, 1000 rows of 64 take 6 us against 12 to 15, 64 tokens 4.7 against 9, 8192 tokens, 1000
 // rows of 256 11 against 18, 4096 tokens, 8000 rows of 515 14 to 16 against 19 to 22.  Not where there is more to add up (4096
-// tokens of 1024 take as long either way, 8192 of 1024 24 us against 20) or where the zeros are what takes the time: the CTAs
+// tokens of 1024 take as long either way, 1024 of 4096 15 us against 13, 8192 of 1024 24 against 20), where there are more
+// columns than SMs for them (every CTA searches), or where the zeros are what takes the time: the CTAs
 // write a piece of a row at a time, single elements where rows start anywhere (30,000 rows of 1024 in bf16, one token: 13 us
 // against 11; of 515: 14 against 8; 100,000 rows of 64 in fp32: 9 against 15).
-constexpr uint64_t kSmallElements = 1 << 22;
+constexpr uint64_t kSmallElements = 3 << 20;
 
 bool small_shape(SmallArgs& a)
 {
     a.column_bits = kLeastColumnBits;
     while (a.column_bits < kSmallColumnBits && 1u << a.column_bits < a.dim) ++a.column_bits;
     const uint32_t tiles = (a.dim + (1u << a.column_bits) - 1) >> a.column_bits;
-    a.groups = tiles < 148 ? 148 / tiles : 1;           // a CTA to each SM
+    if (tiles > 148) return false;
+    a.groups = 148 / tiles;                             // a CTA to each SM
     if (a.groups > a.rows) a.groups = a.rows;
     a.reciprocal = a.groups > 1 ? (uint32_t)(((1ull << 32) + a.groups - 1) / a.groups) : 0;
     a.key_bits = token_key_bits((a.rows - 1) / a.groups);

@@ -181,7 +181,7 @@ def test_gradient_of_few_tokens(tokens, kind, add):
 
 
 @pytest.mark.parametrize("add", [False, True])
-@pytest.mark.parametrize("shape", [(50, 512, 8192), (50, 513, 8192), (50, 24, 8193), (1 << 24, 1, 100), (131_072, 64, 40), (131_073, 64, 40), (64_527, 65, 40), (64_528, 65, 40),
+@pytest.mark.parametrize("shape", [(50, 384, 8192), (50, 385, 8192), (50, 24, 8193), (20, 4736, 600), (20, 4737, 600), (1 << 24, 1, 100), (131_072, 64, 40), (131_073, 64, 40), (64_527, 65, 40), (64_528, 65, 40),
                                    (2, 200_000, 7), (3, 250_000, 7)])
 def test_gradient_where_one_launch_ends(shape, add):
     _check_gradient(shape, "zipf", I64, (F32, F32), add)
