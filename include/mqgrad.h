@@ -352,10 +352,10 @@ mqg_status mqg_server_step_segments(const uint32_t* const* codes, const float* c
  *     c = 1 where N <= max_norm, else max_norm / N
  *
  * N is right for every finite gradient (sums in 64 bits beyond a thread's first 32 elements; no square overflows or
- * vanishes) and rounded to fp32 once (infinity above its range), after c was formed; the order of the sums is fixed, so N
- * and c are reproducible bit for bit on one device model.  A NaN among the elements makes N and c NaN; an infinity makes N
- * infinite and c zero (where max_norm is infinite too: c = 1).  max_norm may be 0 or infinite, not negative or NaN
- * (MQG_ERR_INVALID).
+ * vanishes) and rounded to fp32 once (infinity above its range), after c was formed; the order of the sums is fixed by
+ * the tensors' sizes, types and addresses modulo 16, so N and c are reproducible bit for bit on one device model.  A
+ * NaN among the elements makes N and c NaN; an infinity makes N infinite and c zero (where max_norm is infinite too: c
+ * = 1).  max_norm may be 0 or infinite, not negative or NaN (MQG_ERR_INVALID).
  *   result     [out] 2 floats: N, c.  They stay on the device: no call here waits for them.
  *   workspace  [scratch] DEVICE memory of at least mqg_norm_workspace_floats(count) floats, 8-byte aligned.  Contents on
  *              entry do not matter and are undefined on return; calls that may run concurrently (graphs captured apart
@@ -421,8 +421,8 @@ mqg_status mqg_embedding(const void* table, mqg_dtype table_dtype, uint64_t rows
  *     grad[v] = grad[v] + scale * that sum                               (rows without tokens are not touched)
  * The tokens are sorted by id and a row's summed in ascending order of t in fp32: one after the other, a row of many tokens
  * from sums of at most 32 each, in their order.  The scale and the addition are one rounding each, and a bf16 `grad` is
- * rounded once at the end.  The order of every sum is fixed by the arguments' sizes and the ids: the result is reproducible
- * bit for bit.  What stands in `dout` at empty places is not used, NaN included.
+ * rounded once at the end.  The order of every sum is fixed by the ids and the arguments' sizes, types and addresses
+ * modulo 16: the result is reproducible bit for bit.  What stands in `dout` at empty places is not used, NaN included.
  *   grad       [out] rows x dim elements; with add_into_grad [in/out]
  *   workspace  [scratch] DEVICE memory of at least mqg_embedding_workspace_floats(tokens, rows, dim) floats, 16-byte
  *              aligned; otherwise as for the norm above

@@ -227,8 +227,9 @@ def test_gradient_by_differences():
             assert abs((value(up) - value(down)) / (2 * h) - float(grad[v, c])) < 40 * 64 * 2.0 ** -23
 
 
-def test_gradient_captured_replayed_and_on_another_stream():
-    rows, dim, tokens = 500, 64, 3000
+@pytest.mark.parametrize("tokens", [3000, 20_000, 140_000])
+def test_gradient_captured_replayed_and_on_another_stream(tokens):
+    rows, dim = 500, 64
     ids = [_ids(tokens, rows, "zipf", I64, seed).cuda() for seed in (0, 1)]
     dout = torch.randn(tokens, dim, generator=torch.Generator().manual_seed(2)).cuda()
     floats = mqg.mqg_embedding_workspace_floats(tokens, rows, dim)
@@ -255,6 +256,45 @@ def test_gradient_captured_replayed_and_on_another_stream():
         torch.cuda.synchronize()
         assert same_bits(g.cpu(), want[k])
         assert same_bits(out.cpu(), _lookup(want[k], ids[k].cpu(), 1.0, F32))
+
+
+@pytest.mark.parametrize("shape", [(50, 24, 700), (3000, 40, 12_000)])
+def test_two_gradients_at_once_and_one_with_what_the_stream_still_writes(shape):
+    """Calls on two streams with workspaces of their own, and a call whose ids and output gradient a launch just before it
+    writes."""
+    rows, dim, tokens = shape
+    gen = torch.Generator().manual_seed(3)
+    ids = _ids(tokens, rows, "zipf", I64).cuda()
+    dout = torch.randn(tokens, dim, generator=gen).cuda()
+    floats = mqg.mqg_embedding_workspace_floats(tokens, rows, dim)
+    want = torch.empty(rows, dim, device="cuda")
+    mqg.mqg_embedding_grad(dout, ids, tokens, rows, dim, 2.0, want, torch.empty(floats, device="cuda"))
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    held = [[torch.full_like(ids, -1), torch.zeros_like(dout), torch.full((rows, dim), math.nan, device="cuda"),
+             torch.empty(floats, device="cuda")] for _ in streams]
+    torch.cuda.synchronize()
+    for _ in range(20):
+        for s, (i, d, g, w) in zip(streams, held):
+            with torch.cuda.stream(s):
+                i.copy_(ids)
+                d.copy_(dout)
+                g.fill_(math.nan)
+                mqg.mqg_embedding_grad(d, i, tokens, rows, dim, 2.0, g, w)
+                i.fill_(-1)
+                d.zero_()
+    torch.cuda.synchronize()
+    for _, _, g, _ in held:
+        assert same_bits(g.cpu(), want.cpu())
+
+
+def test_no_tokens_set_the_gradient_to_zero_after_what_the_stream_still_writes():
+    grad = torch.empty(4_000_001, device="cuda")
+    ids, w = torch.empty(0, dtype=I64, device="cuda"), torch.empty(0, device="cuda")
+    for _ in range(10):
+        grad.fill_(math.nan)
+        mqg.mqg_embedding_grad(grad, ids, 0, 4_000_001, 1, 1.0, grad, w)
+    assert (grad.cpu() == 0).all()
 
 
 def test_a_table_beyond_32_bit_offsets():
