@@ -2,7 +2,8 @@
 //
 // Bound by memory: the rows that are used are read, the output is written.  A thread takes words of V elements, 16 bytes of the
 // wider type, so that every access of a warp covers whole sectors, and four of them so that their dependent loads (id, then
-// row) overlap.  (16,384 rows of 1024 from fp32 to bf16: 13.1 us, with eight 15.7, two 14.8, one 20.6.)
+// row) overlap.  (16,384 rows of 1024 from fp32 to bf16: 12.1 us, with eight 13.4, two 14.2; 13.1 with a
+// division for every word, which took three quarters of the issue slots.)
 #include "mqg_tma.cuh"
 #include "mqg_training.h"
 #include "mqg_vector.cuh"
@@ -21,7 +22,18 @@ struct LookupArgs {
     void* out;
     uint64_t rows, dim, tokens;
     float scale;
+    uint32_t reciprocal;     // of the words of a row: ceil(2^32 / words); 0: 1 word, or more than kMostWords
 };
+
+// Rows a CTA's word `local` (counted from the first row it begins in) is beyond the first: a division by the words of a row, of a
+// number below words + kThreads * kVectors, without the 25 instructions that a division is.  The high word of the product with
+// the reciprocal is exact up to kMostWords: the product's error, below words * local, stays below 2^32.
+constexpr uint32_t kMostWords = 32768;
+__device__ __forceinline__ uint32_t rows_beyond(uint32_t local, uint32_t words, uint32_t reciprocal)
+{
+    if (reciprocal != 0) return __umulhi(local, reciprocal);
+    return words == 1 ? local : local >= words ? 1 : 0;
+}
 
 template <int SRC, int DST, int V, typename ID>
 __global__ void __launch_bounds__(kThreads) embedding_kernel(const LookupArgs a)
@@ -31,30 +43,34 @@ __global__ void __launch_bounds__(kThreads) embedding_kernel(const LookupArgs a)
     const uint64_t token0 = quotient(first, row_vectors);
     const uint32_t col0 = (uint32_t)(first - token0 * row_vectors);
     grid_dependency_wait();
-    uint64_t at[kVectors], from[kVectors];
+    const uint32_t held = (uint32_t)min(n - first, (uint64_t)(kThreads * kVectors));
+    const ID* ids = static_cast<const ID*>(a.ids) + token0;
+    const auto* table = static_cast<const typename Element<SRC>::type*>(a.table);
+    const typename Element<SRC>::type* from[kVectors];  // the word of the table, null where the place is empty
 #pragma unroll
     for (int k = 0; k < kVectors; ++k) {
-        const uint32_t local = col0 + threadIdx.x + k * kThreads, over = local / row_vectors;
-        const uint32_t col = local - over * row_vectors;
-        const uint64_t token = token0 + over;
-        at[k] = first + threadIdx.x + k * kThreads;
-        from[k] = ~0ull;
-        if (at[k] < n) {
-            const int64_t id = (int64_t)__ldg(static_cast<const ID*>(a.ids) + token);
-            if (id >= 0 && (uint64_t)id < a.rows) from[k] = (uint64_t)id * row_vectors + col;
-        }
+        const uint32_t i = threadIdx.x + k * kThreads, local = col0 + i, over = rows_beyond(local, row_vectors, a.reciprocal);
+        const int64_t id = i < held ? (int64_t)__ldg(ids + over) : -1;
+        const bool there = (uint64_t)id < a.rows;       // (a negative id is above every count of rows)
+        from[k] = there ? table + ((uint64_t)id * row_vectors + (local - over * row_vectors)) * V : nullptr;
     }
     Packed<SRC, V> x[kVectors];
 #pragma unroll
     for (int k = 0; k < kVectors; ++k)
-        if (from[k] != ~0ull) x[k].load(static_cast<const typename Element<SRC>::type*>(a.table) + from[k] * V);
+        if (from[k] != nullptr) x[k].load(from[k]);
+    auto* out = static_cast<typename Element<DST>::type*>(a.out) + first * V;
 #pragma unroll
     for (int k = 0; k < kVectors; ++k) {
-        if (at[k] >= n) continue;
+        const uint32_t i = threadIdx.x + k * kThreads;
+        if (i >= held) continue;
         Packed<DST, V> y;
 #pragma unroll
-        for (int e = 0; e < V; ++e) y.set(e, from[k] != ~0ull ? a.scale * x[k].get(e) : 0.0f);
-        y.store(static_cast<typename Element<DST>::type*>(a.out) + at[k] * V);
+        for (int e = 0; e < V; ++e) y.set(e, a.scale * x[k].get(e));
+        if (from[k] == nullptr) {
+#pragma unroll
+            for (int j = 0; j < Packed<DST, V>::kWords; ++j) y.w[j] = {};
+        }
+        y.store(out + i * V);
     }
 }
 
@@ -109,9 +125,10 @@ __global__ void __launch_bounds__(kThreads) embedding_rows_kernel(const RowArgs 
 }
 
 template <int SRC, int DST, int V, typename ID>
-cudaError_t launch(const LookupArgs& a, cudaStream_t stream)
+cudaError_t launch(LookupArgs a, cudaStream_t stream)
 {
-    const uint64_t n = a.tokens * (a.dim / V), per_block = kThreads * kVectors;
+    const uint64_t words = a.dim / V, n = a.tokens * words, per_block = kThreads * kVectors;
+    a.reciprocal = words > 1 && words <= kMostWords ? (uint32_t)(((1ull << 32) + words - 1) / words) : 0;
     return launch_pdl(embedding_kernel<SRC, DST, V, ID>, (unsigned)((n + per_block - 1) / per_block), kThreads, stream, a);
 }
 

@@ -66,6 +66,16 @@ def test_lookup(shape, shift, types):
     t.check()
 
 
+@pytest.mark.parametrize("dim", [4, 8, 12, 131_068, 131_072, 131_076, 400_000])
+def test_lookup_of_rows_of_one_and_of_very_many_words(dim):
+    rows, tokens = 3, 1500 if dim < 100 else 5
+    table = torch.randn(rows, dim, generator=torch.Generator().manual_seed(dim))
+    for kind in ("uniform", "outside"):
+        ids, out = _ids(tokens, rows, kind, I64), Buffer(tokens * dim, F32)
+        mqg.mqg_embedding(table.cuda(), rows, dim, ids.cuda(), tokens, -1.7, out.view)
+        assert same_bits(out.cpu(), _lookup(table, ids, -1.7, F32).flatten())
+
+
 def test_lookup_of_nothing_and_from_nothing():
     ids, out = torch.zeros(4, dtype=I64, device="cuda"), Buffer(12, F32)
     mqg.mqg_embedding(torch.empty(0, device="cuda"), 0, 3, ids, 4, 1.0, out.view)
