@@ -557,9 +557,9 @@ cudaError_t launch_clip(const TensorList& list, float max_norm, ClipForm form, v
 {
     uint64_t tiles = 0;
     for (int j = 0; j < list.count; ++j) tiles += tiles_of(list, j);
-    if (list.count <= kClusterTensors && tiles <= kClusterTiles) {
+    if (tiles == 0 || (list.count <= kClusterTensors && tiles <= kClusterTiles)) {
         TensorTable<kClusterTensors> tab;
-        fill_table(list, 0, list.count, 0, tab);
+        fill_table(list, 0, tiles == 0 ? 0 : list.count, 0, tab);   // any number of empty tensors are no tensors
         return form == kMeasureOnly ? cluster_by_size<-2>(tab, max_norm, nullptr, result, stream)
                : form == kInPlace   ? cluster_by_size<-1>(tab, max_norm, nullptr, result, stream)
                : flat_dtype == kF32 ? cluster_by_size<kF32>(tab, max_norm, flat, result, stream)

@@ -118,6 +118,17 @@ def test_cpu_tensors_and_wrong_types_are_refused():
         mqg.mqg_embedding(x, 8, 8, i, 4, 1.0, x, padding=0)
 
 
+@pytest.mark.skipif(torch.cuda.is_available(), reason="tells a launch by its error, which there is without a device only")
+@pytest.mark.parametrize("count", [0, 2, 32, 33, 1024, 1025, 1500])
+def test_lists_without_elements_are_launched(lib, count):
+    """The result of a list of empty tensors is written by a launch like any other's: no call returns without one."""
+    empty = _list(*[(None, 0, j % 2) for j in range(count)])
+    need = mqg.mqg_norm_workspace_floats(count)
+    assert lib.mqg_grad_norm(*empty, 1.0, P, P + 4096, need, None) == mqg.MQG_ERR_CUDA
+    assert lib.mqg_clip_grad_norm(*empty, 1.0, P, P + 4096, need, None) == mqg.MQG_ERR_CUDA
+    assert lib.mqg_clip_flatten(*empty, 1.0, None, 0, P, P + 4096, need, None) == mqg.MQG_ERR_CUDA
+
+
 @pytest.mark.gpu
 def test_sizes_types_and_overlaps_of_device_tensors():
     x, i = torch.zeros(64, device="cuda"), torch.zeros(4, dtype=torch.int64, device="cuda")

@@ -184,6 +184,24 @@ def test_zeros_have_norm_zero_and_factor_one():
     assert result.cpu().tolist() == [0.0, 1.0]
 
 
+@pytest.mark.parametrize("count", [0, 1, 32, 33, 1024, 1025, 1500])
+def test_any_number_of_empty_tensors_have_norm_zero_and_factor_one(count):
+    grads = [torch.empty(0, device="cuda", dtype=t) for t in _types("mixed", count)]
+    for max_norm in (0.0, 0.5, math.inf):
+        for call in (mqg.mqg_grad_norm, mqg.mqg_clip_grad_norm):
+            result, work = _scratch(count)
+            result.view.fill_(math.nan)
+            call(grads, max_norm, result.view, work.view)
+            assert result.cpu().tolist() == [0.0, 1.0]
+            work.check()
+        result, work, flat = *_scratch(count), Buffer(8, F32)
+        result.view.fill_(math.nan)
+        mqg.mqg_clip_flatten(grads, max_norm, flat.view, result.view, work.view)
+        assert result.cpu().tolist() == [0.0, 1.0]
+        assert (flat.cpu().view(torch.uint8) == 0x5A).all()
+        work.check()
+
+
 def test_what_is_not_finite():
     for at in (0, 4999, 9999):
         x = torch.ones(10_000)
