@@ -19,6 +19,7 @@ mqg_apply_clipped).  Prints one JSON line with the share of iteration time spent
 from __future__ import annotations
 
 import argparse
+import contextlib
 import json
 import time
 
@@ -82,18 +83,41 @@ def token_batch(gen, batch):
     return torch.where(torch.arange(LENGTH, device="cuda") < length, ids, -1), y
 
 
-def token_gradients(model, ids, y, workspace):
-    """Loss of a batch and the gradient of every parameter, in their order."""
+def token_gradients(model, ids, y, workspace, library=contextlib.nullcontext()):
+    """Loss of a batch and the gradient of every parameter, in their order; the library's calls run within `library`."""
     n = ids.numel()
     rows = torch.empty(*ids.shape, WIDTH, device="cuda")
-    mqg.mqg_embedding(model.table.data, VOCABULARY, WIDTH, ids, n, model.scale, rows)
+    with library:
+        mqg.mqg_embedding(model.table.data, VOCABULARY, WIDTH, ids, n, model.scale, rows)
     rows.requires_grad_()
     model.zero_grad(set_to_none=True)
     loss = F.cross_entropy(model(rows, ids >= 0), y)
     loss.backward()
     table = torch.empty_like(model.table.data)
-    mqg.mqg_embedding_grad(rows.grad.contiguous(), ids, n, VOCABULARY, WIDTH, model.scale, table, workspace)
+    dout = rows.grad.contiguous()
+    with library:
+        mqg.mqg_embedding_grad(dout, ids, n, VOCABULARY, WIDTH, model.scale, table, workspace)
     return loss, [table, *(p.grad for p in model.parameters() if p is not model.table)]
+
+
+class LibraryTime:
+    """Device time of the library's work: the time between the events around each `with` block."""
+
+    def __init__(self):
+        self.spans = []
+
+    def __enter__(self):
+        self.spans.append([torch.cuda.Event(enable_timing=True) for _ in range(2)])
+        self.spans[-1][0].record()
+
+    def __exit__(self, *_):
+        self.spans[-1][1].record()
+
+    def take(self):
+        """Milliseconds since the last call of this; the device must have finished the blocks."""
+        ms = sum(a.elapsed_time(b) for a, b in self.spans)
+        self.spans.clear()
+        return ms
 
 
 def flatten_parameters(model):
@@ -125,7 +149,7 @@ def run(iters=60, workers=4, batch=128, lr=0.05, selector="window", seed=0, mode
     codes = [torch.zeros(mqg.mqg_code_words(n, 8), dtype=torch.int32, device="cuda") for _ in range(workers)]
     scales = [torch.zeros(mqg.mqg_num_buckets(n, BUCKET), dtype=torch.float32, device="cuda") for _ in range(workers)]
     bits, lib_ms, total_ms, wire = (1 if selector == "window" else 2), 0.0, 0.0, 0
-    losses, chosen = [], []
+    losses, chosen, library = [], [], LibraryTime()
     last_ms = 1.0
     for m in range(iters):
         t0 = time.perf_counter()
@@ -140,28 +164,28 @@ def run(iters=60, workers=4, batch=128, lr=0.05, selector="window", seed=0, mode
                 loss.backward()
                 parts = [p.grad for p in model.parameters()]
             else:
-                loss, parts = token_gradients(model, *token_batch(gen, batch), sums)
+                loss, parts = token_gradients(model, *token_batch(gen, batch), sums, library)
             if clip is not None and clip_at == "worker":
                 grads.append(torch.empty(n, device="cuda"))
-                mqg.mqg_clip_flatten([g.contiguous() for g in parts], clip, grads[w], norms[m, w], norm_workspace)
+                parts = [g.contiguous() for g in parts]
+                with library:
+                    mqg.mqg_clip_flatten(parts, clip, grads[w], norms[m, w], norm_workspace)
             else:
                 grads.append(torch.cat([g.reshape(-1) for g in parts]))
             loss_sum += float(loss.detach())
         loss_m = loss_sum / workers
         bits = sel.step(m, loss_m, last_ms)                       # server MDP: loss in, width out
-        e0, e1 = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
-        e0.record()
-        for w in range(workers):
-            mqg.mqg_quantize(grads[w], n, bits, BUCKET, seed, codes[w], scales[w], worker=w, step=m)
-        if acc is None:
-            mqg.mqg_server_step(codes, scales, workers, bits, n, BUCKET, flat, lr / workers)
-        else:                                                     # the mean's norm is the sum's / workers
-            mqg.mqg_dequant_accumulate(codes, scales, workers, bits, n, acc, BUCKET)
-            mqg.mqg_grad_norm([acc], clip * workers, norms[m, 0], norm_workspace)
-            mqg.mqg_apply_clipped(flat, acc, lr / workers, norms[m, 0, 1:], n)
-        e1.record()
+        with library:
+            for w in range(workers):
+                mqg.mqg_quantize(grads[w], n, bits, BUCKET, seed, codes[w], scales[w], worker=w, step=m)
+            if acc is None:
+                mqg.mqg_server_step(codes, scales, workers, bits, n, BUCKET, flat, lr / workers)
+            else:                                                 # the mean's norm is the sum's / workers
+                mqg.mqg_dequant_accumulate(codes, scales, workers, bits, n, acc, BUCKET)
+                mqg.mqg_grad_norm([acc], clip * workers, norms[m, 0], norm_workspace)
+                mqg.mqg_apply_clipped(flat, acc, lr / workers, norms[m, 0, 1:], n)
         torch.cuda.synchronize()
-        lib_ms += e0.elapsed_time(e1)
+        lib_ms += library.take()
         last_ms = (time.perf_counter() - t0) * 1e3
         total_ms += last_ms
         wire += workers * mqg.mqg_wire_bytes(n, bits, BUCKET)

@@ -24,6 +24,44 @@ def test_the_loop_runs_with_each_model_and_clip(model, clip, clip_at):
         assert all((f == 1) == (clip == 1e6) for f in r["clip_factors"])
 
 
+@pytest.mark.parametrize("model,clip,clip_at", [("cnn", None, "worker"), ("cnn", 0.05, "worker"), ("tokens", 0.05, "worker"),
+                                                ("tokens", 0.05, "server")])
+def test_the_library_share_counts_every_call_into_the_library(monkeypatch, model, clip, clip_at):
+    """Events are recorded in pairs around what is timed: every call that enqueues work stands between the two of one."""
+    from paper_1804_08066_b200 import train_loop as tl
+    recorded, calls = [0], []
+    record = torch.cuda.Event.record
+
+    def count(self, *args, **kwargs):
+        recorded[0] += 1
+        return record(self, *args, **kwargs)
+
+    class Watched:
+        def __getattr__(self, name):
+            value = getattr(mqg, name)
+            if name not in mqg._NATIVE and name not in mqg._NATIVE_AROUND:
+                return value
+
+            def call(*args, **kwargs):
+                calls.append((name, recorded[0] % 2 == 1))
+                return value(*args, **kwargs)
+            return call
+
+    monkeypatch.setattr(torch.cuda.Event, "record", count)
+    monkeypatch.setattr(tl, "mqg", Watched())
+    r = tl.run(iters=2, workers=2, batch=32, model=model, clip=clip, clip_at=clip_at)
+    want = {"mqg_quantize"} | ({"mqg_embedding", "mqg_embedding_grad"} if model == "tokens" else set())
+    if clip is None:
+        want |= {"mqg_server_step"}
+    elif clip_at == "worker":
+        want |= {"mqg_server_step", "mqg_clip_flatten"}
+    else:
+        want |= {"mqg_dequant_accumulate", "mqg_grad_norm", "mqg_apply_clipped"}
+    assert {name for name, _ in calls} == want
+    assert [name for name, timed in calls if not timed] == []
+    assert recorded[0] % 2 == 0 and 0 < r["libmqgrad_share_pct"] < 100
+
+
 def test_a_limit_that_nothing_reaches_changes_nothing():
     from paper_1804_08066_b200.train_loop import run
     plain, limited = (run(iters=4, workers=2, batch=32, seed=3, model="tokens", clip=c) for c in (None, 1e6))
