@@ -613,8 +613,9 @@ uint64_t area(uint64_t a, uint64_t b)
     return __builtin_mul_overflow(a, b, &r) ? ~0ull : r;
 }
 
-// A list of gradient tensors of any sizes.  Everything that is wanted of the items is read at once, and no Python code runs
-// meanwhile.
+// A list (or tuple, or any iterable) of gradient tensors of any sizes.  Everything that is wanted of the items is read at once,
+// and no Python code runs meanwhile.  The items live as long as this: tensors that an iterable made for the call alone are
+// not freed before the launch.
 struct TensorTable {
     static constexpr size_t kInline = 64;
     void* inline_ptr[kInline];
@@ -626,10 +627,11 @@ struct TensorTable {
     mqg_dtype* dtype = inline_dtype;
     size_t n = 0;
     uint64_t total = 0;
+    Reference items = {nullptr};
 
     void read(PyObject* o, Operands& on)
     {
-        const Reference items = {PySequence_Fast(o, "a list of tensors is expected")};
+        items.object = PySequence_Fast(o, "a list of tensors is expected");
         if (!items.object) throw PythonError();
         n = (size_t)PySequence_Fast_GET_SIZE(items.object);
         if (n > kInline) {
@@ -666,11 +668,14 @@ struct TensorTable {
 };
 
 struct NormArgs {
+    TensorTable g;
     float max_norm, *result, *workspace;
     uint64_t floats;
-    void read(PyObject* limit, PyObject* res, PyObject* work, Operands& on)
+    // What may run Python code (a number's conversion, an iterable) comes before the pointers of the other tensors.
+    void read(PyObject* grads, PyObject* limit, PyObject* res, PyObject* work, Operands& on)
     {
         max_norm = to_float(limit);
+        g.read(grads, on);
         result = on.floats(res, "result", 2);
         workspace = on.floats(work, "workspace", 0, &floats);
     }
@@ -679,34 +684,29 @@ struct NormArgs {
 MQG_ENTRY(mqg_grad_norm, 0, 4, "grads", "max_norm", "result", "workspace")
 {
     Operands on;
-    TensorTable g;
     NormArgs a;
-    a.read(v[1], v[2], v[3], on);
-    g.read(v[0], on);
-    return enqueue_on(on, [&](void* s) { return ::mqg_grad_norm(g.ptr, g.size, g.dtype, g.count(), a.max_norm,
+    a.read(v[0], v[1], v[2], v[3], on);
+    return enqueue_on(on, [&](void* s) { return ::mqg_grad_norm(a.g.ptr, a.g.size, a.g.dtype, a.g.count(), a.max_norm,
                                                                 a.result, a.workspace, a.floats, s); });
 }
 
 MQG_ENTRY(mqg_clip_grad_norm, 0, 4, "grads", "max_norm", "result", "workspace")
 {
     Operands on;
-    TensorTable g;
     NormArgs a;
-    a.read(v[1], v[2], v[3], on);
-    g.read(v[0], on);
-    g.check_apart();
-    return enqueue_on(on, [&](void* s) { return ::mqg_clip_grad_norm(g.ptr, g.size, g.dtype, g.count(),
-                                                                     a.max_norm, a.result, a.workspace, a.floats, s); });
+    a.read(v[0], v[1], v[2], v[3], on);
+    a.g.check_apart();
+    return enqueue_on(on, [&](void* s) { return ::mqg_clip_grad_norm(a.g.ptr, a.g.size, a.g.dtype, a.g.count(), a.max_norm,
+                                                                     a.result, a.workspace, a.floats, s); });
 }
 
 MQG_ENTRY(mqg_clip_flatten, 0, 5, "grads", "max_norm", "flat", "result", "workspace")
 {
     Operands on;
-    TensorTable g;
     NormArgs a;
     mqg_dtype type;
-    a.read(v[1], v[3], v[4], on);
-    g.read(v[0], on);
+    a.read(v[0], v[1], v[3], v[4], on);
+    const TensorTable& g = a.g;
     char* flat = static_cast<char*>(on.values(v[2], "flat", g.total, &type));
     const char* end = flat + g.total * (type == MQG_F32 ? 4 : 2);
     for (size_t i = 0; i < g.n; ++i)
@@ -714,19 +714,18 @@ MQG_ENTRY(mqg_clip_flatten, 0, 5, "grads", "max_norm", "flat", "result", "worksp
             PyErr_Format(PyExc_ValueError, "grads[%zu] and flat share memory", i);
             return nullptr;
         }
-    return enqueue_on(on, [&](void* s) { return ::mqg_clip_flatten(g.ptr, g.size, g.dtype, g.count(),
-                                                                   a.max_norm, flat, type, a.result, a.workspace, a.floats, s); });
+    return enqueue_on(on, [&](void* s) { return ::mqg_clip_flatten(g.ptr, g.size, g.dtype, g.count(), a.max_norm, flat, type,
+                                                                   a.result, a.workspace, a.floats, s); });
 }
 
 MQG_ENTRY(mqg_scale_grads, 0, 2, "grads", "factor")
 {
     Operands on;
     TensorTable g;
-    const float* factor = on.floats(v[1], "factor", 1);
     g.read(v[0], on);
+    const float* factor = on.floats(v[1], "factor", 1);
     g.check_apart();
-    return enqueue_on(on, [&](void* s) { return ::mqg_scale_grads(g.ptr, g.size, g.dtype, g.count(),
-                                                                  factor, s); });
+    return enqueue_on(on, [&](void* s) { return ::mqg_scale_grads(g.ptr, g.size, g.dtype, g.count(), factor, s); });
 }
 
 MQG_ENTRY(mqg_apply_clipped, 0, 5, "params", "acc", "lr", "factor", "n")

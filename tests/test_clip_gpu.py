@@ -6,6 +6,7 @@ so the sum of squares is off by at most 13 * 2^-24 of itself, its root by half o
 2^-24 in all, and 8 * 2^-24 with the second-order terms.  The factor has the same error.  Everything after the factor is
 compared bit for bit with one rounding of the product."""
 import math
+import weakref
 
 import pytest
 import torch
@@ -285,3 +286,44 @@ def test_captured_replayed_and_on_another_stream():
     flat.check()
     for b in bufs:
         b.check()
+
+
+@pytest.mark.parametrize("size", [100, 200_000])
+def test_tensors_that_an_iterable_makes_for_the_call_live_until_it_is_enqueued(size):
+    """What is left of a temporary tensor when it is freed is overwritten at once, on the same stream: a call that is enqueued
+    only afterwards would find zeros."""
+    values = [torch.full((size,), float(j + 1)) for j in range(3)]
+
+    def temporaries(kept):
+        for v in values:
+            kept.append(v.cuda())
+            t = kept[-1].view(-1)
+            weakref.finalize(t, kept[-1].zero_)
+            yield t
+            del t
+
+    result, work = _scratch(3)
+    for max_norm, call in ((math.inf, mqg.mqg_grad_norm), (0.5, mqg.mqg_grad_norm)):
+        kept = []
+        call(temporaries(kept), max_norm, result.view, work.view)
+        _check_result(result, values, max_norm)
+        assert all(int(k.count_nonzero()) == 0 for k in kept)          # freed by the end of the call
+    kept, flat = [], Buffer(3 * size, F32)
+    mqg.mqg_clip_flatten(temporaries(kept), 0.5, flat.view, result.view, work.view)
+    c = _check_result(result, values, 0.5)
+    assert same_bits(flat.cpu(), torch.cat([_product(c, v, F32) for v in values]))
+    assert all(int(k.count_nonzero()) == 0 for k in kept)
+
+
+def test_an_iterable_that_replaces_the_result_before_it_is_read():
+    """Python code of the iterable runs before the other tensors' pointers are taken."""
+    old, new, work = torch.zeros(2, device="cuda"), torch.zeros(2, device="cuda"), _scratch(1)[1]
+    result = torch.zeros(2, device="cuda")
+    result.set_(old)
+
+    def items():
+        result.set_(new)
+        yield torch.full((4,), 1.5, device="cuda")
+
+    mqg.mqg_grad_norm(items(), math.inf, result, work.view)
+    assert result.tolist() == [3.0, 1.0] and new.tolist() == [3.0, 1.0] and old.tolist() == [0.0, 0.0]
