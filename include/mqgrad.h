@@ -346,7 +346,9 @@ mqg_status mqg_server_step_segments(const uint32_t* const* codes, const float* c
  *
  * A list of gradient tensors is three HOST arrays of `count` entries, read during the call only: device pointers, element
  * counts, types.  A tensor needs its type's own alignment only (4 or 2 bytes); 16 bytes are faster.  An empty tensor's
- * pointer is not looked at, and count may be 0.  Tensors that are written must not overlap each other or anything else.
+ * pointer is not looked at, and count may be 0.  What is written (tensors, results, workspaces) must not overlap anything
+ * else; of two buffers of a call, or a buffer and a tensor of its list, that do, the call is refused (MQG_ERR_INVALID).  That
+ * the tensors of a list that is scaled in place do not overlap each other is the caller's to see to.
  *
  *     N = sqrt(sum over all elements of all tensors of x^2)
  *     c = 1 where N <= max_norm, else max_norm / N
@@ -397,7 +399,8 @@ mqg_status mqg_scale_grads(void* const* grads, const uint64_t* sizes, const mqg_
 
 /*
  * mqg_apply of the clipped sum: params[i] = fma(-lr, fl(*factor * acc[i]), params[i]), exactly mqg_scale_grads on acc
- * followed by mqg_apply, in one pass that leaves acc as it is.  params and acc as in mqg_apply (16-byte aligned).
+ * followed by mqg_apply, in one pass that leaves acc as it is.  params and acc as in mqg_apply (16-byte aligned); acc may be
+ * params itself.
  */
 mqg_status mqg_apply_clipped(float* params, const float* acc, float lr, const float* factor, uint64_t n, void* cuda_stream);
 

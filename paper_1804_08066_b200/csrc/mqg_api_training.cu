@@ -14,10 +14,43 @@ constexpr uint64_t kMaxRows = 0x7FFFFFFF, kMaxDim = 1u << 22;
 bool aligned(const void* p, uintptr_t bytes) { return (reinterpret_cast<uintptr_t>(p) & (bytes - 1)) == 0; }
 bool known(mqg_dtype t) { return t == MQG_F32 || t == MQG_BF16; }
 uintptr_t bytes_of(mqg_dtype t) { return t == MQG_F32 ? 4 : 2; }
+uintptr_t bytes_of(mqg_index t) { return t == MQG_I64 ? 8 : 4; }
 
 mqg_status cuda_status(const char* what, cudaError_t err)
 {
     return err == cudaSuccess ? MQG_OK : report_error(MQG_ERR_CUDA, "%s: %s", what, cudaGetErrorString(err));
+}
+
+// Memory that a call reads or writes; `bytes` = 0: none.
+struct Region {
+    const char* name;
+    const void* p;
+    uint64_t bytes;
+    bool meets(const Region& r) const
+    {
+        const uintptr_t a = reinterpret_cast<uintptr_t>(p), b = reinterpret_cast<uintptr_t>(r.p);
+        return bytes != 0 && r.bytes != 0 && (a < b ? b - a < bytes : a - b < r.bytes);
+    }
+};
+
+// Whether what is written shares memory with anything else: MQG_OK if not.
+template <int N> mqg_status check_apart(const char* what, const Region& written, const Region (&others)[N])
+{
+    for (const Region& r : others)
+        if (written.meets(r)) return report_error(MQG_ERR_INVALID, "%s: %s and %s share memory", what, written.name, r.name);
+    return MQG_OK;
+}
+
+template <int N>
+mqg_status check_list_apart(const char* what, const void* const* grads, const uint64_t* sizes, const mqg_dtype* dtypes, int count,
+                            const Region (&others)[N])
+{
+    for (int j = 0; j < count; ++j) {
+        const Region tensor = {"", grads[j], sizes[j] * bytes_of(dtypes[j])};
+        for (const Region& r : others)
+            if (tensor.meets(r)) return report_error(MQG_ERR_INVALID, "%s: tensor %d and %s share memory", what, j, r.name);
+    }
+    return MQG_OK;
 }
 
 // A list of tensors.  A launch counts its 16 KB tiles in 32 bits, so a list holds less than 2^44 bytes.
@@ -54,6 +87,16 @@ mqg_status check_norm(const char* what, int count, float max_norm, const float* 
     return MQG_OK;
 }
 
+// What a call that measures writes lies apart: `flat`, if there is one, the result and the workspace.
+mqg_status check_norm_apart(const char* what, const void* const* grads, const uint64_t* sizes, const mqg_dtype* dtypes, int count,
+                            const float* result, const float* workspace, const Region& flat = {"flat", nullptr, 0})
+{
+    const Region out = {"result", result, 8}, scratch = {"workspace", workspace, mqg_norm_workspace_floats(count) * 4};
+    if (mqg_status st = check_apart(what, out, {scratch})) return st;
+    if (mqg_status st = check_apart(what, flat, {out, scratch})) return st;
+    return check_list_apart(what, grads, sizes, dtypes, count, {out, scratch, flat});
+}
+
 mqg::TensorList list_of(const void* const* grads, const uint64_t* sizes, const mqg_dtype* dtypes, int count)
 {
     static_assert(sizeof(mqg_dtype) == sizeof(int), "the list's types are passed on as int");
@@ -69,7 +112,7 @@ mqg_status check_table(const char* what, uint64_t rows, uint64_t dim, uint64_t t
     if (ids_type != MQG_I32 && ids_type != MQG_I64) return report_error(MQG_ERR_INVALID, "%s: unknown index type %d", what, (int)ids_type);
     if (tokens != 0 && dim != 0) {
         if (!ids) return report_error(MQG_ERR_INVALID, "%s: ids is null", what);
-        if (!aligned(ids, ids_type == MQG_I64 ? 8 : 4)) return report_error(MQG_ERR_ALIGN, "%s: ids not aligned", what);
+        if (!aligned(ids, bytes_of(ids_type))) return report_error(MQG_ERR_ALIGN, "%s: ids not aligned", what);
     }
     return MQG_OK;
 }
@@ -95,6 +138,7 @@ mqg_status mqg_grad_norm(const void* const* grads, const uint64_t* sizes, const 
     const char* what = "mqg_grad_norm";
     if (mqg_status st = check_list(what, grads, sizes, dtypes, count)) return st;
     if (mqg_status st = check_norm(what, count, max_norm, result, workspace, workspace_floats)) return st;
+    if (mqg_status st = check_norm_apart(what, grads, sizes, dtypes, count, result, workspace)) return st;
     return cuda_status(what, mqg::launch_clip(list_of(grads, sizes, dtypes, count), max_norm, mqg::kMeasureOnly, nullptr, 0,
                                               result, workspace, static_cast<cudaStream_t>(cuda_stream)));
 }
@@ -105,6 +149,7 @@ mqg_status mqg_clip_grad_norm(void* const* grads, const uint64_t* sizes, const m
     const char* what = "mqg_clip_grad_norm";
     if (mqg_status st = check_list(what, grads, sizes, dtypes, count)) return st;
     if (mqg_status st = check_norm(what, count, max_norm, result, workspace, workspace_floats)) return st;
+    if (mqg_status st = check_norm_apart(what, grads, sizes, dtypes, count, result, workspace)) return st;
     return cuda_status(what, mqg::launch_clip(list_of(grads, sizes, dtypes, count), max_norm, mqg::kInPlace, nullptr, 0,
                                               result, workspace, static_cast<cudaStream_t>(cuda_stream)));
 }
@@ -116,9 +161,11 @@ mqg_status mqg_clip_flatten(const void* const* grads, const uint64_t* sizes, con
     const char* what = "mqg_clip_flatten";
     if (mqg_status st = check_list(what, grads, sizes, dtypes, count)) return st;
     if (mqg_status st = check_norm(what, count, max_norm, result, workspace, workspace_floats)) return st;
-    bool empty = true;
-    for (int j = 0; j < count; ++j) empty = empty && sizes[j] == 0;
-    if (mqg_status st = check_buffer(what, "flat", flat, flat_dtype, empty)) return st;
+    uint64_t total = 0;
+    for (int j = 0; j < count; ++j) total += sizes[j];
+    if (mqg_status st = check_buffer(what, "flat", flat, flat_dtype, total == 0)) return st;
+    const Region to = {"flat", flat, total * bytes_of(flat_dtype)};
+    if (mqg_status st = check_norm_apart(what, grads, sizes, dtypes, count, result, workspace, to)) return st;
     return cuda_status(what, mqg::launch_clip(list_of(grads, sizes, dtypes, count), max_norm, mqg::kFlatten, flat,
                                               (int)flat_dtype, result, workspace, static_cast<cudaStream_t>(cuda_stream)));
 }
@@ -129,6 +176,7 @@ mqg_status mqg_scale_grads(void* const* grads, const uint64_t* sizes, const mqg_
     const char* what = "mqg_scale_grads";
     if (mqg_status st = check_list(what, grads, sizes, dtypes, count)) return st;
     if (mqg_status st = check_buffer(what, "factor", factor, MQG_F32, false)) return st;
+    if (mqg_status st = check_list_apart(what, grads, sizes, dtypes, count, {{"factor", factor, 4}})) return st;
     return cuda_status(what, mqg::launch_scale_tensors(list_of(grads, sizes, dtypes, count), factor,
                                                        static_cast<cudaStream_t>(cuda_stream)));
 }
@@ -140,6 +188,8 @@ mqg_status mqg_apply_clipped(float* params, const float* acc, float lr, const fl
     if (!params || !acc) return report_error(MQG_ERR_INVALID, "%s: params or acc is null", what);
     if (!aligned(params, 16) || !aligned(acc, 16)) return report_error(MQG_ERR_ALIGN, "%s: params or acc not 16-byte aligned", what);
     if (mqg_status st = check_buffer(what, "factor", factor, MQG_F32, false)) return st;
+    const Region from = {"acc", acc, params == acc ? 0 : n * 4};         // (every element is read before it is written)
+    if (mqg_status st = check_apart(what, {"params", params, n * 4}, {from, {"factor", factor, 4}})) return st;
     return cuda_status(what, mqg::launch_apply_clipped(params, acc, lr, factor, n, static_cast<cudaStream_t>(cuda_stream)));
 }
 
@@ -152,6 +202,9 @@ mqg_status mqg_embedding(const void* table, mqg_dtype table_dtype, uint64_t rows
     if (mqg_status st = check_buffer(what, "table", table, table_dtype, empty || rows == 0)) return st;
     if (mqg_status st = check_buffer(what, "out", out, out_dtype, empty)) return st;
     if (empty) return MQG_OK;
+    const Region written = {"out", out, tokens * dim * bytes_of(out_dtype)};
+    if (mqg_status st = check_apart(what, written, {{"table", table, rows * dim * bytes_of(table_dtype)},
+                                                    {"ids", ids, tokens * bytes_of(ids_type)}})) return st;
     return cuda_status(what, mqg::launch_embedding(table, (int)table_dtype, rows, dim, {ids, tokens, ids_type == MQG_I64}, scale,
                                                    out, (int)out_dtype, static_cast<cudaStream_t>(cuda_stream)));
 }
@@ -178,6 +231,10 @@ mqg_status mqg_embedding_grad(const void* dout, mqg_dtype dout_dtype, const void
                             what, (unsigned long long)workspace_floats, (unsigned long long)need);
     if (need != 0 && !workspace) return report_error(MQG_ERR_INVALID, "%s: workspace is null", what);
     if (!aligned(workspace, 16)) return report_error(MQG_ERR_ALIGN, "%s: workspace not 16-byte aligned", what);
+    const Region from = {"dout", dout, tokens * dim * bytes_of(dout_dtype)}, by = {"ids", ids, tokens * bytes_of(ids_type)};
+    const Region written = {"grad", grad, rows * dim * bytes_of(grad_dtype)}, scratch = {"workspace", workspace, need * 4};
+    if (mqg_status st = check_apart(what, written, {from, by, scratch})) return st;
+    if (mqg_status st = check_apart(what, scratch, {from, by})) return st;
     return cuda_status(what, mqg::launch_embedding_grad(dout, (int)dout_dtype, {ids, tokens, ids_type == MQG_I64}, rows, dim,
                                                         scale, grad, (int)grad_dtype, add_into_grad != 0, workspace,
                                                         static_cast<cudaStream_t>(cuda_stream)));

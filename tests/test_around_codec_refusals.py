@@ -97,6 +97,77 @@ def test_tables_are_checked(lib):
     assert grad(work=None) == INVALID and grad(work=ODD8) == ALIGN
 
 
+A, B, C_, D = 0x100000, 0x200000, 0x300000, 0x4000000       # apart from each other
+
+
+def _refused(status, *names):
+    return status == INVALID and "share memory" in mqg.mqg_last_error() and all(n in mqg.mqg_last_error() for n in names)
+
+
+@pytest.mark.parametrize("form", ["norm", "in place", "flatten"])
+def test_what_the_norm_writes_lies_apart(lib, form):
+    need = mqg.mqg_norm_workspace_floats(2)
+
+    def call(result=B, work=C_, flat=D, tensors=((A, 100, 0), (A + 400, 8, 1)), floats=need):
+        l = _list(*tensors)
+        if form == "norm":
+            return lib.mqg_grad_norm(*l, 1.0, result, work, floats, None)
+        if form == "in place":
+            return lib.mqg_clip_grad_norm(*l, 1.0, result, work, floats, None)
+        return lib.mqg_clip_flatten(*l, 1.0, flat, 1, result, work, floats, None)
+
+    assert _refused(call(result=A + 396), "tensor 0", "result") and _refused(call(result=A), "tensor 0", "result")
+    assert _refused(call(result=A + 412), "tensor 1", "result") and _refused(call(result=A - 4), "tensor 0", "result")
+    assert _refused(call(work=A + 408), "tensor 1", "workspace")
+    assert _refused(call(work=A - 4 * need + 8), "tensor 0", "workspace")
+    assert _refused(call(result=C_), "result", "workspace") and _refused(call(result=C_ - 4), "result", "workspace")
+    assert _refused(call(result=C_ + 4 * need - 4), "result", "workspace")
+    # what is behind the floats that a call needs is not touched, nor are empty tensors
+    others = [dict(result=A - 8), dict(result=A + 416), dict(work=A + 416), dict(work=A - 4 * need),
+              dict(result=C_ + 4 * need, floats=need + 8), dict(tensors=((B, 0, 0), (A, 8, 0)))]
+    if form == "flatten":
+        assert _refused(call(flat=A + 414), "tensor 1", "flat") and _refused(call(flat=A - 214), "tensor 0", "flat")
+        assert _refused(call(flat=B - 214), "flat", "result") and _refused(call(flat=C_ + 4 * need - 2), "flat", "workspace")
+        others += [dict(flat=A + 416), dict(flat=A - 216), dict(flat=B - 216), dict(flat=C_ + 4 * need)]
+    if not torch.cuda.is_available():                   # (what is not refused fails at the launch here)
+        assert all(call(**o) == mqg.MQG_ERR_CUDA for o in others)
+
+
+def test_a_factor_lies_apart(lib):
+    l = _list((A, 100, 0), (A + 400, 8, 1))
+    assert _refused(lib.mqg_scale_grads(*l, A + 396, None), "tensor 0", "factor")
+    assert _refused(lib.mqg_scale_grads(*l, A + 412, None), "tensor 1", "factor")
+    assert _refused(lib.mqg_apply_clipped(A, B, 0.1, A + 396, 100, None), "params", "factor")
+    assert _refused(lib.mqg_apply_clipped(A, A + 384, 0.1, B, 100, None), "params", "acc")
+    assert _refused(lib.mqg_apply_clipped(A, A - 384, 0.1, B, 100, None), "params", "acc")
+    if not torch.cuda.is_available():
+        assert lib.mqg_scale_grads(*l, A + 416, None) == lib.mqg_scale_grads(*l, A - 4, None) == mqg.MQG_ERR_CUDA
+        assert lib.mqg_apply_clipped(A, A + 400, 0.1, B, 100, None) == mqg.MQG_ERR_CUDA
+        assert lib.mqg_apply_clipped(A, A, 0.1, A + 400, 100, None) == mqg.MQG_ERR_CUDA      # element by element: in place
+
+
+def test_tables_and_rows_lie_apart(lib):
+    need = mqg.mqg_embedding_workspace_floats(10, 20, 8)
+
+    def lookup(table=A, ids=B, out=C_, it=1):           # 20 rows of 32 bytes, 10 ids, 10 rows of 16 bytes
+        return lib.mqg_embedding(table, 0, 20, 8, ids, it, 10, 1.0, out, 1, None)
+
+    def grad(dout=A, ids=B, table=C_, work=D, tokens=10, floats=need):      # 10 rows of 32 bytes, 10 ids, 20 rows of 16 bytes
+        return lib.mqg_embedding_grad(dout, 0, ids, 1, tokens, 20, 8, 1.0, table, 1, 0, work, floats, None)
+
+    assert _refused(lookup(out=A), "out", "table") and _refused(lookup(out=A + 638), "out", "table")
+    assert _refused(lookup(out=A - 158), "out", "table") and _refused(lookup(out=B), "out", "ids")
+    assert _refused(lookup(out=B + 38, it=0), "out", "ids") and _refused(lookup(out=B + 78), "out", "ids")
+    assert _refused(grad(table=A), "grad", "dout") and _refused(grad(table=A + 318), "grad", "dout")
+    assert _refused(grad(table=B - 318), "grad", "ids") and _refused(grad(table=D + 4 * need - 2), "grad", "workspace")
+    assert _refused(grad(work=A + 304), "workspace", "dout") and _refused(grad(work=B + 64), "workspace", "ids")
+    if not torch.cuda.is_available():
+        for status in (lookup(out=A + 640), lookup(out=A - 160), lookup(out=B + 40, it=0), lookup(out=B + 80), lookup(ids=A),
+                       grad(table=A + 320), grad(table=B - 320), grad(table=D + 4 * need, floats=need + 8),
+                       grad(work=A + 320), grad(work=B + 80), grad(ids=A), grad(dout=C_, tokens=0)):
+            assert status == mqg.MQG_ERR_CUDA
+
+
 def test_workspace_sizes():
     assert mqg.mqg_norm_workspace_floats(0) == mqg.mqg_norm_workspace_floats(1) == mqg.mqg_norm_workspace_floats(1024)
     assert mqg.mqg_norm_workspace_floats(1025) == 2 * mqg.mqg_norm_workspace_floats(1)
@@ -158,3 +229,19 @@ def test_sizes_types_and_overlaps_of_device_tensors():
     # neighbours that touch do not overlap, in any order
     mqg.mqg_scale_grads([x[32:], x[:32]], res + 1)
     assert mqg.mqg_device_timeouts() == 0
+
+
+@pytest.mark.gpu
+def test_device_tensors_that_share_memory():
+    x, i = torch.zeros(4096, device="cuda"), torch.zeros(4, dtype=torch.int64, device="cuda")
+    res, work, y = torch.zeros(2, device="cuda"), torch.zeros(FLOATS, device="cuda"), torch.zeros(64, device="cuda")
+    for call in (lambda: mqg.mqg_grad_norm([y, x], 1.0, x[8:], work), lambda: mqg.mqg_clip_grad_norm([y, x], 1.0, res, x),
+                 lambda: mqg.mqg_clip_flatten([y], 1.0, x, x[60:], work), lambda: mqg.mqg_scale_grads([y, x], x[4095:]),
+                 lambda: mqg.mqg_apply_clipped(x, x[4:], 0.1, res, 64), lambda: mqg.mqg_embedding(x, 8, 4, i, 4, 1.0, x[31:]),
+                 lambda: mqg.mqg_embedding_grad(x, i, 4, 8, 8, 1.0, x[31:], work),
+                 lambda: mqg.mqg_embedding_grad(x, i, 4, 8, 8, 1.0, y, x)):
+        with pytest.raises(mqg.MqgError, match="share memory"):
+            call()
+    mqg.mqg_embedding(x, 8, 4, i, 4, 1.0, x[32:])
+    mqg.mqg_embedding_grad(x, i, 4, 8, 8, 1.0, x[32:], work)
+    mqg.mqg_apply_clipped(x, x, 0.1, res, 64)
