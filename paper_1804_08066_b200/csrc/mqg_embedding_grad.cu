@@ -4,10 +4,13 @@
 //
 // in fp32, tokens in ascending order:
 //   1. the tokens are sorted by id (mqg_token_sort.cu), so that the tokens of a row are neighbours (a run) and no atomic is
-//      needed: the order of every sum is fixed.  Unless the gradient is added to what is there, it is set to zero meanwhile;
+//      needed: the order of every sum is fixed;
 //   2. the sorted tokens are cut into chunks of C; a thread takes eight columns of a chunk and adds up its runs.  A run that
 //      crosses chunks belongs to the chunk it begins in, which follows it, as long as it covers no chunk as a whole (less
-//      than 2 C tokens); of a longer one every chunk leaves its part's sum in the workspace;
+//      than 2 C tokens); of a longer one every chunk leaves its part's sum in the workspace.  Unless the gradient is added to
+//      what is there, further CTAs of the sort's launch set a first part of it to zero, and of this one the rest of the rows
+//      that have no tokens.  (Zeros by a launch of their own that the sort let begin early, beside itself, took as long or up to
+//      3 % less, but they began to write before any wait of theirs said that what came before was done);
 //   3. the parts of the long runs are added up in the order of the chunks.
 #include <atomic>
 
@@ -34,6 +37,11 @@ struct GradArgs {
     uint32_t tiles;          // CTAs side by side over the columns
     int thread_bits;         // 2^this threads of a CTA over the columns, the others over chunks
     float scale;
+    uint32_t sum_ctas;       // the CTAs behind them set rows without tokens to zero,
+    uint32_t zero_from;      // from this one on:
+    uint32_t zero_rows;      // so many each, or,
+    uint32_t zero_parts;     // where a row is more than a CTA's share, one of so many parts of a row
+    uint32_t reciprocal;     // of a row's bytes: ceil(2^32 / bytes), where a CTA has several rows
 };
 
 // The sums of a thread's eight columns are two words of a part: word j of thread t of tile i is word (2 i + j) * threads + t.
@@ -170,6 +178,138 @@ __device__ __forceinline__ uint32_t chunks_of_run(const GradArgs& a, uint32_t ch
     return n;
 }
 
+// ---- rows without tokens ----
+// A CTA has up to 32 KB of the gradient.  It finds the sorted tokens of its rows, marks the rows that have some and sets the
+// others to zero.  It writes no row that has tokens, so that it need not be ordered with the sums, and it begins, like them,
+// when the sort is done.  Bound by the writes to DRAM (200,000 rows of 1000 in fp32, 16,384 tokens: 134 us in all, 800 MB
+// written and 66 read) as long as the turns to memory before them are few: as a rule two, a look at 128 tokens far apart and one
+// at the 512 behind the last of them that is of a row before.  (With 16 KB the CTAs are too short for that: 159 us; with 64
+// there are too few of them at the end: 50,000 rows of 4 KB, 16,384 tokens, 51.6 us instead of 49.4.)
+constexpr uint32_t kZeroBytes = 32768;
+constexpr uint32_t kMaxZeroRows = 1024, kMaxScan = 4096;
+constexpr int kRowsPerThread = kMaxZeroRows / kThreads;
+
+struct UsedRows {
+    uint32_t bits[kMaxZeroRows / 32];
+    uint32_t any;
+    __device__ __forceinline__ bool has(uint32_t row) const { return (bits[row / 32] >> (row & 31)) & 1u; }
+};
+
+// Marks which of the `rows` rows from row0 on have tokens; returns whether any has.
+__device__ __forceinline__ bool find_used(const GradArgs& a, uint32_t row0, uint32_t rows, UsedRows& used)
+{
+    constexpr uint32_t kLooks = 4;
+    const uint32_t lane = threadIdx.x & 31, end = a.tokens;
+    if (threadIdx.x < kMaxZeroRows / 32) used.bits[threadIdx.x] = 0;
+    if (threadIdx.x == 0) used.any = 0;
+    uint32_t begin = 0;                                 // the tokens before are of rows before
+    for (uint32_t n = end; n > kLooks * kThreads;) {
+        const uint32_t step = (n + kThreads - 1) / kThreads, p = begin + (threadIdx.x + 1) * step - 1;
+        begin += step * __syncthreads_count(p < end && __ldcg(&a.sorted[p].x) < row0);
+        n = min(step - 1, end - begin);
+    }
+    for (uint32_t from = begin; from - begin < kMaxScan; from += kLooks * kThreads) {
+        uint32_t row[kLooks];
+#pragma unroll
+        for (uint32_t u = 0; u < kLooks; ++u) {
+            const uint32_t p = from + u * kThreads + threadIdx.x;
+            row[u] = p < end ? __ldcg(&a.sorted[p].x) : ~0u;
+        }
+        if (from == begin) __syncthreads();             // (nothing is marked before all is clear)
+#pragma unroll
+        for (uint32_t u = 0; u < kLooks; ++u) {
+            const uint32_t before = __shfl_up_sync(0xFFFFFFFFu, row[u], 1), r = row[u] - row0;
+            if (row[u] < row0 || r >= rows || (lane != 0 && row[u] == before)) continue;
+            atomicOr(&used.bits[r / 32], 1u << (r & 31));
+            used.any = 1;
+        }
+        const bool beyond = row[kLooks - 1] >= row0 && row[kLooks - 1] - row0 >= rows;
+        if (__syncthreads_or(beyond)) return used.any != 0;
+    }
+    // more tokens than are worth looking at (all but the first 512 are of these rows): a search for every row
+    uint32_t at[kRowsPerThread];                        // the last token whose row is not above, or the first
+#pragma unroll
+    for (int u = 0; u < kRowsPerThread; ++u) at[u] = begin;
+    for (uint32_t left = end - begin; left > 1;) {
+        const uint32_t half = left / 2;
+#pragma unroll
+        for (int u = 0; u < kRowsPerThread; ++u) {
+            if (u * kThreads >= rows) break;
+            if (__ldcg(&a.sorted[at[u] + half].x) <= row0 + u * kThreads + threadIdx.x) at[u] += half;
+        }
+        left -= half;
+    }
+#pragma unroll
+    for (int u = 0; u < kRowsPerThread; ++u) {
+        if (u * kThreads >= rows) break;
+        const bool there = u * kThreads + threadIdx.x < rows && __ldcg(&a.sorted[at[u]].x) == row0 + u * kThreads + threadIdx.x;
+        const uint32_t bits = __ballot_sync(0xFFFFFFFFu, there);
+        if (lane == 0) used.bits[u * (kThreads / 32) + threadIdx.x / 32] = bits;
+    }
+    __syncthreads();
+    return true;
+}
+
+// Zeros into `bytes` bytes of elements T, by `count` threads of which this is number `i`.
+template <typename T> __device__ __forceinline__ void write_zeros(char* p, uint32_t bytes, uint32_t i, uint32_t count)
+{
+    const uint32_t to_boundary = (uint32_t)((16 - (reinterpret_cast<uintptr_t>(p) & 15)) & 15);
+    const uint32_t head = min(to_boundary, bytes), behind = bytes - (bytes - head) % 16;
+#pragma unroll 4
+    for (uint32_t at = head + i * 16; at < behind; at += count * 16) *reinterpret_cast<uint4*>(p + at) = make_uint4(0, 0, 0, 0);
+    const uint32_t at = i * (uint32_t)sizeof(T);
+    if (at < head) *reinterpret_cast<T*>(p + at) = T();
+    if (at < bytes - behind) *reinterpret_cast<T*>(p + behind + at) = T();
+}
+
+// The same for rows of row_bytes of which those that are used stay: of long rows a warp takes one at a time, of others threads go
+// through the vectors side by side.
+constexpr uint32_t kLongRow = 512;
+template <typename T>
+__device__ __forceinline__ void write_zeros_between(char* p, uint32_t rows, uint32_t row_bytes, uint32_t reciprocal, const UsedRows& used)
+{
+    if (row_bytes >= kLongRow) {
+        for (uint32_t r = threadIdx.x / 32; r < rows; r += kThreads / 32)
+            if (!used.has(r)) write_zeros<T>(p + r * row_bytes, row_bytes, threadIdx.x & 31, 32);
+        return;
+    }
+    const uint32_t bytes = rows * row_bytes, to_boundary = (uint32_t)((16 - (reinterpret_cast<uintptr_t>(p) & 15)) & 15);
+    const uint32_t head = min(to_boundary, bytes), behind = bytes - (bytes - head) % 16;
+    const auto row_of = [&](uint32_t at) { return __umulhi(at, reciprocal); };
+    const auto element = [&](uint32_t at) {
+        if (!used.has(row_of(at))) *reinterpret_cast<T*>(p + at) = T();
+    };
+    for (uint32_t at = head + threadIdx.x * 16; at < behind; at += kThreads * 16) {
+        const uint32_t row = row_of(at), last = row_of(at + 16 - (uint32_t)sizeof(T));
+        bool any = used.has(row), all = any;
+        for (uint32_t r = row + 1; r <= last; ++r) {    // rows that start anywhere: some end in the vector
+            any |= used.has(r);
+            all &= used.has(r);
+        }
+        if (!any) {
+            *reinterpret_cast<uint4*>(p + at) = make_uint4(0, 0, 0, 0);
+        } else if (!all) {
+#pragma unroll 1
+            for (uint32_t e = 0; e < 16; e += sizeof(T)) element(at + e);
+        }
+    }
+    const uint32_t at = threadIdx.x * (uint32_t)sizeof(T);
+    if (at < head) element(at);
+    if (at < bytes - behind) element(behind + at);
+}
+
+template <typename T> __device__ __forceinline__ void zero_unused_rows(const GradArgs& a, uint32_t cta, UsedRows& used)
+{
+    const uint32_t group = cta / a.zero_parts, part = cta - group * a.zero_parts;
+    const uint32_t row0 = a.zero_from + group * a.zero_rows, rows = min(a.zero_rows, a.rows - row0);
+    const bool any = find_used(a, row0, rows, used);
+    if (any && a.zero_rows == 1) return;
+    const uint64_t row_bytes = (uint64_t)a.dim * sizeof(T), from = (uint64_t)part * kZeroBytes;
+    char* p = static_cast<char*>(a.grad) + row0 * row_bytes + from;
+    if (any) write_zeros_between<T>(p, rows, (uint32_t)row_bytes, a.reciprocal, used);
+    else write_zeros<T>(p, (uint32_t)min(rows * row_bytes - from, (uint64_t)kZeroBytes), threadIdx.x, kThreads);
+}
+
 // CTAs that read the same rows are neighbours in the grid.  Lanes take neighbouring groups, so that every access of a warp
 // covers whole sectors (two 16-byte stores per thread, 32 bytes apart from lane to lane, made the fp32 sums write half
 // sectors).  kDepth rows are under way for each thread: four with 23 KB of shared memory to a CTA did as well as six, and
@@ -183,6 +323,14 @@ __global__ void __launch_bounds__(kThreads) grad_sum_kernel(const GradArgs a)
     __shared__ typename X::Shared xs;
     __shared__ typename Y::Shared ys;
     __shared__ Window tokens;
+    if constexpr (!ADD) {
+        if (blockIdx.x >= a.sum_ctas) {
+            __shared__ UsedRows used;
+            grid_dependency_wait();
+            zero_unused_rows<typename Element<DST>::type>(a, blockIdx.x - a.sum_ctas, used);
+            return;
+        }
+    }
     const uint32_t across = 1u << a.thread_bits, down = blockIdx.x / a.tiles, tile = blockIdx.x - down * a.tiles;
     const uint32_t t = threadIdx.x & (across - 1), first_chunk = down * (kThreads >> a.thread_bits);
     const uint32_t chunk = first_chunk + (threadIdx.x >> a.thread_bits);
@@ -503,13 +651,15 @@ __global__ void __launch_bounds__(kSortThreads, 1) grad_small_kernel(const Small
 }
 
 // ---- host ----
-constexpr uint64_t round4(uint64_t words) { return (words + 3) & ~3ull; }
+// Sizes in the workspace are whole lines of 128 bytes: with parts that begin in the middle of a sector, 73,903 tokens of 512
+// took 61 us instead of 57.
+constexpr uint64_t whole_lines(uint64_t words) { return (words + 31) & ~31ull; }
 
 struct Layout {
     int chunk_bits, thread_bits;
     uint32_t chunks, tiles;
     uint64_t sorted, runs, scratch, parts, total;       // sizes in words
-    Layout(uint64_t tokens, uint64_t rows, uint64_t dim)
+    Layout(uint64_t tokens, uint64_t dim)
     {
         // 32 tokens to a chunk, down to 8 where that leaves less than a CTA for each of 1024 x 1024 elements
         chunk_bits = kMaxChunkBits;
@@ -519,18 +669,28 @@ struct Layout {
         while ((1 << thread_bits) < kThreads && (uint64_t)kColumns << thread_bits < dim) ++thread_bits;
         const uint64_t tile = (uint64_t)kColumns << thread_bits;
         tiles = (uint32_t)((dim + tile - 1) / tile);
-        sorted = round4(2 * tokens);
-        runs = 4 + 4 * (uint64_t)chunks;
-        scratch = round4(token_sort_words(tokens, rows));
+        sorted = whole_lines(2 * tokens);
+        runs = whole_lines(4 + 4 * (uint64_t)chunks);
+        scratch = whole_lines(token_sort_words(tokens));
         parts = 2 * (uint64_t)chunks * tiles * tile;
         total = sorted + runs + scratch + parts;
     }
 };
 
-template <int SRC, int DST, int W, bool ADD> cudaError_t launch_sums(const GradArgs& a, cudaStream_t stream)
+template <int SRC, int DST, int W, bool ADD> cudaError_t launch_sums(GradArgs a, cudaStream_t stream)
 {
     const uint32_t down = kThreads >> a.thread_bits;
-    const cudaError_t err = launch_pdl(grad_sum_kernel<SRC, DST, W, ADD>, (a.chunks + down - 1) / down * a.tiles, kThreads, stream, a);
+    a.sum_ctas = (a.chunks + down - 1) / down * a.tiles;
+    uint32_t zero_ctas = 0;
+    if (!ADD) {
+        const uint64_t row_bytes = (uint64_t)a.dim * kElemBytes<DST>;
+        const uint64_t fit = kZeroBytes / row_bytes;
+        a.zero_rows = fit < 1 ? 1 : fit > kMaxZeroRows ? kMaxZeroRows : (uint32_t)fit;
+        a.zero_parts = (uint32_t)((row_bytes + kZeroBytes - 1) / kZeroBytes);
+        a.reciprocal = fit < 1 ? 0 : (uint32_t)(((1ull << 32) + row_bytes - 1) / row_bytes);
+        zero_ctas = (uint32_t)(((uint64_t)a.rows - a.zero_from + a.zero_rows - 1) / a.zero_rows * a.zero_parts);
+    }
+    const cudaError_t err = launch_pdl(grad_sum_kernel<SRC, DST, W, ADD>, a.sum_ctas + zero_ctas, kThreads, stream, a);
     if (err != cudaSuccess || a.chunks < 2) return err;                              // a long run is in two chunks at least
     const uint64_t most = (uint64_t)(a.chunks - 1) * (((a.tiles * 2 << a.thread_bits) + kJoinWords - 1) / kJoinWords);
     return launch_pdl(grad_join_kernel<DST, W, ADD>, (unsigned)(most < 1184 ? most : 1184), kJoinThreads, stream, a);
@@ -618,7 +778,7 @@ template <int SRC, int DST> cudaError_t small_by_add(const SmallArgs& a, bool ad
 
 size_t embedding_workspace_floats(uint64_t tokens, uint64_t rows, uint64_t dim)
 {
-    return tokens == 0 || rows == 0 || dim == 0 ? 0 : (size_t)Layout(tokens, rows, dim).total;
+    return tokens == 0 || rows == 0 || dim == 0 ? 0 : (size_t)Layout(tokens, dim).total;
 }
 
 cudaError_t launch_embedding_grad(const void* dout, int dout_dtype, const TokenIds& ids, uint64_t rows, uint64_t dim,
@@ -633,16 +793,18 @@ cudaError_t launch_embedding_grad(const void* dout, int dout_dtype, const TokenI
             return grad_dtype == kF32 ? small_by_add<kF32, kF32>(s, add, stream) : small_by_add<kF32, kBf16>(s, add, stream);
         return grad_dtype == kF32 ? small_by_add<kBf16, kF32>(s, add, stream) : small_by_add<kBf16, kBf16>(s, add, stream);
     }
-    const Layout lay(ids.count, rows, dim);
+    const Layout lay(ids.count, dim);
     uint2* sorted = reinterpret_cast<uint2*>(workspace);
     uint32_t* runs = reinterpret_cast<uint32_t*>(workspace + lay.sorted);
     uint32_t* scratch = runs + lay.runs;
-    const GradArgs a = {sorted, dout, grad, reinterpret_cast<float4*>(scratch + lay.scratch), runs,
+    GradArgs a = {sorted, dout, grad, reinterpret_cast<float4*>(scratch + lay.scratch), runs,
                         reinterpret_cast<uint4*>(runs + 4), (uint32_t)dim, (uint32_t)ids.count, (uint32_t)rows, lay.chunks,
-                        lay.chunk_bits, lay.tiles, lay.thread_bits, scale};
-    const cudaError_t err = launch_token_sort(ids, a.rows, sorted, runs, scratch, add ? nullptr : grad,
-                                              dim * (grad_dtype == kF32 ? 4 : 2), stream);
-    if (err != cudaSuccess || a.chunks == 0) return err;
+                        lay.chunk_bits, lay.tiles, lay.thread_bits, scale, 0, 0, 0, 0, 0};
+    if (ids.count != 0) {
+        const cudaError_t err = launch_token_sort(ids, a.rows, sorted, runs, scratch, add ? nullptr : grad,
+                                                  dim * (grad_dtype == kF32 ? 4 : 2), &a.zero_from, stream);
+        if (err != cudaSuccess) return err;
+    }
     if (dout_dtype == kF32)
         return grad_dtype == kF32 ? by_group<kF32, kF32>(a, add, stream) : by_group<kF32, kBf16>(a, add, stream);
     return grad_dtype == kF32 ? by_group<kBf16, kF32>(a, add, stream) : by_group<kBf16, kBf16>(a, add, stream);

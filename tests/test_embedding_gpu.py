@@ -212,6 +212,25 @@ def test_zeros_beside_rows_in_use_when_both_exceed_l2(shape):
     assert (grad.cpu() == 0.5 * count[:, None]).all()
 
 
+@pytest.mark.parametrize("types", [(F32, F32), (BF16, BF16)])
+@pytest.mark.parametrize("shape", [(40_000, 1024, 33_000), (33_333, 1040, 33_000), (33_000, 4096, 8200), (260_000, 160, 140_000),
+                                   (30_011, 515, 10_007), (3000, 8200, 9000), (900, 20_001, 9001), (70_000, 3, 9000), (1025, 7, 40_000)])
+def test_rows_without_tokens_are_zero_whatever_the_call_before_left(shape, types):
+    """Calls with other ids each time, with one workspace, into a gradient that holds NaN: nothing of the call before may show.
+    Whole numbers: sums are exact, and a bf16 result is rounded once."""
+    rows, dim, tokens = shape
+    d = torch.ones(tokens, dim, device="cuda", dtype=types[0])
+    grad = torch.empty(rows, dim, device="cuda", dtype=types[1])
+    w = torch.empty(mqg.mqg_embedding_workspace_floats(tokens, rows, dim), device="cuda")
+    for seed, kind in enumerate(("zipf", "outside", "same", "uniform", "zipf", "empty")):
+        ids = _ids(tokens, rows, kind, I64, seed).cuda()
+        grad.fill_(math.nan)
+        mqg.mqg_embedding_grad(d, ids, tokens, rows, dim, 0.5, grad, w)
+        held = (ids >= 0) & (ids < rows)
+        count = torch.zeros(rows, device="cuda").index_add_(0, ids[held], torch.ones(tokens, device="cuda")[held])
+        assert bool((grad == (0.5 * count[:, None]).to(types[1])).all()), kind
+
+
 def test_gradient_by_differences():
     """<R, lookup(table)> is linear in the table: its central difference is the gradient of R."""
     rows, dim, tokens, scale, h = 6, 5, 40, 0.75, 0.5
