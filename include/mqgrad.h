@@ -466,6 +466,13 @@ mqg_status mqg_check_timeouts(unsigned int* count, int reset);
  */
 mqg_status mqg_test_wait_override(uint32_t poll_limit, int arm_only);
 
+/*
+ * TEST HOOK, process-wide, not for production use: mqg_embedding_grad sorts tokens as on a device that holds no cluster of more
+ * than most_ctas CTAs (a power of two up to 16; 1: no cluster at all; 0 restores the default).  The result is the same bit for
+ * bit.
+ */
+mqg_status mqg_test_sort_cluster(uint32_t most_ctas);
+
 /* Message of the last error returned to the calling thread ("" if none).  Never NULL. */
 const char* mqg_last_error(void);
 

@@ -15,7 +15,7 @@ Function names and argument order follow the C ABI:
   mqg_test_wait_override.
 Around the codec (the global gradient norm, clipping, the table of a model over tokens):
   mqg_norm_workspace_floats, mqg_grad_norm, mqg_clip_grad_norm, mqg_clip_flatten, mqg_scale_grads, mqg_apply_clipped,
-  mqg_embedding, mqg_embedding_workspace_floats, mqg_embedding_grad.
+  mqg_embedding, mqg_embedding_workspace_floats, mqg_embedding_grad, mqg_test_sort_cluster.
 """
 from __future__ import annotations
 
@@ -85,6 +85,7 @@ def _load() -> C.CDLL:
         "mqg_scale_grads": (i32, [vp, vp, vp, i32, vp, vp]),
         "mqg_apply_clipped": (i32, [vp, vp, f32, vp, u64, vp]),
         "mqg_embedding": (i32, [vp, i32, u64, u64, vp, i32, u64, f32, vp, i32, vp]),
+        "mqg_test_sort_cluster": (i32, [u32]),
         "mqg_embedding_workspace_floats": (C.c_size_t, [u64, u64, u64]),
         "mqg_embedding_grad": (i32, [vp, i32, vp, i32, u64, u64, u64, f32, vp, i32, i32, vp, C.c_size_t, vp]),
     }
@@ -222,6 +223,11 @@ def mqg_norm_workspace_floats(count: int) -> int:
 
 def mqg_embedding_workspace_floats(tokens: int, rows: int, dim: int) -> int:
     return int(_lib.mqg_embedding_workspace_floats(tokens, rows, dim))
+
+
+def mqg_test_sort_cluster(most_ctas: int = 0) -> None:
+    """TEST HOOK: see the header.  0 restores the default."""
+    _check(_lib.mqg_test_sort_cluster(most_ctas))
 
 
 MQG_L2_STATIC_WORKSPACE_FLOATS = 65536

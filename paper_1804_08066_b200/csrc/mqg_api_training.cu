@@ -3,6 +3,7 @@
 
 #include "../../include/mqgrad.h"
 #include "mqg_internal.h"
+#include "mqg_token_sort.h"
 #include "mqg_training.h"
 
 namespace {
@@ -238,6 +239,15 @@ mqg_status mqg_embedding_grad(const void* dout, mqg_dtype dout_dtype, const void
     return cuda_status(what, mqg::launch_embedding_grad(dout, (int)dout_dtype, {ids, tokens, ids_type == MQG_I64}, rows, dim,
                                                         scale, grad, (int)grad_dtype, add_into_grad != 0, workspace,
                                                         static_cast<cudaStream_t>(cuda_stream)));
+}
+
+mqg_status mqg_test_sort_cluster(uint32_t most_ctas)
+{
+    if (most_ctas == 0) most_ctas = 16;
+    if (most_ctas > 16 || (most_ctas & (most_ctas - 1)) != 0)
+        return report_error(MQG_ERR_INVALID, "mqg_test_sort_cluster: %u is no power of two up to 16", most_ctas);
+    mqg::set_token_sort_cluster(most_ctas);
+    return MQG_OK;
 }
 
 }  // extern "C"

@@ -2,7 +2,8 @@
 //
 // Up to 2048 tokens one CTA sorts, in shared memory, by digits of at most six bits: a pass costs little more than ranking.
 // (2048 tokens of 16-bit ids: 8.5 us a launch; 4096: 13.0 in one CTA, 8.6 in a cluster.)
-// Up to 131,072 a thread-block cluster does in one launch, by digits of up to ten bits, since every pass has two cluster
+// Up to 131,072 a thread-block cluster of up to 16 CTAs does in one launch (fewer where the device, or the part of one, holds no
+// cluster of 16: 8192 to a CTA), by digits of up to ten bits, since every pass has two cluster
 // barriers.  In both a thread takes K pairs (key, token) of the order so far, a warp 32 K consecutive ones; it ranks them by
 // ballots, the warps' digit counts are added up in shared memory (and the CTAs' through distributed shared memory), and every
 // pair goes to its place: in shared memory, or, for the cluster, in memory, where the next pass reads it from L2.  (Stores to
@@ -183,50 +184,86 @@ unsigned zero_clusters(const SortArgs& a, unsigned room)
     return want < room ? (unsigned)want : room;
 }
 
-template <typename ID, int K> cudaError_t launch_cluster(const SortArgs& a, cudaStream_t stream)
-{
-    static std::atomic<int> at_once[64][5];             // clusters of 2^i CTAs, by device: how many fit; 0: not asked yet
-    int dev = 0;
-    cudaError_t err = cudaGetDevice(&dev);
-    if (err != cudaSuccess) return err;
-    if (dev < 0 || dev >= 64) return cudaErrorInvalidDevice;
+// The launch of one cluster of `ctas` CTAs; the attributes live as long as this.
+struct ClusterConfig {
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(a.ctas);
-    cfg.blockDim = dim3(kThreads);
-    cfg.dynamicSmemBytes = sort_smem(1 << a.digit_bits);
-    cfg.stream = stream;
     cudaLaunchAttribute attr[2];
-    attr[0].id = cudaLaunchAttributeClusterDimension;
-    attr[0].val.clusterDim.x = a.ctas;
-    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
-    attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr[1].val.programmaticStreamSerializationAllowed = 1;
-    cfg.attrs = attr;
-    std::atomic<int>& fit = at_once[dev][31 - __builtin_clz(a.ctas)];
-    int clusters = fit.load(std::memory_order_relaxed);
-    if (clusters == 0) {
-        err = cudaFuncSetAttribute(sort_cluster_kernel<ID, K>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                   (int)sort_smem(1 << kMaxDigitBits));
+    ClusterConfig(unsigned ctas, size_t smem, cudaStream_t stream)
+    {
+        cfg.gridDim = dim3(ctas);
+        cfg.blockDim = dim3(kThreads);
+        cfg.dynamicSmemBytes = smem;
+        cfg.stream = stream;
+        attr[0].id = cudaLaunchAttributeClusterDimension;
+        attr[0].val.clusterDim.x = ctas;
+        attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+        attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+        attr[1].val.programmaticStreamSerializationAllowed = 1;
+        cfg.attrs = attr;
+        cfg.numAttrs = 2;
+    }
+};
+
+// How many clusters of so many CTAs of a kernel the current device runs at once; 0: it cannot hold one.
+template <typename ID, int K> cudaError_t clusters_at_once(int dev, unsigned ctas, int* clusters)
+{
+    static std::atomic<int> known[64][5];               // by device and log2(ctas): one more than the answer; 0: not asked yet
+    std::atomic<int>& k = known[dev][31 - __builtin_clz(ctas)];
+    int n = k.load(std::memory_order_relaxed);
+    if (n == 0) {
+        cudaError_t err = cudaFuncSetAttribute(sort_cluster_kernel<ID, K>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                               (int)sort_smem(1 << kMaxDigitBits));
         if (err == cudaSuccess)                         // clusters of 16 CTAs
             err = cudaFuncSetAttribute(sort_cluster_kernel<ID, K>, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
-        cfg.numAttrs = 1;
-        if (err == cudaSuccess) err = cudaOccupancyMaxActiveClusters(&clusters, sort_cluster_kernel<ID, K>, &cfg);
         if (err != cudaSuccess) return err;
-        fit.store(clusters, std::memory_order_relaxed);
+        ClusterConfig c(ctas, sort_smem(1 << kMaxDigitBits), nullptr);
+        c.cfg.numAttrs = 1;
+        if (cudaOccupancyMaxActiveClusters(&n, sort_cluster_kernel<ID, K>, &c.cfg) != cudaSuccess) {
+            (void)cudaGetLastError();                   // a size that the device does not know
+            n = 0;
+        }
+        k.store(++n, std::memory_order_relaxed);
     }
-    cfg.gridDim.x += zero_clusters(a, clusters > 1 ? clusters - 1 : 1) * a.ctas;
-    cfg.numAttrs = 2;
-    return cudaLaunchKernelEx(&cfg, sort_cluster_kernel<ID, K>, a);
+    *clusters = n - 1;
+    return cudaSuccess;
+}
+
+cudaError_t current_device(int* dev)
+{
+    const cudaError_t err = cudaGetDevice(dev);
+    if (err != cudaSuccess) return err;
+    return *dev >= 0 && *dev < 64 ? cudaSuccess : cudaErrorInvalidDevice;
+}
+
+// The CTAs of the largest cluster that the current device holds, or 1: a part of a device may hold none of 16.
+std::atomic<unsigned> g_most_ctas{kMaxCluster};
+cudaError_t largest_cluster(unsigned* ctas)
+{
+    int dev, clusters = 0;
+    cudaError_t err = current_device(&dev);
+    *ctas = 2 * g_most_ctas.load(std::memory_order_relaxed);
+    while (err == cudaSuccess && clusters == 0 && (*ctas /= 2) > 1) err = clusters_at_once<int64_t, 8>(dev, *ctas, &clusters);
+    return err;
+}
+
+template <typename ID, int K> cudaError_t launch_cluster(const SortArgs& a, cudaStream_t stream)
+{
+    int dev, clusters;
+    cudaError_t err = current_device(&dev);
+    if (err == cudaSuccess) err = clusters_at_once<ID, K>(dev, a.ctas, &clusters);
+    if (err != cudaSuccess) return err;
+    ClusterConfig c(a.ctas, sort_smem(1 << a.digit_bits), stream);
+    c.cfg.gridDim.x += zero_clusters(a, clusters > 1 ? clusters - 1 : 1) * a.ctas;
+    return cudaLaunchKernelEx(&c.cfg, sort_cluster_kernel<ID, K>, a);
 }
 
 template <typename ID, int K> cudaError_t launch_small(const SortArgs& a, cudaStream_t stream)
 {
     static std::atomic<bool> ready[64];                 // per device (zero-initialised)
     constexpr int kSmem = K * kThreads * (int)sizeof(uint2);
-    int dev = 0;
-    cudaError_t err = cudaGetDevice(&dev);
+    int dev;
+    cudaError_t err = current_device(&dev);
     if (err != cudaSuccess) return err;
-    if (dev < 0 || dev >= 64) return cudaErrorInvalidDevice;
     if (!ready[dev].load(std::memory_order_relaxed)) {
         err = cudaFuncSetAttribute(sort_small_kernel<ID, K>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem);
         if (err != cudaSuccess) return err;
@@ -355,7 +392,7 @@ place_kernel(const PassInput<ID> in, int shift, const uint32_t* __restrict__ cou
 }
 
 // ---- host ----
-constexpr uint32_t kClusterTokens = kMaxCluster * 8 * kThreads, kSmallTokens = 2 * kThreads;
+constexpr uint32_t kTokensPerCta = 8 * kThreads, kSmallTokens = 2 * kThreads;
 
 template <typename ID>
 cudaError_t sort_in_passes(const ID* ids, const SortArgs& s, uint32_t* counts, cudaStream_t stream)
@@ -387,8 +424,11 @@ int token_key_bits(uint32_t rows)
 
 uint64_t token_sort_words(uint64_t tokens)
 {
-    return 2 * tokens + (tokens > kClusterTokens ? (tokens + kTile - 1) / kTile * kBins : 0);
+    // (counts of passes for what a cluster may sort, too: which clusters there are is the device's)
+    return 2 * tokens + (tokens > kSmallTokens ? (tokens + kTile - 1) / kTile * kBins : 0);
 }
+
+void set_token_sort_cluster(unsigned most) { g_most_ctas.store(most, std::memory_order_relaxed); }
 
 // What is set to zero beside the sort, by the SMs that it leaves idle, in about the time it takes: of 50,000 rows of 4 KB, 16,384
 // tokens, 56 MB (49.8 us in all, with 32 MB 51.2, with 80 51.7); of 100,000 rows of 1 KB, 2048 tokens (one CTA sorts), 24.3 us,
@@ -401,7 +441,12 @@ cudaError_t launch_token_sort(const TokenIds& ids, uint32_t rows, uint2* sorted,
     SortArgs a = {ids.ptr, sorted, reinterpret_cast<uint2*>(scratch), counter, (uint32_t)ids.count, rows, token_key_bits(rows), 1, 1,
                   static_cast<char*>(table), 0};
     *zeroed = 0;
-    if (a.tokens > kClusterTokens) {
+    unsigned most_ctas = 1;
+    if (a.tokens > kSmallTokens) {
+        const cudaError_t err = largest_cluster(&most_ctas);
+        if (err != cudaSuccess) return err;
+    }
+    if (a.tokens > (most_ctas == 1 ? kSmallTokens : most_ctas * kTokensPerCta)) {
         uint32_t* counts = scratch + 2 * ids.count;
         return ids.wide ? sort_in_passes(static_cast<const int64_t*>(ids.ptr), a, counts, stream)
                         : sort_in_passes(static_cast<const int32_t*>(ids.ptr), a, counts, stream);
@@ -410,7 +455,7 @@ cudaError_t launch_token_sort(const TokenIds& ids, uint32_t rows, uint2* sorted,
     // launch with four CTAs, 10.5 with two)
     const int passes = (a.bits + kMaxDigitBits - 1) / kMaxDigitBits;
     a.digit_bits = (a.bits + passes - 1) / passes;
-    while (a.tokens > kSmallTokens && a.ctas < kMaxCluster && a.ctas * kThreads < a.tokens) a.ctas *= 2;
+    while (a.tokens > kSmallTokens && a.ctas < most_ctas && a.ctas * kThreads < a.tokens) a.ctas *= 2;
     const uint32_t per_thread = (a.tokens + a.ctas * kThreads - 1) / (a.ctas * kThreads);
     if (table != nullptr) {
         const uint64_t fit = kZeroBesideBytes / row_bytes;

@@ -17,4 +17,7 @@ uint64_t token_sort_words(uint64_t tokens);
 cudaError_t launch_token_sort(const TokenIds& ids, uint32_t rows, uint2* sorted, uint32_t* counter, uint32_t* scratch, void* table,
                               uint64_t row_bytes, uint32_t* zeroed, cudaStream_t stream);
 
+// For tests, process-wide: clusters of at most `most` CTAs, a power of two (1: none) up to 16, which is the default.
+void set_token_sort_cluster(unsigned most);
+
 }  // namespace mqg

@@ -168,6 +168,13 @@ def test_tables_and_rows_lie_apart(lib):
             assert status == mqg.MQG_ERR_CUDA
 
 
+def test_cluster_sizes_of_the_test_hook(lib):
+    for most in (3, 12, 17, 32, 1 << 31):
+        assert lib.mqg_test_sort_cluster(most) == INVALID
+    for most in (16, 8, 4, 2, 1, 0):
+        assert lib.mqg_test_sort_cluster(most) == OK
+
+
 def test_workspace_sizes():
     assert mqg.mqg_norm_workspace_floats(0) == mqg.mqg_norm_workspace_floats(1) == mqg.mqg_norm_workspace_floats(1024)
     assert mqg.mqg_norm_workspace_floats(1025) == 2 * mqg.mqg_norm_workspace_floats(1)

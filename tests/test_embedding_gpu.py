@@ -173,6 +173,29 @@ def test_gradient_of_tables_at_the_digits_edges(rows):
     _check_gradient((rows, 1, 300), "outside", I32, (F32, F32), True)
 
 
+@pytest.mark.parametrize("most_ctas", [8, 4, 2, 1])
+@pytest.mark.parametrize("shape", [(300, 1600, 2049), (500, 800, 4097), (50_000, 3, 8193), (70_001, 5, 16_385), (40_000, 3, 65_537), (300, 7, 131_072),
+                                   (9000, 4, 140_001)])
+def test_gradient_where_the_device_holds_no_large_cluster(shape, most_ctas):
+    """The order of the sums does not depend on how the tokens are sorted: the same bits."""
+    rows, dim, tokens = shape
+    dout = torch.randn(tokens, dim, generator=torch.Generator().manual_seed(4)).cuda()
+    for kind, dtype in (("zipf", I64), ("outside", I32)):
+        ids = _ids(tokens, rows, kind, dtype).cuda()
+        floats = mqg.mqg_embedding_workspace_floats(tokens, rows, dim)
+        got = []
+        for most in (0, most_ctas):
+            grad, work = Buffer(rows * dim, F32), Buffer(floats, F32, values=torch.full((floats,), math.nan))
+            mqg.mqg_test_sort_cluster(most)
+            try:
+                mqg.mqg_embedding_grad(dout, ids, tokens, rows, dim, 0.7, grad.view, work.view)
+            finally:
+                mqg.mqg_test_sort_cluster(0)
+            got.append(grad.cpu())
+            work.check()
+        assert same_bits(*got)
+
+
 @pytest.mark.parametrize("add", [False, True])
 @pytest.mark.parametrize("kind", ["zipf", "uniform", "outside"])
 @pytest.mark.parametrize("tokens", [2047, 2049, 16_385, 65_537, 131_072, 131_073, 150_001])
