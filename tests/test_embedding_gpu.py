@@ -1,10 +1,12 @@
 """Rows of a table looked up for token ids, and the gradient of the table from sorted tokens.
 
 The lookup has one rounding of the product (and one to bf16): compared bit for bit.  The gradient of a row with k tokens is a
-sum in fp32: one after the other, or (some of those with 9 tokens and more, all with 64 and more) sums of at most 32 each, which are
-added up in turn: with at least 8 tokens to each of them but two, no term goes through more than 64 + k / 8 additions, or k in
+sum in fp32: one after the other, or (some of those with 5 tokens and more, all with 64 and more) sums of at most 32 each, which are
+added up in turn.  Each of them but two has 8 tokens at least, or 4 in a CTA of the one-launch form that has up to 256 tokens: no
+term goes through more than 64 + k / 8 additions, or 8 + k / 4 with k up to 256, which is less, or k in
 all where that is less, each off by at most 2^-24 of what it adds to, which is at most the sum of the magnitudes.  Then the product with the scale and, with add_into_grad, the sum with what was there (2^-24 each), and the
-rounding to the output's type (half a step)."""
+rounding to the output's type (half a step).  What these bounds cannot see in long runs, a token that is lost, taken twice or put
+into another row, shows in sums of whole numbers, which are exact."""
 import math
 
 import pytest
@@ -171,6 +173,45 @@ def test_gradient_of_long_and_of_missing_runs(kind, tokens, add):
 def test_gradient_of_tables_at_the_digits_edges(rows):
     _check_gradient((rows, 2, 10_000), "uniform", I64, (F32, F32), False)
     _check_gradient((rows, 1, 300), "outside", I32, (F32, F32), True)
+
+
+def _check_whole_numbers(shape, kind, id_type, types, add, shift=0, seed=0):
+    """Sums of whole numbers that differ from token to token and from column to column: below 2^23 in halves, so that every
+    partial sum, the product with 0.5 and the sum with what was there are exact, and a bf16 result is rounded once."""
+    rows, dim, tokens = shape
+    ids = _ids(tokens, rows, kind, id_type, seed)
+    t, c = torch.arange(tokens)[:, None], torch.arange(dim)[None, :]
+    dout = 1 + (7 * t + 5 * (t // 61) + 3 * c) % 61
+    old = (11 * torch.arange(rows)[:, None] + c) % 201 - 100
+    held = _held(ids, rows)
+    total = torch.zeros(rows, dim, dtype=torch.int64).index_add_(0, ids.long()[held], dout[held])
+    assert int(total.max()) < 2 ** 24 - 512
+    want = (total.double() * 0.5 + (old if add else 0)).to(F32).to(types[1])
+    grad = Buffer(rows * dim, types[1], (3 * shift) % 5, old.to(types[1]).flatten())
+    floats = mqg.mqg_embedding_workspace_floats(tokens, rows, dim)
+    work = Buffer(floats, F32, values=torch.full((floats,), math.nan))
+    mqg.mqg_embedding_grad(Buffer(tokens * dim, types[0], shift, dout.to(types[0]).flatten()).view,
+                           Buffer(tokens, id_type, shift, ids).view, tokens, rows, dim, 0.5, grad.view, work.view, add_into_grad=add)
+    assert same_bits(grad.cpu().view(rows, dim), want)
+    work.check()
+
+
+@pytest.mark.parametrize("add", [False, True])
+@pytest.mark.parametrize("types", [(F32, F32), (F32, BF16), (BF16, F32), (BF16, BF16)])
+@pytest.mark.parametrize("dim", [17, 18, 20, 24])
+@pytest.mark.parametrize("tokens", [5, 33, 250, 257, 2048, 8192, 8193, 16_385, 65_537, 131_073, 150_001])
+def test_every_token_of_long_runs_counts_once(tokens, dim, types, add):
+    for rows, kind in ((40, "same"), (300, "zipf")):
+        _check_whole_numbers((rows, dim, tokens), kind, I64, types, add)
+    _check_whole_numbers((300, dim, tokens), "zipf", I32, types, add, shift=1, seed=1)
+
+
+@pytest.mark.parametrize("add", [False, True])
+@pytest.mark.parametrize("types", [(F32, F32), (BF16, BF16)])
+@pytest.mark.parametrize("shape", [(40, 2055, 2048), (500, 801, 4097), (3, 1536, 2049), (20_000, 3146, 1000), (2000, 515, 10_007)])
+def test_every_token_counts_once_in_wide_rows(shape, types, add):
+    for kind in ("same", "zipf", "ascending"):
+        _check_whole_numbers(shape, kind, I64, types, add)
 
 
 @pytest.mark.parametrize("most_ctas", [8, 4, 2, 1])
