@@ -353,8 +353,8 @@ mqg_status mqg_server_step_segments(const uint32_t* const* codes, const float* c
  *     N = sqrt(sum over all elements of all tensors of x^2)
  *     c = 1 where N <= max_norm, else max_norm / N
  *
- * N is right for every finite gradient (sums in 64 bits beyond a thread's first 32 elements; no square overflows or
- * vanishes) and rounded to fp32 once (infinity above its range), after c was formed; the order of the sums is fixed by
+ * N is right for every finite gradient (at most 33 squares, a thread's share of a 16 KB tile, are summed in fp32, 64 bits from
+ * there on; no square overflows or vanishes) and rounded to fp32 once (infinity above its range), after c was formed; the order of the sums is fixed by
  * the tensors' sizes, types and addresses modulo 16, so N and c are reproducible bit for bit on one device model.  A
  * NaN among the elements makes N and c NaN; an infinity makes N infinite and c zero (where max_norm is infinite too: c
  * = 1).  max_norm may be 0 or infinite, not negative or NaN (MQG_ERR_INVALID).
@@ -371,15 +371,15 @@ mqg_status mqg_grad_norm(const void* const* grads, const uint64_t* sizes, const 
                          float* result, float* workspace, size_t workspace_floats, void* cuda_stream);
 
 /*
- * Measures N and c, and scales every tensor in place: x <- c * x, rounded once to the tensor's type.  Where c is 1 nothing
- * is written.
+ * Measures N and c, and scales every tensor in place: x <- c * x, one rounding to fp32 for the product and, for a bf16 tensor,
+ * one to bf16.  Where c is 1 nothing is written.
  */
 mqg_status mqg_clip_grad_norm(void* const* grads, const uint64_t* sizes, const mqg_dtype* dtypes, int count, float max_norm,
                               float* result, float* workspace, size_t workspace_floats, void* cuda_stream);
 
 /*
  * Measures N and c, and writes c * x of all tensors one after another into `flat` (sum of sizes elements of flat_dtype, each
- * rounded once): the flat gradient that mqg_quantize takes.  The tensors stay as they are; with max_norm infinite it is
+ * rounded as above): the flat gradient that mqg_quantize takes.  The tensors stay as they are; with max_norm infinite it is
  * their concatenation.
  *   flat  [out] needs its type's own alignment (4 or 2 bytes)
  */
@@ -388,7 +388,7 @@ mqg_status mqg_clip_flatten(const void* const* grads, const uint64_t* sizes, con
                             size_t workspace_floats, void* cuda_stream);
 
 /*
- * x <- *factor * x for every tensor of a list, in place, rounded once to its type; where *factor is 1 nothing is written.
+ * x <- *factor * x for every tensor of a list, in place, rounded as above; where *factor is 1 nothing is written.
  * For a factor that comes from elsewhere (the norm of gradients that are spread over several devices), and for clipping a
  * gradient that is encoded already: scaling its `scales` (of mqg_quantize and the L2-norm variant) or `ranges` scales what
  * it decodes to.

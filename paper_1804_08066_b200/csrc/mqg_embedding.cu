@@ -2,8 +2,8 @@
 //
 // Bound by memory: the rows that are used are read, the output is written.  A thread takes words of V elements, 16 bytes of the
 // wider type, so that every access of a warp covers whole sectors, and four of them so that their dependent loads (id, then
-// row) overlap.  (16,384 rows of 1024 from fp32 to bf16: 12.1 us, with eight 13.4, two 14.2; 13.1 with a
-// division for every word, which took three quarters of the issue slots.)
+// row) overlap.  (16,384 rows of 1024 from fp32 to bf16: 12.6 us, with eight 13.7, two 14.8; 13.0 with a division for every
+// word.)
 #include "mqg_tma.cuh"
 #include "mqg_training.h"
 #include "mqg_vector.cuh"

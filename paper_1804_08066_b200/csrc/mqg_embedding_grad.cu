@@ -717,12 +717,12 @@ template <int SRC, int DST> cudaError_t by_group(const GradArgs& a, bool add, cu
 
 namespace {
 
-// One launch instead of four: 2048 tokens, 1000 rows of 64 take 6 us against 12 to 15, 64 tokens 4.7 against 9, 8192 tokens, 1000
-// rows of 256 11 against 18, 4096 tokens, 8000 rows of 515 14 to 16 against 19 to 22.  Not where there is more to add up (4096
-// tokens of 1024 take as long either way, 1024 of 4096 15 us against 13, 8192 of 1024 24 against 20), where there are more
-// columns than SMs for them (every CTA searches), or where the zeros are what takes the time: the CTAs
-// write a piece of a row at a time, single elements where rows start anywhere (30,000 rows of 1024 in bf16, one token: 13 us
-// against 11; of 515: 14 against 8; 100,000 rows of 64 in fp32: 9 against 15).
+// One launch instead of three: 2048 tokens, 1000 rows of 64 take 6 to 7 us against 12 to 16, 64 tokens 5 against 8, 8192 tokens,
+// 1000 rows of 256 11 to 18 against 18 to 19, 4096 tokens, 8000 rows of 515 15 against 18 to 20.  Not where there is more to add up
+// (4096 tokens of 1024 18 us against 17 to 18, 1024 of 4096 15 to 18 against 12 to 16, 8192 of 1024 27 to 30 against 20 to 21),
+// where there are more columns than SMs for them (every CTA searches), or where the zeros are what takes the time: the CTAs
+// write a piece of a row at a time, single elements where rows start anywhere (one token, 30,000 rows of 515 in bf16: 12 us
+// against 8; 30,000 of 1024 11 either way; 100,000 of 64 in fp32 5.6 against 8).
 constexpr uint64_t kSmallElements = 3 << 20;
 
 bool small_shape(SmallArgs& a)
