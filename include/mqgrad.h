@@ -362,7 +362,7 @@ mqg_status mqg_server_step_segments(const uint32_t* const* codes, const float* c
  *   workspace  [scratch] DEVICE memory of at least mqg_norm_workspace_floats(count) floats, 8-byte aligned.  Contents on
  *              entry do not matter and are undefined on return; calls that may run concurrently (graphs captured apart
  *              among them) need separate workspaces.
- * Errors: MQG_ERR_INVALID (null pointers, unknown types, workspace too small), MQG_ERR_ALIGN.
+ * Errors: MQG_ERR_INVALID (null pointers, unknown types, workspace too small, memory shared as above), MQG_ERR_ALIGN.
  */
 size_t mqg_norm_workspace_floats(int count);
 
@@ -412,7 +412,8 @@ typedef enum { MQG_I32 = 0, MQG_I64 = 1 } mqg_index;
  *   table  [in] rows x dim elements, row after row; a slice of the flat parameters, for instance
  *   ids    [in] `tokens` integers;  out [out] tokens x dim elements
  * All buffers need their types' own alignment only; rows whose bytes are a multiple of 16 on 16-byte boundaries are fastest.
- * Errors: MQG_ERR_INVALID (null pointers, unknown types; rows or tokens above 2^31 - 1, dim above 2^22), MQG_ERR_ALIGN.
+ * Errors: MQG_ERR_INVALID (null pointers, unknown types; rows or tokens above 2^31 - 1, dim above 2^22; an output or workspace
+ * that shares memory with another buffer), MQG_ERR_ALIGN.
  */
 mqg_status mqg_embedding(const void* table, mqg_dtype table_dtype, uint64_t rows, uint64_t dim, const void* ids,
                          mqg_index ids_type, uint64_t tokens, float scale, void* out, mqg_dtype out_dtype,

@@ -8,6 +8,10 @@ all where that is less, each off by at most 2^-24 of what it adds to, which is a
 rounding to the output's type (half a step).  What these bounds cannot see in long runs, a token that is lost, taken twice or put
 into another row, shows in sums of whole numbers, which are exact."""
 import math
+import pathlib
+import subprocess
+import sys
+import threading
 
 import pytest
 import torch
@@ -403,3 +407,51 @@ def test_a_table_beyond_32_bit_offsets():
     assert [float(table[r, c]) for r in (rows - 1, 65_536, 0, 1) for c in (0, dim - 1)] == [15, 15, 15, 15, 0, 0, 0, 0]
     mqg.mqg_embedding_grad(out, ids, 6, rows, dim, 1.0, table, w)
     assert [float(table[r, c]) for r in (rows - 1, 65_536, 0, 1) for c in (0, dim - 1)] == [12, 12, 10, 10, 0, 0, 0, 0]
+
+
+FIRST_CALLS = '''
+import torch
+import paper_1804_08066_b200 as mqg
+rows = 500
+for tokens, dim in ((1000, 64), (2000, 1600), (9000, 64), (20_000, 64), (140_000, 64)):
+    ids, d = torch.arange(tokens, device="cuda") * 7 % rows, torch.ones(tokens, dim, device="cuda")
+    g, out = torch.empty(rows, dim, device="cuda"), torch.empty(tokens, dim, device="cuda")
+    w = torch.empty(mqg.mqg_embedding_workspace_floats(tokens, rows, dim), device="cuda")
+    want = torch.bincount(ids, minlength=rows).float()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        mqg.mqg_embedding_grad(d, ids, tokens, rows, dim, 1.0, g, w)
+        mqg.mqg_embedding(g, rows, dim, ids, tokens, 1.0, out)
+    for _ in range(2):
+        g.fill_(float("nan"))
+        graph.replay()
+    assert bool((g == want[:, None]).all()) and bool((out == want[ids][:, None]).all()), tokens
+'''
+
+
+def test_the_first_calls_of_a_process_may_be_captured():
+    subprocess.run([sys.executable, "-c", FIRST_CALLS], check=True, timeout=300, cwd=pathlib.Path(__file__).resolve().parent.parent)
+
+
+def test_gradients_from_several_threads():
+    """Streams and workspaces of their own; the calls run without the interpreter lock."""
+    right = []
+
+    def work(seed):
+        with torch.cuda.stream(torch.cuda.Stream()):
+            for tokens, dim in ((9000, 64), (20_000, 64), (140_000, 16), (2000, 1600), (500, 64)):
+                rows = 500 + seed
+                ids, d = torch.arange(tokens, device="cuda") * 7 % rows, torch.ones(tokens, dim, device="cuda")
+                g = torch.empty(rows, dim, device="cuda")
+                w = torch.empty(mqg.mqg_embedding_workspace_floats(tokens, rows, dim), device="cuda")
+                for _ in range(20):
+                    mqg.mqg_embedding_grad(d, ids, tokens, rows, dim, 1.0, g, w)
+                right.append(bool((g == torch.bincount(ids, minlength=rows)[:, None]).all()))
+
+    threads = [threading.Thread(target=work, args=(k,)) for k in range(4)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert right == [True] * 20
