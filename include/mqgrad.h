@@ -438,6 +438,94 @@ mqg_status mqg_embedding_grad(const void* dout, mqg_dtype dout_dtype, const void
                               float* workspace, size_t workspace_floats, void* cuda_stream);
 
 /*
+ * ---- Beside the codec: AdamW over many tensors, and the layer norm of a model over tokens ----
+ *
+ * AdamW for the server's shared parameters (or a worker's own), in the place of mqg_apply: decay is decoupled, averages are
+ * corrected for their start.  For element x of tensor j, t = step:
+ *     k  = grad_scale * *factor                      g  = k * grad
+ *     m <- b1 m + (1 - b1) g                         v <- b2 v + ((1 - b2) g) g
+ *     p <- p - (lr decay_j p + lr / (1 - b1^t) * (m / (sqrt(v) / sqrt(1 - b2^t) + eps)))
+ * in fp32, every product and sum rounded by itself (m and v are therefore the same bits for whoever follows the formulas; the
+ * root and the quotient are within two units in the last place).  1 - b is formed in 64 bits.  A bf16 parameter is rounded to
+ * nearest: changes below 2^-9 of it are lost, so shared parameters are better held in fp32.
+ *
+ * The lists are HOST arrays of `count` entries, read during the call only: pointers, element counts, types.  A tensor needs its
+ * type's own alignment only; multiples of 4 elements from a 16-byte boundary on are faster.  An empty tensor's pointers are not
+ * looked at, and count may be 0.  params, m, v and scales must not share memory with each other or anything else, within a list or
+ * among them (MQG_ERR_INVALID); tensors of `grads` may.
+ *   params      [in/out] fp32 or bf16;  grads [in] fp32 or bf16, each of its own type
+ *   m, v        [in/out] the two averages; zeros before the first step
+ *   decays      [in] HOST array of `count` floats, or NULL for zeros
+ *   lr >= 0; 0 <= b < 1 (in fp32); eps >= 2^-50; decays >= 0; grad_scale finite (1 / P for the mean of P workers); step >= 1
+ *   factor      [in] NULL, or one float in DEVICE memory: result + 1 of mqg_grad_norm, for instance.  Where it is NaN, infinite or
+ *               0 (a gradient with a NaN or an infinity in it), the call changes nothing.
+ *   schedule    [in] NULL, or 4 floats in DEVICE memory that take the place of lr and step: lr, 1 - b1^t, 1 - b2^t, t (a whole
+ *               number below 2^24).  For calls that are captured into a graph: the other scalars are those of the capture.
+ * Errors: MQG_ERR_INVALID (the above; null pointers, unknown types, 2^42 elements or more), MQG_ERR_ALIGN.
+ */
+mqg_status mqg_adamw(void* const* params, const mqg_dtype* param_dtypes, const void* const* grads, const mqg_dtype* grad_dtypes,
+                     float* const* m, float* const* v, const uint64_t* sizes, const float* decays, int count, double lr,
+                     double beta1, double beta2, double eps, uint32_t step, float grad_scale, const float* factor,
+                     const float* schedule, void* cuda_stream);
+
+/*
+ * The same with m and v in 8 bits each: every block of 256 elements of a tensor, from its first on, has a scale for each.
+ *   m       [in/out] a byte an element, a float of 1 + 4 + 3 bits (e4m3, largest 448): its value is e4m3 * scales[2 b]
+ *   v       [in/out] a byte an element, a float of 1 + 5 + 2 bits (e5m2, largest 57344), never negative: e5m2 * scales[2 b + 1]
+ *   scales  [in/out] HOST array of pointers to mqg_adamw8_scale_floats(size) floats per tensor (two to a block), 4-byte aligned
+ * All three are zeros before the first step.  The parameter's step is computed from m and v before they are rounded.  Then
+ * scales[2 b] = max|m| / 448, scales[2 b + 1] = max v / 57344 of the block (0, and all its codes 0, where that maximum is below
+ * 2^-110), and m * (448 / max|m|), v * (57344 / max v) are rounded to one of their two neighbours at random, up where the share
+ * above the lower neighbour plus (h + 1/2) / 2^16 reaches 1: without bias, while rounding to nearest would not move an average whose
+ * steps are small beside the distance of two codes.  A v above 0 never gets code 0.
+ *   seed    keys the draws: h has 16 bits of the Philox4x32-10 block with key = seed and counter = (q, 0xFFFFFFFF, step).  q = 32 B +
+ *           l, B = blocks before this one in the whole list of the call, draws for the block's elements 4 l .. 4 l + 3 (words 0
+ *           and 1, low half first) and 128 + 4 l .. 128 + 4 l + 3 (words 2 and 3); v takes h with its two bytes swapped.  The
+ *           result is a pure function of the arguments.
+ * Other arguments and errors as mqg_adamw.
+ */
+size_t mqg_adamw8_scale_floats(uint64_t n);
+mqg_status mqg_adamw8(void* const* params, const mqg_dtype* param_dtypes, const void* const* grads, const mqg_dtype* grad_dtypes,
+                      uint8_t* const* m, uint8_t* const* v, float* const* scales, const uint64_t* sizes, const float* decays,
+                      int count, double lr, double beta1, double beta2, double eps, uint32_t step, uint64_t seed,
+                      float grad_scale, const float* factor, const float* schedule, void* cuda_stream);
+
+/*
+ * Layer norm over rows of `dim` elements, each by itself:
+ *     mu = mean(x)    r = 1 / sqrt(mean((x - mu)^2) + eps)    y = (x - mu) * r * weight + bias
+ * in fp32 (a second reading of the row for the squares, no difference of large sums), rounded once to a bf16 `y`.
+ *   x             [in] rows x dim elements, row after row;  y [out] the same, of y_dtype
+ *   weight, bias  [in] dim elements of weight_dtype each; NULL = ones, zeros
+ *   stats         [out] NULL, or 2 floats to a row: mu, r, as the gradient takes them
+ *   eps           above 0.  The rows' deviations and their squares' mean must be in fp32's range.
+ * All buffers need their types' own alignment only; rows whose bytes are a multiple of 16 on 16-byte boundaries are fastest.  What
+ * is written must not share memory with anything else (MQG_ERR_INVALID).  A row without elements, or no rows: nothing is done.
+ * Errors: MQG_ERR_INVALID (null pointers, unknown types, eps; rows above 2^31 - 1, dim above 2^22), MQG_ERR_ALIGN.
+ */
+mqg_status mqg_layer_norm(const void* x, mqg_dtype x_dtype, uint64_t rows, uint64_t dim, const void* weight, const void* bias,
+                          mqg_dtype weight_dtype, float eps, void* y, mqg_dtype y_dtype, float* stats, void* cuda_stream);
+
+/*
+ * Its gradient.  With h = (x - mu) * r and a = weight * dy:
+ *     dx = r * (a - mean(a) - h * mean(a h))    dweight = sum over rows of dy * h    dbias = sum over rows of dy
+ * Sums over rows are formed in fp32 within a part of the rows and in 64 bits over the parts, in an order that rows, dim and the
+ * arguments' types and addresses modulo 16 fix: the result is reproducible bit for bit on one device model.
+ *   dy             [in] rows x dim elements;  x, weight, stats [in] as mqg_layer_norm took and wrote them
+ *   dx             [out] rows x dim elements of x_dtype, or NULL
+ *   dweight, dbias [out] dim elements of dweight_dtype each, or NULL; with add_into_grads the sum over rows is added to what is
+ *                  there (in 64 bits, one rounding), without it `rows` = 0 gives zeros
+ *   workspace      [scratch] DEVICE memory of at least mqg_layer_norm_workspace_floats(rows, dim) floats, 16-byte aligned; may be
+ *                  NULL where dweight and dbias are.  Contents on entry do not matter and are undefined on return; calls that may
+ *                  run concurrently (graphs captured apart among them) need separate workspaces.
+ * Other arguments and errors as mqg_layer_norm.
+ */
+size_t mqg_layer_norm_workspace_floats(uint64_t rows, uint64_t dim);
+mqg_status mqg_layer_norm_grad(const void* dy, mqg_dtype dy_dtype, const void* x, mqg_dtype x_dtype, uint64_t rows, uint64_t dim,
+                               const void* weight, mqg_dtype weight_dtype, const float* stats, void* dx, void* dweight,
+                               void* dbias, mqg_dtype dweight_dtype, int add_into_grads, float* workspace,
+                               size_t workspace_floats, void* cuda_stream);
+
+/*
  * Kernels stage data through shared memory with asynchronous bulk copies and wait for them on
  * barriers with a bounded number of polls; a wait that runs out makes the kernel record it in a
  * per-device counter, abandon its work and return (its outputs are then incomplete) instead of

@@ -16,6 +16,8 @@ Function names and argument order follow the C ABI:
 Around the codec (the global gradient norm, clipping, the table of a model over tokens):
   mqg_norm_workspace_floats, mqg_grad_norm, mqg_clip_grad_norm, mqg_clip_flatten, mqg_scale_grads, mqg_apply_clipped,
   mqg_embedding, mqg_embedding_workspace_floats, mqg_embedding_grad, mqg_test_sort_cluster.
+Beside the codec (AdamW over many tensors, the layer norm of a model over tokens):
+  mqg_adamw, mqg_adamw8, mqg_adamw8_scale_floats, mqg_layer_norm, mqg_layer_norm_grad, mqg_layer_norm_workspace_floats.
 """
 from __future__ import annotations
 
@@ -48,7 +50,7 @@ def _load() -> C.CDLL:
     if not os.path.exists(LIB_PATH):
         raise ImportError(_NOT_BUILT % ("libmqgrad.so", LIB_PATH))
     lib = C.CDLL(LIB_PATH)
-    u64, u32, i32, vp, f32 = C.c_uint64, C.c_uint32, C.c_int, C.c_void_p, C.c_float
+    u64, u32, i32, vp, f32, f64 = C.c_uint64, C.c_uint32, C.c_int, C.c_void_p, C.c_float, C.c_double
     sigs = {
         "mqg_code_words": (C.c_size_t, [u64, i32]),
         "mqg_num_buckets": (C.c_size_t, [u64, u64]),
@@ -88,6 +90,12 @@ def _load() -> C.CDLL:
         "mqg_test_sort_cluster": (i32, [u32]),
         "mqg_embedding_workspace_floats": (C.c_size_t, [u64, u64, u64]),
         "mqg_embedding_grad": (i32, [vp, i32, vp, i32, u64, u64, u64, f32, vp, i32, i32, vp, C.c_size_t, vp]),
+        "mqg_adamw": (i32, [vp, vp, vp, vp, vp, vp, vp, vp, i32, f64, f64, f64, f64, u32, f32, vp, vp, vp]),
+        "mqg_adamw8_scale_floats": (C.c_size_t, [u64]),
+        "mqg_adamw8": (i32, [vp, vp, vp, vp, vp, vp, vp, vp, vp, i32, f64, f64, f64, f64, u32, u64, f32, vp, vp, vp]),
+        "mqg_layer_norm": (i32, [vp, i32, u64, u64, vp, vp, i32, f32, vp, i32, vp, vp]),
+        "mqg_layer_norm_workspace_floats": (C.c_size_t, [u64, u64]),
+        "mqg_layer_norm_grad": (i32, [vp, i32, vp, i32, u64, u64, vp, i32, vp, vp, vp, vp, i32, i32, vp, C.c_size_t, vp]),
     }
     for name, (res, args) in sigs.items():
         fn = getattr(lib, name)
@@ -129,10 +137,10 @@ _NATIVE = frozenset((
     "mqg_quantize_minmax", "mqg_quantize_workers_minmax", "mqg_dequant_accumulate_minmax", "mqg_server_step_minmax",
     "mqg_quantize_l2", "mqg_quantize_workers_l2", "mqg_quantize_segments_l2", "mqg_quantize_segments_l2_static",
     "mqg_quantize_1bit_ef"))
-# those around the codec
+# those around and beside the codec
 _NATIVE_AROUND = frozenset((
     "mqg_grad_norm", "mqg_clip_grad_norm", "mqg_clip_flatten", "mqg_scale_grads", "mqg_apply_clipped", "mqg_embedding",
-    "mqg_embedding_grad"))
+    "mqg_embedding_grad", "mqg_adamw", "mqg_adamw8", "mqg_layer_norm", "mqg_layer_norm_grad"))
 
 
 def _native(name):
@@ -223,6 +231,14 @@ def mqg_norm_workspace_floats(count: int) -> int:
 
 def mqg_embedding_workspace_floats(tokens: int, rows: int, dim: int) -> int:
     return int(_lib.mqg_embedding_workspace_floats(tokens, rows, dim))
+
+
+def mqg_adamw8_scale_floats(n: int) -> int:
+    return int(_lib.mqg_adamw8_scale_floats(n))
+
+
+def mqg_layer_norm_workspace_floats(rows: int, dim: int) -> int:
+    return int(_lib.mqg_layer_norm_workspace_floats(rows, dim))
 
 
 def mqg_test_sort_cluster(most_ctas: int = 0) -> None:

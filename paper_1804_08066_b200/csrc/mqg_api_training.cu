@@ -1,46 +1,15 @@
 // C ABI of the operators around the codec: argument checks and dispatch to the launchers of mqg_training.h.
 #include <cmath>
 
-#include "../../include/mqgrad.h"
-#include "mqg_internal.h"
+#include "mqg_checks.h"
 #include "mqg_token_sort.h"
 #include "mqg_training.h"
 
 namespace {
 
-using mqg::report_error;
+using namespace mqg;
 
 constexpr uint64_t kMaxRows = 0x7FFFFFFF, kMaxDim = 1u << 22;
-
-bool aligned(const void* p, uintptr_t bytes) { return (reinterpret_cast<uintptr_t>(p) & (bytes - 1)) == 0; }
-bool known(mqg_dtype t) { return t == MQG_F32 || t == MQG_BF16; }
-uintptr_t bytes_of(mqg_dtype t) { return t == MQG_F32 ? 4 : 2; }
-uintptr_t bytes_of(mqg_index t) { return t == MQG_I64 ? 8 : 4; }
-
-mqg_status cuda_status(const char* what, cudaError_t err)
-{
-    return err == cudaSuccess ? MQG_OK : report_error(MQG_ERR_CUDA, "%s: %s", what, cudaGetErrorString(err));
-}
-
-// Memory that a call reads or writes; `bytes` = 0: none.
-struct Region {
-    const char* name;
-    const void* p;
-    uint64_t bytes;
-    bool meets(const Region& r) const
-    {
-        const uintptr_t a = reinterpret_cast<uintptr_t>(p), b = reinterpret_cast<uintptr_t>(r.p);
-        return bytes != 0 && r.bytes != 0 && (a < b ? b - a < bytes : a - b < r.bytes);
-    }
-};
-
-// Whether what is written shares memory with anything else: MQG_OK if not.
-template <int N> mqg_status check_apart(const char* what, const Region& written, const Region (&others)[N])
-{
-    for (const Region& r : others)
-        if (written.meets(r)) return report_error(MQG_ERR_INVALID, "%s: %s and %s share memory", what, written.name, r.name);
-    return MQG_OK;
-}
 
 template <int N>
 mqg_status check_list_apart(const char* what, const void* const* grads, const uint64_t* sizes, const mqg_dtype* dtypes, int count,
@@ -115,15 +84,6 @@ mqg_status check_table(const char* what, uint64_t rows, uint64_t dim, uint64_t t
         if (!ids) return report_error(MQG_ERR_INVALID, "%s: ids is null", what);
         if (!aligned(ids, bytes_of(ids_type))) return report_error(MQG_ERR_ALIGN, "%s: ids not aligned", what);
     }
-    return MQG_OK;
-}
-
-mqg_status check_buffer(const char* what, const char* name, const void* p, mqg_dtype t, bool empty)
-{
-    if (!known(t)) return report_error(MQG_ERR_INVALID, "%s: unknown dtype %d of %s", what, (int)t, name);
-    if (empty) return MQG_OK;
-    if (!p) return report_error(MQG_ERR_INVALID, "%s: %s is null", what, name);
-    if (!aligned(p, bytes_of(t))) return report_error(MQG_ERR_ALIGN, "%s: %s is not aligned to its elements", what, name);
     return MQG_OK;
 }
 

@@ -82,6 +82,13 @@ float to_float(PyObject* o)
     if (v == -1.0 && PyErr_Occurred()) throw PythonError();
     return (float)v;
 }
+double to_double(PyObject* o, double absent = 0.0)
+{
+    if (!o) return absent;
+    const double v = PyFloat_AsDouble(o);
+    if (v == -1.0 && PyErr_Occurred()) throw PythonError();
+    return v;
+}
 bool to_bool(PyObject* o)
 {
     if (!o) return false;
@@ -770,6 +777,194 @@ MQG_ENTRY(mqg_embedding_grad, 1, 9, "dout", "ids", "tokens", "rows", "dim", "sca
                                                                      grad, grad_type, add, workspace, floats, s); });
 }
 
+// ---- beside the codec: AdamW over many tensors, and the layer norm of a model over tokens ----
+
+bool absent(PyObject* o) { return !o || o == Py_None; }
+
+// The lists of an AdamW step.  Numbers and iterables, whose conversion may run Python code, are converted before any tensor is
+// looked at; the tensors live as long as this.
+struct AdamwLists {
+    static constexpr int kMost = 5;
+    static constexpr size_t kInline = 64;
+    Reference items[kMost] = {};
+    int nlists = 0;
+    size_t n = 0;
+    std::vector<char> store;
+    char inline_store[kInline * (kMost * sizeof(void*) + sizeof(uint64_t) + 2 * sizeof(mqg_dtype) + sizeof(float))];
+    void** ptr[kMost];
+    uint64_t* size;
+    mqg_dtype* dtype[2];
+    float* decay;
+    bool has_decay = false;
+    Operands on;
+
+    AdamwLists(PyObject* const* lists, int count, PyObject* decays, PyObject* factor, PyObject* schedule) : nlists(count)
+    {
+        for (int k = 0; k < count; ++k) {
+            items[k].object = PySequence_Fast(lists[k], "lists of tensors are expected");
+            if (!items[k].object) throw PythonError();
+        }
+        n = (size_t)PySequence_Fast_GET_SIZE(items[0].object);
+        const Reference numbers = {absent(decays) || PyNumber_Check(decays) ? nullptr : PySequence_Tuple(decays)};
+        const bool one = !absent(decays) && !numbers.object;
+        if (one && PyErr_Occurred()) throw PythonError();
+        const double all = one ? to_double(decays) : 0.0;
+        has_decay = !absent(decays);
+        const size_t per = kMost * sizeof(void*) + sizeof(uint64_t) + 2 * sizeof(mqg_dtype) + sizeof(float);
+        if (n > kInline) store.resize(n * per);
+        char* at = n > kInline ? store.data() : inline_store;
+        for (int k = 0; k < kMost; ++k, at += n * sizeof(void*)) ptr[k] = reinterpret_cast<void**>(at);
+        size = reinterpret_cast<uint64_t*>(at);
+        dtype[0] = reinterpret_cast<mqg_dtype*>(size + n);
+        dtype[1] = dtype[0] + n;
+        decay = reinterpret_cast<float*>(dtype[1] + n);
+        if (numbers.object && (size_t)PyTuple_GET_SIZE(numbers.object) != n) {
+            PyErr_Format(PyExc_ValueError, "decays holds %zd numbers, params %zu tensors", PyTuple_GET_SIZE(numbers.object), n);
+            throw PythonError();
+        }
+        for (size_t j = 0; j < n; ++j) decay[j] = (float)(numbers.object ? to_double(PyTuple_GET_ITEM(numbers.object, j)) : all);
+        // from here on no Python code runs
+        for (int k = 0; k < count; ++k)
+            if ((size_t)PySequence_Fast_GET_SIZE(items[k].object) != n) {
+                PyErr_Format(PyExc_ValueError, "%s holds %zd tensors, params %zu", name(k), PySequence_Fast_GET_SIZE(items[k].object), n);
+                throw PythonError();
+            }
+        for (int k = 0; k < count; ++k)
+            for (size_t j = 0; j < n; ++j) read(k, j, PySequence_Fast_ITEMS(items[k].object)[j]);
+        this->factor = absent(factor) ? nullptr : on.floats(factor, "factor", 1);
+        this->schedule = absent(schedule) ? nullptr : on.floats(schedule, "schedule", 4);
+    }
+    AdamwLists(const AdamwLists&) = delete;
+
+    const float *factor, *schedule;
+
+    static const char* name(int k) { return (const char* const[]){"params", "grads", "m", "v", "scales"}[k]; }
+
+    void read(int k, size_t j, PyObject* o)
+    {
+        if (k < 2) {
+            uint64_t held;
+            ptr[k][j] = on.values(o, name(k), 0, &dtype[k][j], (Py_ssize_t)j, &held);
+            if (k == 0) size[j] = held;
+            check_size(k, j, held);
+            return;
+        }
+        const at::Tensor& t = on.tensor(o, name(k), 0, (Py_ssize_t)j);
+        const at::ScalarType s = t.scalar_type();
+        if (k == 4 || nlists == 4 ? s != at::kFloat : s != at::kByte && s != (k == 2 ? at::kFloat8_e4m3fn : at::kFloat8_e5m2)) {
+            PyErr_Format(PyExc_TypeError, "%s[%zu] must be %s, got %s", name(k), j,
+                         k == 4 || nlists == 4 ? "float32" : k == 2 ? "float8_e4m3fn or uint8" : "float8_e5m2 or uint8", c10::toString(s));
+            throw PythonError();
+        }
+        ptr[k][j] = t.data_ptr();
+        if (k < 4) return check_size(k, j, (uint64_t)t.numel());
+        if ((uint64_t)t.numel() != ::mqg_adamw8_scale_floats(size[j])) {
+            PyErr_Format(PyExc_ValueError, "scales[%zu] holds %lld floats, params[%zu] needs %zu (mqg_adamw8_scale_floats)", j,
+                         (long long)t.numel(), j, ::mqg_adamw8_scale_floats(size[j]));
+            throw PythonError();
+        }
+    }
+    void check_size(int k, size_t j, uint64_t held) const
+    {
+        if (held == size[j]) return;
+        PyErr_Format(PyExc_ValueError, "%s[%zu] holds %llu elements, params[%zu] %llu", name(k), j, (unsigned long long)held, j,
+                     (unsigned long long)size[j]);
+        throw PythonError();
+    }
+    template <typename T> T* const* as(int k) const { return reinterpret_cast<T* const*>(ptr[k]); }
+    const float* decays() const { return has_decay ? decay : nullptr; }
+};
+
+uint32_t to_step(PyObject* o)
+{
+    const uint64_t t = to_u64(o);
+    if (t > 0xFFFFFFFFull) {
+        PyErr_SetString(PyExc_ValueError, "step must be below 2^32");
+        throw PythonError();
+    }
+    return (uint32_t)t;
+}
+
+MQG_ENTRY(mqg_adamw, 3, 13, "params", "grads", "m", "v", "decays", "lr", "beta1", "beta2", "eps", "step", "grad_scale", "factor",
+          "schedule")
+{
+    const double lr = to_double(v[5]), beta1 = to_double(v[6]), beta2 = to_double(v[7]), eps = to_double(v[8]);
+    const uint32_t step = to_step(v[9]);
+    const float grad_scale = (float)to_double(v[10], 1.0);
+    const AdamwLists a(v, 4, v[4], v[11], v[12]);
+    return enqueue_on(a.on, [&](void* s) { return ::mqg_adamw(a.as<void>(0), a.dtype[0], a.as<const void>(1), a.dtype[1], a.as<float>(2),
+                                                              a.as<float>(3), a.size, a.decays(), (int)a.n, lr, beta1, beta2, eps, step,
+                                                              grad_scale, a.factor, a.schedule, s); });
+}
+
+MQG_ENTRY(mqg_adamw8, 3, 15, "params", "grads", "m", "v", "scales", "decays", "lr", "beta1", "beta2", "eps", "step", "seed",
+          "grad_scale", "factor", "schedule")
+{
+    const double lr = to_double(v[6]), beta1 = to_double(v[7]), beta2 = to_double(v[8]), eps = to_double(v[9]);
+    const uint32_t step = to_step(v[10]);
+    const uint64_t seed = to_u64(v[11]);
+    const float grad_scale = (float)to_double(v[12], 1.0);
+    const AdamwLists a(v, 5, v[5], v[13], v[14]);
+    return enqueue_on(a.on, [&](void* s) { return ::mqg_adamw8(a.as<void>(0), a.dtype[0], a.as<const void>(1), a.dtype[1],
+                                                               a.as<uint8_t>(2), a.as<uint8_t>(3), a.as<float>(4), a.size, a.decays(),
+                                                               (int)a.n, lr, beta1, beta2, eps, step, seed, grad_scale, a.factor,
+                                                               a.schedule, s); });
+}
+
+// `weight` and `bias` (or `dweight` and `dbias`): either may be None; both have one type.
+struct Pair {
+    void* ptr[2] = {nullptr, nullptr};
+    mqg_dtype dtype = MQG_F32;
+    Pair(PyObject* a, const char* a_name, PyObject* b, const char* b_name, uint64_t dim, Operands& on)
+    {
+        mqg_dtype types[2];
+        if (!absent(a)) ptr[0] = on.values(a, a_name, dim, &types[0]);
+        if (!absent(b)) ptr[1] = on.values(b, b_name, dim, &types[1]);
+        if (ptr[0] || ptr[1]) dtype = types[ptr[0] ? 0 : 1];
+        if (!absent(a) && !absent(b) && types[0] != types[1]) {
+            PyErr_Format(PyExc_TypeError, "%s and %s must be of one type", a_name, b_name);
+            throw PythonError();
+        }
+    }
+};
+
+MQG_ENTRY(mqg_layer_norm, 1, 8, "x", "rows", "dim", "weight", "bias", "eps", "y", "stats")
+{
+    Operands on;
+    const uint64_t rows = to_u64(v[1]), dim = to_u64(v[2]);
+    const float eps = to_float(v[5]);
+    mqg_dtype x_type, y_type;
+    const void* x = on.values(v[0], "x", area(rows, dim), &x_type);
+    const Pair w(v[3], "weight", v[4], "bias", dim, on);
+    void* y = on.values(v[6], "y", area(rows, dim), &y_type);
+    float* stats = absent(v[7]) ? nullptr : on.floats(v[7], "stats", area(rows, 2));
+    return enqueue_on(on, [&](void* s) { return ::mqg_layer_norm(x, x_type, rows, dim, w.ptr[0], w.ptr[1], w.dtype, eps, y, y_type,
+                                                                 stats, s); });
+}
+
+MQG_ENTRY(mqg_layer_norm_grad, 1, 11, "dy", "x", "rows", "dim", "weight", "stats", "dx", "dweight", "dbias", "workspace",
+          "add_into_grads")
+{
+    Operands on;
+    const uint64_t rows = to_u64(v[2]), dim = to_u64(v[3]);
+    const int add = to_bool(v[10]) ? 1 : 0;
+    mqg_dtype dy_type, x_type, dx_type, w_type = MQG_F32;
+    uint64_t floats = 0;
+    const void* dy = on.values(v[0], "dy", area(rows, dim), &dy_type);
+    const void* x = on.values(v[1], "x", area(rows, dim), &x_type);
+    const void* weight = absent(v[4]) ? nullptr : on.values(v[4], "weight", dim, &w_type);
+    const float* stats = on.floats(v[5], "stats", area(rows, 2));
+    void* dx = absent(v[6]) ? nullptr : on.values(v[6], "dx", area(rows, dim), &dx_type);
+    if (dx && dx_type != x_type) {
+        PyErr_SetString(PyExc_TypeError, "dx and x must be of one type");
+        return nullptr;
+    }
+    const Pair d(v[7], "dweight", v[8], "dbias", dim, on);
+    float* workspace = absent(v[9]) ? nullptr : on.floats(v[9], "workspace", 0, &floats);
+    return enqueue_on(on, [&](void* s) { return ::mqg_layer_norm_grad(dy, dy_type, x, x_type, rows, dim, weight, w_type, stats, dx,
+                                                                      d.ptr[0], d.ptr[1], d.dtype, add, workspace, floats, s); });
+}
+
 PyObject* set_error_class(PyObject*, PyObject* cls)
 {
     Py_XSETREF(g_error_class, Py_NewRef(cls));
@@ -840,6 +1035,20 @@ PyMethodDef kMethods[] = {
                "(dout, ids, tokens, rows, dim, scale, grad, workspace, add_into_grad=False)",
                "The gradient of mqg_embedding's table, written to `grad` or added to it; `workspace`: float32 CUDA tensor\n"
                "of at least mqg_embedding_workspace_floats(tokens, rows, dim) elements."),
+    MQG_METHOD(mqg_adamw,
+               "(params, grads, m, v, decays, lr, beta1, beta2, eps, step, grad_scale=1.0, factor=None, schedule=None)",
+               "One step of AdamW over lists of tensors, in place; m and v are float32.  `decays`: None, a number, or one for\n"
+               "each tensor; `factor` and `schedule`: float32 on the device (1 and 4 elements)."),
+    MQG_METHOD(mqg_adamw8,
+               "(params, grads, m, v, scales, decays, lr, beta1, beta2, eps, step, seed, grad_scale=1.0, factor=None, "
+               "schedule=None)",
+               "mqg_adamw with m (float8_e4m3fn or uint8) and v (float8_e5m2 or uint8) in 8 bits; `scales`: float32 tensors\n"
+               "of mqg_adamw8_scale_floats(numel) elements."),
+    MQG_METHOD(mqg_layer_norm, "(x, rows, dim, weight, bias, eps, y, stats=None)",
+               "Layer norm of rows; `stats` (float32, rows x 2) takes their means and reciprocal deviations."),
+    MQG_METHOD(mqg_layer_norm_grad, "(dy, x, rows, dim, weight, stats, dx, dweight, dbias, workspace, add_into_grads=False)",
+               "The gradients of mqg_layer_norm (each of dx, dweight, dbias may be None); `workspace`: float32 CUDA tensor of at\n"
+               "least mqg_layer_norm_workspace_floats(rows, dim) elements."),
     {"_set_error_class", set_error_class, METH_O, nullptr},
     {nullptr, nullptr, 0, nullptr},
 };
@@ -852,6 +1061,7 @@ Signature* const kSignatures[] = {
     &sig_mqg_quantize_1bit_ef, &sig_mqg_quantize_l2, &sig_mqg_quantize_segments_l2,
     &sig_mqg_quantize_segments_l2_static, &sig_mqg_grad_norm, &sig_mqg_clip_grad_norm, &sig_mqg_clip_flatten,
     &sig_mqg_scale_grads, &sig_mqg_apply_clipped, &sig_mqg_embedding, &sig_mqg_embedding_grad,
+    &sig_mqg_adamw, &sig_mqg_adamw8, &sig_mqg_layer_norm, &sig_mqg_layer_norm_grad,
 };
 
 PyModuleDef kModule = {PyModuleDef_HEAD_INIT, "_binding", "Native entry points of libmqgrad.", -1, kMethods,

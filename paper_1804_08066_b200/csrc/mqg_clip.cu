@@ -15,6 +15,7 @@
 #include <atomic>
 #include <cmath>
 
+#include "mqg_list.cuh"
 #include "mqg_tma.cuh"
 #include "mqg_training.h"
 #include "mqg_vector.cuh"
@@ -50,21 +51,10 @@ struct Tile {
     int dtype;
 };
 
-// The tensor that a tile is in: the last one that starts at or before it.  All lanes of a warp look at once, at every k-th tensor
-// and then at k neighbours, with ordinary loads: a search by halves is ten dependent misses of the constant cache, which a
-// launch begins without its parameters.
+// The tensor that a tile is in.
 template <int CAP> __device__ __forceinline__ int find_tensor(const TensorTable<CAP>& tab, uint32_t tile)
 {
-    const uint32_t* start = tab.tile_start;
-    asm volatile("" : "+l"(start));                     // an address like any other
-    const int lane = threadIdx.x & 31, k = (tab.count + 31) / 32;
-    int base = 0;
-    if (CAP > 32 && k > 1) {
-        const uint32_t first = lane * k < tab.count ? start[lane * k] : ~0u;
-        base = (31 - __clz(__ballot_sync(0xFFFFFFFFu, first <= tile))) * k;
-    }
-    const uint32_t first = lane < k * (k == 1 ? 32 : 1) && base + lane < tab.count ? start[base + lane] : ~0u;
-    return base + 31 - __clz(__ballot_sync(0xFFFFFFFFu, first <= tile));
+    return find_in_list<(CAP > 32)>(tab.tile_start, tab.count, tile);
 }
 
 template <int CAP> __device__ __forceinline__ Tile tile_of(const TensorTable<CAP>& tab, int tensor, uint32_t tile)

@@ -1,0 +1,107 @@
+"""AdamW written from its formulas with numpy: in 64 bits, and in fp32 with one rounding for every operation (what m, v and the codes
+of states in 8 bits are defined by).  Shares no code with the library."""
+import numpy as np
+
+BLOCK = 256
+f32 = np.float32
+TOP_M, TOP_V, LEAST = f32(448.0), f32(57344.0), f32(2.0 ** -110)
+
+
+def step64(p, g, m, v, *, lr, beta1, beta2, eps, step, decay, k=1.0):
+    """p', m', v' in 64 bits, and how far fp32 may be from p' (all arguments exact in 64 bits)."""
+    p, g, m, v = (np.asarray(a, np.float64) for a in (p, g, m, v))
+    g = k * g
+    m2, v2 = beta1 * m + (1 - beta1) * g, beta2 * v + (1 - beta2) * g * g
+    d = np.sqrt(v2) / np.sqrt(1 - beta2 ** step) + eps
+    a = lr / (1 - beta1 ** step)
+    p2 = p - (lr * decay * p + a * m2 / d)
+    # Roundings of 2^-24 each.  m': 3 and those of b1, w1 and k g, of the parts that may cancel.  d: v' 5 and b2, w2, k g twice, halved
+    # by the root; the root 2, r2 3, the product, eps and the sum: 13.  Quotient 2, a 3, product 1: 24 of the whole term.  rate p: 3,
+    # the sum 1; the difference 1 of p'.
+    term = a * (np.abs(beta1 * m) + np.abs((1 - beta1) * g)) / d
+    slack = 2.0 ** -24 * (np.abs(p2) + 5 * np.abs(lr * decay * p) + 26 * term) + 1e-44
+    return p2, m2, v2, slack
+
+
+def moments32(g, m, v, *, beta1, beta2, k=1.0):
+    """m', v' rounded operation by operation."""
+    g = f32(k) * np.asarray(g, f32)
+    m2 = f32(beta1) * m + f32(1 - beta1) * g
+    v2 = f32(beta2) * v + (f32(1 - beta2) * g) * g
+    assert m2.dtype == v2.dtype == f32
+    return m2, v2
+
+
+def philox(counter, key):
+    """Philox4x32-10 of Python integers: four words."""
+    c, k = list(counter), list(key)
+    for _ in range(10):
+        p0, p1 = 0xD2511F53 * c[0], 0xCD9E8D57 * c[2]
+        c = [(p1 >> 32) ^ c[1] ^ k[0], p1 & 0xFFFFFFFF, (p0 >> 32) ^ c[3] ^ k[1], p0 & 0xFFFFFFFF]
+        k = [(k[0] + 0x9E3779B9) & 0xFFFFFFFF, (k[1] + 0xBB67AE85) & 0xFFFFFFFF]
+    return c
+
+
+def draws(block, seed, step):
+    """The 16-bit draws of block number `block`'s elements."""
+    h = np.zeros(BLOCK, np.uint32)
+    for lane in range(32):
+        q = 32 * block + lane
+        words = philox([q & 0xFFFFFFFF, q >> 32, 0xFFFFFFFF, step], [seed & 0xFFFFFFFF, seed >> 32 & 0xFFFFFFFF])
+        for s in range(8):
+            h[(s // 4) * 128 + 4 * lane + s % 4] = words[s // 2] >> 16 * (s % 2) & 0xFFFF
+    return h
+
+
+def values_of(fraction_bits, exponent_bits):
+    """The values of the codes 0 .. 2^(bits) - 1 of a float without sign."""
+    bias = 2 ** (exponent_bits - 1) - 1
+    out = []
+    for code in range(2 ** (fraction_bits + exponent_bits)):
+        e, f = code >> fraction_bits, code % 2 ** fraction_bits
+        out.append((f if e == 0 else f + 2 ** fraction_bits) * 2.0 ** (max(e, 1) - bias - fraction_bits))
+    return np.array(out)
+
+
+E4M3, E5M2 = values_of(3, 4)[:0x7F], values_of(2, 5)[:0x7C]
+
+
+def decode(codes, table, scale):
+    """fp32 values of codes with (for e4m3) a sign."""
+    sign = np.where(codes & 0x80, f32(-1), f32(1))
+    return sign * table.astype(f32)[codes & 0x7F] * f32(scale)
+
+
+def pack(x, top, table, h):
+    """Scale and codes of a block's magnitudes: the lower neighbour's code, and one more where what is above it asks for it."""
+    most = x.max()
+    if not most >= LEAST:
+        return f32(0), np.zeros(x.size, np.uint8)
+    y = (x * (top / most)).astype(np.float64)
+    low = np.searchsorted(table, y, side="right") - 1
+    low = np.minimum(low, table.size - 2)
+    share = (y - table[low]) / (table[low + 1] - table[low])
+    return most / top, (low + (share + (h + 0.5) / 65536 >= 1)).astype(np.uint8)
+
+
+def swapped(h):
+    return (h & 0xFF) << 8 | h >> 8
+
+
+def step8(p, g, m, v, scales, first_block, *, seed, step, beta1, beta2, k=1.0, **rest):
+    """A tensor's step with states in 8 bits: p' and its slack as step64, codes of m and v, scales [blocks, 2]."""
+    n = len(g)
+    m2c, v2c, s2 = np.zeros(n, np.uint8), np.zeros(n, np.uint8), np.zeros_like(scales)
+    wide_m, wide_v = np.zeros(n, f32), np.zeros(n, f32)
+    for b in range(-(-n // BLOCK)):
+        at = slice(b * BLOCK, min(n, (b + 1) * BLOCK))
+        wide_m[at], wide_v[at] = decode(m[at], E4M3, scales[b, 0]), decode(v[at], E5M2, scales[b, 1])
+        m2, v2 = moments32(g[at], wide_m[at], wide_v[at], beta1=beta1, beta2=beta2, k=k)
+        h = draws(first_block + b, seed, step)[:m2.size]
+        s2[b, 0], codes = pack(np.abs(m2), TOP_M, E4M3, h)
+        m2c[at] = codes | np.where(m2 < 0, 0x80, 0).astype(np.uint8)
+        s2[b, 1], codes = pack(v2, TOP_V, E5M2, swapped(h))
+        above = (v2 > 0) & (v2.max() >= LEAST)
+        v2c[at] = np.where((codes == 0) & above, 1, codes)
+    p2, _, _, slack = step64(p, g, wide_m, wide_v, beta1=beta1, beta2=beta2, step=step, k=k, **rest)
+    return p2, slack, m2c, v2c, s2
