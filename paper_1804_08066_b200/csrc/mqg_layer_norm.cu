@@ -22,73 +22,124 @@ struct NormArgs {
     int w_dtype;
 };
 
-constexpr int kThreads = 256;                           // of a CTA with a row to at most a warp
-constexpr int kMostThreads = 512;                       // of one with a row to the CTA
+// Rows on their way to shared memory, each thread's own elements.
+template <int X, int V, int E> struct Ring {
+    static constexpr bool kAsync = V * kElemBytes<X> >= 4;
+    static constexpr int kStages = !kAsync ? 1 : E > 16 ? 2 : E * kElemBytes<X> <= 16 ? 6 : E * kElemBytes<X> <= 32 ? 5 : 3;
+    Packed<X, V> x[kStages][E / V][kRowThreads];
+};
 
-// Sum over the threads that have a row: `lanes` neighbours, or (WIDE) all of a CTA, the `turn`-th of a row.
-template <bool WIDE> __device__ __forceinline__ float row_sum(float v, uint32_t lanes, int turn)
-{
-    v = lanes_sum(v, WIDE ? 32 : lanes);
-    if (WIDE) {
-        __shared__ float warp_sum[2][kMostThreads / 32];
-        if ((threadIdx.x & 31) == 0) warp_sum[turn][threadIdx.x >> 5] = v;
-        __syncthreads();
-        const uint32_t lane = threadIdx.x & 31;
-        v = lanes_sum(lane < blockDim.x / 32 ? warp_sum[turn][lane] : 0.0f, 32);
-    }
-    return v;
-}
+template <int E> constexpr int kResident = E <= 8 ? 2 : 1;
 
-// K vectors of V elements to a thread.  WIDE: a CTA to a row, else `lanes` neighbouring lanes, a power of two.
-template <int X, int Y, int V, int K, bool WIDE>
-__global__ void __launch_bounds__(WIDE ? kMostThreads : kThreads) norm_kernel(const NormArgs a, uint32_t lanes)
+// E elements to a thread, V to a vector.
+template <int X, int Y, int V, int E>
+__global__ void __launch_bounds__(kRowThreads, kResident<E>) norm_rows_kernel(const NormArgs a, uint32_t threads)
 {
-    const uint32_t threads = WIDE ? blockDim.x : lanes, place = WIDE ? threadIdx.x : threadIdx.x & (lanes - 1);
-    const uint64_t row = WIDE ? blockIdx.x : ((uint64_t)blockIdx.x * kThreads + threadIdx.x) / lanes;
-    const uint32_t vectors = row < a.rows ? (uint32_t)(a.dim / V) : 0;
+    using R = Ring<X, V, E>;
+    constexpr int K = E / V;
+    extern __shared__ __align__(16) unsigned char memory[];
+    auto& ring = *reinterpret_cast<R*>(memory);
+    __shared__ RowSums sums;
+    const uint32_t place = threadIdx.x % threads, group = threadIdx.x / threads, groups = blockDim.x / threads;
+    const uint32_t vectors = (uint32_t)(a.dim / V);
+    const uint64_t stride = (uint64_t)gridDim.x * groups;
+    const float per_element = __fdiv_rn(1.0f, (float)a.dim);
     grid_dependency_wait();
-    const auto* x = static_cast<const typename Element<X>::type*>(a.x) + row * a.dim;
-    float v[K][V];
-    float sum = 0.0f;
-    Packed<X, V> in[K];
+    const auto* x = static_cast<const typename Element<X>::type*>(a.x);
+    auto* y = static_cast<typename Element<Y>::type*>(a.y);
+    const auto has_vector = [&](int k) { return place + k * threads < vectors; };
+    const auto fetch = [&](uint64_t row, int slot) {
+        if (row < a.rows)
 #pragma unroll
-    for (int k = 0; k < K; ++k)
-        if (place + k * threads < vectors) in[k].load(x + (place + k * threads) * V);
+            for (int k = 0; k < K; ++k)
+                if (has_vector(k)) copy_async<V * kElemBytes<X>>(&ring.x[slot][k][threadIdx.x], x + row * a.dim + (place + k * threads) * V);
+        commit_copies();
+    };
+    float w[E], b[E];
 #pragma unroll
     for (int k = 0; k < K; ++k) {
-        const bool has = place + k * threads < vectors;
+        float wk[V], bk[V];
 #pragma unroll
-        for (int e = 0; e < V; ++e) {
-            v[k][e] = has ? in[k].get(e) : 0.0f;
-            sum += v[k][e];
+        for (int e = 0; e < V; ++e) wk[e] = bk[e] = 0.0f;
+        if (has_vector(k)) {
+            weights_at<V>(a.weight, a.w_dtype, (place + k * threads) * V, 1.0f, wk);
+            weights_at<V>(a.bias, a.w_dtype, (place + k * threads) * V, 0.0f, bk);
         }
+#pragma unroll
+        for (int e = 0; e < V; ++e) { w[k * V + e] = wk[e]; b[k * V + e] = bk[e]; }
     }
-    const float n = (float)a.dim, mean = __fdiv_rn(row_sum<WIDE>(sum, lanes, 0), n);
-    float squares = 0.0f;
+    if constexpr (R::kAsync) {
+        // places without elements hold zeros, which no copy overwrites
 #pragma unroll
-    for (int k = 0; k < K; ++k) {
-        if (place + k * threads >= vectors) continue;
+        for (int s = 0; s < R::kStages; ++s)
 #pragma unroll
-        for (int e = 0; e < V; ++e) {
-            v[k][e] -= mean;
-            squares = fmaf(v[k][e], v[k][e], squares);
+            for (int k = 0; k < K; ++k)
+                if (!has_vector(k))
+#pragma unroll
+                    for (int e = 0; e < V; ++e) ring.x[s][k][threadIdx.x].set(e, 0.0f);
+#pragma unroll
+        for (int s = 0; s < R::kStages - 1; ++s) fetch((uint64_t)blockIdx.x * groups + group + s * stride, s);
+    }
+    int slot = 0;
+    for (uint64_t base = (uint64_t)blockIdx.x * groups; base < a.rows; base += stride) {
+        const uint64_t row = base + group;
+        const bool has = row < a.rows;
+        float v[E];
+        if constexpr (R::kAsync) {
+            fetch(row + (R::kStages - 1) * stride, slot == 0 ? R::kStages - 1 : slot - 1);
+            wait_copies<R::kStages - 1>();
+#pragma unroll
+            for (int k = 0; k < K; ++k) widen_to<X, V>(ring.x[slot][k][threadIdx.x], v + k * V);
+            slot = slot == R::kStages - 1 ? 0 : slot + 1;
+        } else {
+#pragma unroll
+            for (int k = 0; k < K; ++k) {
+                Packed<X, V> in;
+#pragma unroll
+                for (int e = 0; e < V; ++e) in.set(e, 0.0f);
+                if (has && has_vector(k)) in.load(x + row * a.dim + (place + k * threads) * V);
+                widen_to<X, V>(in, v + k * V);
+            }
         }
-    }
-    const float rstd = reciprocal_deviation(__fdiv_rn(row_sum<WIDE>(squares, lanes, 1), n), a.eps);
-    if (row >= a.rows) return;
-    if (place == 0 && a.stats != nullptr) { a.stats[2 * row] = mean; a.stats[2 * row + 1] = rstd; }
-    auto* y = static_cast<typename Element<Y>::type*>(a.y) + row * a.dim;
+        float2 sum = make_float2(0.0f, 0.0f);
 #pragma unroll
-    for (int k = 0; k < K; ++k) {
-        const uint32_t i = (place + k * threads) * V;
-        if (place + k * threads >= vectors) continue;
-        float w[V], b[V];
-        weights_at<V>(a.weight, a.w_dtype, i, 1.0f, w);
-        weights_at<V>(a.bias, a.w_dtype, i, 0.0f, b);
-        Packed<Y, V> out;
+        for (int e = 0; e < E; e += 2) sum = __fadd2_rn(sum, make_float2(v[e], v[e + 1]));
+        const float mean = sums.one(sum.x + sum.y, threads, group, 0) * per_element;
+        float2 squares = make_float2(0.0f, 0.0f);
+        const float2 minus = make_float2(-mean, -mean);
 #pragma unroll
-        for (int e = 0; e < V; ++e) out.set(e, fmaf(v[k][e] * rstd, w[e], b[e]));
-        out.store(y + i);
+        for (int e = 0; e < E; e += 2) {
+            const float2 d = __fadd2_rn(make_float2(v[e], v[e + 1]), minus);
+            v[e] = d.x;
+            v[e + 1] = d.y;
+            if constexpr (V > 1) {
+                if (has_vector(e / V)) squares = __ffma2_rn(d, d, squares);
+            } else {
+                squares.x = has_vector(e) ? fmaf(d.x, d.x, squares.x) : squares.x;
+                squares.y = has_vector(e + 1) ? fmaf(d.y, d.y, squares.y) : squares.y;
+            }
+        }
+        const float rstd = reciprocal_deviation(sums.one(squares.x + squares.y, threads, group, 1) * per_element, a.eps);
+        if (!has) continue;
+        if (place == 0 && a.stats != nullptr) { a.stats[2 * row] = mean; a.stats[2 * row + 1] = rstd; }
+#pragma unroll
+        for (int k = 0; k < K; ++k) {
+            if (!has_vector(k)) continue;
+            Packed<Y, V> out;
+            if constexpr (V > 1) {
+#pragma unroll
+                for (int e = 0; e < V; e += 2) {
+                    const int i = k * V + e;
+                    const float2 h = __fmul2_rn(make_float2(v[i], v[i + 1]), make_float2(rstd, rstd));
+                    const float2 r = __ffma2_rn(h, make_float2(w[i], w[i + 1]), make_float2(b[i], b[i + 1]));
+                    out.set(e, r.x);
+                    out.set(e + 1, r.y);
+                }
+            } else {
+                out.set(0, fmaf(v[k] * rstd, w[k], b[k]));
+            }
+            out.store(y + row * a.dim + (place + k * threads) * V);
+        }
     }
 }
 
@@ -117,26 +168,25 @@ template <int X, int Y> __global__ void __launch_bounds__(kLongThreads) norm_lon
 
 template <int X, int Y, int V, int E> cudaError_t launch_elements(const NormArgs& a, cudaStream_t stream)
 {
-    constexpr int K = E / V;
-    const uint32_t threads = (uint32_t)((a.dim + E - 1) / E);
-    if (threads > 32)
-        return launch_pdl(norm_kernel<X, Y, V, K, true>, (unsigned)a.rows, (threads + 31) / 32 * 32, stream, a, 32u);
-    uint32_t lanes = 1;
-    while (lanes < threads) lanes *= 2;
-    const uint64_t per_cta = kThreads / lanes;
-    return launch_pdl(norm_kernel<X, Y, V, K, false>, (unsigned)((a.rows + per_cta - 1) / per_cta), kThreads, stream, a, lanes);
+    using R = Ring<X, V, E>;
+    static std::atomic<bool> ready[64];
+    const auto kernel = norm_rows_kernel<X, Y, V, E>;
+    constexpr size_t kBytes = R::kAsync ? sizeof(R) : 0;
+    if (const cudaError_t err = allow_shared(kernel, kBytes, ready)) return err;
+    const RowGroups g = row_groups(a.rows, a.dim, E, kResident<E> * kRowThreads);
+    return launch_pdl_smem(kernel, g.ctas, g.block, kBytes, stream, a, g.threads);
 }
 
 template <int X, int Y, int V> cudaError_t launch_vectors(const NormArgs& a, cudaStream_t stream)
 {
-    // 32 elements to a thread where there are rows for all threads, 8 where there are not, or the row is short
-    if (a.dim <= 8 * 32 || (a.dim <= 8 * kMostThreads && a.rows * a.dim <= 148ull * 2048 * 8)) return launch_elements<X, Y, V, 8>(a, stream);
-    return launch_elements<X, Y, V, 32>(a, stream);
+    return a.dim <= 8 * kRowThreads    ? launch_elements<X, Y, V, 8>(a, stream)
+           : a.dim <= 16 * kRowThreads ? launch_elements<X, Y, V, 16>(a, stream)
+                                       : launch_elements<X, Y, V, 32>(a, stream);
 }
 
 template <int X, int Y> cudaError_t launch(const NormArgs& a, cudaStream_t stream)
 {
-    if (a.dim > 32 * kMostThreads) return launch_pdl(norm_long_kernel<X, Y>, (unsigned)a.rows, kLongThreads, stream, a);
+    if (a.dim > 32 * kRowThreads) return launch_pdl(norm_long_kernel<X, Y>, (unsigned)a.rows, kLongThreads, stream, a);
     constexpr int V = kVector<X, Y>;
     const int w = element_bytes(a.w_dtype);
     const bool fit = vectors_fit(a.x, kElemBytes<X>, V, a.dim) && vectors_fit(a.y, kElemBytes<Y>, V, a.dim) &&

@@ -6,8 +6,6 @@
 // sums over the rows stay in its registers until the CTA's last row; the CTAs' sums are added up by a second launch.  Rows come by
 // asynchronous copies, a few ahead, each thread its own elements: the copies that are on their way take no registers, and no
 // thread waits for another's.
-#include <atomic>
-
 #include "mqg_norm_rows.cuh"
 #include "mqg_tma.cuh"
 #include "mqg_training.h"
@@ -27,160 +25,176 @@ struct GradArgs {
     int w_dtype;
 };
 
-constexpr int kThreads = 512, kCtas = 148 * 2;
-constexpr int kMostElements = 8;                        // of a row to a thread
-
-template <int BYTES> __device__ __forceinline__ void copy_async(void* to, const void* from)
-{
-    const uint32_t at = (uint32_t)__cvta_generic_to_shared(to);
-    if (BYTES == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(at), "l"(from) : "memory");
-    else asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" ::"r"(at), "l"(from), "n"(BYTES) : "memory");
-}
-__device__ __forceinline__ void commit_copies() { asm volatile("cp.async.commit_group;" ::: "memory"); }
-template <int N> __device__ __forceinline__ void wait_copies() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
-
-// One thread's elements of a row: K vectors of V, `threads` vectors apart.
-template <int X, int Y, int V, int K> struct Shares {
+// Rows on their way to shared memory: each thread's own elements, and the rows' stats, which the first thread of a group copies
+// for those of its warp.
+template <int X, int Y, int V, int E> struct Ring {
     static constexpr bool kAsync = V * kElemBytes<X> >= 4 && V * kElemBytes<Y> >= 4;
-    static constexpr int kStages = kAsync ? (kElemBytes<X> + kElemBytes<Y> == 8 ? 3 : 4) : 1;
-    struct Stage {
-        Packed<X, V> x[K][kThreads];
-        Packed<Y, V> dy[K][kThreads];
-    };
+    static constexpr int kBytes = E * (kElemBytes<X> + kElemBytes<Y>);
+    static constexpr int kStages = !kAsync ? 1 : kBytes <= 32 ? 5 : kBytes <= 48 ? 4 : kBytes <= 64 && E > 8 ? 5 : 3;
+    Packed<X, V> x[kStages][E / V][kRowThreads];
+    Packed<Y, V> dy[kStages][E / V][kRowThreads];
+    float2 stats[kStages][kRowThreads];
 };
 
-// Sums of two values over the `threads` threads that have a row; `group` numbers these groups of a CTA.
-struct RowSums {
-    float2 of_warp[2][kThreads / 32];
-    __device__ __forceinline__ float2 add(float2 v, uint32_t threads, uint32_t group, int turn)
-    {
-        v.x = lanes_sum(v.x, threads);
-        v.y = lanes_sum(v.y, threads);
-        if (threads <= 32) return v;
-        const uint32_t warps = threads / 32, lane = threadIdx.x & 31;
-        if (lane == 0) of_warp[turn][threadIdx.x >> 5] = v;
-        asm volatile("bar.sync %0, %1;" ::"r"(group + 1), "r"(threads) : "memory");
-        v = lane < warps ? of_warp[turn][group * warps + lane] : make_float2(0.0f, 0.0f);
-        return make_float2(lanes_sum(v.x, 32), lanes_sum(v.y, 32));
-    }
-};
+template <int E> constexpr int kResident = E <= 8 ? 2 : 1;
 
-// threads: of a row, a power of two.
-template <int X, int Y, int V, int K>
-__global__ void __launch_bounds__(kThreads, 2) grad_rows_kernel(const GradArgs a, uint32_t threads, int sums)
+// E elements to a thread, V to a vector.
+template <int X, int Y, int V, int E>
+__global__ void __launch_bounds__(kRowThreads, kResident<E>) grad_rows_kernel(const GradArgs a, uint32_t threads, int sums)
 {
-    using S = Shares<X, Y, V, K>;
+    using R = Ring<X, Y, V, E>;
+    constexpr int K = E / V;
     extern __shared__ __align__(16) unsigned char memory[];
-    auto* stage = reinterpret_cast<typename S::Stage*>(memory);
+    auto& ring = *reinterpret_cast<R*>(memory);
     __shared__ RowSums row_sums;
-    const uint32_t place = threadIdx.x & (threads - 1), group = threadIdx.x / threads, groups = kThreads / threads;
+    const uint32_t place = threadIdx.x % threads, group = threadIdx.x / threads, groups = blockDim.x / threads;
     const uint32_t vectors = (uint32_t)(a.dim / V);
+    // the first thread of this one's group in its warp
+    const uint32_t first = threads >= 32 ? threadIdx.x & ~31u : threadIdx.x - place;
     const uint64_t stride = (uint64_t)gridDim.x * groups;
-    const float n = (float)a.dim;
+    const float per_element = __fdiv_rn(1.0f, (float)a.dim);
     grid_dependency_wait();
     const auto* x = static_cast<const typename Element<X>::type*>(a.x);
     const auto* dy = static_cast<const typename Element<Y>::type*>(a.dy);
     auto* dx = static_cast<typename Element<X>::type*>(a.dx);
-    float w[K][V], dw[K][V], db[K][V];
-#pragma unroll
-    for (int k = 0; k < K; ++k) {
-        const uint32_t at = place + k * threads;
-        if (at < vectors) weights_at<V>(a.weight, a.w_dtype, at * V, 1.0f, w[k]);
-#pragma unroll
-        for (int e = 0; e < V; ++e) {
-            if (at >= vectors) w[k][e] = 0.0f;
-            dw[k][e] = db[k][e] = 0.0f;
-        }
-    }
+    const auto has_vector = [&](int k) { return place + k * threads < vectors; };
     const auto fetch = [&](uint64_t row, int slot) {
-        if (row < a.rows)
+        if (row < a.rows) {
 #pragma unroll
             for (int k = 0; k < K; ++k) {
-                const uint32_t at = place + k * threads;
-                if (at >= vectors) continue;
-                copy_async<V * kElemBytes<X>>(&stage[slot].x[k][threadIdx.x], x + row * a.dim + at * V);
-                copy_async<V * kElemBytes<Y>>(&stage[slot].dy[k][threadIdx.x], dy + row * a.dim + at * V);
+                if (!has_vector(k)) continue;
+                const uint64_t at = row * a.dim + (place + k * threads) * V;
+                copy_async<V * kElemBytes<X>>(&ring.x[slot][k][threadIdx.x], x + at);
+                copy_async<V * kElemBytes<Y>>(&ring.dy[slot][k][threadIdx.x], dy + at);
             }
+            if (threadIdx.x == first) {
+                copy_async<4>(&ring.stats[slot][first].x, a.stats + 2 * row);
+                copy_async<4>(&ring.stats[slot][first].y, a.stats + 2 * row + 1);
+            }
+        }
         commit_copies();
     };
-    const uint64_t first = (uint64_t)blockIdx.x * groups + group;
-    if constexpr (S::kAsync)
+    float w[E];
+    float2 dw[E / 2], db[E / 2];
 #pragma unroll
-        for (int s = 0; s < S::kStages - 1; ++s) fetch(first + s * stride, s);
+    for (int k = 0; k < K; ++k) {
+        float wk[V];
+#pragma unroll
+        for (int e = 0; e < V; ++e) wk[e] = 0.0f;
+        if (has_vector(k)) weights_at<V>(a.weight, a.w_dtype, (place + k * threads) * V, 1.0f, wk);
+#pragma unroll
+        for (int e = 0; e < V; ++e) w[k * V + e] = wk[e];
+    }
+#pragma unroll
+    for (int e = 0; e < E / 2; ++e) dw[e] = db[e] = make_float2(0.0f, 0.0f);
+    if constexpr (R::kAsync) {
+        // places without elements hold zeros, which no copy overwrites
+#pragma unroll
+        for (int s = 0; s < R::kStages; ++s)
+#pragma unroll
+            for (int k = 0; k < K; ++k)
+                if (!has_vector(k))
+#pragma unroll
+                    for (int e = 0; e < V; ++e) {
+                        ring.x[s][k][threadIdx.x].set(e, 0.0f);
+                        ring.dy[s][k][threadIdx.x].set(e, 0.0f);
+                    }
+#pragma unroll
+        for (int s = 0; s < R::kStages - 1; ++s) fetch((uint64_t)blockIdx.x * groups + group + s * stride, s);
+    }
     int slot = 0, turn = 0;
-    // Every group of a CTA takes as many turns: the barriers of its warps are its own, but lanes of one warp stay together.
+    // Every group of a CTA takes as many turns: the barriers of its warps are its own, but the lanes of one warp stay together.
     for (uint64_t base = (uint64_t)blockIdx.x * groups; base < a.rows; base += stride) {
         const uint64_t row = base + group;
         const bool has = row < a.rows;
-        Packed<X, V> px[K];
-        Packed<Y, V> pdy[K];
+        float vx[E], vd[E];
         float2 stats = make_float2(0.0f, 0.0f);
-        if (has) stats = make_float2(__ldg(a.stats + 2 * row), __ldg(a.stats + 2 * row + 1));
-        if constexpr (S::kAsync) {
-            fetch(row + (S::kStages - 1) * stride, slot == 0 ? S::kStages - 1 : slot - 1);
-            wait_copies<S::kStages - 1>();
+        if constexpr (R::kAsync) {
+            __syncwarp();                               // the stats of the slot that is filled now have been read
+            fetch(row + (R::kStages - 1) * stride, slot == 0 ? R::kStages - 1 : slot - 1);
+            wait_copies<R::kStages - 1>();
+            __syncwarp();
+            if (has) stats = ring.stats[slot][first];
 #pragma unroll
             for (int k = 0; k < K; ++k) {
-                px[k] = stage[slot].x[k][threadIdx.x];
-                pdy[k] = stage[slot].dy[k][threadIdx.x];
+                widen_to<X, V>(ring.x[slot][k][threadIdx.x], vx + k * V);
+                widen_to<Y, V>(ring.dy[slot][k][threadIdx.x], vd + k * V);
             }
-            slot = slot == S::kStages - 1 ? 0 : slot + 1;
+            slot = slot == R::kStages - 1 ? 0 : slot + 1;
         } else {
+            if (has) stats = make_float2(__ldg(a.stats + 2 * row), __ldg(a.stats + 2 * row + 1));
 #pragma unroll
             for (int k = 0; k < K; ++k) {
-                const uint32_t at = place + k * threads;
-                if (!has || at >= vectors) continue;
-                px[k].load(x + row * a.dim + at * V);
-                pdy[k].load(dy + row * a.dim + at * V);
+                Packed<X, V> px;
+                Packed<Y, V> pd;
+#pragma unroll
+                for (int e = 0; e < V; ++e) { px.set(e, 0.0f); pd.set(e, 0.0f); }
+                if (has && has_vector(k)) {
+                    px.load(x + row * a.dim + (place + k * threads) * V);
+                    pd.load(dy + row * a.dim + (place + k * threads) * V);
+                }
+                widen_to<X, V>(px, vx + k * V);
+                widen_to<Y, V>(pd, vd + k * V);
             }
         }
-        float2 sum = make_float2(0.0f, 0.0f);
-        float h[K][V], g[K][V];
+        float2 sum = make_float2(0.0f, 0.0f), along = make_float2(0.0f, 0.0f);
+        const float2 minus = make_float2(-stats.x, -stats.x), rstd = make_float2(stats.y, stats.y);
+        if (has) {
 #pragma unroll
-        for (int k = 0; k < K; ++k) {
-            const bool there = has && place + k * threads < vectors;
-#pragma unroll
-            for (int e = 0; e < V; ++e) {
-                h[k][e] = there ? (px[k].get(e) - stats.x) * stats.y : 0.0f;
-                const float d = there ? pdy[k].get(e) : 0.0f;
-                dw[k][e] = fmaf(d, h[k][e], dw[k][e]);
-                db[k][e] += d;
-                g[k][e] = d * w[k][e];
-                sum.x += g[k][e];
-                sum.y = fmaf(g[k][e], h[k][e], sum.y);
+            for (int e = 0; e < E; e += 2) {
+                const float2 d = make_float2(vd[e], vd[e + 1]);
+                const float2 h = __fmul2_rn(__fadd2_rn(make_float2(vx[e], vx[e + 1]), minus), rstd);
+                const float2 g = __fmul2_rn(d, make_float2(w[e], w[e + 1]));
+                dw[e / 2] = __ffma2_rn(d, h, dw[e / 2]);
+                db[e / 2] = __fadd2_rn(db[e / 2], d);
+                sum = __fadd2_rn(sum, g);
+                along = __ffma2_rn(g, h, along);
+                vx[e] = h.x;
+                vx[e + 1] = h.y;
+                vd[e] = g.x;
+                vd[e + 1] = g.y;
             }
         }
         if (dx == nullptr) continue;
-        sum = row_sums.add(sum, threads, group, turn);
+        const float2 both = row_sums.two(make_float2(sum.x + sum.y, along.x + along.y), threads, group, turn);
         turn ^= 1;
-        const float m1 = __fdiv_rn(sum.x, n), m2 = __fdiv_rn(sum.y, n);
+        if (!has) continue;
+        // r g - r m1 - h (r m2)
+        const float c1 = -stats.y * (both.x * per_element), c2 = -stats.y * (both.y * per_element);
 #pragma unroll
         for (int k = 0; k < K; ++k) {
-            const uint32_t at = place + k * threads;
-            if (!has || at >= vectors) continue;
+            if (!has_vector(k)) continue;
             Packed<X, V> out;
+            if constexpr (V > 1) {
 #pragma unroll
-            for (int e = 0; e < V; ++e) out.set(e, stats.y * (g[k][e] - m1 - h[k][e] * m2));
-            out.store(dx + row * a.dim + at * V);
+                for (int e = 0; e < V; e += 2) {
+                    const int i = k * V + e;
+                    const float2 h = make_float2(vx[i], vx[i + 1]), g = make_float2(vd[i], vd[i + 1]);
+                    const float2 r = __ffma2_rn(g, rstd, __ffma2_rn(h, make_float2(c2, c2), make_float2(c1, c1)));
+                    out.set(e, r.x);
+                    out.set(e + 1, r.y);
+                }
+            } else {
+                out.set(0, fmaf(vd[k], stats.y, fmaf(vx[k], c2, c1)));
+            }
+            out.store(dx + row * a.dim + (place + k * threads) * V);
         }
     }
     if (!sums) return;
     // The groups' sums, in their order, through shared memory.
-    if constexpr (S::kAsync) wait_copies<0>();
+    if constexpr (R::kAsync) wait_copies<0>();
     __syncthreads();
     float* all = reinterpret_cast<float*>(memory);      // [groups][dim] of one sum, then of the other
     const uint32_t dim = (uint32_t)a.dim;
 #pragma unroll
     for (int which = 0; which < 2; ++which) {
 #pragma unroll
-        for (int k = 0; k < K; ++k) {
-            const uint32_t at = place + k * threads;
-            if (at >= vectors) continue;
-#pragma unroll
-            for (int e = 0; e < V; ++e) all[group * dim + at * V + e] = which == 0 ? dw[k][e] : db[k][e];
+        for (int e = 0; e < E; ++e) {
+            const float2 pair = which == 0 ? dw[e / 2] : db[e / 2];
+            if (has_vector(e / V)) all[group * dim + (place + e / V * threads) * V + e % V] = e % 2 ? pair.y : pair.x;
         }
         __syncthreads();
-        for (uint32_t col = threadIdx.x; col < dim; col += kThreads) {
+        for (uint32_t col = threadIdx.x; col < dim; col += blockDim.x) {
             float total = 0.0f;
             for (uint32_t i = 0; i < groups; ++i) total += all[i * dim + col];
             a.partial[((uint64_t)blockIdx.x * 2 + which) * dim + col] = total;
@@ -266,56 +280,45 @@ join_kernel(const float* __restrict__ partial, uint32_t parts, uint64_t dim, voi
 
 uint64_t ceil_div(uint64_t a, uint64_t b) { return (a + b - 1) / b; }
 
-// Threads of a row in the kernel that keeps it in registers; 0: the row is too long.
-uint32_t row_threads(uint64_t dim)
-{
-    uint32_t threads = 1;
-    while (threads <= kThreads && (uint64_t)threads * kMostElements < dim) threads *= 2;
-    return threads <= kThreads ? threads : 0;
-}
+// Elements of a row to a thread in the kernel that keeps it in registers; 0: the row is too long.
+uint32_t row_elements(uint64_t dim) { return dim <= 8 * kRowThreads ? 8 : dim <= 16 * kRowThreads ? 16 : 0; }
+
+RowGroups groups_of(uint64_t rows, uint64_t dim, uint32_t e) { return row_groups(rows, dim, e, (e <= 8 ? kResident<8> : kResident<16>)*kRowThreads); }
 
 // Parts of the rows that leave a sum each: the CTAs of that kernel, or, for long rows, enough for every SM of at least 64 rows.
 uint32_t parts_of(uint64_t rows, uint64_t dim)
 {
-    uint64_t most, want = kCtas;
-    if (const uint32_t threads = row_threads(dim)) {
-        most = ceil_div(rows, kThreads / threads);
-    } else {
-        most = ceil_div(rows, 64);
-        want = ceil_div(148 * 8, ceil_div(dim, kColumns));
-    }
+    if (const uint32_t e = row_elements(dim)) return groups_of(rows, dim, e).ctas;
+    const uint64_t most = ceil_div(rows, 64), want = ceil_div(148 * 8, ceil_div(dim, kColumns));
     return (uint32_t)(most < want ? (most < 1 ? 1 : most) : want);
 }
 
-template <int X, int Y, int V> cudaError_t launch_vectors(const GradArgs& a, uint32_t threads, uint32_t parts, int sums, cudaStream_t stream)
+template <int X, int Y, int V, int E> cudaError_t launch_elements(const GradArgs& a, int sums, cudaStream_t stream)
 {
-    using S = Shares<X, Y, V, kMostElements / V>;
-    constexpr size_t kSums = kThreads * kMostElements * sizeof(float);
-    constexpr size_t kRing = S::kAsync ? S::kStages * sizeof(typename S::Stage) : 0, kBytes = kRing > kSums ? kRing : kSums;
-    const auto kernel = grad_rows_kernel<X, Y, V, kMostElements / V>;
-    static std::atomic<bool> ready[64];                 // by device
-    int dev = 0;
-    cudaError_t err = cudaGetDevice(&dev);
-    if (err != cudaSuccess) return err;
-    if (dev < 0 || dev >= 64) return cudaErrorInvalidDevice;
-    if (!ready[dev].load(std::memory_order_relaxed)) {
-        err = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kBytes);
-        if (err != cudaSuccess) return err;
-        ready[dev].store(true, std::memory_order_relaxed);
-    }
-    return launch_pdl_smem(kernel, parts, kThreads, kBytes, stream, a, threads, sums);
+    using R = Ring<X, Y, V, E>;
+    static std::atomic<bool> ready[64];
+    const auto kernel = grad_rows_kernel<X, Y, V, E>;
+    constexpr size_t kSums = kRowThreads * E * sizeof(float), kBytes = R::kAsync && sizeof(R) > kSums ? sizeof(R) : kSums;
+    if (const cudaError_t err = allow_shared(kernel, kBytes, ready)) return err;
+    const RowGroups g = groups_of(a.rows, a.dim, E);
+    return launch_pdl_smem(kernel, g.ctas, g.block, kBytes, stream, a, g.threads, sums);
+}
+
+template <int X, int Y, int V> cudaError_t launch_vectors(const GradArgs& a, int sums, cudaStream_t stream)
+{
+    return row_elements(a.dim) == 8 ? launch_elements<X, Y, V, 8>(a, sums, stream) : launch_elements<X, Y, V, 16>(a, sums, stream);
 }
 
 template <int X, int Y> cudaError_t launch(const GradArgs& a, const NormGrads& out, cudaStream_t stream)
 {
     const int sums = out.dweight != nullptr || out.dbias != nullptr;
-    const uint32_t parts = parts_of(a.rows, a.dim), threads = row_threads(a.dim);
+    const uint32_t parts = parts_of(a.rows, a.dim);
     cudaError_t err = cudaSuccess;
-    if (threads != 0) {
+    if (row_elements(a.dim) != 0) {
         constexpr int V = kVector<X, Y>;
         const bool fit = vectors_fit(a.x, kElemBytes<X>, V, a.dim) && vectors_fit(a.dx, kElemBytes<X>, V, a.dim) &&
                          vectors_fit(a.dy, kElemBytes<Y>, V, a.dim) && vectors_fit(a.weight, element_bytes(a.w_dtype), V, a.dim);
-        err = fit ? launch_vectors<X, Y, V>(a, threads, parts, sums, stream) : launch_vectors<X, Y, 1>(a, threads, parts, sums, stream);
+        err = fit ? launch_vectors<X, Y, V>(a, sums, stream) : launch_vectors<X, Y, 1>(a, sums, stream);
     } else {
         if (a.dx != nullptr && a.rows != 0) err = launch_pdl(grad_long_kernel<X, Y>, (unsigned)a.rows, kLongThreads, stream, a);
         if (sums && err == cudaSuccess)

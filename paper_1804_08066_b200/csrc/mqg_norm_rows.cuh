@@ -3,6 +3,8 @@
 
 #include <stdint.h>
 
+#include <atomic>
+
 #include "mqg_vector.cuh"
 
 namespace mqg {
@@ -22,15 +24,6 @@ __device__ __forceinline__ double long_sum(double v)
 #pragma unroll
     for (int w = 0; w < kLongThreads / 32; ++w) t += warp_sum[w];
     return t;
-}
-
-// Sum over `lanes` neighbouring lanes, a power of two up to 32.
-__device__ __forceinline__ float lanes_sum(float v, uint32_t lanes)
-{
-#pragma unroll
-    for (uint32_t d = 16; d > 0; d >>= 1)
-        if (d < lanes) v += __shfl_xor_sync(0xFFFFFFFFu, v, d);
-    return v;
 }
 
 __device__ __forceinline__ float reciprocal_deviation(float variance, float eps) { return __frcp_rn(__fsqrt_rn(variance + eps)); }
@@ -62,6 +55,110 @@ template <int V> __device__ __forceinline__ void weights_at(const void* w, int d
     }
 }
 
+// ---- rows by groups of threads ----------------------------------------------------------------------------------------------
+// A row is E elements to a thread: a group of up to 32 lanes, a power of two, or of up to 16 whole warps.  A CTA has as many
+// groups as fit 16 warps.  Thread `place` of a group has the vectors place, place + threads, ... of V elements.
+
+constexpr int kRowThreads = 512;
+
+struct RowGroups {
+    uint32_t threads;        // of a group
+    uint32_t block;          // of a CTA
+    uint32_t ctas;           // a grid that fills the device, where there are rows for it
+};
+
+// E * kRowThreads elements at most.  per_sm: threads that the kernel's registers leave room for.
+inline RowGroups row_groups(uint64_t rows, uint64_t dim, uint32_t e, uint32_t per_sm)
+{
+    RowGroups g;
+    const uint32_t need = (uint32_t)((dim + e - 1) / e);
+    if (need <= 32) {
+        for (g.threads = 1; g.threads < need;) g.threads *= 2;
+        g.block = kRowThreads;
+    } else {
+        g.threads = (need + 31) / 32 * 32;
+        g.block = kRowThreads / g.threads * g.threads;
+    }
+    const uint64_t per_cta = g.block / g.threads, wanted = (rows + per_cta - 1) / per_cta, most = 148ull * (per_sm / g.block);
+    g.ctas = (uint32_t)(wanted < 1 ? 1 : wanted < most ? wanted : most);
+    return g;
+}
+
+// Sum over `lanes` neighbouring lanes, a power of two up to 32.
+__device__ __forceinline__ float lanes_sum(float v, uint32_t lanes)
+{
+#pragma unroll
+    for (uint32_t d = 16; d > 0; d >>= 1)
+        if (d < lanes) v += __shfl_xor_sync(0xFFFFFFFFu, v, d);
+    return v;
+}
+
+__device__ __forceinline__ void group_barrier(uint32_t group, uint32_t threads)
+{
+    asm volatile("bar.sync %0, %1;" ::"r"(group + 1), "r"(threads) : "memory");
+}
+
+// Sums over a group of one or two values of each thread, the same for all of its threads.  A group of several warps meets once for
+// each sum; `turn` alternates, so that nothing is written that a slow warp has yet to read.
+struct RowSums {
+    float2 of_warp[2][kRowThreads / 32];
+
+    __device__ __forceinline__ float one(float v, uint32_t threads, uint32_t group, int turn)
+    {
+        v = lanes_sum(v, threads);
+        if (threads <= 32) return v;
+        const uint32_t warps = threads / 32, lane = threadIdx.x & 31;
+        if (lane == 0) of_warp[turn][threadIdx.x >> 5].x = v;
+        group_barrier(group, threads);
+        return lanes_sum((lane & 15) < warps ? of_warp[turn][group * warps + (lane & 15)].x : 0.0f, 16);
+    }
+    __device__ __forceinline__ float2 two(float2 v, uint32_t threads, uint32_t group, int turn)
+    {
+        if (threads < 32) return make_float2(lanes_sum(v.x, threads), lanes_sum(v.y, threads));
+        // from here on lanes below 16 have the first value and the others the second: six steps for both instead of ten
+        const uint32_t lane = threadIdx.x & 31;
+        const bool low = lane < 16;
+        float mine = (low ? v.x : v.y) + __shfl_xor_sync(0xFFFFFFFFu, low ? v.y : v.x, 16);
+        mine = lanes_sum(mine, 16);
+        if (threads > 32) {
+            const uint32_t warps = threads / 32;
+            float* sums = reinterpret_cast<float*>(of_warp[turn]);
+            if ((lane & 15) == 0) sums[2 * (threadIdx.x >> 5) + (low ? 0 : 1)] = mine;
+            group_barrier(group, threads);
+            mine = lanes_sum((lane & 15) < warps ? sums[2 * (group * warps + (lane & 15)) + (low ? 0 : 1)] : 0.0f, 16);
+        }
+        const float other = __shfl_xor_sync(0xFFFFFFFFu, mine, 16);
+        return low ? make_float2(mine, other) : make_float2(other, mine);
+    }
+};
+
+// ---- asynchronous copies to shared memory ------------------------------------------------------------------------------------
+
+template <int BYTES> __device__ __forceinline__ void copy_async(void* to, const void* from)
+{
+    const uint32_t at = (uint32_t)__cvta_generic_to_shared(to);
+    if (BYTES == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(at), "l"(from) : "memory");
+    else asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" ::"r"(at), "l"(from), "n"(BYTES) : "memory");
+}
+__device__ __forceinline__ void commit_copies() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N> __device__ __forceinline__ void wait_copies() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+
+// V consecutive elements as pairs of fp32 (V = 1: one of a pair).
+template <int DTYPE, int V> __device__ __forceinline__ void widen_to(const Packed<DTYPE, V>& in, float* out)
+{
+    if constexpr (DTYPE == kBf16 && V > 1) {
+        const auto* w = reinterpret_cast<const uint32_t*>(&in);
+#pragma unroll
+        for (int k = 0; k < V / 2; ++k) {
+            out[2 * k] = __uint_as_float(w[k] << 16);
+            out[2 * k + 1] = __uint_as_float(w[k] & 0xFFFF0000u);
+        }
+    } else {
+#pragma unroll
+        for (int e = 0; e < V; ++e) out[e] = in.get(e);
+    }
+}
+
 // The elements of a vector: 16 bytes where both types are bf16 or fp32 (x and y of a call), 4 elements of mixed ones.
 template <int A, int B> constexpr int kVector = A == kBf16 && B == kBf16 ? 8 : 4;
 
@@ -73,5 +170,20 @@ inline bool vectors_fit(const void* p, int bytes, int v, uint64_t dim)
 }
 
 inline int element_bytes(int dtype) { return dtype == kF32 ? 4 : 2; }
+
+// Lets `kernel` use `bytes` of dynamic shared memory on the current device.  `ready`: of this kernel, by device.
+template <typename Kernel> cudaError_t allow_shared(Kernel kernel, size_t bytes, std::atomic<bool> (&ready)[64])
+{
+    int dev = 0;
+    cudaError_t err = cudaGetDevice(&dev);
+    if (err != cudaSuccess) return err;
+    if (dev < 0 || dev >= 64) return cudaErrorInvalidDevice;
+    if (!ready[dev].load(std::memory_order_relaxed)) {
+        err = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
+        if (err != cudaSuccess) return err;
+        ready[dev].store(true, std::memory_order_relaxed);
+    }
+    return cudaSuccess;
+}
 
 }  // namespace mqg
