@@ -25,14 +25,14 @@ struct NormArgs {
 // Rows on their way to shared memory, each thread's own elements.
 template <int X, int V, int E> struct Ring {
     static constexpr bool kAsync = V * kElemBytes<X> >= 4;
-    static constexpr int kStages = !kAsync ? 1 : E > 16 ? 2 : E * kElemBytes<X> <= 16 ? 6 : E * kElemBytes<X> <= 32 ? 5 : 3;
+    static constexpr int kStages = !kAsync ? 1 : E > 16 ? (X == kBf16 ? 4 : 3) : E * kElemBytes<X> <= 16 ? 6 : E * kElemBytes<X> <= 32 ? 5 : 3;
     Packed<X, V> x[kStages][E / V][kRowThreads];
 };
 
 template <int E> constexpr int kResident = E <= 8 ? 2 : 1;
 
 // E elements to a thread, V to a vector.
-template <int X, int Y, int V, int E>
+template <int X, int Y, int V, int E, bool WIDE>
 __global__ void __launch_bounds__(kRowThreads, kResident<E>) norm_rows_kernel(const NormArgs a, uint32_t threads)
 {
     using R = Ring<X, V, E>;
@@ -41,18 +41,18 @@ __global__ void __launch_bounds__(kRowThreads, kResident<E>) norm_rows_kernel(co
     auto& ring = *reinterpret_cast<R*>(memory);
     __shared__ RowSums sums;
     const uint32_t place = threadIdx.x % threads, group = threadIdx.x / threads, groups = blockDim.x / threads;
-    const uint32_t vectors = (uint32_t)(a.dim / V);
+    const RowPlace<V, K, WIDE> at(a.dim, place, threads);
     const uint64_t stride = (uint64_t)gridDim.x * groups;
     const float per_element = __fdiv_rn(1.0f, (float)a.dim);
     grid_dependency_wait();
     const auto* x = static_cast<const typename Element<X>::type*>(a.x);
     auto* y = static_cast<typename Element<Y>::type*>(a.y);
-    const auto has_vector = [&](int k) { return place + k * threads < vectors; };
     const auto fetch = [&](uint64_t row, int slot) {
+        const auto* from = x + row * a.dim;
         if (row < a.rows)
 #pragma unroll
             for (int k = 0; k < K; ++k)
-                if (has_vector(k)) copy_async<V * kElemBytes<X>>(&ring.x[slot][k][threadIdx.x], x + row * a.dim + (place + k * threads) * V);
+                if (at.has(k)) copy_async<V * kElemBytes<X>>(&ring.x[slot][k][threadIdx.x], from + at.element(k));
         commit_copies();
     };
     float w[E], b[E];
@@ -61,9 +61,9 @@ __global__ void __launch_bounds__(kRowThreads, kResident<E>) norm_rows_kernel(co
         float wk[V], bk[V];
 #pragma unroll
         for (int e = 0; e < V; ++e) wk[e] = bk[e] = 0.0f;
-        if (has_vector(k)) {
-            weights_at<V>(a.weight, a.w_dtype, (place + k * threads) * V, 1.0f, wk);
-            weights_at<V>(a.bias, a.w_dtype, (place + k * threads) * V, 0.0f, bk);
+        if (at.has(k)) {
+            weights_at<V>(a.weight, a.w_dtype, at.element(k), 1.0f, wk);
+            weights_at<V>(a.bias, a.w_dtype, at.element(k), 0.0f, bk);
         }
 #pragma unroll
         for (int e = 0; e < V; ++e) { w[k * V + e] = wk[e]; b[k * V + e] = bk[e]; }
@@ -74,7 +74,7 @@ __global__ void __launch_bounds__(kRowThreads, kResident<E>) norm_rows_kernel(co
         for (int s = 0; s < R::kStages; ++s)
 #pragma unroll
             for (int k = 0; k < K; ++k)
-                if (!has_vector(k))
+                if (!at.has(k))
 #pragma unroll
                     for (int e = 0; e < V; ++e) ring.x[s][k][threadIdx.x].set(e, 0.0f);
 #pragma unroll
@@ -97,7 +97,7 @@ __global__ void __launch_bounds__(kRowThreads, kResident<E>) norm_rows_kernel(co
                 Packed<X, V> in;
 #pragma unroll
                 for (int e = 0; e < V; ++e) in.set(e, 0.0f);
-                if (has && has_vector(k)) in.load(x + row * a.dim + (place + k * threads) * V);
+                if (has && at.has(k)) in.load(x + row * a.dim + at.element(k));
                 widen_to<X, V>(in, v + k * V);
             }
         }
@@ -113,10 +113,10 @@ __global__ void __launch_bounds__(kRowThreads, kResident<E>) norm_rows_kernel(co
             v[e] = d.x;
             v[e + 1] = d.y;
             if constexpr (V > 1) {
-                if (has_vector(e / V)) squares = __ffma2_rn(d, d, squares);
+                if (at.has(e / V)) squares = __ffma2_rn(d, d, squares);
             } else {
-                squares.x = has_vector(e) ? fmaf(d.x, d.x, squares.x) : squares.x;
-                squares.y = has_vector(e + 1) ? fmaf(d.y, d.y, squares.y) : squares.y;
+                squares.x = at.has(e) ? fmaf(d.x, d.x, squares.x) : squares.x;
+                squares.y = at.has(e + 1) ? fmaf(d.y, d.y, squares.y) : squares.y;
             }
         }
         const float rstd = reciprocal_deviation(sums.one(squares.x + squares.y, threads, group, 1) * per_element, a.eps);
@@ -124,7 +124,7 @@ __global__ void __launch_bounds__(kRowThreads, kResident<E>) norm_rows_kernel(co
         if (place == 0 && a.stats != nullptr) { a.stats[2 * row] = mean; a.stats[2 * row + 1] = rstd; }
 #pragma unroll
         for (int k = 0; k < K; ++k) {
-            if (!has_vector(k)) continue;
+            if (!at.has(k)) continue;
             Packed<Y, V> out;
             if constexpr (V > 1) {
 #pragma unroll
@@ -138,7 +138,7 @@ __global__ void __launch_bounds__(kRowThreads, kResident<E>) norm_rows_kernel(co
             } else {
                 out.set(0, fmaf(v[k] * rstd, w[k], b[k]));
             }
-            out.store(y + row * a.dim + (place + k * threads) * V);
+            out.store(y + row * a.dim + at.element(k));
         }
     }
 }
@@ -166,22 +166,31 @@ template <int X, int Y> __global__ void __launch_bounds__(kLongThreads) norm_lon
     }
 }
 
-template <int X, int Y, int V, int E> cudaError_t launch_elements(const NormArgs& a, cudaStream_t stream)
+template <int X, int Y, int V, int E, bool WIDE> cudaError_t launch_groups(const NormArgs& a, const RowGroups& g, cudaStream_t stream)
 {
     using R = Ring<X, V, E>;
     static std::atomic<bool> ready[64];
-    const auto kernel = norm_rows_kernel<X, Y, V, E>;
+    const auto kernel = norm_rows_kernel<X, Y, V, E, WIDE>;
     constexpr size_t kBytes = R::kAsync ? sizeof(R) : 0;
     if (const cudaError_t err = allow_shared(kernel, kBytes, ready)) return err;
-    const RowGroups g = row_groups(a.rows, a.dim, E, kResident<E> * kRowThreads);
     return launch_pdl_smem(kernel, g.ctas, g.block, kBytes, stream, a, g.threads);
 }
 
+template <int X, int Y, int V, int E> cudaError_t launch_elements(const NormArgs& a, cudaStream_t stream)
+{
+    const RowGroups g = row_groups(a.rows, a.dim, E, kResident<E> * kRowThreads);
+    return g.threads > 32 ? launch_groups<X, Y, V, E, true>(a, g, stream) : launch_groups<X, Y, V, E, false>(a, g, stream);
+}
+
+// The more elements a thread has, the fewer shuffles and barriers there are to a row, and the more is under way: with 8 / 16 / 32 elements
+// 65,536 rows of 4096 in bf16 take 268 / 242 / 164 us, 16,384 of 1024 19.7 / 16.8 / 13.6, 60,000 of 512 31.7 / 22.3 / 23.7, 131,072 of 64
+// 9.6 / 7.8 / 10.7; in fp32 4096 of 4096 24.9 / 23.2 / 25.0.  A million rows of 16: 14 / 20 / 20, lanes then skip memory.  Single
+// elements are bound by instructions: 10,007 rows of 515 in fp32 14.7 / 15.6 / 35.
 template <int X, int Y, int V> cudaError_t launch_vectors(const NormArgs& a, cudaStream_t stream)
 {
-    return a.dim <= 8 * kRowThreads    ? launch_elements<X, Y, V, 8>(a, stream)
-           : a.dim <= 16 * kRowThreads ? launch_elements<X, Y, V, 16>(a, stream)
-                                       : launch_elements<X, Y, V, 32>(a, stream);
+    if (a.dim <= 32 || (a.dim <= 8 * kRowThreads && (V == 1 || few_elements(a.rows, a.dim)))) return launch_elements<X, Y, V, 8>(a, stream);
+    if (a.dim <= (V == 1 || X == kF32 ? 16 * kRowThreads : 512)) return launch_elements<X, Y, V, 16>(a, stream);
+    return launch_elements<X, Y, V, 32>(a, stream);
 }
 
 template <int X, int Y> cudaError_t launch(const NormArgs& a, cudaStream_t stream)

@@ -30,7 +30,7 @@ struct GradArgs {
 template <int X, int Y, int V, int E> struct Ring {
     static constexpr bool kAsync = V * kElemBytes<X> >= 4 && V * kElemBytes<Y> >= 4;
     static constexpr int kBytes = E * (kElemBytes<X> + kElemBytes<Y>);
-    static constexpr int kStages = !kAsync ? 1 : kBytes <= 32 ? 5 : kBytes <= 48 ? 4 : kBytes <= 64 && E > 8 ? 5 : 3;
+    static constexpr int kStages = !kAsync ? 1 : kBytes <= 32 ? 5 : kBytes <= 48 ? 4 : kBytes <= 64 && E > 8 ? 5 : E > 16 ? (kBytes <= 128 ? 3 : kBytes <= 192 ? 2 : 1) : 3;
     Packed<X, V> x[kStages][E / V][kRowThreads];
     Packed<Y, V> dy[kStages][E / V][kRowThreads];
     float2 stats[kStages][kRowThreads];
@@ -38,8 +38,11 @@ template <int X, int Y, int V, int E> struct Ring {
 
 template <int E> constexpr int kResident = E <= 8 ? 2 : 1;
 
+// Rows of more elements leave the sums over the rows to a kernel of their own: registers hold no more.
+template <int E> constexpr bool kSums = E <= 16;
+
 // E elements to a thread, V to a vector.
-template <int X, int Y, int V, int E>
+template <int X, int Y, int V, int E, bool WIDE>
 __global__ void __launch_bounds__(kRowThreads, kResident<E>) grad_rows_kernel(const GradArgs a, uint32_t threads, int sums)
 {
     using R = Ring<X, Y, V, E>;
@@ -48,7 +51,7 @@ __global__ void __launch_bounds__(kRowThreads, kResident<E>) grad_rows_kernel(co
     auto& ring = *reinterpret_cast<R*>(memory);
     __shared__ RowSums row_sums;
     const uint32_t place = threadIdx.x % threads, group = threadIdx.x / threads, groups = blockDim.x / threads;
-    const uint32_t vectors = (uint32_t)(a.dim / V);
+    const RowPlace<V, K, WIDE> at(a.dim, place, threads);
     // the first thread of this one's group in its warp
     const uint32_t first = threads >= 32 ? threadIdx.x & ~31u : threadIdx.x - place;
     const uint64_t stride = (uint64_t)gridDim.x * groups;
@@ -57,15 +60,13 @@ __global__ void __launch_bounds__(kRowThreads, kResident<E>) grad_rows_kernel(co
     const auto* x = static_cast<const typename Element<X>::type*>(a.x);
     const auto* dy = static_cast<const typename Element<Y>::type*>(a.dy);
     auto* dx = static_cast<typename Element<X>::type*>(a.dx);
-    const auto has_vector = [&](int k) { return place + k * threads < vectors; };
     const auto fetch = [&](uint64_t row, int slot) {
         if (row < a.rows) {
 #pragma unroll
             for (int k = 0; k < K; ++k) {
-                if (!has_vector(k)) continue;
-                const uint64_t at = row * a.dim + (place + k * threads) * V;
-                copy_async<V * kElemBytes<X>>(&ring.x[slot][k][threadIdx.x], x + at);
-                copy_async<V * kElemBytes<Y>>(&ring.dy[slot][k][threadIdx.x], dy + at);
+                if (!at.has(k)) continue;
+                copy_async<V * kElemBytes<X>>(&ring.x[slot][k][threadIdx.x], x + row * a.dim + at.element(k));
+                copy_async<V * kElemBytes<Y>>(&ring.dy[slot][k][threadIdx.x], dy + row * a.dim + at.element(k));
             }
             if (threadIdx.x == first) {
                 copy_async<4>(&ring.stats[slot][first].x, a.stats + 2 * row);
@@ -81,7 +82,7 @@ __global__ void __launch_bounds__(kRowThreads, kResident<E>) grad_rows_kernel(co
         float wk[V];
 #pragma unroll
         for (int e = 0; e < V; ++e) wk[e] = 0.0f;
-        if (has_vector(k)) weights_at<V>(a.weight, a.w_dtype, (place + k * threads) * V, 1.0f, wk);
+        if (at.has(k)) weights_at<V>(a.weight, a.w_dtype, at.element(k), 1.0f, wk);
 #pragma unroll
         for (int e = 0; e < V; ++e) w[k * V + e] = wk[e];
     }
@@ -93,7 +94,7 @@ __global__ void __launch_bounds__(kRowThreads, kResident<E>) grad_rows_kernel(co
         for (int s = 0; s < R::kStages; ++s)
 #pragma unroll
             for (int k = 0; k < K; ++k)
-                if (!has_vector(k))
+                if (!at.has(k))
 #pragma unroll
                     for (int e = 0; e < V; ++e) {
                         ring.x[s][k][threadIdx.x].set(e, 0.0f);
@@ -129,9 +130,9 @@ __global__ void __launch_bounds__(kRowThreads, kResident<E>) grad_rows_kernel(co
                 Packed<Y, V> pd;
 #pragma unroll
                 for (int e = 0; e < V; ++e) { px.set(e, 0.0f); pd.set(e, 0.0f); }
-                if (has && has_vector(k)) {
-                    px.load(x + row * a.dim + (place + k * threads) * V);
-                    pd.load(dy + row * a.dim + (place + k * threads) * V);
+                if (has && at.has(k)) {
+                    px.load(x + row * a.dim + at.element(k));
+                    pd.load(dy + row * a.dim + at.element(k));
                 }
                 widen_to<X, V>(px, vx + k * V);
                 widen_to<Y, V>(pd, vd + k * V);
@@ -145,8 +146,10 @@ __global__ void __launch_bounds__(kRowThreads, kResident<E>) grad_rows_kernel(co
                 const float2 d = make_float2(vd[e], vd[e + 1]);
                 const float2 h = __fmul2_rn(__fadd2_rn(make_float2(vx[e], vx[e + 1]), minus), rstd);
                 const float2 g = __fmul2_rn(d, make_float2(w[e], w[e + 1]));
-                dw[e / 2] = __ffma2_rn(d, h, dw[e / 2]);
-                db[e / 2] = __fadd2_rn(db[e / 2], d);
+                if constexpr (kSums<E>) {
+                    dw[e / 2] = __ffma2_rn(d, h, dw[e / 2]);
+                    db[e / 2] = __fadd2_rn(db[e / 2], d);
+                }
                 sum = __fadd2_rn(sum, g);
                 along = __ffma2_rn(g, h, along);
                 vx[e] = h.x;
@@ -163,7 +166,7 @@ __global__ void __launch_bounds__(kRowThreads, kResident<E>) grad_rows_kernel(co
         const float c1 = -stats.y * (both.x * per_element), c2 = -stats.y * (both.y * per_element);
 #pragma unroll
         for (int k = 0; k < K; ++k) {
-            if (!has_vector(k)) continue;
+            if (!at.has(k)) continue;
             Packed<X, V> out;
             if constexpr (V > 1) {
 #pragma unroll
@@ -177,10 +180,10 @@ __global__ void __launch_bounds__(kRowThreads, kResident<E>) grad_rows_kernel(co
             } else {
                 out.set(0, fmaf(vd[k], stats.y, fmaf(vx[k], c2, c1)));
             }
-            out.store(dx + row * a.dim + (place + k * threads) * V);
+            out.store(dx + row * a.dim + at.element(k));
         }
     }
-    if (!sums) return;
+    if (!kSums<E> || !sums) return;
     // The groups' sums, in their order, through shared memory.
     if constexpr (R::kAsync) wait_copies<0>();
     __syncthreads();
@@ -191,7 +194,7 @@ __global__ void __launch_bounds__(kRowThreads, kResident<E>) grad_rows_kernel(co
 #pragma unroll
         for (int e = 0; e < E; ++e) {
             const float2 pair = which == 0 ? dw[e / 2] : db[e / 2];
-            if (has_vector(e / V)) all[group * dim + (place + e / V * threads) * V + e % V] = e % 2 ? pair.y : pair.x;
+            if (at.has(e / V)) all[group * dim + at.element(e / V) + e % V] = e % 2 ? pair.y : pair.x;
         }
         __syncthreads();
         for (uint32_t col = threadIdx.x; col < dim; col += blockDim.x) {
@@ -225,32 +228,58 @@ template <int X, int Y> __global__ void __launch_bounds__(kLongThreads) grad_lon
     }
 }
 
-// Sums over a part of the rows, a thread to a column.
-constexpr int kColumns = 64, kStripes = 4;
-template <int X, int Y> __global__ void __launch_bounds__(kColumns* kStripes) columns_kernel(const GradArgs a, uint64_t per_part)
+// Sums over a part of the rows: a thread has V columns of every kStripes-th row, and four of these rows under way.
+constexpr int kStripes = 8, kColumnLanes = 32, kAhead = 4;
+template <int X, int Y, int V>
+__global__ void __launch_bounds__(kColumnLanes* kStripes) columns_kernel(const GradArgs a, uint64_t per_part)
 {
-    __shared__ float sums[kStripes][2][kColumns];
-    const uint32_t at = threadIdx.x % kColumns, stripe = threadIdx.x / kColumns;
-    grid_dependency_wait();
-    const uint64_t col = (uint64_t)blockIdx.x * kColumns + at;
+    __shared__ float2 sums[kStripes][V][kColumnLanes];
+    const uint32_t lane = threadIdx.x % kColumnLanes, stripe = threadIdx.x / kColumnLanes;
+    const uint64_t col = ((uint64_t)blockIdx.x * kColumnLanes + lane) * V;
     const uint64_t first = blockIdx.y * per_part, last = min(first + per_part, a.rows);
+    grid_dependency_wait();
     const auto* x = static_cast<const typename Element<X>::type*>(a.x) + col;
     const auto* dy = static_cast<const typename Element<Y>::type*>(a.dy) + col;
-    float dw = 0.0f, db = 0.0f;
+    float2 sum[V];                                      // of dweight and dbias
+#pragma unroll
+    for (int e = 0; e < V; ++e) sum[e] = make_float2(0.0f, 0.0f);
     if (col < a.dim)
-        for (uint64_t row = first + stripe; row < last; row += kStripes) {
-            const float g = widen(dy[row * a.dim]), h = (widen(x[row * a.dim]) - a.stats[2 * row]) * a.stats[2 * row + 1];
-            dw = fmaf(g, h, dw);
-            db += g;
+#pragma unroll 1
+        for (uint64_t row0 = first + stripe; row0 < last; row0 += kAhead * kStripes) {
+            Packed<X, V> px[kAhead];
+            Packed<Y, V> pd[kAhead];
+            float2 stats[kAhead];
+#pragma unroll
+            for (int i = 0; i < kAhead; ++i) {
+                const uint64_t row = min(row0 + i * kStripes, last - 1);
+                px[i].load(x + row * a.dim);
+                pd[i].load(dy + row * a.dim);
+                stats[i] = make_float2(__ldg(a.stats + 2 * row), __ldg(a.stats + 2 * row + 1));
+            }
+#pragma unroll
+            for (int i = 0; i < kAhead; ++i) {
+                if (row0 + i * kStripes >= last) break;
+                float vx[V], vd[V];
+                widen_to<X, V>(px[i], vx);
+                widen_to<Y, V>(pd[i], vd);
+#pragma unroll
+                for (int e = 0; e < V; ++e) {
+                    sum[e].x = fmaf(vd[e], (vx[e] - stats[i].x) * stats[i].y, sum[e].x);
+                    sum[e].y += vd[e];
+                }
+            }
         }
-    sums[stripe][0][at] = dw;
-    sums[stripe][1][at] = db;
+#pragma unroll
+    for (int e = 0; e < V; ++e) sums[stripe][e][lane] = sum[e];
     __syncthreads();
     if (stripe != 0 || col >= a.dim) return;
 #pragma unroll
-    for (int k = 1; k < kStripes; ++k) { dw += sums[k][0][at]; db += sums[k][1][at]; }
-    a.partial[(blockIdx.y * 2 + 0) * a.dim + col] = dw;
-    a.partial[(blockIdx.y * 2 + 1) * a.dim + col] = db;
+    for (int e = 0; e < V; ++e) {
+#pragma unroll
+        for (int k = 1; k < kStripes; ++k) sum[e] = __fadd2_rn(sum[e], sums[k][e][lane]);
+        a.partial[(blockIdx.y * 2ull + 0) * a.dim + col + e] = sum[e].x;
+        a.partial[(blockIdx.y * 2ull + 1) * a.dim + col + e] = sum[e].y;
+    }
 }
 
 // The parts' sums, in 64 bits: stripes of the parts side by side, then the stripes in order.
@@ -280,51 +309,70 @@ join_kernel(const float* __restrict__ partial, uint32_t parts, uint64_t dim, voi
 
 uint64_t ceil_div(uint64_t a, uint64_t b) { return (a + b - 1) / b; }
 
-// Elements of a row to a thread in the kernel that keeps it in registers; 0: the row is too long.
-uint32_t row_elements(uint64_t dim) { return dim <= 8 * kRowThreads ? 8 : dim <= 16 * kRowThreads ? 16 : 0; }
+// The longest row whose sums over the rows stay in registers: a row to a CTA.
+constexpr uint64_t kSumsDim = 16 * kRowThreads;
 
 RowGroups groups_of(uint64_t rows, uint64_t dim, uint32_t e) { return row_groups(rows, dim, e, (e <= 8 ? kResident<8> : kResident<16>)*kRowThreads); }
 
-// Parts of the rows that leave a sum each: the CTAs of that kernel, or, for long rows, enough for every SM of at least 64 rows.
-uint32_t parts_of(uint64_t rows, uint64_t dim)
+// Parts of the rows that leave a sum each.  Longer rows: enough for every SM of at least 64 rows.
+uint32_t long_parts(uint64_t rows, uint64_t dim)
 {
-    if (const uint32_t e = row_elements(dim)) return groups_of(rows, dim, e).ctas;
-    const uint64_t most = ceil_div(rows, 64), want = ceil_div(148 * 8, ceil_div(dim, kColumns));
+    const uint64_t most = ceil_div(rows, 64), want = ceil_div(148 * 4, ceil_div(dim, kColumnLanes * 8));
     return (uint32_t)(most < want ? (most < 1 ? 1 : most) : want);
+}
+
+template <int X, int Y, int V, int E, bool WIDE> cudaError_t launch_groups(const GradArgs& a, const RowGroups& g, int sums, cudaStream_t stream)
+{
+    using R = Ring<X, Y, V, E>;
+    static std::atomic<bool> ready[64];
+    const auto kernel = grad_rows_kernel<X, Y, V, E, WIDE>;
+    constexpr size_t kAll = kSums<E> ? kRowThreads * E * sizeof(float) : 16, kBytes = R::kAsync && sizeof(R) > kAll ? sizeof(R) : kAll;
+    if (const cudaError_t err = allow_shared(kernel, kBytes, ready)) return err;
+    return launch_pdl_smem(kernel, g.ctas, g.block, kBytes, stream, a, g.threads, sums);
 }
 
 template <int X, int Y, int V, int E> cudaError_t launch_elements(const GradArgs& a, int sums, cudaStream_t stream)
 {
-    using R = Ring<X, Y, V, E>;
-    static std::atomic<bool> ready[64];
-    const auto kernel = grad_rows_kernel<X, Y, V, E>;
-    constexpr size_t kSums = kRowThreads * E * sizeof(float), kBytes = R::kAsync && sizeof(R) > kSums ? sizeof(R) : kSums;
-    if (const cudaError_t err = allow_shared(kernel, kBytes, ready)) return err;
     const RowGroups g = groups_of(a.rows, a.dim, E);
-    return launch_pdl_smem(kernel, g.ctas, g.block, kBytes, stream, a, g.threads, sums);
+    return g.threads > 32 ? launch_groups<X, Y, V, E, true>(a, g, sums, stream) : launch_groups<X, Y, V, E, false>(a, g, sums, stream);
 }
 
-template <int X, int Y, int V> cudaError_t launch_vectors(const GradArgs& a, int sums, cudaStream_t stream)
+// Elements to a thread.  More of them cost fewer shuffles and barriers to a row: with 8 / 16 65,536 rows of 4096 in bf16 take 326 / 270 us,
+// 16,384 of 1024 27.7 / 24.0, but 64 of 4096 7.6 / 9.5; 4096 of 4096 in fp32 39.3 / 40.3; a million rows of 16 27 / 40; 10,007 of 515
+// by single elements 18.5 / 21.
+template <int X, int Y, int V> uint32_t elements_of(uint64_t rows, uint64_t dim)
 {
-    return row_elements(a.dim) == 8 ? launch_elements<X, Y, V, 8>(a, sums, stream) : launch_elements<X, Y, V, 16>(a, sums, stream);
+    if (dim > 8 * kRowThreads) return 16;
+    return V == 1 || (X == kF32 && Y == kF32) || dim <= 32 || few_elements(rows, dim) ? 8 : 16;
+}
+
+// dx, and the sums of `parts` parts of the rows.
+template <int X, int Y, int V> cudaError_t launch_vectors(const GradArgs& a, int sums, uint32_t* parts, cudaStream_t stream)
+{
+    if (a.dim <= kSumsDim) {
+        const uint32_t e = elements_of<X, Y, V>(a.rows, a.dim);
+        *parts = groups_of(a.rows, a.dim, e).ctas;
+        return e == 8 ? launch_elements<X, Y, V, 8>(a, sums, stream) : launch_elements<X, Y, V, 16>(a, sums, stream);
+    }
+    cudaError_t err = cudaSuccess;
+    if (a.dx != nullptr && a.rows != 0) {
+        if (V > 1 && a.dim <= 32 * kRowThreads) err = launch_elements<X, Y, V, V == 1 ? 16 : 32>(a, 0, stream);
+        else err = launch_pdl(grad_long_kernel<X, Y>, (unsigned)a.rows, kLongThreads, stream, a);
+    }
+    if (!sums || err != cudaSuccess) return err;
+    *parts = long_parts(a.rows, a.dim);
+    return launch_pdl_grid(columns_kernel<X, Y, V>, dim3((unsigned)ceil_div(a.dim, kColumnLanes * V), *parts), kColumnLanes * kStripes, 0,
+                           stream, a, ceil_div(a.rows, *parts));
 }
 
 template <int X, int Y> cudaError_t launch(const GradArgs& a, const NormGrads& out, cudaStream_t stream)
 {
     const int sums = out.dweight != nullptr || out.dbias != nullptr;
-    const uint32_t parts = parts_of(a.rows, a.dim);
-    cudaError_t err = cudaSuccess;
-    if (row_elements(a.dim) != 0) {
-        constexpr int V = kVector<X, Y>;
-        const bool fit = vectors_fit(a.x, kElemBytes<X>, V, a.dim) && vectors_fit(a.dx, kElemBytes<X>, V, a.dim) &&
-                         vectors_fit(a.dy, kElemBytes<Y>, V, a.dim) && vectors_fit(a.weight, element_bytes(a.w_dtype), V, a.dim);
-        err = fit ? launch_vectors<X, Y, V>(a, sums, stream) : launch_vectors<X, Y, 1>(a, sums, stream);
-    } else {
-        if (a.dx != nullptr && a.rows != 0) err = launch_pdl(grad_long_kernel<X, Y>, (unsigned)a.rows, kLongThreads, stream, a);
-        if (sums && err == cudaSuccess)
-            err = launch_pdl_grid(columns_kernel<X, Y>, dim3((unsigned)ceil_div(a.dim, kColumns), parts), kColumns * kStripes, 0, stream, a,
-                                  ceil_div(a.rows, parts));
-    }
+    constexpr int V = kVector<X, Y>;
+    const bool fit = vectors_fit(a.x, kElemBytes<X>, V, a.dim) && vectors_fit(a.dx, kElemBytes<X>, V, a.dim) &&
+                     vectors_fit(a.dy, kElemBytes<Y>, V, a.dim) && vectors_fit(a.weight, element_bytes(a.w_dtype), V, a.dim);
+    uint32_t parts = 0;
+    const cudaError_t err = fit ? launch_vectors<X, Y, V>(a, sums, &parts, stream) : launch_vectors<X, Y, 1>(a, sums, &parts, stream);
     if (err != cudaSuccess || !sums) return err;
     const unsigned blocks = (unsigned)ceil_div(2 * a.dim, kJoinColumns);
     const auto join = out.dw_dtype == kF32 ? join_kernel<kF32> : join_kernel<kBf16>;
@@ -333,7 +381,12 @@ template <int X, int Y> cudaError_t launch(const GradArgs& a, const NormGrads& o
 
 }  // namespace
 
-size_t layer_norm_workspace_floats(uint64_t rows, uint64_t dim) { return (size_t)(parts_of(rows, dim) * 2 * dim); }
+// (8 elements to a thread leave the most parts)
+size_t layer_norm_workspace_floats(uint64_t rows, uint64_t dim)
+{
+    const uint64_t parts = dim > kSumsDim ? long_parts(rows, dim) : groups_of(rows, dim, dim <= 8 * kRowThreads ? 8 : 16).ctas;
+    return (size_t)(parts * 2 * dim);
+}
 
 cudaError_t launch_layer_norm_grad(const void* dy, int dy_dtype, const NormRows& in, const float* stats, const NormGrads& out,
                                    float* workspace, cudaStream_t stream)

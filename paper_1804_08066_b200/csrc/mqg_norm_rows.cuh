@@ -56,8 +56,10 @@ template <int V> __device__ __forceinline__ void weights_at(const void* w, int d
 }
 
 // ---- rows by groups of threads ----------------------------------------------------------------------------------------------
-// A row is E elements to a thread: a group of up to 32 lanes, a power of two, or of up to 16 whole warps.  A CTA has as many
-// groups as fit 16 warps.  Thread `place` of a group has the vectors place, place + threads, ... of V elements.
+// A row is E elements to a thread: a group of up to 32 lanes, a power of two, or of up to 16 whole warps (WIDE).  A CTA has as many
+// groups as fit 16 warps.  A thread has K vectors of V elements, those of a group's threads side by side; single elements (V = 1)
+// of a group of several warps, those of a warp's lanes, so that the distance between a thread's elements is a constant (10,007 rows
+// of 515 in fp32: 14.7 us, 18.3 without; for vectors it makes no difference or, in long rows, costs up to a sixth).
 
 constexpr int kRowThreads = 512;
 
@@ -83,6 +85,17 @@ inline RowGroups row_groups(uint64_t rows, uint64_t dim, uint32_t e, uint32_t pe
     g.ctas = (uint32_t)(wanted < 1 ? 1 : wanted < most ? wanted : most);
     return g;
 }
+
+// A thread's vectors: their places in the row, which of them the row has.
+template <int V, int K, bool WIDE> struct RowPlace {
+    static constexpr bool kByWarp = WIDE && V == 1;
+    uint32_t start, threads, vectors;
+    __device__ __forceinline__ RowPlace(uint64_t dim, uint32_t place, uint32_t group_threads)
+        : start(kByWarp ? (place & ~31u) * K + (place & 31) : place), threads(group_threads), vectors((uint32_t)(dim / V)) {}
+    __device__ __forceinline__ uint32_t step() const { return kByWarp ? 32 : threads; }
+    __device__ __forceinline__ bool has(int k) const { return start + k * step() < vectors; }
+    __device__ __forceinline__ uint32_t element(int k) const { return (start + k * step()) * V; }
+};
 
 // Sum over `lanes` neighbouring lanes, a power of two up to 32.
 __device__ __forceinline__ float lanes_sum(float v, uint32_t lanes)
@@ -158,6 +171,10 @@ template <int DTYPE, int V> __device__ __forceinline__ void widen_to(const Packe
         for (int e = 0; e < V; ++e) out[e] = in.get(e);
     }
 }
+
+// Whether rows x dim elements keep less than the threads of a device busy, 8 elements to a thread: then more elements to a thread
+// take longer.
+inline bool few_elements(uint64_t rows, uint64_t dim) { return rows * dim <= 148ull * 2 * kRowThreads * 8; }
 
 // The elements of a vector: 16 bytes where both types are bf16 or fp32 (x and y of a call), 4 elements of mixed ones.
 template <int A, int B> constexpr int kVector = A == kBf16 && B == kBf16 ? 8 : 4;
