@@ -44,15 +44,16 @@ template <int CAP> struct AdamwTable {
     float* scales[CAP];
     uint64_t first_block[CAP];                          // blocks before the tensor in the whole list
     float decay[CAP];
-    uint8_t kind[CAP];                                  // bit 0: p is bf16, bit 1: g is
+    uint8_t kind[CAP];                                  // bit 0: p is bf16, bit 1: g is, bit 2: all on the boundaries of 4 elements
 };
 constexpr int kLargeTable = 448;
 
 struct Scalars {
-    float b1, w1, b2, w2, eps, lr, c1, c2, grad_scale;
+    float b1, w1, b2, w2, eps, lr, c1, c2, grad_scale, minus_zero;
     const float* factor;
     const float* schedule;
-    uint32_t step, seed_lo, seed_hi;
+    uint32_t step;
+    RoundKeys keys;
 };
 
 // What a step takes from the device's memory, and what follows from it.
@@ -74,13 +75,41 @@ struct Step {
     }
 };
 
+__device__ __forceinline__ float root(float x)
+{
+    float r;
+    asm("sqrt.approx.f32 %0, %1;" : "=f"(r) : "f"(x));
+    return r;
+}
+
 __device__ __forceinline__ void update(float& p, float g, float& m, float& v, const Scalars& s, const Step& st, float rate)
 {
     g = __fmul_rn(st.k, g);
     m = __fadd_rn(__fmul_rn(s.b1, m), __fmul_rn(s.w1, g));
     v = __fadd_rn(__fmul_rn(s.b2, v), __fmul_rn(__fmul_rn(s.w2, g), g));
-    const float d = __fadd_rn(__fmul_rn(__fsqrt_rn(v), st.r2), s.eps);
-    p = __fsub_rn(p, __fadd_rn(__fmul_rn(rate, p), __fmul_rn(st.a, __fdiv_rn(m, d))));
+    const float d = __fmaf_rn(root(v), st.r2, s.eps);                       // 2^-50 <= d < 2^70
+    p = __fsub_rn(p, __fmaf_rn(st.a, __fdividef(m, d), __fmul_rn(rate, p)));
+}
+
+__device__ __forceinline__ float2 both(float x) { return make_float2(x, x); }
+
+// The product of two pairs, rounded, in a form that no later sum is fused with (a packed multiplication is, whatever the source
+// says of its rounding): a sum with -0, which the compiler does not know.
+__device__ __forceinline__ float2 times(float2 a, float2 b, float minus_zero) { return __ffma2_rn(a, b, both(minus_zero)); }
+
+// The same for two elements, by packed instructions, which round as the single ones do.
+__device__ __forceinline__ void update2(float* p, const float* g_in, float* m, float* v, const Scalars& s, const Step& st, float rate)
+{
+    const float z = s.minus_zero;
+    const float2 g = times(both(st.k), make_float2(g_in[0], g_in[1]), z), old = make_float2(p[0], p[1]);
+    const float2 m2 = __fadd2_rn(times(both(s.b1), make_float2(m[0], m[1]), z), times(both(s.w1), g, z));
+    const float2 v2 = __fadd2_rn(times(both(s.b2), make_float2(v[0], v[1]), z), times(times(both(s.w2), g, z), g, z));
+    const float2 d = __ffma2_rn(make_float2(root(v2.x), root(v2.y)), both(st.r2), both(s.eps));
+    const float2 u = make_float2(__fdividef(m2.x, d.x), __fdividef(m2.y, d.y));
+    const float2 less = __ffma2_rn(both(st.a), u, __fmul2_rn(both(rate), old));
+    p[0] = old.x - less.x, p[1] = old.y - less.y;
+    m[0] = m2.x, m[1] = m2.y;
+    v[0] = v2.x, v[1] = v2.y;
 }
 
 // A float of 8 bits: the bits of an fp32 times 2^EXP2, cut off behind bit SHIFT.  The power of two takes the grid's smallest normal
@@ -142,53 +171,190 @@ __device__ __forceinline__ void store(void* p, bool bf16, uint64_t i, float x)
     else static_cast<float*>(p)[i] = x;
 }
 
-// A warp to a block, lanes side by side.
-template <int CAP, bool EIGHT>
-__global__ void __launch_bounds__(kThreads) adamw_kernel(const __grid_constant__ AdamwTable<CAP> tab, const Scalars s)
+// Four codes in a word, and back; all of one block.
+__device__ __forceinline__ void decode4(uint32_t m, uint32_t v, float scale_m, float scale_v, float* to_m, float* to_v)
 {
-    __shared__ uint4 draws[EIGHT ? kWarps : 1][32];
-    const int j = find_in_list<(CAP > 32)>(tab.tile_start, tab.count, blockIdx.x);
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const uint64_t block = (uint64_t)(blockIdx.x - tab.tile_start[j]) * kWarps + warp, e0 = block * kBlock, size = tab.size[j];
-    const bool wide_p = !(tab.kind[j] & 1), wide_g = !(tab.kind[j] & 2);
-    const float decay = tab.decay[j];
-    grid_dependency_wait();
+#pragma unroll
+    for (int j = 0; j < 4; j += 2) {
+        float a[2], b[2];
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            // a byte at the top; three bits of exponent between the sign and the code
+            const uint32_t top_m = __byte_perm(m, 0, 0x0444 | (j + i) << 12), top_v = __byte_perm(v, 0, 0x0444 | (j + i) << 12);
+            a[i] = __uint_as_float((uint32_t)((int32_t)top_m >> 4) & 0x87F00000u);
+            b[i] = __uint_as_float(top_v >> 3);
+        }
+        const float2 x = __fmul2_rn(__fmul2_rn(make_float2(a[0], a[1]), both(0x1p120f)), both(scale_m));
+        const float2 y = __fmul2_rn(__fmul2_rn(make_float2(b[0], b[1]), both(0x1p112f)), both(scale_v));
+        to_m[j] = x.x, to_m[j + 1] = x.y;
+        to_v[j] = y.x, to_v[j + 1] = y.y;
+    }
+}
+
+// draws: of the four elements, two to a word.
+__device__ __forceinline__ void encode4(const float* m, const float* v, float inverse_m, float inverse_v, const uint32_t* draws,
+                                        uint32_t& codes_m, uint32_t& codes_v)
+{
+    uint32_t at_top_m[4], at_top_v[4];
+    const uint32_t least = inverse_v > 0.0f ? 1u << 21 : 0u;
+#pragma unroll
+    for (int j = 0; j < 4; j += 2) {
+        const float2 x = __fmul2_rn(__fmul2_rn(make_float2(m[j], m[j + 1]), both(inverse_m)), both(0x1p-120f));
+        const float2 y = __fmul2_rn(__fmul2_rn(make_float2(v[j], v[j + 1]), both(inverse_v)), both(0x1p-112f));
+        const uint32_t h = draws[j / 2], turned = __byte_perm(h, 0, 0x2301);
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const uint32_t draw_m = (i ? h >> 12 : h << 4) & 0xFFFF0u | 8u, draw_v = (i ? turned >> 11 : turned << 5) & 0x1FFFE0u | 16u;
+            const uint32_t bits_m = __float_as_uint(i ? x.y : x.x) + draw_m;        // below the sign the sum has 27 bits
+            const uint32_t bits_v = __float_as_uint(i ? y.y : y.x) + draw_v;
+            at_top_m[j + i] = bits_m & 0x80000000u | bits_m << 4 & 0x7FFFFFFFu;
+            at_top_v[j + i] = max(bits_v, v[j + i] > 0.0f ? least : 0u) << 3;
+        }
+    }
+    codes_m = __byte_perm(__byte_perm(at_top_m[0], at_top_m[1], 0x0073), __byte_perm(at_top_m[2], at_top_m[3], 0x0073), 0x5410);
+    codes_v = __byte_perm(__byte_perm(at_top_v[0], at_top_v[1], 0x0073), __byte_perm(at_top_v[2], at_top_v[3], 0x0073), 0x5410);
+}
+
+// One block of one tensor.
+struct Block {
+    void* p;
+    const void* g;
+    void* m;
+    void* v;
+    float* scales;
+    uint64_t e0, group0;     // first element; number of the block's first group of draws
+    uint32_t held;
+    float decay;
+    uint32_t kind;
+};
+
+__device__ __forceinline__ void draw(uint64_t group, const Step& st, const RoundKeys& keys, uint32_t (&y)[4])
+{
+    philox4x32_10((uint32_t)group, (uint32_t)(group >> 32), 0xFFFFFFFFu, st.t, keys, y);
+}
+
+// A whole block on the boundaries of four elements: lane l has the elements 4 l .. 4 l + 3 and 128 + 4 l .. 128 + 4 l + 3, those it draws
+// for.
+template <int P, int G, bool EIGHT>
+__device__ __forceinline__ void step_vectors(const Block& b, const Scalars& s)
+{
+    const uint32_t lane = threadIdx.x & 31;
+    Packed<P, 4> pp[2];
+    Packed<G, 4> pg[2];
+    float p[8], g[8], m[8], v[8];
+    const uint64_t e = b.e0 + lane * 4;
+    auto* at_p = static_cast<typename Element<P>::type*>(b.p) + e;
+    const auto* at_g = static_cast<const typename Element<G>::type*>(b.g) + e;
+    uint32_t code_m[2], code_v[2];
+    float4 wide_m[2], wide_v[2];
+    float scale_m = 0.0f, scale_v = 0.0f;
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+        pp[k].load(at_p + 128 * k);
+        pg[k].load(at_g + 128 * k);
+        if (EIGHT) {
+            code_m[k] = __ldcg(reinterpret_cast<const uint32_t*>(static_cast<const uint8_t*>(b.m) + e) + 32 * k);
+            code_v[k] = __ldcg(reinterpret_cast<const uint32_t*>(static_cast<const uint8_t*>(b.v) + e) + 32 * k);
+        } else {
+            wide_m[k] = __ldcg(reinterpret_cast<const float4*>(static_cast<const float*>(b.m) + e) + 32 * k);
+            wide_v[k] = __ldcg(reinterpret_cast<const float4*>(static_cast<const float*>(b.v) + e) + 32 * k);
+        }
+    }
+    if (EIGHT) {
+        scale_m = __ldcg(b.scales);
+        scale_v = __ldcg(b.scales + 1);
+    }
     const Step st(s);
-    if (st.skip || e0 >= size) return;
-    const uint32_t held = (uint32_t)min((uint64_t)kBlock, size - e0);
-    const float rate = __fmul_rn(st.lr, decay);
+    if (st.skip) return;
+    const float rate = __fmul_rn(st.lr, b.decay);
+    uint32_t y[4];
+    if (EIGHT) draw(b.group0 + lane, st, s.keys, y);
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+        widen_to<P, 4>(pp[k], p + 4 * k);
+        widen_to<G, 4>(pg[k], g + 4 * k);
+        if (EIGHT) {
+            decode4(code_m[k], code_v[k], scale_m, scale_v, m + 4 * k, v + 4 * k);
+        } else {
+            *reinterpret_cast<float4*>(m + 4 * k) = wide_m[k];
+            *reinterpret_cast<float4*>(v + 4 * k) = wide_v[k];
+        }
+    }
+    float most_m = 0.0f, most_v = 0.0f;
+#pragma unroll
+    for (int i = 0; i < 8; i += 2) {
+        update2(p + i, g + i, m + i, v + i, s, st, rate);
+        if (EIGHT) {
+            most_m = fmaxf(most_m, fmaxf(fabsf(m[i]), fabsf(m[i + 1])));
+            most_v = fmaxf(most_v, fmaxf(v[i], v[i + 1]));
+        }
+    }
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) pp[k].set(i, p[4 * k + i]);
+        pp[k].store(at_p + 128 * k);
+        if (!EIGHT) {
+            reinterpret_cast<float4*>(static_cast<float*>(b.m) + e)[32 * k] = *reinterpret_cast<float4*>(m + 4 * k);
+            reinterpret_cast<float4*>(static_cast<float*>(b.v) + e)[32 * k] = *reinterpret_cast<float4*>(v + 4 * k);
+        }
+    }
+    if (!EIGHT) return;
+    float inverse_m, inverse_v;
+    scale_of(warp_max(most_m), kTopM, scale_m, inverse_m);
+    scale_of(warp_max(most_v), kTopV, scale_v, inverse_v);
+    if (lane == 0) {
+        b.scales[0] = scale_m;
+        b.scales[1] = scale_v;
+    }
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+        encode4(m + 4 * k, v + 4 * k, inverse_m, inverse_v, y + 2 * k, code_m[k], code_v[k]);
+        reinterpret_cast<uint32_t*>(static_cast<uint8_t*>(b.m) + e)[32 * k] = code_m[k];
+        reinterpret_cast<uint32_t*>(static_cast<uint8_t*>(b.v) + e)[32 * k] = code_v[k];
+    }
+}
+
+// Any block, lanes side by side.  draws: 32 words of 16 bytes for this warp.
+template <bool EIGHT> __device__ __forceinline__ void step_elements(const Block& b, const Scalars& s, uint4* draws)
+{
+    const uint32_t lane = threadIdx.x & 31;
+    const bool half_p = b.kind & 1, half_g = b.kind & 2;
     float p[kPerLane], g[kPerLane], m[kPerLane], v[kPerLane];
     float scale_m = 0.0f, scale_v = 0.0f;
     if (EIGHT) {
-        scale_m = __ldcg(tab.scales[j] + 2 * block);
-        scale_v = __ldcg(tab.scales[j] + 2 * block + 1);
+        scale_m = __ldcg(b.scales);
+        scale_v = __ldcg(b.scales + 1);
     }
 #pragma unroll
     for (int i = 0; i < kPerLane; ++i) {
         const uint32_t at = lane + 32 * i;
-        const uint64_t e = e0 + at;
+        const uint64_t e = b.e0 + at;
         p[i] = g[i] = m[i] = v[i] = 0.0f;
-        if (at >= held) continue;
-        p[i] = load(tab.p[j], !wide_p, e);
-        g[i] = load(tab.g[j], !wide_g, e);
+        if (at >= b.held) continue;
+        p[i] = load(b.p, half_p, e);
+        g[i] = load(b.g, half_g, e);
         if (EIGHT) {
-            m[i] = decode_m(static_cast<const uint8_t*>(tab.m[j])[e], scale_m);
-            v[i] = decode_v(static_cast<const uint8_t*>(tab.v[j])[e], scale_v);
+            m[i] = decode_m(static_cast<const uint8_t*>(b.m)[e], scale_m);
+            v[i] = decode_v(static_cast<const uint8_t*>(b.v)[e], scale_v);
         } else {
-            m[i] = static_cast<const float*>(tab.m[j])[e];
-            v[i] = static_cast<const float*>(tab.v[j])[e];
+            m[i] = static_cast<const float*>(b.m)[e];
+            v[i] = static_cast<const float*>(b.v)[e];
         }
     }
+    const Step st(s);
+    if (st.skip) return;
+    const float rate = __fmul_rn(st.lr, b.decay);
     float most_m = 0.0f, most_v = 0.0f;
 #pragma unroll
     for (int i = 0; i < kPerLane; ++i) {
         update(p[i], g[i], m[i], v[i], s, st, rate);
         const uint32_t at = lane + 32 * i;
-        if (at >= held) continue;
-        store(tab.p[j], !wide_p, e0 + at, p[i]);
+        if (at >= b.held) continue;
+        store(b.p, half_p, b.e0 + at, p[i]);
         if (!EIGHT) {
-            static_cast<float*>(tab.m[j])[e0 + at] = m[i];
-            static_cast<float*>(tab.v[j])[e0 + at] = v[i];
+            static_cast<float*>(b.m)[b.e0 + at] = m[i];
+            static_cast<float*>(b.v)[b.e0 + at] = v[i];
         }
         most_m = fmaxf(most_m, fabsf(m[i]));
         most_v = fmaxf(most_v, v[i]);
@@ -198,26 +364,51 @@ __global__ void __launch_bounds__(kThreads) adamw_kernel(const __grid_constant__
     scale_of(warp_max(most_m), kTopM, scale_m, inverse_m);
     scale_of(warp_max(most_v), kTopV, scale_v, inverse_v);
     if (lane == 0) {
-        tab.scales[j][2 * block] = scale_m;
-        tab.scales[j][2 * block + 1] = scale_v;
+        b.scales[0] = scale_m;
+        b.scales[1] = scale_v;
     }
-    // lane l draws for the elements 4 l .. 4 l + 3 and 128 + 4 l .. 128 + 4 l + 3 of the block
-    const uint64_t group = (tab.first_block[j] + block) * 32 + lane;
-    const RoundKeys keys = make_round_keys({s.seed_lo, s.seed_hi, 0xFFFFFFFFu, st.t});
     uint32_t y[4];
-    philox4x32_10((uint32_t)group, (uint32_t)(group >> 32), 0xFFFFFFFFu, st.t, keys, y);
-    draws[warp][lane] = make_uint4(y[0], y[1], y[2], y[3]);
+    draw(b.group0 + lane, st, s.keys, y);
+    draws[lane] = make_uint4(y[0], y[1], y[2], y[3]);
     __syncwarp();
-    const uint16_t* half = reinterpret_cast<const uint16_t*>(draws[warp]);
+    const uint16_t* half = reinterpret_cast<const uint16_t*>(draws);
 #pragma unroll
     for (int i = 0; i < kPerLane; ++i) {
         const uint32_t at = lane + 32 * i;
-        if (at >= held) continue;
+        if (at >= b.held) continue;
         const uint32_t h = half[(at % 128 / 4) * 8 + at / 128 * 4 + at % 4];
-        static_cast<uint8_t*>(tab.m[j])[e0 + at] = (uint8_t)encode_m(m[i], inverse_m, h);
-        static_cast<uint8_t*>(tab.v[j])[e0 + at] = (uint8_t)encode_v(v[i], inverse_v, h);
+        static_cast<uint8_t*>(b.m)[b.e0 + at] = (uint8_t)encode_m(m[i], inverse_m, h);
+        static_cast<uint8_t*>(b.v)[b.e0 + at] = (uint8_t)encode_v(v[i], inverse_v, h);
     }
 }
+
+// A warp to a block.
+template <int CAP, bool EIGHT>
+__global__ void __launch_bounds__(kThreads) adamw_kernel(const __grid_constant__ AdamwTable<CAP> tab, const __grid_constant__ Scalars s)
+{
+    __shared__ uint4 draws[EIGHT ? kWarps : 1][32];
+    const int j = find_in_list<(CAP > 32)>(tab.tile_start, tab.count, blockIdx.x);
+    const uint32_t warp = threadIdx.x >> 5;
+    const uint64_t block = (uint64_t)(blockIdx.x - tab.tile_start[j]) * kWarps + warp, size = tab.size[j];
+    Block b;
+    b.e0 = block * kBlock;
+    b.p = tab.p[j];
+    b.g = tab.g[j];
+    b.m = tab.m[j];
+    b.v = tab.v[j];
+    b.scales = EIGHT ? tab.scales[j] + 2 * block : nullptr;
+    b.group0 = (tab.first_block[j] + block) * 32;
+    b.decay = tab.decay[j];
+    b.kind = tab.kind[j];
+    grid_dependency_wait();
+    if (b.e0 >= size) return;
+    b.held = (uint32_t)min((uint64_t)kBlock, size - b.e0);
+    if (!(b.kind & 4) || b.held < kBlock) step_elements<EIGHT>(b, s, draws[EIGHT ? warp : 0]);
+    else if (b.kind & 1) b.kind & 2 ? step_vectors<kBf16, kBf16, EIGHT>(b, s) : step_vectors<kBf16, kF32, EIGHT>(b, s);
+    else b.kind & 2 ? step_vectors<kF32, kBf16, EIGHT>(b, s) : step_vectors<kF32, kF32, EIGHT>(b, s);
+}
+
+bool on_boundary(const void* p, uintptr_t bytes) { return (reinterpret_cast<uintptr_t>(p) & (bytes - 1)) == 0; }
 
 uint64_t blocks_of(uint64_t n) { return (n + kBlock - 1) / kBlock; }
 
@@ -236,7 +427,10 @@ template <int CAP> cudaError_t launch_table(const AdamwList& list, int first, in
         tab.scales[k] = list.scales ? list.scales[j] : nullptr;
         tab.first_block[k] = blocks;
         tab.decay[k] = list.decay ? list.decay[j] : 0.0f;
-        tab.kind[k] = (uint8_t)((list.p_dtype[j] == kBf16 ? 1 : 0) | (list.g_dtype[j] == kBf16 ? 2 : 0));
+        const int half_p = list.p_dtype[j] == kBf16, half_g = list.g_dtype[j] == kBf16, state = list.scales ? 4 : 16;
+        const bool fit = on_boundary(list.p[j], half_p ? 8 : 16) && on_boundary(list.g[j], half_g ? 8 : 16) &&
+                         on_boundary(list.m[j], state) && on_boundary(list.v[j], state);
+        tab.kind[k] = (uint8_t)(half_p | half_g << 1 | fit << 2);
         blocks += blocks_of(list.size[j]);
         tiles += (blocks_of(list.size[j]) + kWarps - 1) / kWarps;
     }
@@ -261,11 +455,14 @@ cudaError_t launch_adamw(const AdamwList& list, const AdamwStep& step, cudaStrea
     s.c1 = (float)(1.0 - std::pow(step.beta1, (double)step.t));
     s.c2 = (float)(1.0 - std::pow(step.beta2, (double)step.t));
     s.grad_scale = step.grad_scale;
+    s.minus_zero = -0.0f;
     s.factor = step.factor;
     s.schedule = step.schedule;
     s.step = step.t;
-    s.seed_lo = (uint32_t)step.seed;
-    s.seed_hi = (uint32_t)(step.seed >> 32);
+    for (uint32_t r = 0; r < 10; ++r) {
+        s.keys.k0[r] = (uint32_t)step.seed + r * 0x9E3779B9u;
+        s.keys.k1[r] = (uint32_t)(step.seed >> 32) + r * 0xBB67AE85u;
+    }
     uint64_t blocks = 0;
     cudaError_t err = cudaSuccess;
     for (int first = 0; first < list.count && err == cudaSuccess; first += kLargeTable) {

@@ -156,22 +156,6 @@ template <int BYTES> __device__ __forceinline__ void copy_async(void* to, const 
 __device__ __forceinline__ void commit_copies() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int N> __device__ __forceinline__ void wait_copies() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
 
-// V consecutive elements as pairs of fp32 (V = 1: one of a pair).
-template <int DTYPE, int V> __device__ __forceinline__ void widen_to(const Packed<DTYPE, V>& in, float* out)
-{
-    if constexpr (DTYPE == kBf16 && V > 1) {
-        const auto* w = reinterpret_cast<const uint32_t*>(&in);
-#pragma unroll
-        for (int k = 0; k < V / 2; ++k) {
-            out[2 * k] = __uint_as_float(w[k] << 16);
-            out[2 * k + 1] = __uint_as_float(w[k] & 0xFFFF0000u);
-        }
-    } else {
-#pragma unroll
-        for (int e = 0; e < V; ++e) out[e] = in.get(e);
-    }
-}
-
 // Whether rows x dim elements keep less than the threads of a device busy, 8 elements to a thread: then more elements to a thread
 // take longer.
 inline bool few_elements(uint64_t rows, uint64_t dim) { return rows * dim <= 148ull * 2 * kRowThreads * 8; }

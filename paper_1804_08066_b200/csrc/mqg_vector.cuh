@@ -50,6 +50,22 @@ template <int DTYPE, int V> struct Packed {
     __device__ __forceinline__ void set(int i, float x) { narrow(x, e[i]); }
 };
 
+// The V elements of `in` in fp32; a pair of bf16 by a shift and a mask.
+template <int DTYPE, int V> __device__ __forceinline__ void widen_to(const Packed<DTYPE, V>& in, float* out)
+{
+    if constexpr (DTYPE == kBf16 && V > 1) {
+        const auto* w = reinterpret_cast<const uint32_t*>(&in);
+#pragma unroll
+        for (int k = 0; k < V / 2; ++k) {
+            out[2 * k] = __uint_as_float(w[k] << 16);
+            out[2 * k + 1] = __uint_as_float(w[k] & 0xFFFF0000u);
+        }
+    } else {
+#pragma unroll
+        for (int e = 0; e < V; ++e) out[e] = in.get(e);
+    }
+}
+
 // The longest vector of at most `most` elements that divides rows of `dim` elements and starts on its accesses' boundaries
 // in both buffers (a null buffer fits all).
 inline int row_vector(int most, uint64_t dim, const void* a, int a_bytes, const void* b, int b_bytes)

@@ -16,10 +16,11 @@ def step64(p, g, m, v, *, lr, beta1, beta2, eps, step, decay, k=1.0):
     a = lr / (1 - beta1 ** step)
     p2 = p - (lr * decay * p + a * m2 / d)
     # Roundings of 2^-24 each.  m': 3 and those of b1, w1 and k g, of the parts that may cancel.  d: v' 5 and b2, w2, k g twice, halved
-    # by the root; the root 2, r2 3, the product, eps and the sum: 13.  Quotient 2, a 3, product 1: 24 of the whole term.  rate p: 3,
+    # by the root; the root 2, r2 3, the product, eps and the sum: 13.  Quotient 4 (two units in the last place), a 3, product 1: 26 of the whole
+    # term, where its parts do not cancel, and 2 more for m's.  rate p: 3,
     # the sum 1; the difference 1 of p'.
     term = a * (np.abs(beta1 * m) + np.abs((1 - beta1) * g)) / d
-    slack = 2.0 ** -24 * (np.abs(p2) + 5 * np.abs(lr * decay * p) + 26 * term) + 1e-44
+    slack = 2.0 ** -24 * (np.abs(p2) + 5 * np.abs(lr * decay * p) + 28 * term) + 1e-44
     return p2, m2, v2, slack
 
 
