@@ -16,6 +16,8 @@
 // under the root.
 //
 // Bound by memory: 28 bytes an element in fp32, 16 with states in 8 bits.
+#include <cuda_fp16.h>
+
 #include <cmath>
 
 #include "mqg_common.cuh"
@@ -35,7 +37,7 @@ constexpr float kTopM = 448.0f, kTopV = 57344.0f, kLeast = 0x1p-110f;       // b
 // Tensors of one launch, passed by value: a kernel's parameters hold 32,764 bytes.
 template <int CAP> struct AdamwTable {
     int count;
-    uint32_t tile_start[CAP + 1];                       // a tile is kWarps blocks
+    uint32_t tile_start[CAP + 1];                       // a tile is the blocks of a CTA
     uint64_t size[CAP];
     void* p[CAP];
     const void* g[CAP];
@@ -48,47 +50,69 @@ template <int CAP> struct AdamwTable {
 };
 constexpr int kLargeTable = 448;
 
+// Turns of a warp, where there are blocks for four times the warps that the device holds.
+constexpr uint32_t kTurns = 4, kManyBlocks = 148 * 4 * kWarps * 4;
+
 struct Scalars {
-    float b1, w1, b2, w2, eps, lr, c1, c2, grad_scale, minus_zero;
+    float b1, w1, b2, w2, eps, lr, a, r2, grad_scale, minus_zero;
     const float* factor;
     const float* schedule;
     uint32_t step;
     RoundKeys keys;
 };
 
+// lr / c1 and 1 / sqrt(c2), each operation rounded; the same on the host and on the device.
+__host__ __device__ inline float step_size(float lr, float c1)
+{
+#ifdef __CUDA_ARCH__
+    return __fdiv_rn(lr, c1);
+#else
+    return lr / c1;
+#endif
+}
+__host__ __device__ inline float reciprocal_root(float c2)
+{
+#ifdef __CUDA_ARCH__
+    return __fdiv_rn(1.0f, __fsqrt_rn(c2));
+#else
+    return 1.0f / std::sqrt(c2);
+#endif
+}
+
 // What a step takes from the device's memory, and what follows from it.
 struct Step {
     float k, a, r2, lr;
     uint32_t t;
     bool skip;
-    __device__ __forceinline__ explicit Step(const Scalars& s)
+    __device__ __forceinline__ explicit Step(const Scalars& s) : k(s.grad_scale), a(s.a), r2(s.r2), lr(s.lr), t(s.step), skip(false)
     {
-        const bool from_device = s.schedule != nullptr;
-        lr = from_device ? __ldcg(s.schedule) : s.lr;
-        const float c1 = from_device ? __ldcg(s.schedule + 1) : s.c1, c2 = from_device ? __ldcg(s.schedule + 2) : s.c2;
-        t = from_device ? (uint32_t)__ldcg(s.schedule + 3) : s.step;
-        const float f = s.factor != nullptr ? __ldcg(s.factor) : 1.0f;
-        k = __fmul_rn(s.grad_scale, f);
-        skip = !(fabsf(f) > 0.0f && fabsf(f) < INFINITY);
-        a = __fdiv_rn(lr, c1);
-        r2 = __fdiv_rn(1.0f, __fsqrt_rn(c2));
+        if (s.factor != nullptr) {
+            const float f = __ldcg(s.factor);
+            skip = !(fabsf(f) > 0.0f && fabsf(f) < INFINITY);
+            k = __fmul_rn(s.grad_scale, f);
+        }
+        if (s.schedule != nullptr) {
+            lr = __ldcg(s.schedule);
+            a = step_size(lr, __ldcg(s.schedule + 1));
+            r2 = reciprocal_root(__ldcg(s.schedule + 2));
+            t = (uint32_t)__ldcg(s.schedule + 3);
+        }
     }
 };
 
+// sqrt(x), x >= 0, within two roundings; zero below 2^-126.
 __device__ __forceinline__ float root(float x)
 {
     float r;
-    asm("sqrt.approx.f32 %0, %1;" : "=f"(r) : "f"(x));
+    asm("sqrt.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
     return r;
 }
-
-__device__ __forceinline__ void update(float& p, float g, float& m, float& v, const Scalars& s, const Step& st, float rate)
+// 1 / d within two roundings, 2^-50 <= d < 2^77.
+__device__ __forceinline__ float reciprocal(float d)
 {
-    g = __fmul_rn(st.k, g);
-    m = __fadd_rn(__fmul_rn(s.b1, m), __fmul_rn(s.w1, g));
-    v = __fadd_rn(__fmul_rn(s.b2, v), __fmul_rn(__fmul_rn(s.w2, g), g));
-    const float d = __fmaf_rn(root(v), st.r2, s.eps);                       // 2^-50 <= d < 2^70
-    p = __fsub_rn(p, __fmaf_rn(st.a, __fdividef(m, d), __fmul_rn(rate, p)));
+    float r;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(d));
+    return r;
 }
 
 __device__ __forceinline__ float2 both(float x) { return make_float2(x, x); }
@@ -97,7 +121,7 @@ __device__ __forceinline__ float2 both(float x) { return make_float2(x, x); }
 // says of its rounding): a sum with -0, which the compiler does not know.
 __device__ __forceinline__ float2 times(float2 a, float2 b, float minus_zero) { return __ffma2_rn(a, b, both(minus_zero)); }
 
-// The same for two elements, by packed instructions, which round as the single ones do.
+// The step of two elements, by packed instructions, which round as the single ones do.
 __device__ __forceinline__ void update2(float* p, const float* g_in, float* m, float* v, const Scalars& s, const Step& st, float rate)
 {
     const float z = s.minus_zero;
@@ -105,7 +129,7 @@ __device__ __forceinline__ void update2(float* p, const float* g_in, float* m, f
     const float2 m2 = __fadd2_rn(times(both(s.b1), make_float2(m[0], m[1]), z), times(both(s.w1), g, z));
     const float2 v2 = __fadd2_rn(times(both(s.b2), make_float2(v[0], v[1]), z), times(times(both(s.w2), g, z), g, z));
     const float2 d = __ffma2_rn(make_float2(root(v2.x), root(v2.y)), both(st.r2), both(s.eps));
-    const float2 u = make_float2(__fdividef(m2.x, d.x), __fdividef(m2.y, d.y));
+    const float2 u = __fmul2_rn(m2, make_float2(reciprocal(d.x), reciprocal(d.y)));
     const float2 less = __ffma2_rn(both(st.a), u, __fmul2_rn(both(rate), old));
     p[0] = old.x - less.x, p[1] = old.y - less.y;
     m[0] = m2.x, m[1] = m2.y;
@@ -150,42 +174,31 @@ __device__ __forceinline__ uint32_t encode_v(float v, float inverse, uint32_t h)
     return max(code, min(__float_as_uint(v), inverse > 0.0f ? 1u : 0u));
 }
 
-// A block's scale and what its elements are multiplied with for their codes, from its largest magnitude.
-__device__ __forceinline__ void scale_of(float most, float top, float& scale, float& inverse)
-{
-    const bool held = most >= kLeast;
-    scale = held ? __fdiv_rn(most, top) : 0.0f;
-    inverse = held ? __fdiv_rn(top, most) : 0.0f;
-}
-
 // Largest of a warp's non-negative floats.
 __device__ __forceinline__ float warp_max(float x) { return __uint_as_float(__reduce_max_sync(0xFFFFFFFFu, __float_as_uint(x))); }
 
-__device__ __forceinline__ float load(const void* p, bool bf16, uint64_t i)
+// A block's two scales, which it stores, and what its elements are multiplied with for their codes.  One division for the warp: lane
+// 0 has m's scale, 1 its inverse, 2 and 3 those of v.
+__device__ __forceinline__ void new_scales(float most_m, float most_v, float* scales, float& inverse_m, float& inverse_v)
 {
-    return bf16 ? __bfloat162float(static_cast<const __nv_bfloat16*>(p)[i]) : static_cast<const float*>(p)[i];
-}
-__device__ __forceinline__ void store(void* p, bool bf16, uint64_t i, float x)
-{
-    if (bf16) static_cast<__nv_bfloat16*>(p)[i] = __float2bfloat16_rn(x);
-    else static_cast<float*>(p)[i] = x;
+    const uint32_t lane = threadIdx.x & 31;
+    const float all_m = warp_max(most_m), all_v = warp_max(most_v), most = lane & 2 ? all_v : all_m, top = lane & 2 ? kTopV : kTopM;
+    const float q = most >= kLeast ? __fdiv_rn(lane & 1 ? top : most, lane & 1 ? most : top) : 0.0f;
+    if (lane == 0 || lane == 2) scales[lane >> 1] = q;
+    inverse_m = __shfl_sync(0xFFFFFFFFu, q, 1);
+    inverse_v = __shfl_sync(0xFFFFFFFFu, q, 3);
 }
 
-// Four codes in a word, and back; all of one block.
+// Four codes in a word, and back; all of one block.  fp16 holds the values of both formats: e5m2 is its upper byte.
 __device__ __forceinline__ void decode4(uint32_t m, uint32_t v, float scale_m, float scale_v, float* to_m, float* to_v)
 {
 #pragma unroll
     for (int j = 0; j < 4; j += 2) {
-        float a[2], b[2];
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            // a byte at the top; three bits of exponent between the sign and the code
-            const uint32_t top_m = __byte_perm(m, 0, 0x0444 | (j + i) << 12), top_v = __byte_perm(v, 0, 0x0444 | (j + i) << 12);
-            a[i] = __uint_as_float((uint32_t)((int32_t)top_m >> 4) & 0x87F00000u);
-            b[i] = __uint_as_float(top_v >> 3);
-        }
-        const float2 x = __fmul2_rn(__fmul2_rn(make_float2(a[0], a[1]), both(0x1p120f)), both(scale_m));
-        const float2 y = __fmul2_rn(__fmul2_rn(make_float2(b[0], b[1]), both(0x1p112f)), both(scale_v));
+        uint32_t half_m;
+        asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(half_m) : "h"((uint16_t)(j ? m >> 16 : m)));
+        const uint32_t half_v = __byte_perm(v, 0, j ? 0x3424 : 0x1404);
+        const float2 x = __fmul2_rn(__half22float2(*reinterpret_cast<const __half2*>(&half_m)), both(scale_m));
+        const float2 y = __fmul2_rn(__half22float2(*reinterpret_cast<const __half2*>(&half_v)), both(scale_v));
         to_m[j] = x.x, to_m[j + 1] = x.y;
         to_v[j] = y.x, to_v[j + 1] = y.y;
     }
@@ -214,6 +227,9 @@ __device__ __forceinline__ void encode4(const float* m, const float* v, float in
     codes_m = __byte_perm(__byte_perm(at_top_m[0], at_top_m[1], 0x0073), __byte_perm(at_top_m[2], at_top_m[3], 0x0073), 0x5410);
     codes_v = __byte_perm(__byte_perm(at_top_v[0], at_top_v[1], 0x0073), __byte_perm(at_top_v[2], at_top_v[3], 0x0073), 0x5410);
 }
+
+template <bool EIGHT> struct StateType { using type = float; };
+template <> struct StateType<true> { using type = uint8_t; };
 
 // One block of one tensor.
 struct Block {
@@ -301,12 +317,7 @@ __device__ __forceinline__ void step_vectors(const Block& b, const Scalars& s)
     }
     if (!EIGHT) return;
     float inverse_m, inverse_v;
-    scale_of(warp_max(most_m), kTopM, scale_m, inverse_m);
-    scale_of(warp_max(most_v), kTopV, scale_v, inverse_v);
-    if (lane == 0) {
-        b.scales[0] = scale_m;
-        b.scales[1] = scale_v;
-    }
+    new_scales(most_m, most_v, b.scales, inverse_m, inverse_v);
 #pragma unroll
     for (int k = 0; k < 2; ++k) {
         encode4(m + 4 * k, v + 4 * k, inverse_m, inverse_v, y + 2 * k, code_m[k], code_v[k]);
@@ -315,104 +326,129 @@ __device__ __forceinline__ void step_vectors(const Block& b, const Scalars& s)
     }
 }
 
-// Any block, lanes side by side.  draws: 32 words of 16 bytes for this warp.
-template <bool EIGHT> __device__ __forceinline__ void step_elements(const Block& b, const Scalars& s, uint4* draws)
+// Any block, lanes side by side.  WHOLE: it has all of its elements.  draws: 32 words of 16 bytes for this warp.
+template <int P, int G, bool EIGHT, bool WHOLE>
+__device__ __forceinline__ void step_elements(const Block& b, const Scalars& s, uint4* draws)
 {
+    using State = typename StateType<EIGHT>::type;
     const uint32_t lane = threadIdx.x & 31;
-    const bool half_p = b.kind & 1, half_g = b.kind & 2;
-    float p[kPerLane], g[kPerLane], m[kPerLane], v[kPerLane];
+    const uint64_t first = b.e0 + lane;
+    auto* at_p = static_cast<typename Element<P>::type*>(b.p) + first;
+    const auto* at_g = static_cast<const typename Element<G>::type*>(b.g) + first;
+    auto* at_m = static_cast<State*>(b.m) + first;
+    auto* at_v = static_cast<State*>(b.v) + first;
+    const auto has = [&](int i) { return WHOLE || lane + 32 * i < b.held; };
+    typename Element<P>::type in_p[kPerLane];
+    typename Element<G>::type in_g[kPerLane];
+    State in_m[kPerLane], in_v[kPerLane];
     float scale_m = 0.0f, scale_v = 0.0f;
+#pragma unroll
+    for (int i = 0; i < kPerLane; ++i) {
+        in_p[i] = has(i) ? __ldcg(at_p + 32 * i) : typename Element<P>::type(0.0f);
+        in_g[i] = has(i) ? __ldcg(at_g + 32 * i) : typename Element<G>::type(0.0f);
+        in_m[i] = has(i) ? __ldcg(at_m + 32 * i) : State(0);
+        in_v[i] = has(i) ? __ldcg(at_v + 32 * i) : State(0);
+    }
     if (EIGHT) {
         scale_m = __ldcg(b.scales);
         scale_v = __ldcg(b.scales + 1);
     }
-#pragma unroll
-    for (int i = 0; i < kPerLane; ++i) {
-        const uint32_t at = lane + 32 * i;
-        const uint64_t e = b.e0 + at;
-        p[i] = g[i] = m[i] = v[i] = 0.0f;
-        if (at >= b.held) continue;
-        p[i] = load(b.p, half_p, e);
-        g[i] = load(b.g, half_g, e);
-        if (EIGHT) {
-            m[i] = decode_m(static_cast<const uint8_t*>(b.m)[e], scale_m);
-            v[i] = decode_v(static_cast<const uint8_t*>(b.v)[e], scale_v);
-        } else {
-            m[i] = static_cast<const float*>(b.m)[e];
-            v[i] = static_cast<const float*>(b.v)[e];
-        }
-    }
     const Step st(s);
     if (st.skip) return;
     const float rate = __fmul_rn(st.lr, b.decay);
+    float p[kPerLane], g[kPerLane], m[kPerLane], v[kPerLane];
     float most_m = 0.0f, most_v = 0.0f;
 #pragma unroll
     for (int i = 0; i < kPerLane; ++i) {
-        update(p[i], g[i], m[i], v[i], s, st, rate);
-        const uint32_t at = lane + 32 * i;
-        if (at >= b.held) continue;
-        store(b.p, half_p, b.e0 + at, p[i]);
-        if (!EIGHT) {
-            static_cast<float*>(b.m)[b.e0 + at] = m[i];
-            static_cast<float*>(b.v)[b.e0 + at] = v[i];
+        p[i] = widen(in_p[i]);
+        g[i] = widen(in_g[i]);
+        if constexpr (EIGHT) {
+            m[i] = decode_m(in_m[i], scale_m);
+            v[i] = decode_v(in_v[i], scale_v);
+        } else {
+            m[i] = in_m[i];
+            v[i] = in_v[i];
         }
-        most_m = fmaxf(most_m, fabsf(m[i]));
-        most_v = fmaxf(most_v, v[i]);
     }
-    if (!EIGHT) return;
-    float inverse_m, inverse_v;
-    scale_of(warp_max(most_m), kTopM, scale_m, inverse_m);
-    scale_of(warp_max(most_v), kTopV, scale_v, inverse_v);
-    if (lane == 0) {
-        b.scales[0] = scale_m;
-        b.scales[1] = scale_v;
+#pragma unroll
+    for (int i = 0; i < kPerLane; i += 2) {
+        update2(p + i, g + i, m + i, v + i, s, st, rate);
+        if (EIGHT) {
+            most_m = fmaxf(most_m, fmaxf(fabsf(m[i]), fabsf(m[i + 1])));            // (places without elements stay zeros)
+            most_v = fmaxf(most_v, fmaxf(v[i], v[i + 1]));
+        }
     }
-    uint32_t y[4];
-    draw(b.group0 + lane, st, s.keys, y);
-    draws[lane] = make_uint4(y[0], y[1], y[2], y[3]);
-    __syncwarp();
-    const uint16_t* half = reinterpret_cast<const uint16_t*>(draws);
 #pragma unroll
     for (int i = 0; i < kPerLane; ++i) {
-        const uint32_t at = lane + 32 * i;
-        if (at >= b.held) continue;
-        const uint32_t h = half[(at % 128 / 4) * 8 + at / 128 * 4 + at % 4];
-        static_cast<uint8_t*>(b.m)[b.e0 + at] = (uint8_t)encode_m(m[i], inverse_m, h);
-        static_cast<uint8_t*>(b.v)[b.e0 + at] = (uint8_t)encode_v(v[i], inverse_v, h);
+        if (!has(i)) continue;
+        narrow(p[i], at_p[32 * i]);
+        if constexpr (!EIGHT) {
+            at_m[32 * i] = m[i];
+            at_v[32 * i] = v[i];
+        }
+    }
+    if constexpr (EIGHT) {
+        float inverse_m, inverse_v;
+        new_scales(most_m, most_v, b.scales, inverse_m, inverse_v);
+        uint32_t y[4];
+        draw(b.group0 + lane, st, s.keys, y);
+        __syncwarp();                                   // the draws of the block before have been read
+        draws[lane] = make_uint4(y[0], y[1], y[2], y[3]);
+        __syncwarp();
+        // element lane + 32 i: group lane / 4 + 8 (i % 4), place 4 (i / 4) + lane % 4
+        const uint16_t* half = reinterpret_cast<const uint16_t*>(draws) + (lane / 4) * 8 + lane % 4;
+#pragma unroll
+        for (int i = 0; i < kPerLane; ++i) {
+            const uint32_t h = half[(i % 4) * 64 + (i / 4) * 4];
+            if (!has(i)) continue;
+            at_m[32 * i] = (uint8_t)encode_m(m[i], inverse_m, h);
+            at_v[32 * i] = (uint8_t)encode_v(v[i], inverse_v, h);
+        }
     }
 }
 
-// A warp to a block.
+template <int P, int G, bool EIGHT> __device__ __forceinline__ void step_block(const Block& b, const Scalars& s, uint4* draws)
+{
+    if (b.held < kBlock) step_elements<P, G, EIGHT, false>(b, s, draws);
+    else if (b.kind & 4) step_vectors<P, G, EIGHT>(b, s);
+    else step_elements<P, G, EIGHT, true>(b, s, draws);
+}
+
+// A warp to a block, `turns` times; a tile is the blocks that a CTA takes.
 template <int CAP, bool EIGHT>
-__global__ void __launch_bounds__(kThreads) adamw_kernel(const __grid_constant__ AdamwTable<CAP> tab, const __grid_constant__ Scalars s)
+__global__ void __launch_bounds__(kThreads, 4) adamw_kernel(const __grid_constant__ AdamwTable<CAP> tab, const __grid_constant__ Scalars s, uint32_t turns)
 {
     __shared__ uint4 draws[EIGHT ? kWarps : 1][32];
     const int j = find_in_list<(CAP > 32)>(tab.tile_start, tab.count, blockIdx.x);
     const uint32_t warp = threadIdx.x >> 5;
-    const uint64_t block = (uint64_t)(blockIdx.x - tab.tile_start[j]) * kWarps + warp, size = tab.size[j];
+    const uint64_t size = tab.size[j], first = (uint64_t)(blockIdx.x - tab.tile_start[j]) * (kWarps * turns) + warp;
     Block b;
-    b.e0 = block * kBlock;
     b.p = tab.p[j];
     b.g = tab.g[j];
     b.m = tab.m[j];
     b.v = tab.v[j];
-    b.scales = EIGHT ? tab.scales[j] + 2 * block : nullptr;
-    b.group0 = (tab.first_block[j] + block) * 32;
     b.decay = tab.decay[j];
     b.kind = tab.kind[j];
     grid_dependency_wait();
-    if (b.e0 >= size) return;
-    b.held = (uint32_t)min((uint64_t)kBlock, size - b.e0);
-    if (!(b.kind & 4) || b.held < kBlock) step_elements<EIGHT>(b, s, draws[EIGHT ? warp : 0]);
-    else if (b.kind & 1) b.kind & 2 ? step_vectors<kBf16, kBf16, EIGHT>(b, s) : step_vectors<kBf16, kF32, EIGHT>(b, s);
-    else b.kind & 2 ? step_vectors<kF32, kBf16, EIGHT>(b, s) : step_vectors<kF32, kF32, EIGHT>(b, s);
+    for (uint32_t turn = 0; turn < turns; ++turn) {
+        const uint64_t block = first + turn * kWarps;
+        b.e0 = block * kBlock;
+        if (b.e0 >= size) return;
+        b.held = (uint32_t)min((uint64_t)kBlock, size - b.e0);
+        b.scales = EIGHT ? tab.scales[j] + 2 * block : nullptr;
+        b.group0 = (tab.first_block[j] + block) * 32;
+        uint4* of_warp = draws[EIGHT ? warp : 0];
+        if (b.kind & 1) b.kind & 2 ? step_block<kBf16, kBf16, EIGHT>(b, s, of_warp) : step_block<kBf16, kF32, EIGHT>(b, s, of_warp);
+        else b.kind & 2 ? step_block<kF32, kBf16, EIGHT>(b, s, of_warp) : step_block<kF32, kF32, EIGHT>(b, s, of_warp);
+    }
 }
 
 bool on_boundary(const void* p, uintptr_t bytes) { return (reinterpret_cast<uintptr_t>(p) & (bytes - 1)) == 0; }
 
 uint64_t blocks_of(uint64_t n) { return (n + kBlock - 1) / kBlock; }
 
-template <int CAP> cudaError_t launch_table(const AdamwList& list, int first, int last, uint64_t& blocks, const Scalars& s, cudaStream_t stream)
+template <int CAP>
+cudaError_t launch_table(const AdamwList& list, int first, int last, uint64_t& blocks, const Scalars& s, uint32_t turns, cudaStream_t stream)
 {
     AdamwTable<CAP> tab;
     uint64_t tiles = 0;
@@ -432,13 +468,13 @@ template <int CAP> cudaError_t launch_table(const AdamwList& list, int first, in
                          on_boundary(list.m[j], state) && on_boundary(list.v[j], state);
         tab.kind[k] = (uint8_t)(half_p | half_g << 1 | fit << 2);
         blocks += blocks_of(list.size[j]);
-        tiles += (blocks_of(list.size[j]) + kWarps - 1) / kWarps;
+        tiles += (blocks_of(list.size[j]) + kWarps * turns - 1) / (kWarps * turns);
     }
     tab.tile_start[k] = (uint32_t)tiles;
     tab.count = k;
     if (tiles == 0) return cudaSuccess;
-    return list.scales ? launch_pdl(adamw_kernel<CAP, true>, (unsigned)tiles, kThreads, stream, tab, s)
-                       : launch_pdl(adamw_kernel<CAP, false>, (unsigned)tiles, kThreads, stream, tab, s);
+    return list.scales ? launch_pdl(adamw_kernel<CAP, true>, (unsigned)tiles, kThreads, stream, tab, s, turns)
+                       : launch_pdl(adamw_kernel<CAP, false>, (unsigned)tiles, kThreads, stream, tab, s, turns);
 }
 
 }  // namespace
@@ -452,8 +488,8 @@ cudaError_t launch_adamw(const AdamwList& list, const AdamwStep& step, cudaStrea
     s.w2 = (float)(1.0 - step.beta2);
     s.eps = (float)step.eps;
     s.lr = (float)step.lr;
-    s.c1 = (float)(1.0 - std::pow(step.beta1, (double)step.t));
-    s.c2 = (float)(1.0 - std::pow(step.beta2, (double)step.t));
+    s.a = step_size(s.lr, (float)(1.0 - std::pow(step.beta1, (double)step.t)));
+    s.r2 = reciprocal_root((float)(1.0 - std::pow(step.beta2, (double)step.t)));
     s.grad_scale = step.grad_scale;
     s.minus_zero = -0.0f;
     s.factor = step.factor;
@@ -464,12 +500,15 @@ cudaError_t launch_adamw(const AdamwList& list, const AdamwStep& step, cudaStrea
         s.keys.k1[r] = (uint32_t)(step.seed >> 32) + r * 0xBB67AE85u;
     }
     uint64_t blocks = 0;
+    for (int j = 0; j < list.count; ++j) blocks += blocks_of(list.size[j]);
+    const uint32_t turns = blocks > (uint64_t)kManyBlocks ? kTurns : 1;
+    blocks = 0;
     cudaError_t err = cudaSuccess;
     for (int first = 0; first < list.count && err == cudaSuccess; first += kLargeTable) {
         const int last = list.count - first > kLargeTable ? first + kLargeTable : list.count, n = last - first;
-        err = n <= 16   ? launch_table<16>(list, first, last, blocks, s, stream)
-              : n <= 96 ? launch_table<96>(list, first, last, blocks, s, stream)
-                        : launch_table<kLargeTable>(list, first, last, blocks, s, stream);
+        err = n <= 16   ? launch_table<16>(list, first, last, blocks, s, turns, stream)
+              : n <= 96 ? launch_table<96>(list, first, last, blocks, s, turns, stream)
+                        : launch_table<kLargeTable>(list, first, last, blocks, s, turns, stream);
     }
     return err;
 }
