@@ -477,7 +477,8 @@ mqg_status mqg_adamw(void* const* params, const mqg_dtype* param_dtypes, const v
  * scales[2 b] = max|m| / 448, scales[2 b + 1] = max v / 57344 of the block (0, and all its codes 0, where that maximum is below
  * 2^-110), and m * (448 / max|m|), v * (57344 / max v) are rounded to one of their two neighbours at random, up where the share
  * above the lower neighbour plus (h + 1/2) / 2^16 reaches 1: without bias, while rounding to nearest would not move an average whose
- * steps are small beside the distance of two codes.  A v above 0 never gets code 0.
+ * steps are small beside the distance of two codes.  A v of 2^-128 or more never
+ * gets code 0.
  *   seed    keys the draws: h has 16 bits of the Philox4x32-10 block with key = seed and counter = (q, 0xFFFFFFFF, step).  q = 32 B +
  *           l, B = blocks before this one in the whole list of the call, draws for the block's elements 4 l .. 4 l + 3 (words 0
  *           and 1, low half first) and 128 + 4 l .. 128 + 4 l + 3 (words 2 and 3); v takes h with its two bytes swapped.  The

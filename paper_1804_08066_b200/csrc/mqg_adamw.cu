@@ -20,6 +20,7 @@
 
 #include <cmath>
 
+#include "mqg_async.cuh"
 #include "mqg_common.cuh"
 #include "mqg_list.cuh"
 #include "mqg_tma.cuh"
@@ -79,23 +80,32 @@ __host__ __device__ inline float reciprocal_root(float c2)
 #endif
 }
 
-// What a step takes from the device's memory, and what follows from it.
+// What a step takes from the device's memory.
+struct FromDevice {
+    float factor, schedule[4];
+    __device__ __forceinline__ explicit FromDevice(const Scalars& s) : factor(s.factor != nullptr ? __ldcg(s.factor) : 1.0f)
+    {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) schedule[i] = s.schedule != nullptr ? __ldcg(s.schedule + i) : 0.0f;
+    }
+};
+
+// And what follows from it: to be formed behind a block's loads, which then do not wait for these.
 struct Step {
     float k, a, r2, lr;
     uint32_t t;
     bool skip;
-    __device__ __forceinline__ explicit Step(const Scalars& s) : k(s.grad_scale), a(s.a), r2(s.r2), lr(s.lr), t(s.step), skip(false)
+    __device__ __forceinline__ Step(const Scalars& s, const FromDevice& d) : k(s.grad_scale), a(s.a), r2(s.r2), lr(s.lr), t(s.step), skip(false)
     {
         if (s.factor != nullptr) {
-            const float f = __ldcg(s.factor);
-            skip = !(fabsf(f) > 0.0f && fabsf(f) < INFINITY);
-            k = __fmul_rn(s.grad_scale, f);
+            skip = !(fabsf(d.factor) > 0.0f && fabsf(d.factor) < INFINITY);
+            k = __fmul_rn(s.grad_scale, d.factor);
         }
         if (s.schedule != nullptr) {
-            lr = __ldcg(s.schedule);
-            a = step_size(lr, __ldcg(s.schedule + 1));
-            r2 = reciprocal_root(__ldcg(s.schedule + 2));
-            t = (uint32_t)__ldcg(s.schedule + 3);
+            lr = d.schedule[0];
+            a = step_size(lr, d.schedule[1]);
+            r2 = reciprocal_root(d.schedule[2]);
+            t = (uint32_t)d.schedule[3];
         }
     }
 };
@@ -167,11 +177,11 @@ __device__ __forceinline__ uint32_t encode_m(float m, float inverse, uint32_t h)
 {
     return FormatM::code(FormatM::bits(__fmul_rn(fabsf(m), inverse)), h) | (m < 0.0f ? 0x80u : 0u);
 }
-// (also a v that `inverse` takes below fp32's range stays above zero)
+// (a v of 2^-128 or more never becomes zero, also where `inverse` takes it below fp32's range)
 __device__ __forceinline__ uint32_t encode_v(float v, float inverse, uint32_t h)
 {
     const uint32_t code = FormatV::code(FormatV::bits(__fmul_rn(v, inverse)), (h & 0xFF) << 8 | h >> 8);
-    return max(code, min(__float_as_uint(v), inverse > 0.0f ? 1u : 0u));
+    return max(code, min(__float_as_uint(v), inverse > 0.0f ? 1u << 21 : 0u) >> 21);
 }
 
 // Largest of a warp's non-negative floats.
@@ -204,6 +214,9 @@ __device__ __forceinline__ void decode4(uint32_t m, uint32_t v, float scale_m, f
     }
 }
 
+// One half of a word of draws, times 2^p, plus x; `half`: 2^p in the byte that meets that half in a two-way dot product.
+__device__ __forceinline__ uint32_t add_draw(uint32_t draws, uint32_t half, uint32_t x) { return __dp2a_lo(draws, half, x); }
+
 // draws: of the four elements, two to a word.
 __device__ __forceinline__ void encode4(const float* m, const float* v, float inverse_m, float inverse_v, const uint32_t* draws,
                                         uint32_t& codes_m, uint32_t& codes_v)
@@ -217,11 +230,10 @@ __device__ __forceinline__ void encode4(const float* m, const float* v, float in
         const uint32_t h = draws[j / 2], turned = __byte_perm(h, 0, 0x2301);
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
-            const uint32_t draw_m = (i ? h >> 12 : h << 4) & 0xFFFF0u | 8u, draw_v = (i ? turned >> 11 : turned << 5) & 0x1FFFE0u | 16u;
-            const uint32_t bits_m = __float_as_uint(i ? x.y : x.x) + draw_m;        // below the sign the sum has 27 bits
-            const uint32_t bits_v = __float_as_uint(i ? y.y : y.x) + draw_v;
-            at_top_m[j + i] = bits_m & 0x80000000u | bits_m << 4 & 0x7FFFFFFFu;
-            at_top_v[j + i] = max(bits_v, v[j + i] > 0.0f ? least : 0u) << 3;
+            const uint32_t bits_m = add_draw(h, i ? 16u << 8 : 16u, __float_as_uint(i ? x.y : x.x));   // (27 bits below the sign)
+            const uint32_t bits_v = add_draw(turned, i ? 32u << 8 : 32u, __float_as_uint(i ? y.y : y.x));
+            at_top_m[j + i] = __float_as_uint(m[j + i]) & 0x80000000u | bits_m * 16u + 8u * 16u & 0x7FFFFFFFu;
+            at_top_v[j + i] = max(bits_v + 16u, min(__float_as_uint(v[j + i]), least)) * 8u;
         }
     }
     codes_m = __byte_perm(__byte_perm(at_top_m[0], at_top_m[1], 0x0073), __byte_perm(at_top_m[2], at_top_m[3], 0x0073), 0x5410);
@@ -239,9 +251,16 @@ struct Block {
     void* v;
     float* scales;
     uint64_t e0, group0;     // first element; number of the block's first group of draws
-    uint32_t held;
+    uint32_t held;           // elements of the last block
     float decay;
     uint32_t kind;
+    // the warp's block so many turns further on
+    __device__ __forceinline__ void advance(uint32_t turns)
+    {
+        e0 += (uint64_t)turns * (kWarps * kBlock);
+        group0 += (uint64_t)turns * (kWarps * 32);
+        if (scales != nullptr) scales += (uint64_t)turns * (kWarps * 2);
+    }
 };
 
 __device__ __forceinline__ void draw(uint64_t group, const Step& st, const RoundKeys& keys, uint32_t (&y)[4])
@@ -249,51 +268,105 @@ __device__ __forceinline__ void draw(uint64_t group, const Step& st, const Round
     philox4x32_10((uint32_t)group, (uint32_t)(group >> 32), 0xFFFFFFFFu, st.t, keys, y);
 }
 
-// A whole block on the boundaries of four elements: lane l has the elements 4 l .. 4 l + 3 and 128 + 4 l .. 128 + 4 l + 3, those it draws
-// for.
-template <int P, int G, bool EIGHT>
-__device__ __forceinline__ void step_vectors(const Block& b, const Scalars& s)
-{
-    const uint32_t lane = threadIdx.x & 31;
-    Packed<P, 4> pp[2];
-    Packed<G, 4> pg[2];
-    float p[8], g[8], m[8], v[8];
-    const uint64_t e = b.e0 + lane * 4;
-    auto* at_p = static_cast<typename Element<P>::type*>(b.p) + e;
-    const auto* at_g = static_cast<const typename Element<G>::type*>(b.g) + e;
-    uint32_t code_m[2], code_v[2];
-    float4 wide_m[2], wide_v[2];
-    float scale_m = 0.0f, scale_v = 0.0f;
+// Where a lane's elements of a whole block on the boundaries of four elements are: lane l has the elements 4 l .. 4 l + 3 and
+// 128 + 4 l .. 128 + 4 l + 3, those it draws for.
+template <int P, int G, bool EIGHT> struct Place {
+    using Four = typename Word<EIGHT ? 4 : 16>::type;    // of m or v
+    typename Element<P>::type* p;
+    const typename Element<G>::type* g;
+    Four* m;
+    Four* v;
+    float* scales;
+    __device__ __forceinline__ explicit Place(const Block& b)
+    {
+        const uint64_t e = b.e0 + (threadIdx.x & 31) * 4;
+        p = static_cast<typename Element<P>::type*>(b.p) + e;
+        g = static_cast<const typename Element<G>::type*>(b.g) + e;
+        m = static_cast<Four*>(b.m) + e / 4;
+        v = static_cast<Four*>(b.v) + e / 4;
+        scales = b.scales;
+    }
+    __device__ __forceinline__ void advance()
+    {
+        p += kWarps * kBlock;
+        g += kWarps * kBlock;
+        m += kWarps * kBlock / 4;
+        v += kWarps * kBlock / 4;
+        if (EIGHT) scales += kWarps * 2;
+    }
+};
+
+// What a lane has of it.
+template <int P, int G, bool EIGHT> struct Inputs {
+    using Four = typename Place<P, G, EIGHT>::Four;
+    Packed<P, 4> p[2];
+    Packed<G, 4> g[2];
+    Four m[2], v[2];
+    float scale_m, scale_v;
+
+    __device__ __forceinline__ explicit Inputs(const Place<P, G, EIGHT>& at)
+    {
 #pragma unroll
-    for (int k = 0; k < 2; ++k) {
-        pp[k].load(at_p + 128 * k);
-        pg[k].load(at_g + 128 * k);
-        if (EIGHT) {
-            code_m[k] = __ldcg(reinterpret_cast<const uint32_t*>(static_cast<const uint8_t*>(b.m) + e) + 32 * k);
-            code_v[k] = __ldcg(reinterpret_cast<const uint32_t*>(static_cast<const uint8_t*>(b.v) + e) + 32 * k);
-        } else {
-            wide_m[k] = __ldcg(reinterpret_cast<const float4*>(static_cast<const float*>(b.m) + e) + 32 * k);
-            wide_v[k] = __ldcg(reinterpret_cast<const float4*>(static_cast<const float*>(b.v) + e) + 32 * k);
+        for (int k = 0; k < 2; ++k) {
+            p[k].load(at.p + 128 * k);
+            g[k].load(at.g + 128 * k);
+            m[k] = __ldcg(at.m + 32 * k);
+            v[k] = __ldcg(at.v + 32 * k);
         }
     }
-    if (EIGHT) {
-        scale_m = __ldcg(b.scales);
-        scale_v = __ldcg(b.scales + 1);
+
+    // The same by way of shared memory: asynchronous copies, of each lane's own but for the scales.
+    struct Stage {
+        Packed<P, 4> p[2][32];
+        Packed<G, 4> g[2][32];
+        Four m[2][32], v[2][32];
+        float scales[2];
+    };
+    // The block `ahead` turns further on.
+    static __device__ __forceinline__ void fetch(const Place<P, G, EIGHT>& at, int ahead, Stage& to)
+    {
+        const uint32_t lane = threadIdx.x & 31;
+        const int skip = ahead * kWarps;
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            copy_async<4 * kElemBytes<P>>(&to.p[k][lane], at.p + 128 * k + skip * kBlock);
+            copy_async<4 * kElemBytes<G>>(&to.g[k][lane], at.g + 128 * k + skip * kBlock);
+            copy_async<sizeof(Four)>(&to.m[k][lane], at.m + 32 * k + skip * (kBlock / 4));
+            copy_async<sizeof(Four)>(&to.v[k][lane], at.v + 32 * k + skip * (kBlock / 4));
+        }
+        if (lane < 2) copy_async<4>(&to.scales[lane], at.scales + lane + skip * 2);
     }
-    const Step st(s);
-    if (st.skip) return;
-    const float rate = __fmul_rn(st.lr, b.decay);
+    __device__ __forceinline__ explicit Inputs(const Stage& from)
+    {
+        const uint32_t lane = threadIdx.x & 31;
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            p[k] = from.p[k][lane];
+            g[k] = from.g[k][lane];
+            m[k] = from.m[k][lane];
+            v[k] = from.v[k][lane];
+        }
+        scale_m = from.scales[0];
+        scale_v = from.scales[1];
+    }
+};
+
+template <int P, int G, bool EIGHT>
+__device__ __forceinline__ void step_vectors(const Place<P, G, EIGHT>& at, uint64_t group, Inputs<P, G, EIGHT>& in, const Scalars& s,
+                                             const Step& st, float rate)
+{
+    float p[8], g[8], m[8], v[8];
     uint32_t y[4];
-    if (EIGHT) draw(b.group0 + lane, st, s.keys, y);
+    if (EIGHT) draw(group, st, s.keys, y);
 #pragma unroll
     for (int k = 0; k < 2; ++k) {
-        widen_to<P, 4>(pp[k], p + 4 * k);
-        widen_to<G, 4>(pg[k], g + 4 * k);
-        if (EIGHT) {
-            decode4(code_m[k], code_v[k], scale_m, scale_v, m + 4 * k, v + 4 * k);
+        widen_to<P, 4>(in.p[k], p + 4 * k);
+        widen_to<G, 4>(in.g[k], g + 4 * k);
+        if constexpr (EIGHT) {
+            decode4(in.m[k], in.v[k], in.scale_m, in.scale_v, m + 4 * k, v + 4 * k);
         } else {
-            *reinterpret_cast<float4*>(m + 4 * k) = wide_m[k];
-            *reinterpret_cast<float4*>(v + 4 * k) = wide_v[k];
+            *reinterpret_cast<uint4*>(m + 4 * k) = in.m[k];
+            *reinterpret_cast<uint4*>(v + 4 * k) = in.v[k];
         }
     }
     float most_m = 0.0f, most_v = 0.0f;
@@ -301,34 +374,36 @@ __device__ __forceinline__ void step_vectors(const Block& b, const Scalars& s)
     for (int i = 0; i < 8; i += 2) {
         update2(p + i, g + i, m + i, v + i, s, st, rate);
         if (EIGHT) {
-            most_m = fmaxf(most_m, fmaxf(fabsf(m[i]), fabsf(m[i + 1])));
-            most_v = fmaxf(most_v, fmaxf(v[i], v[i + 1]));
+            most_m = max3_abs(most_m, m[i], m[i + 1]);
+            most_v = max3_abs(most_v, v[i], v[i + 1]);
         }
     }
 #pragma unroll
     for (int k = 0; k < 2; ++k) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) pp[k].set(i, p[4 * k + i]);
-        pp[k].store(at_p + 128 * k);
-        if (!EIGHT) {
-            reinterpret_cast<float4*>(static_cast<float*>(b.m) + e)[32 * k] = *reinterpret_cast<float4*>(m + 4 * k);
-            reinterpret_cast<float4*>(static_cast<float*>(b.v) + e)[32 * k] = *reinterpret_cast<float4*>(v + 4 * k);
+        for (int i = 0; i < 4; ++i) in.p[k].set(i, p[4 * k + i]);
+        in.p[k].store(at.p + 128 * k);
+        if constexpr (!EIGHT) {
+            at.m[32 * k] = *reinterpret_cast<uint4*>(m + 4 * k);
+            at.v[32 * k] = *reinterpret_cast<uint4*>(v + 4 * k);
         }
     }
-    if (!EIGHT) return;
-    float inverse_m, inverse_v;
-    new_scales(most_m, most_v, b.scales, inverse_m, inverse_v);
+    if constexpr (EIGHT) {
+        float inverse_m, inverse_v;
+        new_scales(most_m, most_v, at.scales, inverse_m, inverse_v);
 #pragma unroll
-    for (int k = 0; k < 2; ++k) {
-        encode4(m + 4 * k, v + 4 * k, inverse_m, inverse_v, y + 2 * k, code_m[k], code_v[k]);
-        reinterpret_cast<uint32_t*>(static_cast<uint8_t*>(b.m) + e)[32 * k] = code_m[k];
-        reinterpret_cast<uint32_t*>(static_cast<uint8_t*>(b.v) + e)[32 * k] = code_v[k];
+        for (int k = 0; k < 2; ++k) {
+            uint32_t codes_m, codes_v;
+            encode4(m + 4 * k, v + 4 * k, inverse_m, inverse_v, y + 2 * k, codes_m, codes_v);
+            at.m[32 * k] = codes_m;
+            at.v[32 * k] = codes_v;
+        }
     }
 }
 
 // Any block, lanes side by side.  WHOLE: it has all of its elements.  draws: 32 words of 16 bytes for this warp.
 template <int P, int G, bool EIGHT, bool WHOLE>
-__device__ __forceinline__ void step_elements(const Block& b, const Scalars& s, uint4* draws)
+__device__ __forceinline__ void step_elements(const Block& b, const Scalars& s, const FromDevice& d, uint4* draws)
 {
     using State = typename StateType<EIGHT>::type;
     const uint32_t lane = threadIdx.x & 31;
@@ -353,7 +428,7 @@ __device__ __forceinline__ void step_elements(const Block& b, const Scalars& s, 
         scale_m = __ldcg(b.scales);
         scale_v = __ldcg(b.scales + 1);
     }
-    const Step st(s);
+    const Step st(s, d);
     if (st.skip) return;
     const float rate = __fmul_rn(st.lr, b.decay);
     float p[kPerLane], g[kPerLane], m[kPerLane], v[kPerLane];
@@ -374,8 +449,8 @@ __device__ __forceinline__ void step_elements(const Block& b, const Scalars& s, 
     for (int i = 0; i < kPerLane; i += 2) {
         update2(p + i, g + i, m + i, v + i, s, st, rate);
         if (EIGHT) {
-            most_m = fmaxf(most_m, fmaxf(fabsf(m[i]), fabsf(m[i + 1])));            // (places without elements stay zeros)
-            most_v = fmaxf(most_v, fmaxf(v[i], v[i + 1]));
+            most_m = max3_abs(most_m, m[i], m[i + 1]);  // (places without elements stay zeros)
+            most_v = max3_abs(most_v, v[i], v[i + 1]);
         }
     }
 #pragma unroll
@@ -407,40 +482,94 @@ __device__ __forceinline__ void step_elements(const Block& b, const Scalars& s, 
     }
 }
 
-template <int P, int G, bool EIGHT> __device__ __forceinline__ void step_block(const Block& b, const Scalars& s, uint4* draws)
+// The blocks of a tensor that a warp takes, kWarps apart: `whole` of 256 elements, and perhaps the last one of fewer.
+struct Run {
+    uint32_t whole, rest;    // rest: elements of the last one; 0: another warp's, or there is none
+    __device__ __forceinline__ Run(uint64_t first, uint64_t size, uint32_t turns)
+    {
+        const uint64_t blocks = size / kBlock, left = blocks > first ? blocks - first : 0;
+        whole = (uint32_t)min((left + kWarps - 1) / kWarps, (uint64_t)turns);
+        rest = whole < turns && first + (uint64_t)whole * kWarps == blocks ? (uint32_t)(size % kBlock) : 0;
+    }
+};
+
+constexpr int kStages = 2;
+constexpr int kWarpBytes = kStages * sizeof(Inputs<kF32, kF32, true>::Stage);
+
+// States in 8 bits: a block's inputs come by way of shared memory while the one before is computed, since arithmetic and memory
+// take about as long; in 32 bits, where memory does, straight to registers.
+template <int P, int G, bool EIGHT>
+__device__ __forceinline__ void step_run(Block b, const Run& run, const Scalars& s, unsigned char* memory, uint4* draws)
 {
-    if (b.held < kBlock) step_elements<P, G, EIGHT, false>(b, s, draws);
-    else if (b.kind & 4) step_vectors<P, G, EIGHT>(b, s);
-    else step_elements<P, G, EIGHT, true>(b, s, draws);
+    const FromDevice d(s);
+    using In = Inputs<P, G, EIGHT>;
+    if (!(b.kind & 4)) {
+#pragma unroll 1
+        for (uint32_t turn = 0; turn < run.whole; ++turn, b.advance(1)) step_elements<P, G, EIGHT, true>(b, s, d, draws);
+    } else {
+        Place<P, G, EIGHT> at(b);
+        uint64_t group = b.group0 + (threadIdx.x & 31);
+        if constexpr (EIGHT) {
+            auto* stage = reinterpret_cast<typename In::Stage*>(memory);
+            if (run.whole > 0) In::fetch(at, 0, stage[0]);
+            commit_copies();
+            const Step st(s, d);
+            const float rate = __fmul_rn(st.lr, b.decay);
+            if (!st.skip)
+#pragma unroll 1
+                for (uint32_t turn = 0; turn < run.whole; ++turn) {
+                    __syncwarp();                       // the scales of the stage that is filled now have been read
+                    if (turn + 1 < run.whole) In::fetch(at, 1, stage[(turn + 1) & 1]);
+                    commit_copies();
+                    wait_copies<1>();
+                    __syncwarp();
+                    In in(stage[turn & 1]);
+                    step_vectors<P, G, EIGHT>(at, group, in, s, st, rate);
+                    at.advance();
+                    group += kWarps * 32;
+                }
+            wait_copies<0>();
+        } else {
+#pragma unroll 1
+            for (uint32_t turn = 0; turn < run.whole; ++turn) {
+                In in(at);
+                const Step st(s, d);
+                if (st.skip) return;
+                step_vectors<P, G, EIGHT>(at, group, in, s, st, __fmul_rn(st.lr, b.decay));
+                at.advance();
+            }
+        }
+        b.advance(run.whole);
+    }
+    if (run.rest != 0) step_elements<P, G, EIGHT, false>(b, s, d, draws);
 }
 
 // A warp to a block, `turns` times; a tile is the blocks that a CTA takes.
 template <int CAP, bool EIGHT>
-__global__ void __launch_bounds__(kThreads, 4) adamw_kernel(const __grid_constant__ AdamwTable<CAP> tab, const __grid_constant__ Scalars s, uint32_t turns)
+__global__ void __launch_bounds__(kThreads, 3) adamw_kernel(const __grid_constant__ AdamwTable<CAP> tab, const __grid_constant__ Scalars s, uint32_t turns)
 {
+    __shared__ __align__(16) unsigned char stages[EIGHT ? kWarps : 1][EIGHT ? kWarpBytes : 16];
     __shared__ uint4 draws[EIGHT ? kWarps : 1][32];
     const int j = find_in_list<(CAP > 32)>(tab.tile_start, tab.count, blockIdx.x);
     const uint32_t warp = threadIdx.x >> 5;
-    const uint64_t size = tab.size[j], first = (uint64_t)(blockIdx.x - tab.tile_start[j]) * (kWarps * turns) + warp;
+    const uint64_t first = (uint64_t)(blockIdx.x - tab.tile_start[j]) * (kWarps * turns) + warp;
+    const Run run(first, tab.size[j], turns);
     Block b;
     b.p = tab.p[j];
     b.g = tab.g[j];
     b.m = tab.m[j];
     b.v = tab.v[j];
+    b.scales = EIGHT ? tab.scales[j] + 2 * first : nullptr;
+    b.e0 = first * kBlock;
+    b.group0 = (tab.first_block[j] + first) * 32;
+    b.held = run.rest;
     b.decay = tab.decay[j];
     b.kind = tab.kind[j];
+    unsigned char* memory = stages[EIGHT ? warp : 0];
+    uint4* of_warp = draws[EIGHT ? warp : 0];
     grid_dependency_wait();
-    for (uint32_t turn = 0; turn < turns; ++turn) {
-        const uint64_t block = first + turn * kWarps;
-        b.e0 = block * kBlock;
-        if (b.e0 >= size) return;
-        b.held = (uint32_t)min((uint64_t)kBlock, size - b.e0);
-        b.scales = EIGHT ? tab.scales[j] + 2 * block : nullptr;
-        b.group0 = (tab.first_block[j] + block) * 32;
-        uint4* of_warp = draws[EIGHT ? warp : 0];
-        if (b.kind & 1) b.kind & 2 ? step_block<kBf16, kBf16, EIGHT>(b, s, of_warp) : step_block<kBf16, kF32, EIGHT>(b, s, of_warp);
-        else b.kind & 2 ? step_block<kF32, kBf16, EIGHT>(b, s, of_warp) : step_block<kF32, kF32, EIGHT>(b, s, of_warp);
-    }
+    if (b.kind & 1) b.kind & 2 ? step_run<kBf16, kBf16, EIGHT>(b, run, s, memory, of_warp) : step_run<kBf16, kF32, EIGHT>(b, run, s, memory, of_warp);
+    else b.kind & 2 ? step_run<kF32, kBf16, EIGHT>(b, run, s, memory, of_warp) : step_run<kF32, kF32, EIGHT>(b, run, s, memory, of_warp);
 }
 
 bool on_boundary(const void* p, uintptr_t bytes) { return (reinterpret_cast<uintptr_t>(p) & (bytes - 1)) == 0; }
@@ -473,8 +602,8 @@ cudaError_t launch_table(const AdamwList& list, int first, int last, uint64_t& b
     tab.tile_start[k] = (uint32_t)tiles;
     tab.count = k;
     if (tiles == 0) return cudaSuccess;
-    return list.scales ? launch_pdl(adamw_kernel<CAP, true>, (unsigned)tiles, kThreads, stream, tab, s, turns)
-                       : launch_pdl(adamw_kernel<CAP, false>, (unsigned)tiles, kThreads, stream, tab, s, turns);
+    if (list.scales) return launch_pdl(adamw_kernel<CAP, true>, (unsigned)tiles, kThreads, stream, tab, s, turns);
+    return launch_pdl(adamw_kernel<CAP, false>, (unsigned)tiles, kThreads, stream, tab, s, turns);
 }
 
 }  // namespace

@@ -3,8 +3,7 @@
 
 #include <stdint.h>
 
-#include <atomic>
-
+#include "mqg_async.cuh"
 #include "mqg_vector.cuh"
 
 namespace mqg {
@@ -145,17 +144,6 @@ struct RowSums {
     }
 };
 
-// ---- asynchronous copies to shared memory ------------------------------------------------------------------------------------
-
-template <int BYTES> __device__ __forceinline__ void copy_async(void* to, const void* from)
-{
-    const uint32_t at = (uint32_t)__cvta_generic_to_shared(to);
-    if (BYTES == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(at), "l"(from) : "memory");
-    else asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" ::"r"(at), "l"(from), "n"(BYTES) : "memory");
-}
-__device__ __forceinline__ void commit_copies() { asm volatile("cp.async.commit_group;" ::: "memory"); }
-template <int N> __device__ __forceinline__ void wait_copies() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
-
 // Whether rows x dim elements keep less than the threads of a device busy, 8 elements to a thread: then more elements to a thread
 // take longer.
 inline bool few_elements(uint64_t rows, uint64_t dim) { return rows * dim <= 148ull * 2 * kRowThreads * 8; }
@@ -171,20 +159,5 @@ inline bool vectors_fit(const void* p, int bytes, int v, uint64_t dim)
 }
 
 inline int element_bytes(int dtype) { return dtype == kF32 ? 4 : 2; }
-
-// Lets `kernel` use `bytes` of dynamic shared memory on the current device.  `ready`: of this kernel, by device.
-template <typename Kernel> cudaError_t allow_shared(Kernel kernel, size_t bytes, std::atomic<bool> (&ready)[64])
-{
-    int dev = 0;
-    cudaError_t err = cudaGetDevice(&dev);
-    if (err != cudaSuccess) return err;
-    if (dev < 0 || dev >= 64) return cudaErrorInvalidDevice;
-    if (!ready[dev].load(std::memory_order_relaxed)) {
-        err = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
-        if (err != cudaSuccess) return err;
-        ready[dev].store(true, std::memory_order_relaxed);
-    }
-    return cudaSuccess;
-}
 
 }  // namespace mqg
