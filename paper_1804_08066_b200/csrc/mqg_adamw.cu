@@ -596,8 +596,9 @@ cudaError_t launch_table(const AdamwList& list, int first, int last, uint64_t& b
         const bool fit = on_boundary(list.p[j], half_p ? 8 : 16) && on_boundary(list.g[j], half_g ? 8 : 16) &&
                          on_boundary(list.m[j], state) && on_boundary(list.v[j], state);
         tab.kind[k] = (uint8_t)(half_p | half_g << 1 | fit << 2);
-        blocks += blocks_of(list.size[j]);
-        tiles += (blocks_of(list.size[j]) + kWarps * turns - 1) / (kWarps * turns);
+        const uint64_t n_blocks = blocks_of(list.size[j]);
+        blocks += n_blocks;
+        tiles += turns == 1 ? (n_blocks + kWarps - 1) / kWarps : (n_blocks + kWarps * kTurns - 1) / (kWarps * kTurns);
     }
     tab.tile_start[k] = (uint32_t)tiles;
     tab.count = k;

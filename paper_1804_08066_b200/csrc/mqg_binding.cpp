@@ -829,8 +829,13 @@ struct AdamwLists {
                 PyErr_Format(PyExc_ValueError, "%s holds %zd tensors, params %zu", name(k), PySequence_Fast_GET_SIZE(items[k].object), n);
                 throw PythonError();
             }
-        for (int k = 0; k < count; ++k)
-            for (size_t j = 0; j < n; ++j) read(k, j, PySequence_Fast_ITEMS(items[k].object)[j]);
+        for (int k = 0; k < count; ++k) {
+            PyObject** item = PySequence_Fast_ITEMS(items[k].object);
+            for (size_t j = 0; j < n; ++j) {
+                look_ahead(item, j, n);
+                read(k, j, item[j]);
+            }
+        }
         this->factor = absent(factor) ? nullptr : on.floats(factor, "factor", 1);
         this->schedule = absent(schedule) ? nullptr : on.floats(schedule, "schedule", 4);
     }
@@ -840,6 +845,16 @@ struct AdamwLists {
 
     static const char* name(int k) { return (const char* const[]){"params", "grads", "m", "v", "scales"}[k]; }
 
+    // Brings the objects that come next into the cache: a list's tensors lie wherever they were made, and waiting for them is most
+    // of what reading a list of hundreds takes.
+    static void look_ahead(PyObject** item, size_t j, size_t n)
+    {
+        if (j + 16 < n) __builtin_prefetch(item[j + 16]);
+        if (j + 8 < n && is_tensor(item[j + 8])) {
+            const char* impl = reinterpret_cast<const char*>(THPVariable_Unpack(item[j + 8]).unsafeGetTensorImpl());
+            for (int line = 0; line < 4; ++line) __builtin_prefetch(impl + 64 * line);
+        }
+    }
     void read(int k, size_t j, PyObject* o)
     {
         if (k < 2) {

@@ -1,7 +1,8 @@
 """The whole MQGrad loop on one GPU with simulated workers (Algorithm 1 end to end):
 
     python -m paper_1804_08066_b200.train_loop [--iters 60] [--workers 4] [--selector window|sarsa]
-                                               [--model cnn|tokens] [--clip C] [--clip-at worker|server]
+                                               [--model cnn|tokens] [--norm] [--clip C] [--clip-at worker|server]
+                                               [--optimizer sgd|adamw|adamw8] [--lr LR]
 
 A small CNN (3x3 convolutions 3-32-64-128, two fully connected layers) is trained on synthetic
 32x32x3 images (ten fixed Gaussian class means plus unit noise), batch 128 per worker.  Every
@@ -13,7 +14,9 @@ sequences (synthetic too: every class prefers some tokens, lengths vary) whose t
 by mqg_embedding and gets its gradient from mqg_embedding_grad; with `--clip C` a worker's
 gradients are clipped to norm C on their way into the flat vector (mqg_clip_flatten), or the
 server measures the mean of the decoded gradients and applies it clipped (mqg_grad_norm,
-mqg_apply_clipped).  Prints one JSON line with the share of iteration time spent inside libmqgrad
+mqg_apply_clipped); with `--norm` the rows looked up are normalised before anything else
+(mqg_layer_norm, mqg_layer_norm_grad); with `--optimizer adamw` or `adamw8` the server's update is
+AdamW's, with states in 32 or in 8 bits (mqg_adamw, mqg_adamw8).  Prints one JSON line with the share of iteration time spent inside libmqgrad
 (the paper's Table 3 reports 4.1-13.3 % for quantize + de-quantize + MDP on its CPU clusters).
 """
 from __future__ import annotations
@@ -56,18 +59,23 @@ VOCABULARY, WIDTH, LENGTH = 1000, 64, 16         # tokens, elements of a table's
 
 
 class TokenClassifier(nn.Module):
-    """The mean of a sequence's table rows (times sqrt(WIDTH)), and two fully connected layers."""
+    """The mean of a sequence's table rows (times sqrt(WIDTH); with `norm`, of their layer norm), and two fully connected layers."""
 
     scale = WIDTH ** 0.5
+    eps = 1e-5
 
-    def __init__(self):
+    def __init__(self, norm=False):
         super().__init__()
         self.table = nn.Parameter(torch.randn(VOCABULARY, WIDTH) / WIDTH)
+        self.gain, self.shift = (nn.Parameter(make(WIDTH)) if norm else None for make in (torch.ones, torch.zeros))
         self.f1 = nn.Linear(WIDTH, 128)
         self.f2 = nn.Linear(128, 10)
 
     def forward(self, rows, held):
-        """`rows`: the scaled table rows of [batch, LENGTH] places, zero in the empty ones; `held`: which are not empty."""
+        """`rows`: the scaled (and normalised) table rows of [batch, LENGTH] places, of which those in empty places, zeros without
+        the norm, do not count; `held`: which are not empty."""
+        if self.gain is not None:
+            rows = rows * held[..., None]
         mean = rows.sum(1) / held.sum(1, keepdim=True).clamp(min=1)
         return self.f2(F.relu(self.f1(mean)))
 
@@ -83,21 +91,62 @@ def token_batch(gen, batch):
     return torch.where(torch.arange(LENGTH, device="cuda") < length, ids, -1), y
 
 
+def token_workspace(n):
+    """Scratch memory of token_gradients for `n` places."""
+    return torch.empty(max(mqg.mqg_embedding_workspace_floats(n, VOCABULARY, WIDTH), mqg.mqg_layer_norm_workspace_floats(n, WIDTH)),
+                       device="cuda")
+
+
 def token_gradients(model, ids, y, workspace, library=contextlib.nullcontext()):
     """Loss of a batch and the gradient of every parameter, in their order; the library's calls run within `library`."""
     n = ids.numel()
     rows = torch.empty(*ids.shape, WIDTH, device="cuda")
+    norm = model.gain is not None
+    inner = torch.empty_like(rows) if norm else rows
+    stats = torch.empty(n, 2, device="cuda")
     with library:
         mqg.mqg_embedding(model.table.data, VOCABULARY, WIDTH, ids, n, model.scale, rows)
-    rows.requires_grad_()
+        if norm:
+            mqg.mqg_layer_norm(rows, n, WIDTH, model.gain.data, model.shift.data, model.eps, inner, stats)
+    inner.requires_grad_()
     model.zero_grad(set_to_none=True)
-    loss = F.cross_entropy(model(rows, ids >= 0), y)
+    loss = F.cross_entropy(model(inner, ids >= 0), y)
     loss.backward()
     table = torch.empty_like(model.table.data)
-    dout = rows.grad.contiguous()
+    dout = inner.grad.contiguous()
+    own = [table]
     with library:
+        if norm:
+            drows, dgain, dshift = torch.empty_like(rows), torch.empty(WIDTH, device="cuda"), torch.empty(WIDTH, device="cuda")
+            mqg.mqg_layer_norm_grad(dout, rows, n, WIDTH, model.gain.data, stats, drows, dgain, dshift, workspace)
+            dout = drows
+            own += [dgain, dshift]
         mqg.mqg_embedding_grad(dout, ids, n, VOCABULARY, WIDTH, model.scale, table, workspace)
-    return loss, [table, *(p.grad for p in model.parameters() if p is not model.table)]
+    mine = {id(p) for p in (model.table, model.gain, model.shift)}
+    return loss, own + [p.grad for p in model.parameters() if id(p) not in mine]
+
+
+class AdamW:
+    """AdamW's states for the shared parameters: one tensor of each kind for every parameter of the model, in `bits` bits."""
+
+    beta1, beta2, eps, decay = 0.9, 0.999, 1e-8, 0.01
+
+    def __init__(self, model, bits):
+        self.params = [p.data for p in model.parameters()]
+        self.decays = [self.decay if p.dim() > 1 else 0.0 for p in self.params]      # weights, not biases
+        types = (torch.float32, torch.float32) if bits == 32 else (torch.float8_e4m3fn, torch.float8_e5m2)
+        self.states = [[torch.zeros(p.numel(), dtype=t, device="cuda") for p in self.params] for t in types]
+        if bits == 8:
+            self.states.append([torch.zeros(mqg.mqg_adamw8_scale_floats(p.numel()), device="cuda") for p in self.params])
+
+    def step(self, flat_grad, t, lr, grad_scale, seed, factor=None):
+        """The t-th step (from 1) with slices of `flat_grad`, times grad_scale and, if given, the float in `factor`."""
+        grads = flat_grad.split([p.numel() for p in self.params])
+        hyper = dict(lr=lr, beta1=self.beta1, beta2=self.beta2, eps=self.eps, step=t, grad_scale=grad_scale, factor=factor)
+        if len(self.states) == 3:
+            mqg.mqg_adamw8(self.params, grads, *self.states, self.decays, seed=seed, **hyper)
+        else:
+            mqg.mqg_adamw(self.params, grads, *self.states, self.decays, **hyper)
 
 
 class LibraryTime:
@@ -132,19 +181,26 @@ def flatten_parameters(model):
     return flat
 
 
-def run(iters=60, workers=4, batch=128, lr=0.05, selector="window", seed=0, model="cnn", clip=None, clip_at="worker"):
+LEARNING_RATES = {"sgd": 0.05, "adamw": 2e-3, "adamw8": 2e-3}
+
+
+def run(iters=60, workers=4, batch=128, lr=None, selector="window", seed=0, model="cnn", clip=None, clip_at="worker", norm=False,
+        optimizer="sgd"):
+    lr = LEARNING_RATES[optimizer] if lr is None else lr
     torch.manual_seed(seed)
-    kind, model = model, (SmallCnn() if model == "cnn" else TokenClassifier()).cuda()
+    kind, model = model, (SmallCnn() if model == "cnn" else TokenClassifier(norm)).cuda()
     flat = flatten_parameters(model)
     n = flat.numel()
     gen = torch.Generator(device="cuda").manual_seed(seed + 1)
     if kind == "cnn":
         means = torch.randn(10, 3, 32, 32, generator=gen, device="cuda")
     else:
-        sums = torch.empty(mqg.mqg_embedding_workspace_floats(batch * LENGTH, VOCABULARY, WIDTH), device="cuda")
+        sums = token_workspace(batch * LENGTH)
     norms = torch.zeros(iters, workers if clip_at == "worker" else 1, 2, device="cuda")       # norm and factor
     norm_workspace = torch.empty(mqg.mqg_norm_workspace_floats(len(list(model.parameters()))), device="cuda")
-    acc = torch.empty(n, device="cuda") if clip is not None and clip_at == "server" else None
+    adamw = None if optimizer == "sgd" else AdamW(model, 8 if optimizer == "adamw8" else 32)
+    at_server = clip is not None and clip_at == "server"
+    acc = torch.empty(n, device="cuda") if at_server or adamw is not None else None
     sel = WindowQSelector(seed=seed) if selector == "window" else SarsaBitSelector(seed=seed)
     codes = [torch.zeros(mqg.mqg_code_words(n, 8), dtype=torch.int32, device="cuda") for _ in range(workers)]
     scales = [torch.zeros(mqg.mqg_num_buckets(n, BUCKET), dtype=torch.float32, device="cuda") for _ in range(workers)]
@@ -182,8 +238,12 @@ def run(iters=60, workers=4, batch=128, lr=0.05, selector="window", seed=0, mode
                 mqg.mqg_server_step(codes, scales, workers, bits, n, BUCKET, flat, lr / workers)
             else:                                                 # the mean's norm is the sum's / workers
                 mqg.mqg_dequant_accumulate(codes, scales, workers, bits, n, acc, BUCKET)
-                mqg.mqg_grad_norm([acc], clip * workers, norms[m, 0], norm_workspace)
-                mqg.mqg_apply_clipped(flat, acc, lr / workers, norms[m, 0, 1:], n)
+                if at_server:
+                    mqg.mqg_grad_norm([acc], clip * workers, norms[m, 0], norm_workspace)
+                if adamw is not None:
+                    adamw.step(acc, m + 1, lr, 1.0 / workers, seed, norms[m, 0, 1:] if at_server else None)
+                else:
+                    mqg.mqg_apply_clipped(flat, acc, lr / workers, norms[m, 0, 1:], n)
         torch.cuda.synchronize()
         lib_ms += library.take()
         last_ms = (time.perf_counter() - t0) * 1e3
@@ -192,6 +252,7 @@ def run(iters=60, workers=4, batch=128, lr=0.05, selector="window", seed=0, mode
         losses.append(loss_m), chosen.append(bits)
     assert mqg.mqg_device_timeouts() == 0
     return {"iters": iters, "workers": workers, "parameters": n, "selector": selector, "model": kind,
+            "norm": norm, "optimizer": optimizer,
             "clip_norm": clip, "clip_factors": None if clip is None else norms[..., 1].mean(1).tolist(),
             "first_loss": losses[0], "last_loss": losses[-1], "bits_chosen": chosen,
             "libmqgrad_ms_per_iter": lib_ms / iters, "iteration_ms": total_ms / iters,
@@ -209,5 +270,9 @@ if __name__ == "__main__":
     ap.add_argument("--model", default="cnn", choices=["cnn", "tokens"])
     ap.add_argument("--clip", type=float, default=None, help="largest norm of a gradient")
     ap.add_argument("--clip-at", default="worker", choices=["worker", "server"])
+    ap.add_argument("--norm", action="store_true", help="layer norm of the rows looked up (--model tokens)")
+    ap.add_argument("--optimizer", default="sgd", choices=["sgd", "adamw", "adamw8"])
+    ap.add_argument("--lr", type=float, default=None)
     a = ap.parse_args()
-    print(json.dumps(run(a.iters, a.workers, selector=a.selector, model=a.model, clip=a.clip, clip_at=a.clip_at)))
+    print(json.dumps(run(a.iters, a.workers, lr=a.lr, selector=a.selector, model=a.model, clip=a.clip, clip_at=a.clip_at, norm=a.norm,
+                         optimizer=a.optimizer)))
