@@ -25,7 +25,8 @@ struct NormArgs {
 // Rows on their way to shared memory, each thread's own elements.
 template <int X, int V, int E> struct Ring {
     static constexpr bool kAsync = V * kElemBytes<X> >= 4;
-    static constexpr int kStages = !kAsync ? 1 : E > 16 ? (X == kBf16 ? 4 : 3) : E * kElemBytes<X> <= 16 ? 6 : E * kElemBytes<X> <= 32 ? 5 : 3;
+    static constexpr int kStageBytes = kRowThreads * E * kElemBytes<X>, kFit = (E <= 8 ? 100 : 200) * 1024 / kStageBytes;
+    static constexpr int kStages = !kAsync ? 1 : kFit < 5 ? kFit : 5;
     Packed<X, V> x[kStages][E / V][kRowThreads];
 };
 
@@ -80,6 +81,16 @@ __global__ void __launch_bounds__(kRowThreads, kResident<E>) norm_rows_kernel(co
 #pragma unroll
         for (int s = 0; s < R::kStages - 1; ++s) fetch((uint64_t)blockIdx.x * groups + group + s * stride, s);
     }
+    // where there is no asynchronous copy: the next row
+    Packed<X, V> next[R::kAsync ? 1 : K];
+    const auto load_next = [&](uint64_t row) {
+#pragma unroll
+        for (int k = 0; k < K; ++k) {
+            next[k].set(0, 0.0f);
+            if (row < a.rows && at.has(k)) next[k].load(x + row * a.dim + at.element(k));
+        }
+    };
+    if constexpr (!R::kAsync) load_next((uint64_t)blockIdx.x * groups + group);
     int slot = 0;
     for (uint64_t base = (uint64_t)blockIdx.x * groups; base < a.rows; base += stride) {
         const uint64_t row = base + group;
@@ -92,14 +103,10 @@ __global__ void __launch_bounds__(kRowThreads, kResident<E>) norm_rows_kernel(co
             for (int k = 0; k < K; ++k) widen_to<X, V>(ring.x[slot][k][threadIdx.x], v + k * V);
             slot = slot == R::kStages - 1 ? 0 : slot + 1;
         } else {
+            static_assert(R::kAsync || V == 1, "only vectors of one element are too short for an asynchronous copy");
 #pragma unroll
-            for (int k = 0; k < K; ++k) {
-                Packed<X, V> in;
-#pragma unroll
-                for (int e = 0; e < V; ++e) in.set(e, 0.0f);
-                if (has && at.has(k)) in.load(x + row * a.dim + at.element(k));
-                widen_to<X, V>(in, v + k * V);
-            }
+            for (int k = 0; k < K; ++k) widen_to<X, V>(next[k], v + k * V);
+            load_next(row + stride);
         }
         float2 sum = make_float2(0.0f, 0.0f);
 #pragma unroll
@@ -179,18 +186,32 @@ template <int X, int Y, int V, int E, bool WIDE> cudaError_t launch_groups(const
 template <int X, int Y, int V, int E> cudaError_t launch_elements(const NormArgs& a, cudaStream_t stream)
 {
     const RowGroups g = row_groups(a.rows, a.dim, E, kResident<E> * kRowThreads);
-    return g.threads > 32 ? launch_groups<X, Y, V, E, true>(a, g, stream) : launch_groups<X, Y, V, E, false>(a, g, stream);
+    if constexpr (V > 1 || E <= 8)
+        if (g.threads < 32) return launch_groups<X, Y, V, E, false>(a, g, stream);
+    return launch_groups<X, Y, V, E, true>(a, g, stream);
 }
 
 // The more elements a thread has, the fewer shuffles and barriers there are to a row, and the more is under way: with 8 / 16 / 32 elements
 // 65,536 rows of 4096 in bf16 take 268 / 242 / 164 us, 16,384 of 1024 19.7 / 16.8 / 13.6, 60,000 of 512 31.7 / 22.3 / 23.7, 131,072 of 64
-// 9.6 / 7.8 / 10.7; in fp32 4096 of 4096 24.9 / 23.2 / 25.0.  A million rows of 16: 14 / 20 / 20, lanes then skip memory.  Single
-// elements are bound by instructions: 10,007 rows of 515 in fp32 14.7 / 15.6 / 35.
+// 9.6 / 7.8 / 10.7; in fp32 4096 of 4096 24.9 / 23.2 / 25.0.  A million rows of 16: 14 / 20 / 20, lanes then skip memory.
 template <int X, int Y, int V> cudaError_t launch_vectors(const NormArgs& a, cudaStream_t stream)
 {
-    if (a.dim <= 32 || (a.dim <= 8 * kRowThreads && (V == 1 || few_elements(a.rows, a.dim)))) return launch_elements<X, Y, V, 8>(a, stream);
-    if (a.dim <= (V == 1 || X == kF32 ? 16 * kRowThreads : 512)) return launch_elements<X, Y, V, 16>(a, stream);
+    if (a.dim <= 32 || (a.dim <= 8 * kRowThreads && few_elements(a.rows, a.dim))) return launch_elements<X, Y, V, 8>(a, stream);
+    if (a.dim <= (X == kF32 ? 16 * kRowThreads : 512)) return launch_elements<X, Y, V, 16>(a, stream);
     return launch_elements<X, Y, V, 32>(a, stream);
+}
+
+template <int X, int Y> cudaError_t launch_single(const NormArgs& a, cudaStream_t stream)
+{
+    constexpr int kChoices[] = {8, 12, 16, 20, 24, 32};
+    switch (a.dim <= 256 || few_elements(a.rows, a.dim) ? (a.dim <= 8 * kRowThreads ? 8 : 32) : single_elements(a.dim, kChoices, 6, 5)) {
+    case 8: return launch_elements<X, Y, 1, 8>(a, stream);
+    case 12: return launch_elements<X, Y, 1, 12>(a, stream);
+    case 16: return launch_elements<X, Y, 1, 16>(a, stream);
+    case 20: return launch_elements<X, Y, 1, 20>(a, stream);
+    case 24: return launch_elements<X, Y, 1, 24>(a, stream);
+    default: return launch_elements<X, Y, 1, 32>(a, stream);
+    }
 }
 
 template <int X, int Y> cudaError_t launch(const NormArgs& a, cudaStream_t stream)
@@ -200,7 +221,7 @@ template <int X, int Y> cudaError_t launch(const NormArgs& a, cudaStream_t strea
     const int w = element_bytes(a.w_dtype);
     const bool fit = vectors_fit(a.x, kElemBytes<X>, V, a.dim) && vectors_fit(a.y, kElemBytes<Y>, V, a.dim) &&
                      vectors_fit(a.weight, w, V, a.dim) && vectors_fit(a.bias, w, V, a.dim);
-    return fit ? launch_vectors<X, Y, V>(a, stream) : launch_vectors<X, Y, 1>(a, stream);
+    return fit ? launch_vectors<X, Y, V>(a, stream) : launch_single<X, Y>(a, stream);
 }
 
 }  // namespace

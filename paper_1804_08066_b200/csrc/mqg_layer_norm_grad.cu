@@ -20,7 +20,10 @@ struct GradArgs {
     const void* weight;
     const float* stats;
     void* dx;
-    float* partial;          // [parts][2][dim]: sums for dweight and dbias
+    float* partial;          // [parts][2][dim]: sums for dweight and dbias; nullptr: the grid is one cluster, which adds them up itself
+    void* dweight;
+    void* dbias;
+    int dw_dtype, add;
     uint64_t rows, dim;
     int w_dtype;
 };
@@ -36,14 +39,39 @@ template <int X, int Y, int V, int E> struct Ring {
     float2 stats[kStages][kRowThreads];
 };
 
-template <int E> constexpr int kResident = E <= 8 ? 2 : 1;
+// CTAs to an SM: what the registers leave room for, the next row's among them where it is loaded ahead.
+template <int X, int Y, int V, int E> constexpr int kResident = E <= 8 && Ring<X, Y, V, E>::kAsync ? 2 : 1;
+
+__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
+__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
+// What the cluster's CTA `rank` has where this one has *p, in shared memory.
+__device__ __forceinline__ float cluster_load(const float* p, uint32_t rank)
+{
+    uint32_t at;
+    float v;
+    asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"(smem_u32(p)), "r"(rank));
+    asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(at));
+    return v;
+}
+
+constexpr uint32_t kClusterCtas = 8;                    // (portable)
+
+// Column i of dweight, or i - dim of dbias.
+template <int W> __device__ __forceinline__ void store_sum(void* dweight, void* dbias, uint64_t dim, uint64_t i, double sum, int add)
+{
+    auto* to = static_cast<typename Element<W>::type*>(i < dim ? dweight : dbias);
+    if (to == nullptr) return;
+    const uint64_t col = i < dim ? i : i - dim;
+    if (add) sum += (double)widen(to[col]);
+    narrow((float)sum, to[col]);
+}
 
 // Rows of more elements leave the sums over the rows to a kernel of their own: registers hold no more.
 template <int E> constexpr bool kSums = E <= 16;
 
 // E elements to a thread, V to a vector.
 template <int X, int Y, int V, int E, bool WIDE>
-__global__ void __launch_bounds__(kRowThreads, kResident<E>) grad_rows_kernel(const GradArgs a, uint32_t threads, int sums)
+__global__ void __launch_bounds__(kRowThreads, (kResident<X, Y, V, E>)) grad_rows_kernel(const GradArgs a, uint32_t threads, int sums)
 {
     using R = Ring<X, Y, V, E>;
     constexpr int K = E / V;
@@ -103,6 +131,23 @@ __global__ void __launch_bounds__(kRowThreads, kResident<E>) grad_rows_kernel(co
 #pragma unroll
         for (int s = 0; s < R::kStages - 1; ++s) fetch((uint64_t)blockIdx.x * groups + group + s * stride, s);
     }
+    // where there is no asynchronous copy: the next row
+    Packed<X, V> next_x[R::kAsync ? 1 : K];
+    Packed<Y, V> next_dy[R::kAsync ? 1 : K];
+    float2 next_stats = make_float2(0.0f, 0.0f);
+    const auto load_next = [&](uint64_t row) {
+#pragma unroll
+        for (int k = 0; k < K; ++k) {
+            next_x[k].set(0, 0.0f);
+            next_dy[k].set(0, 0.0f);
+            if (row < a.rows && at.has(k)) {
+                next_x[k].load(x + row * a.dim + at.element(k));
+                next_dy[k].load(dy + row * a.dim + at.element(k));
+            }
+        }
+        if (row < a.rows) next_stats = make_float2(__ldg(a.stats + 2 * row), __ldg(a.stats + 2 * row + 1));
+    };
+    if constexpr (!R::kAsync) load_next((uint64_t)blockIdx.x * groups + group);
     int slot = 0, turn = 0;
     // Every group of a CTA takes as many turns: the barriers of its warps are its own, but the lanes of one warp stay together.
     for (uint64_t base = (uint64_t)blockIdx.x * groups; base < a.rows; base += stride) {
@@ -123,20 +168,14 @@ __global__ void __launch_bounds__(kRowThreads, kResident<E>) grad_rows_kernel(co
             }
             slot = slot == R::kStages - 1 ? 0 : slot + 1;
         } else {
-            if (has) stats = make_float2(__ldg(a.stats + 2 * row), __ldg(a.stats + 2 * row + 1));
+            static_assert(R::kAsync || V == 1, "only vectors of one element are too short for an asynchronous copy");
+            if (has) stats = next_stats;
 #pragma unroll
             for (int k = 0; k < K; ++k) {
-                Packed<X, V> px;
-                Packed<Y, V> pd;
-#pragma unroll
-                for (int e = 0; e < V; ++e) { px.set(e, 0.0f); pd.set(e, 0.0f); }
-                if (has && at.has(k)) {
-                    px.load(x + row * a.dim + at.element(k));
-                    pd.load(dy + row * a.dim + at.element(k));
-                }
-                widen_to<X, V>(px, vx + k * V);
-                widen_to<Y, V>(pd, vd + k * V);
+                widen_to<X, V>(next_x[k], vx + k * V);
+                widen_to<Y, V>(next_dy[k], vd + k * V);
             }
+            load_next(row + stride);
         }
         float2 sum = make_float2(0.0f, 0.0f), along = make_float2(0.0f, 0.0f);
         const float2 minus = make_float2(-stats.x, -stats.x), rstd = make_float2(stats.y, stats.y);
@@ -188,6 +227,7 @@ __global__ void __launch_bounds__(kRowThreads, kResident<E>) grad_rows_kernel(co
     if constexpr (R::kAsync) wait_copies<0>();
     __syncthreads();
     float* all = reinterpret_cast<float*>(memory);      // [groups][dim] of one sum, then of the other
+    float* totals = all + kRowThreads * E;              // [2][dim]
     const uint32_t dim = (uint32_t)a.dim;
 #pragma unroll
     for (int which = 0; which < 2; ++which) {
@@ -200,10 +240,27 @@ __global__ void __launch_bounds__(kRowThreads, kResident<E>) grad_rows_kernel(co
         for (uint32_t col = threadIdx.x; col < dim; col += blockDim.x) {
             float total = 0.0f;
             for (uint32_t i = 0; i < groups; ++i) total += all[i * dim + col];
-            a.partial[((uint64_t)blockIdx.x * 2 + which) * dim + col] = total;
+            if (a.partial != nullptr) a.partial[((uint64_t)blockIdx.x * 2 + which) * dim + col] = total;
+            else totals[which * dim + col] = total;
         }
         __syncthreads();
     }
+    if (a.partial != nullptr) return;
+    // Every CTA of the cluster adds up the totals of its share of the columns, in the CTAs' order.
+    cluster_arrive();
+    cluster_wait();
+    for (uint32_t i = blockIdx.x * blockDim.x + threadIdx.x; i < 2 * dim; i += gridDim.x * blockDim.x) {
+        float of_cta[kClusterCtas];                     // all under way at once
+#pragma unroll
+        for (uint32_t rank = 0; rank < kClusterCtas; ++rank) of_cta[rank] = rank < gridDim.x ? cluster_load(totals + i, rank) : 0.0f;
+        double total = 0.0;
+#pragma unroll
+        for (uint32_t rank = 0; rank < kClusterCtas; ++rank) total += (double)of_cta[rank];
+        if (a.dw_dtype == kF32) store_sum<kF32>(a.dweight, a.dbias, dim, i, total, a.add);
+        else store_sum<kBf16>(a.dweight, a.dbias, dim, i, total, a.add);
+    }
+    cluster_arrive();                                   // no CTA's totals go before all have read them
+    cluster_wait();
 }
 
 // Rows of any length: a CTA to a row, which it reads twice, sums in 64 bits.
@@ -300,11 +357,7 @@ join_kernel(const float* __restrict__ partial, uint32_t parts, uint64_t dim, voi
     if (stripe != 0 || i >= 2 * dim) return;
 #pragma unroll
     for (int k = 1; k < kJoinStripes; ++k) sum += sums[k][at];
-    auto* to = static_cast<typename Element<W>::type*>(i < dim ? dweight : dbias);
-    if (to == nullptr) return;
-    const uint64_t col = i < dim ? i : i - dim;
-    if (add) sum += (double)widen(to[col]);
-    narrow((float)sum, to[col]);
+    store_sum<W>(dweight, dbias, dim, i, sum, add);
 }
 
 uint64_t ceil_div(uint64_t a, uint64_t b) { return (a + b - 1) / b; }
@@ -312,7 +365,15 @@ uint64_t ceil_div(uint64_t a, uint64_t b) { return (a + b - 1) / b; }
 // The longest row whose sums over the rows stay in registers: a row to a CTA.
 constexpr uint64_t kSumsDim = 16 * kRowThreads;
 
-RowGroups groups_of(uint64_t rows, uint64_t dim, uint32_t e) { return row_groups(rows, dim, e, (e <= 8 ? kResident<8> : kResident<16>)*kRowThreads); }
+// The CTAs of a cluster that does everything in one launch, for few elements; 0: a grid and a second launch.  (One row of 64: 4.6 us,
+// 8.2 by two launches; 512 of 64 5.6 and 8.0, 256 of 256 5.7 and 5.6 to 7.8; 2048 of 64 7.3 and 5.6, one of 4096 7.5 and 7.0.)
+uint32_t cluster_of(uint64_t rows, uint64_t dim, const RowGroups& g)
+{
+    if (dim > 1024 || rows * dim > 65536) return 0;
+    uint32_t ctas = 1;
+    while ((ctas < g.ctas || ctas * kRowThreads < 2 * dim) && ctas < kClusterCtas) ctas *= 2;
+    return ctas;
+}
 
 // Parts of the rows that leave a sum each.  Longer rows: enough for every SM of at least 64 rows.
 uint32_t long_parts(uint64_t rows, uint64_t dim)
@@ -321,42 +382,68 @@ uint32_t long_parts(uint64_t rows, uint64_t dim)
     return (uint32_t)(most < want ? (most < 1 ? 1 : most) : want);
 }
 
-template <int X, int Y, int V, int E, bool WIDE> cudaError_t launch_groups(const GradArgs& a, const RowGroups& g, int sums, cudaStream_t stream)
+template <int X, int Y, int V, int E, bool WIDE>
+cudaError_t launch_groups(const GradArgs& a, const RowGroups& g, uint32_t cluster, int sums, cudaStream_t stream)
 {
     using R = Ring<X, Y, V, E>;
     static std::atomic<bool> ready[64];
     const auto kernel = grad_rows_kernel<X, Y, V, E, WIDE>;
-    constexpr size_t kAll = kSums<E> ? kRowThreads * E * sizeof(float) : 16, kBytes = R::kAsync && sizeof(R) > kAll ? sizeof(R) : kAll;
+    constexpr size_t kAll = kSums<E> ? 3 * kRowThreads * E * sizeof(float) : 16, kBytes = R::kAsync && sizeof(R) > kAll ? sizeof(R) : kAll;
     if (const cudaError_t err = allow_shared(kernel, kBytes, ready)) return err;
-    return launch_pdl_smem(kernel, g.ctas, g.block, kBytes, stream, a, g.threads, sums);
+    if (cluster == 0) return launch_pdl_smem(kernel, g.ctas, g.block, kBytes, stream, a, g.threads, sums);
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(cluster);
+    cfg.blockDim = dim3(g.block);
+    cfg.dynamicSmemBytes = kBytes;
+    cfg.stream = stream;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = cluster;
+    attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 2;
+    return cudaLaunchKernelEx(&cfg, kernel, a, g.threads, sums);
 }
 
-template <int X, int Y, int V, int E> cudaError_t launch_elements(const GradArgs& a, int sums, cudaStream_t stream)
+template <int X, int Y, int V, int E> cudaError_t launch_elements(GradArgs a, int sums, uint32_t* parts, cudaStream_t stream)
 {
-    const RowGroups g = groups_of(a.rows, a.dim, E);
-    return g.threads > 32 ? launch_groups<X, Y, V, E, true>(a, g, sums, stream) : launch_groups<X, Y, V, E, false>(a, g, sums, stream);
+    const RowGroups g = row_groups(a.rows, a.dim, E, kResident<X, Y, V, E> * kRowThreads);
+    const uint32_t cluster = E <= 8 && sums ? cluster_of(a.rows, a.dim, g) : 0;
+    *parts = g.ctas;
+    if (cluster != 0) {
+        a.partial = nullptr;
+        *parts = 0;
+    }
+    if constexpr (V > 1 || E <= 8)
+        if (g.threads < 32) return launch_groups<X, Y, V, E, false>(a, g, cluster, sums, stream);
+    return launch_groups<X, Y, V, E, true>(a, g, cluster, sums, stream);
 }
 
 // Elements to a thread.  More of them cost fewer shuffles and barriers to a row: with 8 / 16 65,536 rows of 4096 in bf16 take 326 / 270 us,
-// 16,384 of 1024 27.7 / 24.0, but 64 of 4096 7.6 / 9.5; 4096 of 4096 in fp32 39.3 / 40.3; a million rows of 16 27 / 40; 10,007 of 515
-// by single elements 18.5 / 21.
-template <int X, int Y, int V> uint32_t elements_of(uint64_t rows, uint64_t dim)
+// 16,384 of 1024 27.7 / 24.0, but 64 of 4096 7.6 / 9.5; 4096 of 4096 in fp32 39.3 / 40.3; a million rows of 16 27 / 40.
+template <int X, int Y, int V> int elements_of(uint64_t rows, uint64_t dim)
 {
+    constexpr int kChoices[] = {8, 12, 16};
     if (dim > 8 * kRowThreads) return 16;
-    return V == 1 || (X == kF32 && Y == kF32) || dim <= 32 || few_elements(rows, dim) ? 8 : 16;
+    if (dim <= 32 || few_elements(rows, dim)) return 8;
+    if (V == 1) return dim <= 256 ? 8 : single_elements(dim, kChoices, 3, 4);
+    return X == kF32 && Y == kF32 ? 8 : 16;
 }
 
-// dx, and the sums of `parts` parts of the rows.
+// dx, and the sums of `parts` parts of the rows (0: all of them are added up already).
 template <int X, int Y, int V> cudaError_t launch_vectors(const GradArgs& a, int sums, uint32_t* parts, cudaStream_t stream)
 {
     if (a.dim <= kSumsDim) {
-        const uint32_t e = elements_of<X, Y, V>(a.rows, a.dim);
-        *parts = groups_of(a.rows, a.dim, e).ctas;
-        return e == 8 ? launch_elements<X, Y, V, 8>(a, sums, stream) : launch_elements<X, Y, V, 16>(a, sums, stream);
+        const int e = elements_of<X, Y, V>(a.rows, a.dim);
+        if constexpr (V == 1)
+            if (e == 12) return launch_elements<X, Y, V, 12>(a, sums, parts, stream);
+        return e == 8 ? launch_elements<X, Y, V, 8>(a, sums, parts, stream) : launch_elements<X, Y, V, 16>(a, sums, parts, stream);
     }
     cudaError_t err = cudaSuccess;
     if (a.dx != nullptr && a.rows != 0) {
-        if (V > 1 && a.dim <= 32 * kRowThreads) err = launch_elements<X, Y, V, V == 1 ? 16 : 32>(a, 0, stream);
+        if (V > 1 && a.dim <= 32 * kRowThreads) err = launch_elements<X, Y, V, V == 1 ? 16 : 32>(a, 0, parts, stream);
         else err = launch_pdl(grad_long_kernel<X, Y>, (unsigned)a.rows, kLongThreads, stream, a);
     }
     if (!sums || err != cudaSuccess) return err;
@@ -373,7 +460,7 @@ template <int X, int Y> cudaError_t launch(const GradArgs& a, const NormGrads& o
                      vectors_fit(a.dy, kElemBytes<Y>, V, a.dim) && vectors_fit(a.weight, element_bytes(a.w_dtype), V, a.dim);
     uint32_t parts = 0;
     const cudaError_t err = fit ? launch_vectors<X, Y, V>(a, sums, &parts, stream) : launch_vectors<X, Y, 1>(a, sums, &parts, stream);
-    if (err != cudaSuccess || !sums) return err;
+    if (err != cudaSuccess || !sums || parts == 0) return err;
     const unsigned blocks = (unsigned)ceil_div(2 * a.dim, kJoinColumns);
     const auto join = out.dw_dtype == kF32 ? join_kernel<kF32> : join_kernel<kBf16>;
     return launch_pdl(join, blocks, kJoinColumns * kJoinStripes, stream, a.partial, parts, a.dim, out.dweight, out.dbias, (int)out.add);
@@ -381,17 +468,18 @@ template <int X, int Y> cudaError_t launch(const GradArgs& a, const NormGrads& o
 
 }  // namespace
 
-// (8 elements to a thread leave the most parts)
+// (8 elements to a thread, two CTAs to an SM leave the most parts)
 size_t layer_norm_workspace_floats(uint64_t rows, uint64_t dim)
 {
-    const uint64_t parts = dim > kSumsDim ? long_parts(rows, dim) : groups_of(rows, dim, dim <= 8 * kRowThreads ? 8 : 16).ctas;
+    const uint64_t parts = dim > kSumsDim ? long_parts(rows, dim) : row_groups(rows, dim, dim <= 8 * kRowThreads ? 8 : 16, 2 * kRowThreads).ctas;
     return (size_t)(parts * 2 * dim);
 }
 
 cudaError_t launch_layer_norm_grad(const void* dy, int dy_dtype, const NormRows& in, const float* stats, const NormGrads& out,
                                    float* workspace, cudaStream_t stream)
 {
-    const GradArgs a = {in.x, dy, in.weight, stats, out.dx, workspace, in.rows, in.dim, in.w_dtype};
+    const GradArgs a = {in.x,  dy,           in.weight,    stats,   out.dx, workspace, out.dweight, out.dbias, out.dw_dtype,
+                        out.add, in.rows, in.dim, in.w_dtype};
     return in.x_dtype == kF32 ? (dy_dtype == kF32 ? launch<kF32, kF32>(a, out, stream) : launch<kF32, kBf16>(a, out, stream))
                               : (dy_dtype == kF32 ? launch<kBf16, kF32>(a, out, stream) : launch<kBf16, kBf16>(a, out, stream));
 }
