@@ -36,7 +36,7 @@ constexpr int kPerLane = kBlock / 32;
 constexpr float kTopM = 448.0f, kTopV = 57344.0f, kLeast = 0x1p-110f;       // below kLeast a block counts as zero
 
 // Tensors of one launch, passed by value: a kernel's parameters hold 32,764 bytes.
-template <int CAP> struct AdamwTable {
+template <int CAP, bool EIGHT> struct AdamwTable {
     int count;
     uint32_t tile_start[CAP + 1];                       // a tile is the blocks of a CTA
     uint64_t size[CAP];
@@ -44,12 +44,12 @@ template <int CAP> struct AdamwTable {
     const void* g[CAP];
     void* m[CAP];
     void* v[CAP];
-    float* scales[CAP];
-    uint64_t first_block[CAP];                          // blocks before the tensor in the whole list
+    float* scales[EIGHT ? CAP : 1];
+    uint64_t first_block[EIGHT ? CAP : 1];              // blocks before the tensor in the whole list
     float decay[CAP];
     uint8_t kind[CAP];                                  // bit 0: p is bf16, bit 1: g is, bit 2: all on the boundaries of 4 elements
 };
-constexpr int kLargeTable = 448;
+template <bool EIGHT> constexpr int kLargeTable = EIGHT ? 448 : 640;
 
 // Turns of a warp, where there are blocks for four times the warps that the device holds.
 constexpr uint32_t kTurns = 4, kManyBlocks = 148 * 4 * kWarps * 4;
@@ -546,7 +546,7 @@ __device__ __forceinline__ void step_run(Block b, const Run& run, const Scalars&
 
 // A warp to a block, `turns` times; a tile is the blocks that a CTA takes.
 template <int CAP, bool EIGHT>
-__global__ void __launch_bounds__(kThreads, 3) adamw_kernel(const __grid_constant__ AdamwTable<CAP> tab, const __grid_constant__ Scalars s, uint32_t turns)
+__global__ void __launch_bounds__(kThreads, 3) adamw_kernel(const __grid_constant__ AdamwTable<CAP, EIGHT> tab, const __grid_constant__ Scalars s, uint32_t turns)
 {
     __shared__ __align__(16) unsigned char stages[EIGHT ? kWarps : 1][EIGHT ? kWarpBytes : 16];
     __shared__ uint4 draws[EIGHT ? kWarps : 1][32];
@@ -561,7 +561,7 @@ __global__ void __launch_bounds__(kThreads, 3) adamw_kernel(const __grid_constan
     b.v = tab.v[j];
     b.scales = EIGHT ? tab.scales[j] + 2 * first : nullptr;
     b.e0 = first * kBlock;
-    b.group0 = (tab.first_block[j] + first) * 32;
+    b.group0 = EIGHT ? (tab.first_block[j] + first) * 32 : 0;
     b.held = run.rest;
     b.decay = tab.decay[j];
     b.kind = tab.kind[j];
@@ -572,39 +572,57 @@ __global__ void __launch_bounds__(kThreads, 3) adamw_kernel(const __grid_constan
     else b.kind & 2 ? step_run<kF32, kBf16, EIGHT>(b, run, s, memory, of_warp) : step_run<kF32, kF32, EIGHT>(b, run, s, memory, of_warp);
 }
 
-bool on_boundary(const void* p, uintptr_t bytes) { return (reinterpret_cast<uintptr_t>(p) & (bytes - 1)) == 0; }
-
 uint64_t blocks_of(uint64_t n) { return (n + kBlock - 1) / kBlock; }
 
-template <int CAP>
+// `blocks`: before tensor `first` in the whole list; moved on.
+template <int CAP, bool EIGHT>
 cudaError_t launch_table(const AdamwList& list, int first, int last, uint64_t& blocks, const Scalars& s, uint32_t turns, cudaStream_t stream)
 {
-    AdamwTable<CAP> tab;
+    AdamwTable<CAP, EIGHT> tab;
     uint64_t tiles = 0;
     int k = 0;
     for (int j = first; j < last; ++j, ++k) {
+        const int half_p = list.p_dtype[j] == kBf16, half_g = list.g_dtype[j] == kBf16;
+        const auto at = [](const void* p) { return reinterpret_cast<uintptr_t>(p); };
+        const uintptr_t off = (at(list.p[j]) << half_p | at(list.g[j]) << half_g) & 15;       // of 4 bf16 elements: 8 bytes
+        const uintptr_t state_off = (at(list.m[j]) | at(list.v[j])) & (EIGHT ? 3 : 15);
+        const uint64_t n_blocks = blocks_of(list.size[j]);
         tab.tile_start[k] = (uint32_t)tiles;
         tab.size[k] = list.size[j];
         tab.p[k] = list.p[j];
         tab.g[k] = list.g[j];
         tab.m[k] = list.m[j];
         tab.v[k] = list.v[j];
-        tab.scales[k] = list.scales ? list.scales[j] : nullptr;
-        tab.first_block[k] = blocks;
+        if constexpr (EIGHT) {
+            tab.scales[k] = list.scales[j];
+            tab.first_block[k] = blocks;
+        }
         tab.decay[k] = list.decay ? list.decay[j] : 0.0f;
-        const int half_p = list.p_dtype[j] == kBf16, half_g = list.g_dtype[j] == kBf16, state = list.scales ? 4 : 16;
-        const bool fit = on_boundary(list.p[j], half_p ? 8 : 16) && on_boundary(list.g[j], half_g ? 8 : 16) &&
-                         on_boundary(list.m[j], state) && on_boundary(list.v[j], state);
-        tab.kind[k] = (uint8_t)(half_p | half_g << 1 | fit << 2);
-        const uint64_t n_blocks = blocks_of(list.size[j]);
+        tab.kind[k] = (uint8_t)(half_p | half_g << 1 | ((off | state_off) == 0) << 2);
         blocks += n_blocks;
         tiles += turns == 1 ? (n_blocks + kWarps - 1) / kWarps : (n_blocks + kWarps * kTurns - 1) / (kWarps * kTurns);
     }
     tab.tile_start[k] = (uint32_t)tiles;
     tab.count = k;
     if (tiles == 0) return cudaSuccess;
-    if (list.scales) return launch_pdl(adamw_kernel<CAP, true>, (unsigned)tiles, kThreads, stream, tab, s, turns);
-    return launch_pdl(adamw_kernel<CAP, false>, (unsigned)tiles, kThreads, stream, tab, s, turns);
+    return launch_pdl(adamw_kernel<CAP, EIGHT>, (unsigned)tiles, kThreads, stream, tab, s, turns);
+}
+
+template <bool EIGHT> cudaError_t launch_list(const AdamwList& list, const Scalars& s, cudaStream_t stream)
+{
+    uint64_t blocks = 0;
+    for (int j = 0; j < list.count; ++j) blocks += blocks_of(list.size[j]);
+    const uint32_t turns = blocks > (uint64_t)kManyBlocks ? kTurns : 1;
+    blocks = 0;
+    cudaError_t err = cudaSuccess;
+    for (int first = 0; first < list.count && err == cudaSuccess; first += kLargeTable<EIGHT>) {
+        const int last = list.count - first > kLargeTable<EIGHT> ? first + kLargeTable<EIGHT> : list.count, n = last - first;
+        err = n <= 16    ? launch_table<16, EIGHT>(list, first, last, blocks, s, turns, stream)
+              : n <= 96  ? launch_table<96, EIGHT>(list, first, last, blocks, s, turns, stream)
+              : n <= 320 ? launch_table<320, EIGHT>(list, first, last, blocks, s, turns, stream)
+                         : launch_table<kLargeTable<EIGHT>, EIGHT>(list, first, last, blocks, s, turns, stream);
+    }
+    return err;
 }
 
 }  // namespace
@@ -629,18 +647,7 @@ cudaError_t launch_adamw(const AdamwList& list, const AdamwStep& step, cudaStrea
         s.keys.k0[r] = (uint32_t)step.seed + r * 0x9E3779B9u;
         s.keys.k1[r] = (uint32_t)(step.seed >> 32) + r * 0xBB67AE85u;
     }
-    uint64_t blocks = 0;
-    for (int j = 0; j < list.count; ++j) blocks += blocks_of(list.size[j]);
-    const uint32_t turns = blocks > (uint64_t)kManyBlocks ? kTurns : 1;
-    blocks = 0;
-    cudaError_t err = cudaSuccess;
-    for (int first = 0; first < list.count && err == cudaSuccess; first += kLargeTable) {
-        const int last = list.count - first > kLargeTable ? first + kLargeTable : list.count, n = last - first;
-        err = n <= 16   ? launch_table<16>(list, first, last, blocks, s, turns, stream)
-              : n <= 96 ? launch_table<96>(list, first, last, blocks, s, turns, stream)
-                        : launch_table<kLargeTable>(list, first, last, blocks, s, turns, stream);
-    }
-    return err;
+    return list.scales ? launch_list<true>(list, s, stream) : launch_list<false>(list, s, stream);
 }
 
 }  // namespace mqg

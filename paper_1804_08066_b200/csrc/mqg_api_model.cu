@@ -30,34 +30,48 @@ struct BufferList {
     }
 };
 
-// Whether everything that is written shares no memory with anything else.  Lists of slices of one vector each, in its order,
-// are seen at a glance; others are sorted.
+// What a look at every buffer of a call finds, without a branch for each: a reason to look closely, or none.  Lists of slices of
+// one vector each, in its order, are seen to share no memory.
+template <int N>
+bool plainly_good(const BufferList (&lists)[N], const uint64_t* sizes, const float* decays, int count, const Region (&scalars)[2])
+{
+    struct Span { uintptr_t from, to; };
+    Span span[N];
+    for (Span& s : span) s = {~(uintptr_t)0, 0};
+    uint64_t total = 0;
+    bool bad = false;
+    for (int j = 0; j < count; ++j) {
+        const uint64_t n = sizes[j];
+        bad |= n >= (1ull << 42) || (unsigned)lists[0].dtype[j] > 1u || (unsigned)lists[1].dtype[j] > 1u;
+        bad |= decays != nullptr && !(decays[j] >= 0.0f && decays[j] <= 3.4e38f);
+        total += n;
+        if (n == 0) continue;
+        bad |= total >= (1ull << 42);
+        for (int k = 0; k < N; ++k) {
+            const BufferList& l = lists[k];
+            const uintptr_t p = reinterpret_cast<uintptr_t>(l.ptr[j]);
+            const unsigned shift = k < 2 ? 2u - (unsigned)(lists[k].dtype[j] & 1) : k < 4 && l.unit == 1 ? 0u : 2u;
+            const uint64_t bytes = k < 4 ? n << shift : state_blocks(n) * 8;
+            bad |= p == 0 || (p & ((1u << shift) - 1)) != 0 || (l.written && p < span[k].to);
+            span[k].from = std::min(span[k].from, p);
+            span[k].to = std::max(span[k].to, p + bytes);
+        }
+    }
+    for (int k = 0; k < N; ++k) {
+        for (int i = 0; i < k; ++i)
+            bad |= (lists[k].written || lists[i].written) && span[k].from < span[i].to && span[i].from < span[k].to;
+        for (const Region& r : scalars) {
+            const uintptr_t p = reinterpret_cast<uintptr_t>(r.p);
+            bad |= lists[k].written && r.bytes != 0 && span[k].from < p + r.bytes && p < span[k].to;
+        }
+    }
+    return !bad;
+}
+
+// Whether everything that is written shares no memory with anything else: the buffers in the order of their addresses.
 mqg_status check_lists_apart(const char* what, const BufferList* lists, int nlists, const uint64_t* sizes, int count,
                              const Region (&scalars)[2])
 {
-    struct Span { uintptr_t from, to; };
-    Span span[5];
-    bool plain = true;
-    for (int k = 0; k < nlists && plain; ++k) {
-        const BufferList& l = lists[k];
-        Span s = {~(uintptr_t)0, 0};
-        for (int j = 0; j < count && plain; ++j) {
-            const uint64_t n = l.bytes(sizes, j);
-            if (n == 0) continue;
-            const uintptr_t p = reinterpret_cast<uintptr_t>(l.ptr[j]);
-            if (l.written && p < s.to) plain = false;
-            s.from = std::min(s.from, p);
-            s.to = std::max(s.to, p + n);
-        }
-        for (int i = 0; i < k && plain; ++i)
-            if ((l.written || lists[i].written) && s.from < span[i].to && span[i].from < s.to) plain = false;
-        for (const Region& r : scalars) {
-            const uintptr_t p = reinterpret_cast<uintptr_t>(r.p);
-            if (l.written && r.bytes != 0 && s.from < p + r.bytes && p < s.to) plain = false;
-        }
-        span[k] = s;
-    }
-    if (plain) return MQG_OK;
     struct Piece { uintptr_t from, to; int list, tensor; };
     std::vector<Piece> pieces;
     pieces.reserve((size_t)nlists * count + 2);
@@ -86,7 +100,8 @@ mqg_status check_lists_apart(const char* what, const BufferList* lists, int nlis
     return MQG_OK;
 }
 
-mqg_status check_adamw(const char* what, const BufferList* lists, int nlists, const uint64_t* sizes, const float* decays, int count,
+template <int N>
+mqg_status check_adamw(const char* what, const BufferList (&lists)[N], const uint64_t* sizes, const float* decays, int count,
                        const AdamwStep& s)
 {
     if (count < 0) return report_error(MQG_ERR_INVALID, "%s: count = %d is negative", what, count);
@@ -101,8 +116,10 @@ mqg_status check_adamw(const char* what, const BufferList* lists, int nlists, co
     if (!aligned(s.factor, 4) || !aligned(s.schedule, 4)) return report_error(MQG_ERR_ALIGN, "%s: factor or schedule not 4-byte aligned", what);
     if (count == 0) return MQG_OK;
     if (!sizes) return report_error(MQG_ERR_INVALID, "%s: sizes is null", what);
-    for (int k = 0; k < nlists; ++k)
+    for (int k = 0; k < N; ++k)
         if (!lists[k].ptr) return report_error(MQG_ERR_INVALID, "%s: %s is null", what, lists[k].name);
+    const Region scalars[2] = {{"factor", s.factor, s.factor ? 4u : 0u}, {"schedule", s.schedule, s.schedule ? 16u : 0u}};
+    if (plainly_good(lists, sizes, decays, count, scalars)) return MQG_OK;
     uint64_t total = 0;
     for (int j = 0; j < count; ++j) {
         for (int k = 0; k < 2; ++k)
@@ -113,22 +130,22 @@ mqg_status check_adamw(const char* what, const BufferList* lists, int nlists, co
         if (sizes[j] == 0) continue;
         if (sizes[j] >= (1ull << 42) || (total += sizes[j]) >= (1ull << 42))
             return report_error(MQG_ERR_INVALID, "%s: the tensors hold 2^42 elements or more", what);
-        for (int k = 0; k < nlists; ++k) {
+        for (int k = 0; k < N; ++k) {
             const BufferList& l = lists[k];
             if (!l.ptr[j]) return report_error(MQG_ERR_INVALID, "%s: %s, tensor %d is null", what, l.name, j);
             if (!aligned(l.ptr[j], l.dtype ? bytes_of(l.dtype[j]) : l.unit ? l.unit : 4))
                 return report_error(MQG_ERR_ALIGN, "%s: %s, tensor %d is not aligned to its elements", what, l.name, j);
         }
     }
-    return check_lists_apart(what, lists, nlists, sizes, count,
-                             {{"factor", s.factor, s.factor ? 4u : 0u}, {"schedule", s.schedule, s.schedule ? 16u : 0u}});
+    return check_lists_apart(what, lists, N, sizes, count, scalars);
 }
 
-mqg_status run_adamw(const char* what, const BufferList* lists, int nlists, const AdamwList& list, const AdamwStep& step, void* stream)
+template <int N>
+mqg_status run_adamw(const char* what, const BufferList (&lists)[N], const AdamwList& list, const AdamwStep& step, void* stream)
 {
     static_assert(sizeof(mqg_dtype) == sizeof(int), "the lists' types are passed on as int");
     try {
-        if (mqg_status st = check_adamw(what, lists, nlists, list.size, list.decay, list.count, step)) return st;
+        if (mqg_status st = check_adamw(what, lists, list.size, list.decay, list.count, step)) return st;
     } catch (const std::exception& e) {                 // no memory to sort the list in
         return report_error(MQG_ERR_INVALID, "%s: %s", what, e.what());
     }
@@ -169,7 +186,7 @@ mqg_status mqg_adamw(void* const* params, const mqg_dtype* param_dtypes, const v
                                  {"m", states[0], nullptr, 4, true},
                                  {"v", states[1], nullptr, 4, true}};
     const AdamwList list = {params, as_int(param_dtypes), grads, as_int(grad_dtypes), states[0], states[1], nullptr, sizes, decays, count};
-    return run_adamw(what, lists, 4, list, {lr, beta1, beta2, eps, step, 0, grad_scale, factor, schedule}, cuda_stream);
+    return run_adamw(what, lists, list, {lr, beta1, beta2, eps, step, 0, grad_scale, factor, schedule}, cuda_stream);
 }
 
 mqg_status mqg_adamw8(void* const* params, const mqg_dtype* param_dtypes, const void* const* grads, const mqg_dtype* grad_dtypes,
@@ -187,7 +204,7 @@ mqg_status mqg_adamw8(void* const* params, const mqg_dtype* param_dtypes, const 
                                  {"v", states[1], nullptr, 1, true},
                                  {"scales", reinterpret_cast<void* const*>(scales), nullptr, 0, true}};
     const AdamwList list = {params, as_int(param_dtypes), grads, as_int(grad_dtypes), states[0], states[1], scales, sizes, decays, count};
-    return run_adamw(what, lists, 5, list, {lr, beta1, beta2, eps, step, seed, grad_scale, factor, schedule}, cuda_stream);
+    return run_adamw(what, lists, list, {lr, beta1, beta2, eps, step, seed, grad_scale, factor, schedule}, cuda_stream);
 }
 
 mqg_status mqg_layer_norm(const void* x, mqg_dtype x_dtype, uint64_t rows, uint64_t dim, const void* weight, const void* bias,
