@@ -24,7 +24,7 @@ struct NormArgs {
 
 // Rows on their way to shared memory, each thread's own elements.
 template <int X, int V, int E> struct Ring {
-    static constexpr bool kAsync = V * kElemBytes<X> >= 4;
+    static constexpr bool kAsync = V > 1;
     static constexpr int kStageBytes = kRowThreads * E * kElemBytes<X>, kFit = (E <= 8 ? 100 : 200) * 1024 / kStageBytes;
     static constexpr int kStages = !kAsync ? 1 : kFit < 5 ? kFit : 5;
     Packed<X, V> x[kStages][E / V][kRowThreads];
@@ -81,7 +81,8 @@ __global__ void __launch_bounds__(kRowThreads, kResident<E>) norm_rows_kernel(co
 #pragma unroll
         for (int s = 0; s < R::kStages - 1; ++s) fetch((uint64_t)blockIdx.x * groups + group + s * stride, s);
     }
-    // where there is no asynchronous copy: the next row
+    // single elements: the next row, where registers hold one more
+    constexpr bool kAhead = !R::kAsync && E <= 24;
     Packed<X, V> next[R::kAsync ? 1 : K];
     const auto load_next = [&](uint64_t row) {
 #pragma unroll
@@ -90,7 +91,7 @@ __global__ void __launch_bounds__(kRowThreads, kResident<E>) norm_rows_kernel(co
             if (row < a.rows && at.has(k)) next[k].load(x + row * a.dim + at.element(k));
         }
     };
-    if constexpr (!R::kAsync) load_next((uint64_t)blockIdx.x * groups + group);
+    if constexpr (kAhead) load_next((uint64_t)blockIdx.x * groups + group);
     int slot = 0;
     for (uint64_t base = (uint64_t)blockIdx.x * groups; base < a.rows; base += stride) {
         const uint64_t row = base + group;
@@ -103,10 +104,10 @@ __global__ void __launch_bounds__(kRowThreads, kResident<E>) norm_rows_kernel(co
             for (int k = 0; k < K; ++k) widen_to<X, V>(ring.x[slot][k][threadIdx.x], v + k * V);
             slot = slot == R::kStages - 1 ? 0 : slot + 1;
         } else {
-            static_assert(R::kAsync || V == 1, "only vectors of one element are too short for an asynchronous copy");
+            if constexpr (!kAhead) load_next(row);
 #pragma unroll
             for (int k = 0; k < K; ++k) widen_to<X, V>(next[k], v + k * V);
-            load_next(row + stride);
+            if constexpr (kAhead) load_next(row + stride);
         }
         float2 sum = make_float2(0.0f, 0.0f);
 #pragma unroll
@@ -201,17 +202,13 @@ template <int X, int Y, int V> cudaError_t launch_vectors(const NormArgs& a, cud
     return launch_elements<X, Y, V, 32>(a, stream);
 }
 
+// Single elements are bound by instructions: with 8 / 12 / 16 / 20 / 24 elements 10,007 rows of 515 in fp32 take 11.9 / 13.3 / 15.6 / 12.0 / 12.2 us, 3000
+// of 3333 18.5 / 26.1 / 21.1 / 21.0 / 18.6; 2000 of 6001 with 12 / 24 24.1 / 21.4.
 template <int X, int Y> cudaError_t launch_single(const NormArgs& a, cudaStream_t stream)
 {
-    constexpr int kChoices[] = {8, 12, 16, 20, 24, 32};
-    switch (a.dim <= 256 || few_elements(a.rows, a.dim) ? (a.dim <= 8 * kRowThreads ? 8 : 32) : single_elements(a.dim, kChoices, 6, 5)) {
-    case 8: return launch_elements<X, Y, 1, 8>(a, stream);
-    case 12: return launch_elements<X, Y, 1, 12>(a, stream);
-    case 16: return launch_elements<X, Y, 1, 16>(a, stream);
-    case 20: return launch_elements<X, Y, 1, 20>(a, stream);
-    case 24: return launch_elements<X, Y, 1, 24>(a, stream);
-    default: return launch_elements<X, Y, 1, 32>(a, stream);
-    }
+    return a.dim <= 8 * kRowThreads    ? launch_elements<X, Y, 1, 8>(a, stream)
+           : a.dim <= 24 * kRowThreads ? launch_elements<X, Y, 1, 24>(a, stream)
+                                       : launch_elements<X, Y, 1, 32>(a, stream);
 }
 
 template <int X, int Y> cudaError_t launch(const NormArgs& a, cudaStream_t stream)

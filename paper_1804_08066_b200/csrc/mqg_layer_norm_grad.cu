@@ -31,7 +31,7 @@ struct GradArgs {
 // Rows on their way to shared memory: each thread's own elements, and the rows' stats, which the first thread of a group copies
 // for those of its warp.
 template <int X, int Y, int V, int E> struct Ring {
-    static constexpr bool kAsync = V * kElemBytes<X> >= 4 && V * kElemBytes<Y> >= 4;
+    static constexpr bool kAsync = V > 1;
     static constexpr int kBytes = E * (kElemBytes<X> + kElemBytes<Y>);
     static constexpr int kStages = !kAsync ? 1 : kBytes <= 32 ? 5 : kBytes <= 48 ? 4 : kBytes <= 64 && E > 8 ? 5 : E > 16 ? (kBytes <= 128 ? 3 : kBytes <= 192 ? 2 : 1) : 3;
     Packed<X, V> x[kStages][E / V][kRowThreads];
@@ -131,7 +131,8 @@ __global__ void __launch_bounds__(kRowThreads, (kResident<X, Y, V, E>)) grad_row
 #pragma unroll
         for (int s = 0; s < R::kStages - 1; ++s) fetch((uint64_t)blockIdx.x * groups + group + s * stride, s);
     }
-    // where there is no asynchronous copy: the next row
+    // single elements: the next row, where registers hold one more
+    constexpr bool kAhead = !R::kAsync && E <= 12;
     Packed<X, V> next_x[R::kAsync ? 1 : K];
     Packed<Y, V> next_dy[R::kAsync ? 1 : K];
     float2 next_stats = make_float2(0.0f, 0.0f);
@@ -147,7 +148,7 @@ __global__ void __launch_bounds__(kRowThreads, (kResident<X, Y, V, E>)) grad_row
         }
         if (row < a.rows) next_stats = make_float2(__ldg(a.stats + 2 * row), __ldg(a.stats + 2 * row + 1));
     };
-    if constexpr (!R::kAsync) load_next((uint64_t)blockIdx.x * groups + group);
+    if constexpr (kAhead) load_next((uint64_t)blockIdx.x * groups + group);
     int slot = 0, turn = 0;
     // Every group of a CTA takes as many turns: the barriers of its warps are its own, but the lanes of one warp stay together.
     for (uint64_t base = (uint64_t)blockIdx.x * groups; base < a.rows; base += stride) {
@@ -168,14 +169,14 @@ __global__ void __launch_bounds__(kRowThreads, (kResident<X, Y, V, E>)) grad_row
             }
             slot = slot == R::kStages - 1 ? 0 : slot + 1;
         } else {
-            static_assert(R::kAsync || V == 1, "only vectors of one element are too short for an asynchronous copy");
+            if constexpr (!kAhead) load_next(row);
             if (has) stats = next_stats;
 #pragma unroll
             for (int k = 0; k < K; ++k) {
                 widen_to<X, V>(next_x[k], vx + k * V);
                 widen_to<Y, V>(next_dy[k], vd + k * V);
             }
-            load_next(row + stride);
+            if constexpr (kAhead) load_next(row + stride);
         }
         float2 sum = make_float2(0.0f, 0.0f), along = make_float2(0.0f, 0.0f);
         const float2 minus = make_float2(-stats.x, -stats.x), rstd = make_float2(stats.y, stats.y);
@@ -423,12 +424,13 @@ template <int X, int Y, int V, int E> cudaError_t launch_elements(GradArgs a, in
 
 // Elements to a thread.  More of them cost fewer shuffles and barriers to a row: with 8 / 16 65,536 rows of 4096 in bf16 take 326 / 270 us,
 // 16,384 of 1024 27.7 / 24.0, but 64 of 4096 7.6 / 9.5; 4096 of 4096 in fp32 39.3 / 40.3; a million rows of 16 27 / 40.
+// Single elements with 8 / 12: 10,007 rows of 515 in fp32 19.7 / 18.2, 3000 of 2001 20.5 / 21.6, 3000 of 3333 31.5 / 32.8.
 template <int X, int Y, int V> int elements_of(uint64_t rows, uint64_t dim)
 {
-    constexpr int kChoices[] = {8, 12, 16};
+    if (V == 1 && dim > 8 * kRowThreads) return dim <= 12 * kRowThreads ? 12 : 16;
     if (dim > 8 * kRowThreads) return 16;
     if (dim <= 32 || few_elements(rows, dim)) return 8;
-    if (V == 1) return dim <= 256 ? 8 : single_elements(dim, kChoices, 3, 4);
+    if (V == 1) return dim <= 256 || dim > 1536 ? 8 : 12;
     return X == kF32 && Y == kF32 ? 8 : 16;
 }
 
@@ -443,7 +445,7 @@ template <int X, int Y, int V> cudaError_t launch_vectors(const GradArgs& a, int
     }
     cudaError_t err = cudaSuccess;
     if (a.dx != nullptr && a.rows != 0) {
-        if (V > 1 && a.dim <= 32 * kRowThreads) err = launch_elements<X, Y, V, V == 1 ? 16 : 32>(a, 0, parts, stream);
+        if (a.dim <= 32 * kRowThreads) err = launch_elements<X, Y, V, 32>(a, 0, parts, stream);
         else err = launch_pdl(grad_long_kernel<X, Y>, (unsigned)a.rows, kLongThreads, stream, a);
     }
     if (!sums || err != cudaSuccess) return err;

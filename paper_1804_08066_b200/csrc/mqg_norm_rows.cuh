@@ -58,7 +58,8 @@ template <int V> __device__ __forceinline__ void weights_at(const void* w, int d
 // A row is E elements to a thread: a group of 1, 2, 4, 8 or 16 lanes, or of up to 16 whole warps (WIDE).  A CTA has as many groups as
 // fit 16 warps.  A thread has K vectors of V elements, those of a group's threads side by side; single elements (V = 1) of a WIDE
 // group, those of a warp's lanes, so that the distance between a thread's elements is a constant (10,007 rows of 515 in fp32: 14.7 us,
-// 18.3 without; for vectors it makes no difference or, in long rows, costs up to a sixth).
+// 18.3 without; for vectors it makes no difference or, in long rows, costs up to a sixth).  Vectors come to shared memory by asynchronous
+// copies, rows ahead; single elements straight to registers, one row ahead (copies of 4 bytes each: 14.7 us, so 11.9).
 
 constexpr int kRowThreads = 512;
 
@@ -96,21 +97,6 @@ template <int V, int K, bool WIDE> struct RowPlace {
     __device__ __forceinline__ bool has(int k) const { return kByWarp ? (uint32_t)k < held : start + k * step() < vectors; }
     __device__ __forceinline__ uint32_t element(int k) const { return (start + k * step()) * V; }
 };
-
-// Elements to a thread of rows that are read one by one: the number whose threads have the least to do, a row's sums and barriers
-// counted as `fixed` elements of each thread.  (515: one warp of 20, not three of 8.)
-inline int single_elements(uint64_t dim, const int* choices, int count, int fixed)
-{
-    int best = 0;
-    uint64_t least = ~0ull;
-    for (int i = 0; i < count; ++i) {
-        const uint64_t threads = (dim + choices[i] - 1) / choices[i], whole = (threads + 31) / 32 * 32;
-        if (whole > kRowThreads) continue;
-        const uint64_t cost = whole * (choices[i] + fixed + (whole > 32 ? fixed / 2 : 0));
-        if (cost < least) { least = cost; best = choices[i]; }
-    }
-    return best;
-}
 
 // Sum over `lanes` neighbouring lanes, a power of two up to 32.
 __device__ __forceinline__ float lanes_sum(float v, uint32_t lanes)
