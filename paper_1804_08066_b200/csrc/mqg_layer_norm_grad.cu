@@ -224,27 +224,43 @@ __global__ void __launch_bounds__(kRowThreads, (kResident<X, Y, V, E>)) grad_row
         }
     }
     if (!kSums<E> || !sums) return;
-    // The groups' sums, in their order, through shared memory.
+    // The groups' sums through shared memory, in a fixed order: where there are more threads than columns, each adds up the groups of
+    // one of several stripes, and then one the stripes.
     if constexpr (R::kAsync) wait_copies<0>();
     __syncthreads();
-    float* all = reinterpret_cast<float*>(memory);      // [groups][dim] of one sum, then of the other
-    float* totals = all + kRowThreads * E;              // [2][dim]
-    const uint32_t dim = (uint32_t)a.dim;
+    const uint32_t dim = (uint32_t)a.dim, columns = 2 * dim;        // of dweight and of dbias
+    float* all = reinterpret_cast<float*>(memory);      // [2][groups][dim]
+    float* totals = all + 2 * kRowThreads * E;          // [stripes][2][dim]
 #pragma unroll
-    for (int which = 0; which < 2; ++which) {
-#pragma unroll
-        for (int e = 0; e < E; ++e) {
-            const float2 pair = which == 0 ? dw[e / 2] : db[e / 2];
-            if (at.has(e / V)) all[group * dim + at.element(e / V) + e % V] = e % 2 ? pair.y : pair.x;
+    for (int e = 0; e < E; ++e)
+        if (at.has(e / V)) {
+            float* to = all + group * dim + at.element(e / V) + e % V;
+            to[0] = e % 2 ? dw[e / 2].y : dw[e / 2].x;
+            to[groups * dim] = e % 2 ? db[e / 2].y : db[e / 2].x;
+        }
+    __syncthreads();
+    float* left = a.partial != nullptr ? a.partial + (uint64_t)blockIdx.x * columns : totals;
+    if (columns >= blockDim.x) {
+        for (uint32_t i = threadIdx.x; i < columns; i += blockDim.x) {
+            const float* from = all + (i < dim ? i : groups * dim + i - dim);
+            float total = from[0];
+            for (uint32_t g = 1; g < groups; ++g) total += from[g * dim];
+            left[i] = total;
+        }
+    } else {
+        const uint32_t stripes = blockDim.x / columns, stripe = threadIdx.x / columns, column = threadIdx.x - stripe * columns;
+        float total = 0.0f;
+        if (stripe < stripes) {
+            const float* from = all + (column < dim ? column : groups * dim + column - dim);
+#pragma unroll 4
+            for (uint32_t g = stripe; g < groups; g += stripes) total += from[g * dim];
+            totals[threadIdx.x] = total;
         }
         __syncthreads();
-        for (uint32_t col = threadIdx.x; col < dim; col += blockDim.x) {
-            float total = 0.0f;
-            for (uint32_t i = 0; i < groups; ++i) total += all[i * dim + col];
-            if (a.partial != nullptr) a.partial[((uint64_t)blockIdx.x * 2 + which) * dim + col] = total;
-            else totals[which * dim + col] = total;
+        if (stripe == 0) {
+            for (uint32_t k = 1; k < stripes; ++k) total += totals[k * columns + column];
+            left[column] = total;                       // (where that is in `totals`: what this thread alone has read)
         }
-        __syncthreads();
     }
     if (a.partial != nullptr) return;
     // Every CTA of the cluster adds up the totals of its share of the columns, in the CTAs' order.
