@@ -32,8 +32,8 @@ template <int X, int V, int E> struct Ring {
 
 template <int E> constexpr int kResident = E <= 8 ? 2 : 1;
 
-// E elements to a thread, V to a vector.
-template <int X, int Y, int V, int E, bool WIDE>
+// E elements to a thread, V to a vector.  FULL: rows of E times the threads of a group, without a condition on any vector.
+template <int X, int Y, int V, int E, bool WIDE, bool FULL>
 __global__ void __launch_bounds__(kRowThreads, kResident<E>) norm_rows_kernel(const NormArgs a, uint32_t threads)
 {
     using R = Ring<X, V, E>;
@@ -42,7 +42,7 @@ __global__ void __launch_bounds__(kRowThreads, kResident<E>) norm_rows_kernel(co
     auto& ring = *reinterpret_cast<R*>(memory);
     __shared__ RowSums sums;
     const uint32_t place = threadIdx.x % threads, group = threadIdx.x / threads, groups = blockDim.x / threads;
-    const RowPlace<V, K, WIDE> at(a.dim, place, threads);
+    const RowPlace<V, K, WIDE, FULL> at(a.dim, place, threads);
     const uint64_t stride = (uint64_t)gridDim.x * groups;
     const float per_element = __fdiv_rn(1.0f, (float)a.dim);
     grid_dependency_wait();
@@ -174,11 +174,11 @@ template <int X, int Y> __global__ void __launch_bounds__(kLongThreads) norm_lon
     }
 }
 
-template <int X, int Y, int V, int E, bool WIDE> cudaError_t launch_groups(const NormArgs& a, const RowGroups& g, cudaStream_t stream)
+template <int X, int Y, int V, int E, bool WIDE, bool FULL> cudaError_t launch_groups(const NormArgs& a, const RowGroups& g, cudaStream_t stream)
 {
     using R = Ring<X, V, E>;
     static std::atomic<bool> ready[64];
-    const auto kernel = norm_rows_kernel<X, Y, V, E, WIDE>;
+    const auto kernel = norm_rows_kernel<X, Y, V, E, WIDE, FULL>;
     constexpr size_t kBytes = R::kAsync ? sizeof(R) : 0;
     if (const cudaError_t err = allow_shared(kernel, kBytes, ready)) return err;
     return launch_pdl_smem(kernel, g.ctas, g.block, kBytes, stream, a, g.threads);
@@ -187,9 +187,14 @@ template <int X, int Y, int V, int E, bool WIDE> cudaError_t launch_groups(const
 template <int X, int Y, int V, int E> cudaError_t launch_elements(const NormArgs& a, cudaStream_t stream)
 {
     const RowGroups g = row_groups(a.rows, a.dim, E, kResident<E> * kRowThreads);
-    if constexpr (V > 1 || E <= 8)
-        if (g.threads < 32) return launch_groups<X, Y, V, E, false>(a, g, stream);
-    return launch_groups<X, Y, V, E, true>(a, g, stream);
+    if constexpr (V > 1) {
+        if (a.dim == (uint64_t)g.threads * E)
+            return g.threads < 32 ? launch_groups<X, Y, V, E, false, true>(a, g, stream) : launch_groups<X, Y, V, E, true, true>(a, g, stream);
+    }
+    if constexpr (V > 1 || E <= 8) {
+        if (g.threads < 32) return launch_groups<X, Y, V, E, false, false>(a, g, stream);
+    }
+    return launch_groups<X, Y, V, E, true, false>(a, g, stream);
 }
 
 // The more elements a thread has, the fewer shuffles and barriers there are to a row, and the more is under way: with 8 / 16 / 32 elements

@@ -69,8 +69,8 @@ template <int W> __device__ __forceinline__ void store_sum(void* dweight, void* 
 // Rows of more elements leave the sums over the rows to a kernel of their own: registers hold no more.
 template <int E> constexpr bool kSums = E <= 16;
 
-// E elements to a thread, V to a vector.
-template <int X, int Y, int V, int E, bool WIDE>
+// E elements to a thread, V to a vector.  FULL: rows of E times the threads of a group, without a condition on any vector.
+template <int X, int Y, int V, int E, bool WIDE, bool FULL>
 __global__ void __launch_bounds__(kRowThreads, (kResident<X, Y, V, E>)) grad_rows_kernel(const GradArgs a, uint32_t threads, int sums)
 {
     using R = Ring<X, Y, V, E>;
@@ -79,7 +79,7 @@ __global__ void __launch_bounds__(kRowThreads, (kResident<X, Y, V, E>)) grad_row
     auto& ring = *reinterpret_cast<R*>(memory);
     __shared__ RowSums row_sums;
     const uint32_t place = threadIdx.x % threads, group = threadIdx.x / threads, groups = blockDim.x / threads;
-    const RowPlace<V, K, WIDE> at(a.dim, place, threads);
+    const RowPlace<V, K, WIDE, FULL> at(a.dim, place, threads);
     // the first thread of this one's group in its warp
     const uint32_t first = threads >= 32 ? threadIdx.x & ~31u : threadIdx.x - place;
     const uint64_t stride = (uint64_t)gridDim.x * groups;
@@ -399,12 +399,12 @@ uint32_t long_parts(uint64_t rows, uint64_t dim)
     return (uint32_t)(most < want ? (most < 1 ? 1 : most) : want);
 }
 
-template <int X, int Y, int V, int E, bool WIDE>
+template <int X, int Y, int V, int E, bool WIDE, bool FULL>
 cudaError_t launch_groups(const GradArgs& a, const RowGroups& g, uint32_t cluster, int sums, cudaStream_t stream)
 {
     using R = Ring<X, Y, V, E>;
     static std::atomic<bool> ready[64];
-    const auto kernel = grad_rows_kernel<X, Y, V, E, WIDE>;
+    const auto kernel = grad_rows_kernel<X, Y, V, E, WIDE, FULL>;
     constexpr size_t kAll = kSums<E> ? 3 * kRowThreads * E * sizeof(float) : 16, kBytes = R::kAsync && sizeof(R) > kAll ? sizeof(R) : kAll;
     if (const cudaError_t err = allow_shared(kernel, kBytes, ready)) return err;
     if (cluster == 0) return launch_pdl_smem(kernel, g.ctas, g.block, kBytes, stream, a, g.threads, sums);
@@ -433,9 +433,15 @@ template <int X, int Y, int V, int E> cudaError_t launch_elements(GradArgs a, in
         a.partial = nullptr;
         *parts = 0;
     }
-    if constexpr (V > 1 || E <= 8)
-        if (g.threads < 32) return launch_groups<X, Y, V, E, false>(a, g, cluster, sums, stream);
-    return launch_groups<X, Y, V, E, true>(a, g, cluster, sums, stream);
+    if constexpr (V > 1) {
+        if (a.dim == (uint64_t)g.threads * E)
+            return g.threads < 32 ? launch_groups<X, Y, V, E, false, true>(a, g, cluster, sums, stream)
+                                  : launch_groups<X, Y, V, E, true, true>(a, g, cluster, sums, stream);
+    }
+    if constexpr (V > 1 || E <= 8) {
+        if (g.threads < 32) return launch_groups<X, Y, V, E, false, false>(a, g, cluster, sums, stream);
+    }
+    return launch_groups<X, Y, V, E, true, false>(a, g, cluster, sums, stream);
 }
 
 // Elements to a thread.  More of them cost fewer shuffles and barriers to a row: with 8 / 16 65,536 rows of 4096 in bf16 take 326 / 270 us,

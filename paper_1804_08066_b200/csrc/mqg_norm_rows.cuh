@@ -86,15 +86,15 @@ inline RowGroups row_groups(uint64_t rows, uint64_t dim, uint32_t e, uint32_t pe
     return g;
 }
 
-// A thread's vectors: their places in the row, which of them the row has.
-template <int V, int K, bool WIDE> struct RowPlace {
+// A thread's vectors: their places in the row, which of them the row has (FULL: all, of every thread).
+template <int V, int K, bool WIDE, bool FULL> struct RowPlace {
     static constexpr bool kByWarp = WIDE && V == 1;
     uint32_t start, threads, vectors, held;
     __device__ __forceinline__ RowPlace(uint64_t dim, uint32_t place, uint32_t group_threads)
         : start(kByWarp ? (place & ~31u) * K + (place & 31) : place), threads(group_threads), vectors((uint32_t)(dim / V)),
           held(vectors > start ? (vectors - start + 31) / 32 : 0) {}
     __device__ __forceinline__ uint32_t step() const { return kByWarp ? 32 : threads; }
-    __device__ __forceinline__ bool has(int k) const { return kByWarp ? (uint32_t)k < held : start + k * step() < vectors; }
+    __device__ __forceinline__ bool has(int k) const { return FULL || (kByWarp ? (uint32_t)k < held : start + k * step() < vectors); }
     __device__ __forceinline__ uint32_t element(int k) const { return (start + k * step()) * V; }
 };
 
