@@ -96,6 +96,7 @@ template <int V, int K, bool WIDE, bool FULL> struct RowPlace {
     __device__ __forceinline__ uint32_t step() const { return kByWarp ? 32 : threads; }
     __device__ __forceinline__ bool has(int k) const { return FULL || (kByWarp ? (uint32_t)k < held : start + k * step() < vectors); }
     __device__ __forceinline__ uint32_t element(int k) const { return (start + k * step()) * V; }
+    __device__ __forceinline__ uint32_t beyond(int k) const { return k * step() * V; }          // element(k) - element(0)
 };
 
 // Sum over `lanes` neighbouring lanes, a power of two up to 32.
