@@ -458,7 +458,8 @@ mqg_status mqg_embedding_grad(const void* dout, mqg_dtype dout_dtype, const void
  *   decays      [in] HOST array of `count` floats, or NULL for zeros
  *   lr >= 0; 0 <= b < 1 (in fp32); eps >= 2^-50; decays >= 0; grad_scale finite (1 / P for the mean of P workers); step >= 1
  *   factor      [in] NULL, or one float in DEVICE memory: result + 1 of mqg_grad_norm, for instance.  Where it is NaN, infinite or
- *               0 (a gradient with a NaN or an infinity in it), the call changes nothing.
+ *               0 (a gradient with a NaN or an infinity in it), the call changes nothing.  Without it a NaN or an infinity reaches
+ *               its element's parameter and averages, and with averages in 8 bits those of its block.
  *   schedule    [in] NULL, or 4 floats in DEVICE memory that take the place of lr and step: lr, 1 - b1^t, 1 - b2^t, t (a whole
  *               number below 2^24).  For calls that are captured into a graph: the other scalars are those of the capture.
  * Errors: MQG_ERR_INVALID (the above; null pointers, unknown types, 2^42 elements or more), MQG_ERR_ALIGN.

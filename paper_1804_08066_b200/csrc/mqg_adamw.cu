@@ -184,7 +184,14 @@ __device__ __forceinline__ uint32_t encode_v(float v, float inverse, uint32_t h)
     return max(code, min(__float_as_uint(v), inverse > 0.0f ? 1u << 21 : 0u) >> 21);
 }
 
-// Largest of a warp's non-negative floats.
+// Largest magnitude; a NaN among them stays one.
+__device__ __forceinline__ float largest(float most, float a, float b)
+{
+    float r;
+    asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(most), "f"(fabsf(a)), "f"(fabsf(b)));
+    return r;
+}
+// Largest of a warp's non-negative floats (as numbers their bits are in the same order, and a NaN's are above all).
 __device__ __forceinline__ float warp_max(float x) { return __uint_as_float(__reduce_max_sync(0xFFFFFFFFu, __float_as_uint(x))); }
 
 // A block's two scales, which it stores, and what its elements are multiplied with for their codes.  One division for the warp: lane
@@ -193,7 +200,7 @@ __device__ __forceinline__ void new_scales(float most_m, float most_v, float* sc
 {
     const uint32_t lane = threadIdx.x & 31;
     const float all_m = warp_max(most_m), all_v = warp_max(most_v), most = lane & 2 ? all_v : all_m, top = lane & 2 ? kTopV : kTopM;
-    const float q = most >= kLeast ? __fdiv_rn(lane & 1 ? top : most, lane & 1 ? most : top) : 0.0f;
+    const float q = most < kLeast ? 0.0f : __fdiv_rn(lane & 1 ? top : most, lane & 1 ? most : top);      // (of a NaN: NaN)
     if (lane == 0 || lane == 2) scales[lane >> 1] = q;
     inverse_m = __shfl_sync(0xFFFFFFFFu, q, 1);
     inverse_v = __shfl_sync(0xFFFFFFFFu, q, 3);
@@ -374,8 +381,8 @@ __device__ __forceinline__ void step_vectors(const Place<P, G, EIGHT>& at, uint6
     for (int i = 0; i < 8; i += 2) {
         update2(p + i, g + i, m + i, v + i, s, st, rate);
         if (EIGHT) {
-            most_m = max3_abs(most_m, m[i], m[i + 1]);
-            most_v = max3_abs(most_v, v[i], v[i + 1]);
+            most_m = largest(most_m, m[i], m[i + 1]);
+            most_v = largest(most_v, v[i], v[i + 1]);
         }
     }
 #pragma unroll
@@ -449,8 +456,8 @@ __device__ __forceinline__ void step_elements(const Block& b, const Scalars& s, 
     for (int i = 0; i < kPerLane; i += 2) {
         update2(p + i, g + i, m + i, v + i, s, st, rate);
         if (EIGHT) {
-            most_m = max3_abs(most_m, m[i], m[i + 1]);  // (places without elements stay zeros)
-            most_v = max3_abs(most_v, v[i], v[i + 1]);
+            most_m = largest(most_m, m[i], m[i + 1]);  // (places without elements stay zeros)
+            most_v = largest(most_v, v[i], v[i + 1]);
         }
     }
 #pragma unroll

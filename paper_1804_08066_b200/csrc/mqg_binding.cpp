@@ -805,9 +805,9 @@ struct AdamwLists {
             if (!items[k].object) throw PythonError();
         }
         n = (size_t)PySequence_Fast_GET_SIZE(items[0].object);
-        const Reference numbers = {absent(decays) || PyNumber_Check(decays) ? nullptr : PySequence_Tuple(decays)};
-        const bool one = !absent(decays) && !numbers.object;
-        if (one && PyErr_Occurred()) throw PythonError();
+        const bool several = !absent(decays) && (PySequence_Check(decays) || PyIter_Check(decays)), one = !absent(decays) && !several;
+        const Reference numbers = {several ? PySequence_Tuple(decays) : nullptr};
+        if (several && !numbers.object) throw PythonError();
         const double all = one ? to_double(decays) : 0.0;
         has_decay = !absent(decays);
         const size_t per = kMost * sizeof(void*) + sizeof(uint64_t) + 2 * sizeof(mqg_dtype) + sizeof(float);

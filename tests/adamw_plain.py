@@ -33,24 +33,27 @@ def moments32(g, m, v, *, beta1, beta2, k=1.0):
     return m2, v2
 
 
-def philox(counter, key):
-    """Philox4x32-10 of Python integers: four words."""
-    c, k = list(counter), list(key)
+def philox(c0, c1, c2, c3, key):
+    """Philox4x32-10 of arrays of 32-bit numbers held in 64 bits: four words."""
+    u = np.uint64
+    low, shift = u(0xFFFFFFFF), u(32)
+    c = [np.asarray(x, u) for x in (c0, c1, c2, c3)]
+    k = [key & 0xFFFFFFFF, key >> 32 & 0xFFFFFFFF]
     for _ in range(10):
-        p0, p1 = 0xD2511F53 * c[0], 0xCD9E8D57 * c[2]
-        c = [(p1 >> 32) ^ c[1] ^ k[0], p1 & 0xFFFFFFFF, (p0 >> 32) ^ c[3] ^ k[1], p0 & 0xFFFFFFFF]
+        p0, p1 = u(0xD2511F53) * c[0], u(0xCD9E8D57) * c[2]
+        c = [p1 >> shift ^ c[1] ^ u(k[0]), p1 & low, p0 >> shift ^ c[3] ^ u(k[1]), p0 & low]
         k = [(k[0] + 0x9E3779B9) & 0xFFFFFFFF, (k[1] + 0xBB67AE85) & 0xFFFFFFFF]
     return c
 
 
-def draws(block, seed, step):
-    """The 16-bit draws of block number `block`'s elements."""
-    h = np.zeros(BLOCK, np.uint32)
-    for lane in range(32):
-        q = 32 * block + lane
-        words = philox([q & 0xFFFFFFFF, q >> 32, 0xFFFFFFFF, step], [seed & 0xFFFFFFFF, seed >> 32 & 0xFFFFFFFF])
-        for s in range(8):
-            h[(s // 4) * 128 + 4 * lane + s % 4] = words[s // 2] >> 16 * (s % 2) & 0xFFFF
+def draws(first_block, count, seed, step):
+    """The 16-bit draws of the elements of `count` blocks."""
+    q = np.arange(32 * count, dtype=np.uint64) + np.uint64(32 * first_block)
+    words = philox(q & np.uint64(0xFFFFFFFF), q >> np.uint64(32), np.full_like(q, 0xFFFFFFFF), np.full_like(q, step), seed)
+    h = np.zeros((count, BLOCK), np.uint32)
+    lane = 4 * np.arange(32)
+    for s in range(8):
+        h[:, (s // 4) * 128 + lane + s % 4] = (words[s // 2] >> np.uint64(16 * (s % 2)) & np.uint64(0xFFFF)).reshape(count, 32)
     return h
 
 
@@ -94,11 +97,13 @@ def step8(p, g, m, v, scales, first_block, *, seed, step, beta1, beta2, k=1.0, *
     n = len(g)
     m2c, v2c, s2 = np.zeros(n, np.uint8), np.zeros(n, np.uint8), np.zeros_like(scales)
     wide_m, wide_v = np.zeros(n, f32), np.zeros(n, f32)
-    for b in range(-(-n // BLOCK)):
+    blocks = -(-n // BLOCK)
+    all_draws = draws(first_block, blocks, seed, step)
+    for b in range(blocks):
         at = slice(b * BLOCK, min(n, (b + 1) * BLOCK))
         wide_m[at], wide_v[at] = decode(m[at], E4M3, scales[b, 0]), decode(v[at], E5M2, scales[b, 1])
         m2, v2 = moments32(g[at], wide_m[at], wide_v[at], beta1=beta1, beta2=beta2, k=k)
-        h = draws(first_block + b, seed, step)[:m2.size]
+        h = all_draws[b, :m2.size]
         s2[b, 0], codes = pack(np.abs(m2), TOP_M, E4M3, h)
         m2c[at] = codes | np.where(m2 < 0, 0x80, 0).astype(np.uint8)
         s2[b, 1], codes = pack(v2, TOP_V, E5M2, swapped(h))

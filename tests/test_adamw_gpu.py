@@ -1,6 +1,9 @@
 """AdamW over many tensors against its formulas: m and v bit for bit with fp32 operations rounded one by one, parameters within
 the roundings of the 64-bit result, codes and scales of states in 8 bits bit for bit."""
 import math
+import pathlib
+import subprocess
+import sys
 
 import numpy as np
 import pytest
@@ -331,3 +334,84 @@ def test_what_the_binding_takes_and_refuses():
     mqg.mqg_adamw8(iter([t]), (torch.ones(300, device="cuda") for _ in range(1)), [eight], [eight.clone()], [s], iter([0.5]), seed=1,
                    **hyper)
     assert ((t + HYPER["lr"]).abs() <= 1e-3 * HYPER["lr"]).all()
+
+
+@pytest.mark.parametrize("eight", [False, True], ids=["32", "8"])
+@pytest.mark.parametrize("types,shift", [((F32, F32), 0), ((BF16, BF16), 4), ((F32, BF16), 1)], ids=str)
+def test_lists_that_give_a_warp_several_blocks(types, shift, eight):
+    """More blocks than four times the warps that the device holds: whole runs of them, ends within a run, and tails."""
+    sizes = [2_900_000, 1000, 2_000_000 + 37, 256 * 9, 0, 255, 256 * 32 + 1]
+    lists = Lists(sizes, *types, eight=eight, shift=shift, seed=11)
+    decays = [0.1 * (j % 2) for j in range(len(sizes))]
+    before = lists.state()
+    lists.step(3, decays, factor=torch.tensor([0.5], device="cuda"))
+    after = lists.state()
+    check(lists, before, after, 3, decays, k=0.5)
+    lists.step(4, decays, factor=torch.tensor([math.nan], device="cuda"))
+    again = lists.state()
+    assert all(same(a, b) for x in after for a, b in zip(after[x], again[x]))
+
+
+def test_a_nan_without_a_factor_stays_in_its_block():
+    lists = Lists([3 * BLOCK, 40], eight=True)
+    clean = Lists([3 * BLOCK, 40], eight=True)
+    lists.g[0].view[BLOCK + 5] = math.nan
+    lists.step(2), clean.step(2)
+    a, b = lists.state(), clean.state()
+    assert np.isnan(a["s"][0][1]).all() and np.isnan(a["p"][0][BLOCK + 5])
+    other = np.r_[0:BLOCK, 2 * BLOCK:3 * BLOCK]
+    for x in "pmv":
+        assert same(a[x][0][other], b[x][0][other]) and same(a[x][1], b[x][1])
+    assert np.isnan(a["p"][0]).sum() == 1 and same(a["s"][0][[0, 2]], b["s"][0][[0, 2]])
+
+
+def test_decays_in_every_form():
+    want = Lists([300, 20])
+    want.step(2, [0.25, 0.5])
+    for decays in (np.array([0.25, 0.5]), (0.25, 0.5), iter([0.25, 0.5])):
+        lists = Lists([300, 20])
+        lists.step(2, decays)
+        assert all(same(a, b) for a, b in zip(want.state()["p"], lists.state()["p"]))
+    same_for_all = [Lists([300, 20]) for _ in range(3)]
+    for lists, decay in zip(same_for_all, (0.25, np.float32(0.25), [0.25, 0.25])):
+        lists.step(2, decay)
+    none = [Lists([300, 20]) for _ in range(2)]
+    none[0].step(2, None), none[1].step(2, 0)
+    for group in (same_for_all, none):
+        assert all(same(a, b) for lists in group[1:] for a, b in zip(group[0].state()["p"], lists.state()["p"]))
+
+
+FIRST_CALLS = """
+import torch, paper_1804_08066_b200 as mqg
+x = torch.randn({rows}, {dim}, device="cuda")
+y, dx, stats = torch.empty_like(x), torch.empty_like(x), torch.empty({rows}, 2, device="cuda")
+w, dw, db = (torch.ones({dim}, device="cuda") for _ in range(3))
+work = torch.empty(mqg.mqg_layer_norm_workspace_floats({rows}, {dim}), device="cuda")
+t = [torch.zeros(300, device="cuda") for _ in range(4)]
+s = torch.zeros(4, device="cuda")
+codes = [torch.zeros(300, dtype=torch.uint8, device="cuda") for _ in range(2)]
+hyper = dict(lr=1e-3, beta1=0.9, beta2=0.999, eps=1e-8, step=1)
+torch.cuda.synchronize()
+graph = torch.cuda.CUDAGraph()
+with torch.cuda.graph(graph):
+    mqg.mqg_layer_norm(x, {rows}, {dim}, w, None, 1e-5, y, stats)
+    mqg.mqg_layer_norm_grad(y, x, {rows}, {dim}, w, stats, dx, dw, db, work)
+    mqg.mqg_adamw([t[0]], [t[1]], [t[2]], [t[3]], 0.0, **hyper)
+    mqg.mqg_adamw8([t[0]], [t[1]], [codes[0]], [codes[1]], [s], 0.0, seed=1, **hyper)
+t[1].fill_(1.0)
+graph.replay()
+torch.cuda.synchronize()
+got = y.clone(), dx.clone(), dw.clone(), t[0].clone()
+assert abs(float(y[0].mean())) < 1e-3 and (t[0] < -1.9e-3).all() and s[0] > 0
+mqg.mqg_layer_norm(x, {rows}, {dim}, w, None, 1e-5, y, stats)
+mqg.mqg_layer_norm_grad(y, x, {rows}, {dim}, w, stats, dx, dw, db, work)
+assert torch.equal(got[0], y) and torch.equal(got[1], dx) and torch.equal(got[2], dw)
+print("same")
+"""
+
+
+@pytest.mark.parametrize("rows,dim", [(40, 256), (3000, 1024), (500, 515), (60, 9000)])
+def test_the_first_calls_of_a_process_may_be_captured(rows, dim):
+    root = pathlib.Path(__file__).resolve().parent.parent
+    r = subprocess.run([sys.executable, "-c", FIRST_CALLS.format(rows=rows, dim=dim)], cwd=root, capture_output=True, text=True, timeout=300)
+    assert r.returncode == 0 and r.stdout.split() == ["same"], r.stderr[-2000:]

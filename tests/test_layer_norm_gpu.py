@@ -80,11 +80,17 @@ def test_forward_without_weights_or_stats():
             check(x, 5, dim, ww, bb, y, None)
 
 
-@pytest.mark.parametrize("rows,dim", [(70_000, 64), (20_011, 515), (5_000, 1024), (3_000, 4096), (700, 9000)])
-def test_forward_of_many_rows(rows, dim):
-    x = made((rows, dim), BF16, 0, 1.0, 0.3)
+MANY = [(70_000, 64, (BF16, BF16)), (20_011, 515, (BF16, BF16)), (5_000, 1024, (BF16, BF16)), (3_000, 4096, (BF16, BF16)), (700, 9000, (BF16, BF16)),
+        (9_000, 256, (F32, F32)), (3_000, 1028, (F32, BF16)), (3_000, 1024, (BF16, F32)), (900, 2056, (F32, F32)), (90_000, 33, (F32, F32)),
+        (200_000, 16, (BF16, BF16)), (3_000, 1001, (BF16, F32)), (1_500, 3333, (F32, F32)), (500, 6001, (F32, F32)), (300, 7000, (BF16, BF16)),
+        (400, 8192, (F32, F32)), (200, 15_001, (F32, BF16)), (150, 16_384, (F32, F32)), (2_500, 768, (BF16, BF16))]
+
+
+@pytest.mark.parametrize("rows,dim,types", MANY, ids=str)
+def test_forward_of_many_rows(rows, dim, types):
+    x = made((rows, dim), types[0], 0, 1.0, 0.3)
     w, b = made((dim,), F32, 0, 0.3, 1.0, seed=1), made((dim,), F32, 0, 0.5, seed=2)
-    y, stats = Buffer(rows * dim, BF16, 0), Buffer(rows * 2, F32, 0)
+    y, stats = Buffer(rows * dim, types[1], 0), Buffer(rows * 2, F32, 0)
     run(x, rows, dim, w, b, y, stats)
     check(x, rows, dim, w, b, y, stats)
 
@@ -108,13 +114,14 @@ def test_no_rows_and_no_elements():
     mqg.mqg_layer_norm(e, 0, 64, None, None, EPS, y.view)
     mqg.mqg_layer_norm(e, 7, 0, None, None, EPS, y.view)
     assert torch.equal(before.view(torch.int32), y.cpu().view(torch.int32))
-    dw = torch.full((64,), 3.0, device="cuda")
-    db = torch.full((64,), 4.0, device="cuda")
-    work = torch.empty(mqg.mqg_layer_norm_workspace_floats(0, 64), device="cuda")
-    mqg.mqg_layer_norm_grad(e, e, 0, 64, None, e, None, dw, db, work, add_into_grads=True)
-    assert (dw == 3).all() and (db == 4).all()
-    mqg.mqg_layer_norm_grad(e, e, 0, 64, None, e, None, dw, db, work)
-    assert not dw.any() and not db.any()
+    for dim in (64, 515, 1024, 4096, 6000, 17000):
+        dw = torch.full((dim,), 3.0, device="cuda")
+        db = torch.full((dim,), 4.0, device="cuda")
+        work = torch.empty(mqg.mqg_layer_norm_workspace_floats(0, dim), device="cuda")
+        mqg.mqg_layer_norm_grad(e, e, 0, dim, None, e, None, dw, db, work, add_into_grads=True)
+        assert (dw == 3).all() and (db == 4).all()
+        mqg.mqg_layer_norm_grad(e, e, 0, dim, None, e, None, dw, db, work)
+        assert not dw.any() and not db.any()
 
 
 def grad(dy, x, rows, dim, w, stats, dx, dw, db, add=False):
@@ -167,9 +174,9 @@ def test_gradient(dim, types):
         grad_check(*c)
 
 
-@pytest.mark.parametrize("rows,dim", [(70_000, 64), (20_011, 515), (5_000, 1024), (3_000, 4096), (700, 9000)])
-def test_gradient_of_many_rows(rows, dim):
-    c = grad_case(rows, dim, (BF16, BF16))
+@pytest.mark.parametrize("rows,dim,types", MANY, ids=str)
+def test_gradient_of_many_rows(rows, dim, types):
+    c = grad_case(rows, dim, types)
     grad(*c)
     grad_check(*c)
 
