@@ -797,6 +797,8 @@ struct AdamwLists {
     float* decay;
     bool has_decay = false;
     Operands on;
+    const c10::StorageImpl* last_storage = nullptr;
+    char* last_start = nullptr;
 
     AdamwLists(PyObject* const* lists, int count, PyObject* decays, PyObject* factor, PyObject* schedule) : nlists(count)
     {
@@ -831,10 +833,7 @@ struct AdamwLists {
             }
         for (int k = 0; k < count; ++k) {
             PyObject** item = PySequence_Fast_ITEMS(items[k].object);
-            for (size_t j = 0; j < n; ++j) {
-                look_ahead(item, j, n);
-                read(k, j, item[j]);
-            }
+            for (size_t j = 0; j < n; ++j) read(k, j, item[j]);
         }
         this->factor = absent(factor) ? nullptr : on.floats(factor, "factor", 1);
         this->schedule = absent(schedule) ? nullptr : on.floats(schedule, "schedule", 4);
@@ -845,39 +844,46 @@ struct AdamwLists {
 
     static const char* name(int k) { return (const char* const[]){"params", "grads", "m", "v", "scales"}[k]; }
 
-    // Brings the objects that come next into the cache: a list's tensors lie wherever they were made, and waiting for them is most
-    // of what reading a list of hundreds takes.
-    static void look_ahead(PyObject** item, size_t j, size_t n)
+    // A tensor's address.  Of tensors one after the other that are slices of one vector, only the first one's is asked for, which takes
+    // as long as everything else that is wanted of a tensor.
+    void* address(const at::Tensor& t, uint64_t held, int64_t bytes)
     {
-        if (j + 16 < n) __builtin_prefetch(item[j + 16]);
-        if (j + 8 < n && is_tensor(item[j + 8])) {
-            const char* impl = reinterpret_cast<const char*>(THPVariable_Unpack(item[j + 8]).unsafeGetTensorImpl());
-            for (int line = 0; line < 4; ++line) __builtin_prefetch(impl + 64 * line);
+        const at::TensorImpl* impl = t.unsafeGetTensorImpl();
+        const c10::StorageImpl* from = impl->unsafe_storage().unsafeGetStorageImpl();
+        if (held != 0 && from == last_storage) return last_start + impl->storage_offset() * bytes;
+        void* p = t.data_ptr();
+        if (held != 0) {
+            last_storage = from;
+            last_start = static_cast<char*>(p) - impl->storage_offset() * bytes;
         }
+        return p;
     }
     void read(int k, size_t j, PyObject* o)
     {
-        if (k < 2) {
-            uint64_t held;
-            ptr[k][j] = on.values(o, name(k), 0, &dtype[k][j], (Py_ssize_t)j, &held);
-            if (k == 0) size[j] = held;
-            check_size(k, j, held);
-            return;
-        }
         const at::Tensor& t = on.tensor(o, name(k), 0, (Py_ssize_t)j);
         const at::ScalarType s = t.scalar_type();
-        if (k == 4 || nlists == 4 ? s != at::kFloat : s != at::kByte && s != (k == 2 ? at::kFloat8_e4m3fn : at::kFloat8_e5m2)) {
-            PyErr_Format(PyExc_TypeError, "%s[%zu] must be %s, got %s", name(k), j,
-                         k == 4 || nlists == 4 ? "float32" : k == 2 ? "float8_e4m3fn or uint8" : "float8_e5m2 or uint8", c10::toString(s));
+        const uint64_t held = (uint64_t)t.numel();
+        if (k < 2) {
+            if (s != at::kFloat && s != at::kBFloat16) wrong_type(k, j, "float32 or bfloat16", s);
+            dtype[k][j] = s == at::kFloat ? MQG_F32 : MQG_BF16;
+            if (k == 0) size[j] = held;
+        } else if (k == 4 || nlists == 4) {
+            if (s != at::kFloat) wrong_type(k, j, "float32", s);
+        } else if (s != at::kByte && s != (k == 2 ? at::kFloat8_e4m3fn : at::kFloat8_e5m2)) {
+            wrong_type(k, j, k == 2 ? "float8_e4m3fn or uint8" : "float8_e5m2 or uint8", s);
+        }
+        ptr[k][j] = address(t, held, s == at::kFloat ? 4 : s == at::kBFloat16 ? 2 : 1);
+        if (k < 4) return check_size(k, j, held);
+        if (held != ::mqg_adamw8_scale_floats(size[j])) {
+            PyErr_Format(PyExc_ValueError, "scales[%zu] holds %llu floats, params[%zu] needs %zu (mqg_adamw8_scale_floats)", j,
+                         (unsigned long long)held, j, ::mqg_adamw8_scale_floats(size[j]));
             throw PythonError();
         }
-        ptr[k][j] = t.data_ptr();
-        if (k < 4) return check_size(k, j, (uint64_t)t.numel());
-        if ((uint64_t)t.numel() != ::mqg_adamw8_scale_floats(size[j])) {
-            PyErr_Format(PyExc_ValueError, "scales[%zu] holds %lld floats, params[%zu] needs %zu (mqg_adamw8_scale_floats)", j,
-                         (long long)t.numel(), j, ::mqg_adamw8_scale_floats(size[j]));
-            throw PythonError();
-        }
+    }
+    [[noreturn]] static void wrong_type(int k, size_t j, const char* wanted, at::ScalarType s)
+    {
+        PyErr_Format(PyExc_TypeError, "%s[%zu] must be %s, got %s", name(k), j, wanted, c10::toString(s));
+        throw PythonError();
     }
     void check_size(int k, size_t j, uint64_t held) const
     {
