@@ -445,8 +445,8 @@ mqg_status mqg_embedding_grad(const void* dout, mqg_dtype dout_dtype, const void
  *     k  = grad_scale * *factor                      g  = k * grad
  *     m <- b1 m + (1 - b1) g                         v <- b2 v + ((1 - b2) g) g
  *     p <- p - (lr decay_j p + lr / (1 - b1^t) * (m / (sqrt(v) / sqrt(1 - b2^t) + eps)))
- * in fp32, every product and sum rounded by itself (m and v are therefore the same bits for whoever follows the formulas; the
- * root and the quotient are within two units in the last place).  1 - b is formed in 64 bits.  A bf16 parameter is rounded to
+ * in fp32.  For m and v every product and sum is rounded by itself, so that they are the same bits for whoever follows the formulas; for
+ * p the root and the quotient are within two units in the last place.  1 - b is formed in 64 bits.  A bf16 parameter is rounded to
  * nearest: changes below 2^-9 of it are lost, so shared parameters are better held in fp32.
  *
  * The lists are HOST arrays of `count` entries, read during the call only: pointers, element counts, types.  A tensor needs its
@@ -495,7 +495,8 @@ mqg_status mqg_adamw8(void* const* params, const mqg_dtype* param_dtypes, const 
 /*
  * Layer norm over rows of `dim` elements, each by itself:
  *     mu = mean(x)    r = 1 / sqrt(mean((x - mu)^2) + eps)    y = (x - mu) * r * weight + bias
- * in fp32 (a second reading of the row for the squares, no difference of large sums), rounded once to a bf16 `y`.
+ * in fp32 (the squares are those of the differences, no difference of large sums; the order of the sums is fixed by dim, the types
+ * and the addresses modulo 16), rounded once to a bf16 `y`.
  *   x             [in] rows x dim elements, row after row;  y [out] the same, of y_dtype
  *   weight, bias  [in] dim elements of weight_dtype each; NULL = ones, zeros
  *   stats         [out] NULL, or 2 floats to a row: mu, r, as the gradient takes them

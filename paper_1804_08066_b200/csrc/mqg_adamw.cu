@@ -15,7 +15,9 @@
 // largest as the root of v.  A v' above zero never becomes zero: its element's next step would have nothing but its own square
 // under the root.
 //
-// Bound by memory: 28 bytes an element in fp32, 16 with states in 8 bits.
+// In 32 bits bound by memory, 28 bytes an element in fp32: 25 M elements in 106 us, 1.02 of the copy rate.  In 8 bits, 14 bytes with
+// bf16 gradients, by instructions, 60 an element: 100 M in 246 us after an idle moment (0.89 of the copy rate), 268 at the power
+// limit.  A block's inputs come by way of shared memory while the one before is computed, which took 288 us to 267.
 #include <cuda_fp16.h>
 
 #include <cmath>
@@ -51,7 +53,8 @@ template <int CAP, bool EIGHT> struct AdamwTable {
 };
 template <bool EIGHT> constexpr int kLargeTable = EIGHT ? 448 : 640;
 
-// Turns of a warp, where there are blocks for four times the warps that the device holds.
+// Turns of a warp, where there are blocks for four times the warps that the device holds.  (100 M elements with states in 8 bits by 2 / 4 / 8 /
+// 16 turns: 263 / 251 / 257 / 267 us.)
 constexpr uint32_t kTurns = 4, kManyBlocks = 148 * 4 * kWarps * 4;
 
 struct Scalars {
@@ -175,7 +178,7 @@ __device__ __forceinline__ float decode_v(uint32_t code, float scale) { return _
 
 __device__ __forceinline__ uint32_t encode_m(float m, float inverse, uint32_t h)
 {
-    return FormatM::code(FormatM::bits(__fmul_rn(fabsf(m), inverse)), h) | (m < 0.0f ? 0x80u : 0u);
+    return FormatM::code(FormatM::bits(__fmul_rn(fabsf(m), inverse)), h) | (__float_as_uint(m) >> 24 & 0x80u);
 }
 // (a v of 2^-128 or more never becomes zero, also where `inverse` takes it below fp32's range)
 __device__ __forceinline__ uint32_t encode_v(float v, float inverse, uint32_t h)
@@ -240,6 +243,7 @@ __device__ __forceinline__ void encode4(const float* m, const float* v, float in
             const uint32_t bits_m = add_draw(h, i ? 16u << 8 : 16u, __float_as_uint(i ? x.y : x.x));   // (27 bits below the sign)
             const uint32_t bits_v = add_draw(turned, i ? 32u << 8 : 32u, __float_as_uint(i ? y.y : y.x));
             at_top_m[j + i] = __float_as_uint(m[j + i]) & 0x80000000u | bits_m * 16u + 8u * 16u & 0x7FFFFFFFu;
+            // (shifted before the maximum, the code of every second element came out three bits too low, with nvcc 12.9)
             at_top_v[j + i] = max(bits_v + 16u, min(__float_as_uint(v[j + i]), least)) * 8u;
         }
     }
@@ -272,7 +276,7 @@ struct Block {
 
 __device__ __forceinline__ void draw(uint64_t group, const Step& st, const RoundKeys& keys, uint32_t (&y)[4])
 {
-    philox4x32_10((uint32_t)group, (uint32_t)(group >> 32), 0xFFFFFFFFu, st.t, keys, y);
+    philox4x32_10((uint32_t)group, (uint32_t)(group >> 32), 0xFFFFFFFFu, st.t, keys, y);   // (no worker's draws of the codec)
 }
 
 // Where a lane's elements of a whole block on the boundaries of four elements are: lane l has the elements 4 l .. 4 l + 3 and
@@ -551,7 +555,8 @@ __device__ __forceinline__ void step_run(Block b, const Run& run, const Scalars&
     if (run.rest != 0) step_elements<P, G, EIGHT, false>(b, s, d, draws);
 }
 
-// A warp to a block, `turns` times; a tile is the blocks that a CTA takes.
+// A warp to a block, `turns` times; a tile is the blocks that a CTA takes.  (Three CTAs to an SM: with four, 64 registers spill, for the
+// same time.)
 template <int CAP, bool EIGHT>
 __global__ void __launch_bounds__(kThreads, 3) adamw_kernel(const __grid_constant__ AdamwTable<CAP, EIGHT> tab, const __grid_constant__ Scalars s, uint32_t turns)
 {

@@ -790,7 +790,7 @@ struct AdamwLists {
     int nlists = 0;
     size_t n = 0;
     std::vector<char> store;
-    char inline_store[kInline * (kMost * sizeof(void*) + sizeof(uint64_t) + 2 * sizeof(mqg_dtype) + sizeof(float))];
+    alignas(8) char inline_store[kInline * (kMost * sizeof(void*) + sizeof(uint64_t) + 2 * sizeof(mqg_dtype) + sizeof(float))];
     void** ptr[kMost];
     uint64_t* size;
     mqg_dtype* dtype[2];

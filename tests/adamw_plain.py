@@ -105,7 +105,7 @@ def step8(p, g, m, v, scales, first_block, *, seed, step, beta1, beta2, k=1.0, *
         m2, v2 = moments32(g[at], wide_m[at], wide_v[at], beta1=beta1, beta2=beta2, k=k)
         h = all_draws[b, :m2.size]
         s2[b, 0], codes = pack(np.abs(m2), TOP_M, E4M3, h)
-        m2c[at] = codes | np.where(m2 < 0, 0x80, 0).astype(np.uint8)
+        m2c[at] = codes | np.where(np.signbit(m2), 0x80, 0).astype(np.uint8)
         s2[b, 1], codes = pack(v2, TOP_V, E5M2, swapped(h))
         above = (v2 >= f32(2.0 ** -128)) & (v2.max() >= LEAST)
         v2c[at] = np.where((codes == 0) & above, 1, codes)

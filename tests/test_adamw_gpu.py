@@ -415,3 +415,22 @@ def test_the_first_calls_of_a_process_may_be_captured(rows, dim):
     root = pathlib.Path(__file__).resolve().parent.parent
     r = subprocess.run([sys.executable, "-c", FIRST_CALLS.format(rows=rows, dim=dim)], cwd=root, capture_output=True, text=True, timeout=300)
     assert r.returncode == 0 and r.stdout.split() == ["same"], r.stderr[-2000:]
+
+
+def test_zeros_of_either_sign_and_places_on_and_off_the_boundaries():
+    """A gradient of zeros of both signs beside others, over steps that round small averages to zeros of either sign: the same bits
+    wherever the tensors start."""
+    results = []
+    for shift in (0, 1, 3):
+        lists = Lists([2 * BLOCK, 300], eight=True, zeros=True, shift=shift, seed=5)
+        for t in range(1, 5):
+            for b in lists.g:
+                n = b.view.numel()
+                i = torch.arange(n, device="cuda")
+                b.view.copy_(torch.where(i % 3 == 0, torch.where(i % 2 == 0, 0.0, -0.0), (i % 7 - 3.0) * 10.0 ** (-(i % 9).float() - t % 2)))
+            before = lists.state()
+            lists.step(t, 0.0)
+            check(lists, before, lists.state(), t, 0.0)
+        results.append(lists.state())
+    for other in results[1:]:
+        assert all(same(a, b) for x in "pmvs" for a, b in zip(results[0][x], other[x]))
