@@ -199,21 +199,35 @@ template <int X, int Y, int V, int E> cudaError_t launch_elements(const NormArgs
 
 // The more elements a thread has, the fewer shuffles and barriers there are to a row, and the more is under way: with 8 / 16 / 32 elements
 // 65,536 rows of 4096 in bf16 take 268 / 242 / 164 us, 16,384 of 1024 19.7 / 16.8 / 13.6, 60,000 of 512 31.7 / 22.3 / 23.7, 131,072 of 64
-// 9.6 / 7.8 / 10.7; in fp32 4096 of 4096 24.9 / 23.2 / 25.0.  A million rows of 16: 14 / 20 / 20, lanes then skip memory.
+// 9.6 / 7.8 / 10.7; in fp32 4096 of 4096 24.9 / 23.2 / 25.0.  A million rows of 16: 14 / 20 / 20, lanes then skip memory.  Rows that do not fill
+// the threads of their group take 24 where that puts more of them on an SM, or as many with fewer threads idle: 24 million elements in
+// rows of 264 in bf16 with 16 / 24 31.8 / 22.3, of 2304 with 32 / 24 22.6 / 19.6, of 1544 (fewer of them with 24) 22.7 / 26.8, in fp32 of 520 with
+// 16 / 24 44.3 / 33.7, of 4104 45.2 / 35.8.
 template <int X, int Y, int V> cudaError_t launch_vectors(const NormArgs& a, cudaStream_t stream)
 {
     if (a.dim <= 32 || (a.dim <= 8 * kRowThreads && few_elements(a.rows, a.dim))) return launch_elements<X, Y, V, 8>(a, stream);
-    if (a.dim <= (X == kF32 ? 16 * kRowThreads : 512)) return launch_elements<X, Y, V, 16>(a, stream);
-    return launch_elements<X, Y, V, 32>(a, stream);
+    const uint32_t e = a.dim <= (X == kF32 ? 16 * kRowThreads : 512) ? 16 : 32;
+    if (a.dim > (X == kF32 ? 128 : 64) && a.dim <= 24 * kRowThreads && many_elements(a.rows, a.dim)) {
+        const RowGroups g = row_groups(a.rows, a.dim, e, kRowThreads);
+        const uint32_t by_24 = rows_at_once(a.dim, 24, kRowThreads), by_e = rows_at_once(a.dim, e, kRowThreads);
+        if (a.dim != (uint64_t)g.threads * e && (e == 16 ? by_24 > by_e : by_24 >= by_e)) return launch_elements<X, Y, V, 24>(a, stream);
+    }
+    return e == 16 ? launch_elements<X, Y, V, 16>(a, stream) : launch_elements<X, Y, V, 32>(a, stream);
 }
 
-// Single elements are bound by instructions: with 8 / 12 / 16 / 20 / 24 elements 10,007 rows of 515 in fp32 take 11.9 / 13.3 / 15.6 / 12.0 / 12.2 us, 3000
-// of 3333 18.5 / 26.1 / 21.1 / 21.0 / 18.6; 2000 of 6001 with 12 / 24 24.1 / 21.4.
+// Single elements are bound by instructions: with 8 / 24 elements 24 million in rows of 515 take 43 / 36 us in fp32, 42.6 / 27.1 in bf16, of 2050
+// 39.8 / 35.0 and 35.9 / 28.1; of 770, of which an SM has as many at once either way, 40.5 / 41.5 and 37.1 / 39.6.  With less to do, 24
+// have to put half as many rows again on an SM: 6 million in rows of 515 in bf16 13.2 / 10.7, of 1537 11.9 / 13.3, in fp32 13.1 / 12.8 and 12.6 / 14.4;
+// 3 million of 515 8.2 / 8.3.
 template <int X, int Y> cudaError_t launch_single(const NormArgs& a, cudaStream_t stream)
 {
-    return a.dim <= 8 * kRowThreads    ? launch_elements<X, Y, 1, 8>(a, stream)
-           : a.dim <= 24 * kRowThreads ? launch_elements<X, Y, 1, 24>(a, stream)
-                                       : launch_elements<X, Y, 1, 32>(a, stream);
+    if (a.dim > 24 * kRowThreads) return launch_elements<X, Y, 1, 32>(a, stream);
+    bool by_24 = a.dim > 8 * kRowThreads;
+    if (!by_24 && a.dim > 24 * 16 && many_elements(a.rows, a.dim)) {
+        const uint32_t rows_24 = rows_at_once(a.dim, 24, kResident<24> * kRowThreads), rows_8 = rows_at_once(a.dim, 8, kResident<8> * kRowThreads);
+        by_24 = a.rows * a.dim >= 12000000 ? rows_24 > rows_8 : X == kBf16 && 2 * rows_24 > 3 * rows_8;
+    }
+    return by_24 ? launch_elements<X, Y, 1, 24>(a, stream) : launch_elements<X, Y, 1, 8>(a, stream);
 }
 
 template <int X, int Y> cudaError_t launch(const NormArgs& a, cudaStream_t stream)

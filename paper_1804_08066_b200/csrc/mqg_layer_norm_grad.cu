@@ -315,57 +315,71 @@ template <int X, int Y> __global__ void __launch_bounds__(kLongThreads) grad_lon
     }
 }
 
-// Sums over a part of the rows: a thread has V columns of every kStripes-th row, and four of these rows under way.
+// Sums over a part of the rows: a thread has C times V columns of every kStripes-th row, and four of these rows under way.
+// (Single elements: four columns share the row's stats; 2399 rows of 10,001 in fp32, with dx, 156 us with one column, 148 with four.)
 constexpr int kStripes = 8, kColumnLanes = 32, kAhead = 4;
+template <int V> constexpr int kColumns = V == 1 ? 4 : 1;
 template <int X, int Y, int V>
 __global__ void __launch_bounds__(kColumnLanes* kStripes) columns_kernel(const GradArgs a, uint64_t per_part)
 {
-    __shared__ float2 sums[kStripes][V][kColumnLanes];
+    constexpr int C = kColumns<V>;
+    __shared__ float2 sums[kStripes][C * V][kColumnLanes];
     const uint32_t lane = threadIdx.x % kColumnLanes, stripe = threadIdx.x / kColumnLanes;
-    const uint64_t col = ((uint64_t)blockIdx.x * kColumnLanes + lane) * V;
+    const uint64_t col = ((uint64_t)blockIdx.x * kColumnLanes * C + lane) * V;
     const uint64_t first = blockIdx.y * per_part, last = min(first + per_part, a.rows);
     grid_dependency_wait();
     const auto* x = static_cast<const typename Element<X>::type*>(a.x) + col;
     const auto* dy = static_cast<const typename Element<Y>::type*>(a.dy) + col;
-    float2 sum[V];                                      // of dweight and dbias
+    const auto has = [&](int c) { return col + c * kColumnLanes * V < a.dim; };
+    float2 sum[C * V];                                  // of dweight and dbias
 #pragma unroll
-    for (int e = 0; e < V; ++e) sum[e] = make_float2(0.0f, 0.0f);
+    for (int e = 0; e < C * V; ++e) sum[e] = make_float2(0.0f, 0.0f);
     if (col < a.dim)
 #pragma unroll 1
         for (uint64_t row0 = first + stripe; row0 < last; row0 += kAhead * kStripes) {
-            Packed<X, V> px[kAhead];
-            Packed<Y, V> pd[kAhead];
+            Packed<X, V> px[kAhead][C];
+            Packed<Y, V> pd[kAhead][C];
             float2 stats[kAhead];
 #pragma unroll
             for (int i = 0; i < kAhead; ++i) {
                 const uint64_t row = min(row0 + i * kStripes, last - 1);
-                px[i].load(x + row * a.dim);
-                pd[i].load(dy + row * a.dim);
+#pragma unroll
+                for (int c = 0; c < C; ++c) {
+                    const uint64_t from = row * a.dim + (has(c) ? c * kColumnLanes * V : 0);       // (what is added to no sum that counts)
+                    px[i][c].load(x + from);
+                    pd[i][c].load(dy + from);
+                }
                 stats[i] = make_float2(__ldg(a.stats + 2 * row), __ldg(a.stats + 2 * row + 1));
             }
 #pragma unroll
             for (int i = 0; i < kAhead; ++i) {
                 if (row0 + i * kStripes >= last) break;
-                float vx[V], vd[V];
-                widen_to<X, V>(px[i], vx);
-                widen_to<Y, V>(pd[i], vd);
 #pragma unroll
-                for (int e = 0; e < V; ++e) {
-                    sum[e].x = fmaf(vd[e], (vx[e] - stats[i].x) * stats[i].y, sum[e].x);
-                    sum[e].y += vd[e];
+                for (int c = 0; c < C; ++c) {
+                    float vx[V], vd[V];
+                    widen_to<X, V>(px[i][c], vx);
+                    widen_to<Y, V>(pd[i][c], vd);
+#pragma unroll
+                    for (int e = 0; e < V; ++e) {
+                        float2& to = sum[c * V + e];
+                        to.x = fmaf(vd[e], (vx[e] - stats[i].x) * stats[i].y, to.x);
+                        to.y += vd[e];
+                    }
                 }
             }
         }
 #pragma unroll
-    for (int e = 0; e < V; ++e) sums[stripe][e][lane] = sum[e];
+    for (int e = 0; e < C * V; ++e) sums[stripe][e][lane] = sum[e];
     __syncthreads();
-    if (stripe != 0 || col >= a.dim) return;
+    if (stripe != 0) return;
 #pragma unroll
-    for (int e = 0; e < V; ++e) {
+    for (int e = 0; e < C * V; ++e) {
+        if (!has(e / V)) continue;
 #pragma unroll
         for (int k = 1; k < kStripes; ++k) sum[e] = __fadd2_rn(sum[e], sums[k][e][lane]);
-        a.partial[(blockIdx.y * 2ull + 0) * a.dim + col + e] = sum[e].x;
-        a.partial[(blockIdx.y * 2ull + 1) * a.dim + col + e] = sum[e].y;
+        const uint64_t i = col + e / V * kColumnLanes * V + e % V;
+        a.partial[(blockIdx.y * 2ull + 0) * a.dim + i] = sum[e].x;
+        a.partial[(blockIdx.y * 2ull + 1) * a.dim + i] = sum[e].y;
     }
 }
 
@@ -439,7 +453,8 @@ cudaError_t launch_groups(const GradArgs& a, const RowGroups& g, uint32_t cluste
 
 template <int X, int Y, int V, int E> cudaError_t launch_elements(GradArgs a, int sums, uint32_t* parts, cudaStream_t stream)
 {
-    const RowGroups g = row_groups(a.rows, a.dim, E, kResident<X, Y, V, E> * kRowThreads);
+    constexpr int kCtas = kResident<X, Y, V, E>;
+    const RowGroups g = row_groups(a.rows, a.dim, E, kCtas * kRowThreads, kCtas);
     const uint32_t cluster = E <= 8 && sums ? cluster_of(a.rows, a.dim, g) : 0;
     *parts = g.ctas;
     if (cluster != 0) {
@@ -458,15 +473,23 @@ template <int X, int Y, int V, int E> cudaError_t launch_elements(GradArgs a, in
 }
 
 // Elements to a thread.  More of them cost fewer shuffles and barriers to a row: with 8 / 16 65,536 rows of 4096 in bf16 take 326 / 270 us,
-// 16,384 of 1024 27.7 / 24.0, but 64 of 4096 7.6 / 9.5; 4096 of 4096 in fp32 39.3 / 40.3; a million rows of 16 27 / 40.
-// Single elements with 8 / 12: 10,007 rows of 515 in fp32 19.7 / 18.2, 3000 of 2001 20.5 / 21.6, 3000 of 3333 31.5 / 32.8.
+// 16,384 of 1024 27.7 / 24.0, but 64 of 4096 7.6 / 9.5; 4096 of 4096 in fp32 39.3 / 40.3; a million rows of 16 27 / 40.  In fp32 16 where 8 leave
+// much of an SM's threads idle and 16 have as many rows on it: 24 million in rows of 264 61.5 / 51.4, of 2056 59.5 / 53.5, of 520 55.5 / 54.0, of 392
+// 52.2 / 52.1, of 904 51.5 / 52.5.
+// Single elements take 12 where that puts more rows on an SM: 24 million in rows of 515 with 8 / 12 in fp32 65.4 / 57.1, of 2050 75.4 / 57.7, of
+// 3201 (one row either way) 62.4 / 63.1; 16 where these are a warp's, and 12 are more: of 385 with 8 / 12 / 16 60.9 / 63.9 / 54.9.
 template <int X, int Y, int V> int elements_of(uint64_t rows, uint64_t dim)
 {
     if (V == 1 && dim > 8 * kRowThreads) return dim <= 12 * kRowThreads ? 12 : 16;
     if (dim > 8 * kRowThreads) return 16;
     if (dim <= 32 || few_elements(rows, dim)) return 8;
-    if (V == 1) return dim <= 256 || dim > 1536 ? 8 : 12;
-    return X == kF32 && Y == kF32 ? 8 : 16;
+    if (V == 1) {
+        if (dim > 12 * 32 && dim <= 16 * 32) return 16;
+        return dim > 12 * 16 && rows_at_once(dim, 12, kRowThreads) > rows_at_once(dim, 8, kRowThreads) ? 12 : 8;
+    }
+    if (X != kF32 || Y != kF32) return 16;
+    const uint32_t by_8 = rows_at_once(dim, 8, 2 * kRowThreads, 2);
+    return many_elements(rows, dim) && by_8 * dim * 10 < 2ull * kRowThreads * 8 * 6 && rows_at_once(dim, 16, kRowThreads) >= by_8 ? 16 : 8;
 }
 
 // dx, and the sums of `parts` parts of the rows (0: all of them are added up already).
@@ -485,7 +508,7 @@ template <int X, int Y, int V> cudaError_t launch_vectors(const GradArgs& a, int
     }
     if (!sums || err != cudaSuccess) return err;
     *parts = long_parts(a.rows, a.dim);
-    return launch_pdl_grid(columns_kernel<X, Y, V>, dim3((unsigned)ceil_div(a.dim, kColumnLanes * V), *parts), kColumnLanes * kStripes, 0,
+    return launch_pdl_grid(columns_kernel<X, Y, V>, dim3((unsigned)ceil_div(a.dim, kColumnLanes * kColumns<V> * V), *parts), kColumnLanes * kStripes, 0,
                            stream, a, ceil_div(a.rows, *parts));
 }
 

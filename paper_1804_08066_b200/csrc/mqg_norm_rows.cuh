@@ -69,8 +69,8 @@ struct RowGroups {
     uint32_t ctas;           // a grid that fills the device, where there are rows for it
 };
 
-// E * kRowThreads elements at most.  per_sm: threads that the kernel's registers leave room for.
-inline RowGroups row_groups(uint64_t rows, uint64_t dim, uint32_t e, uint32_t per_sm)
+// E * kRowThreads elements at most.  per_sm: threads that the kernel's registers leave room for; most_ctas: CTAs that its shared memory does.
+inline RowGroups row_groups(uint64_t rows, uint64_t dim, uint32_t e, uint32_t per_sm, uint32_t most_ctas = 32)
 {
     RowGroups g;
     const uint32_t need = (uint32_t)((dim + e - 1) / e);
@@ -81,7 +81,8 @@ inline RowGroups row_groups(uint64_t rows, uint64_t dim, uint32_t e, uint32_t pe
         g.threads = (need + 31) / 32 * 32;
         g.block = kRowThreads / g.threads * g.threads;
     }
-    const uint64_t per_cta = g.block / g.threads, wanted = (rows + per_cta - 1) / per_cta, most = 148ull * (per_sm / g.block);
+    const uint64_t per_cta = g.block / g.threads, wanted = (rows + per_cta - 1) / per_cta;
+    const uint64_t most = 148ull * (per_sm / g.block < most_ctas ? per_sm / g.block : most_ctas);
     g.ctas = (uint32_t)(wanted < 1 ? 1 : wanted < most ? wanted : most);
     return g;
 }
@@ -147,9 +148,18 @@ struct RowSums {
     }
 };
 
+// Rows that an SM has at once, where there are many: what rounding up to whole warps and whole CTAs leaves of its threads.
+inline uint32_t rows_at_once(uint64_t dim, uint32_t e, uint32_t per_sm, uint32_t most_ctas = 32)
+{
+    const RowGroups g = row_groups(1ull << 40, dim, e, per_sm, most_ctas);
+    return g.ctas / 148 * (g.block / g.threads);
+}
+
 // Whether rows x dim elements keep less than the threads of a device busy, 8 elements to a thread: then more elements to a thread
 // take longer.
 inline bool few_elements(uint64_t rows, uint64_t dim) { return rows * dim <= 148ull * 2 * kRowThreads * 8; }
+// Whether they are enough for several turns, where the rows that an SM has at once count.
+inline bool many_elements(uint64_t rows, uint64_t dim) { return rows * dim >= 4000000; }
 
 // The elements of a vector: 16 bytes where both types are bf16 or fp32 (x and y of a call), 4 elements of mixed ones.
 template <int A, int B> constexpr int kVector = A == kBf16 && B == kBf16 ? 8 : 4;

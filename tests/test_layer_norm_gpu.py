@@ -95,6 +95,17 @@ def test_forward_of_many_rows(rows, dim, types):
     check(x, rows, dim, w, b, y, stats)
 
 
+# enough elements for several turns, where the elements to a thread follow from how rows of that length fill the device
+TURNS = [(16_000, 264, (BF16, BF16)), (5_500, 768, (BF16, F32)), (2_000, 2304, (F32, BF16)), (1_000, 4104, (F32, F32)), (60_000, 72, (F32, F32)),
+         (24_000, 515, (F32, F32)), (8_000, 643, (BF16, F32)), (500, 8200, (BF16, BF16)), (400, 12_288, (F32, F32)), (12_000, 385, (BF16, BF16)),
+         (2_000, 2050, (F32, BF16)), (2_000, 2056, (F32, F32)), (8_000, 2001, (BF16, BF16)), (600, 9001, (F32, BF16))]
+
+
+@pytest.mark.parametrize("rows,dim,types", TURNS, ids=str)
+def test_forward_of_several_turns(rows, dim, types):
+    test_forward_of_many_rows(rows, dim, types)
+
+
 def test_rows_far_from_zero_and_constant_rows():
     """A mean 1000 times the deviation costs what the mean's own rounding costs, and no more; a constant row has no deviation."""
     for dim in (64, 1024, 4099, 17000):
@@ -179,6 +190,11 @@ def test_gradient_of_many_rows(rows, dim, types):
     c = grad_case(rows, dim, types)
     grad(*c)
     grad_check(*c)
+
+
+@pytest.mark.parametrize("rows,dim,types", TURNS, ids=str)
+def test_gradient_of_several_turns(rows, dim, types):
+    test_gradient_of_many_rows(rows, dim, types)
 
 
 def test_gradient_added_to_what_is_there():
