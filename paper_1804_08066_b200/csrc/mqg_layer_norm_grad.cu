@@ -315,14 +315,17 @@ template <int X, int Y> __global__ void __launch_bounds__(kLongThreads) grad_lon
     }
 }
 
-// Sums over a part of the rows: a thread has C times V columns of every kStripes-th row, and four of these rows under way.
-// (Single elements: four columns share the row's stats; 2399 rows of 10,001 in fp32, with dx, 156 us with one column, 148 with four.)
-constexpr int kStripes = 8, kColumnLanes = 32, kAhead = 4;
+// Sums over a part of the rows: a thread has C times V columns of every kStripes-th row.  Threads to an SM hide the loads better than rows
+// ahead do: 2400 rows of 10,000, with dx, take 102.8 / 99.7 / 97.6 us in fp32 with 4 / 2 / 1 rows under way, 58.9 / 59.3 / 53.3 in bf16.
+// Of single elements four columns share the row's stats: 2399 rows of 10,001 in fp32 156 us with one, 148 with four; 2926 of 8201 with 4 / 2 / 1
+// rows under way 148.9 / 127.6 / 128.4, 132.3 / 106.7 / 108.7 in bf16, 1499 of 16,001 124.2 / 99.5 / 92.0, of two types 139.6 / 118.3 / 137.1.
+constexpr int kStripes = 8, kColumnLanes = 32;
+template <int X, int Y, int V> constexpr int kRowsAhead = V == 1 && X != Y ? 2 : 1;
 template <int V> constexpr int kColumns = V == 1 ? 4 : 1;
 template <int X, int Y, int V>
 __global__ void __launch_bounds__(kColumnLanes* kStripes) columns_kernel(const GradArgs a, uint64_t per_part)
 {
-    constexpr int C = kColumns<V>;
+    constexpr int C = kColumns<V>, kAhead = kRowsAhead<X, Y, V>;
     __shared__ float2 sums[kStripes][C * V][kColumnLanes];
     const uint32_t lane = threadIdx.x % kColumnLanes, stripe = threadIdx.x / kColumnLanes;
     const uint64_t col = ((uint64_t)blockIdx.x * kColumnLanes * C + lane) * V;
