@@ -495,8 +495,8 @@ mqg_status mqg_adamw8(void* const* params, const mqg_dtype* param_dtypes, const 
 /*
  * Layer norm over rows of `dim` elements, each by itself:
  *     mu = mean(x)    r = 1 / sqrt(mean((x - mu)^2) + eps)    y = (x - mu) * r * weight + bias
- * in fp32 (the squares are those of the differences, no difference of large sums; the order of the sums is fixed by dim, the types
- * and the addresses modulo 16), rounded once to a bf16 `y`.
+ * in fp32 (the squares are those of the differences, no difference of large sums; the order of the sums is fixed by rows, dim, the
+ * types and the addresses modulo 16), rounded once to a bf16 `y`.
  *   x             [in] rows x dim elements, row after row;  y [out] the same, of y_dtype
  *   weight, bias  [in] dim elements of weight_dtype each; NULL = ones, zeros
  *   stats         [out] NULL, or 2 floats to a row: mu, r, as the gradient takes them

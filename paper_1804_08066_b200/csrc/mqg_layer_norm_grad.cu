@@ -6,6 +6,8 @@
 // sums over the rows stay in its registers until the CTA's last row; the CTAs' sums are added up by a second launch.  Rows come by
 // asynchronous copies, a few ahead, each thread its own elements: the copies that are on their way take no registers, and no
 // thread waits for another's.
+#include <algorithm>
+
 #include "mqg_norm_rows.cuh"
 #include "mqg_tma.cuh"
 #include "mqg_training.h"
@@ -56,6 +58,40 @@ __device__ __forceinline__ float cluster_load(const float* p, uint32_t rank)
 
 constexpr uint32_t kClusterCtas = 8;                    // (portable)
 
+__device__ __forceinline__ uint32_t cluster_ctas()
+{
+    uint32_t n;
+    asm("mov.u32 %0, %%cluster_nctaid.x;" : "=r"(n));
+    return n;
+}
+__device__ __forceinline__ uint32_t cluster_rank()
+{
+    uint32_t r;
+    asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+    return r;
+}
+
+// The sums of a row whose columns are shared out among a cluster's CTAs, in the CTAs' order.  Two turns' places: a CTA writes to a place
+// again when all have been through the barrier of the turn between, and so have read it.
+struct ClusterSums {
+    float2 of_cta[2][kClusterCtas];
+
+    __device__ __forceinline__ float2 operator()(float2 v, uint32_t ctas, uint32_t rank, int turn)
+    {
+        if (threadIdx.x < ctas) {
+            uint32_t at;
+            asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"(smem_u32(&of_cta[turn][rank])), "r"(threadIdx.x));
+            asm volatile("st.shared::cluster.v2.f32 [%0], {%1, %2};" ::"r"(at), "f"(v.x), "f"(v.y) : "memory");
+        }
+        __syncwarp();
+        cluster_arrive();
+        cluster_wait();
+        float2 total = of_cta[turn][0];
+        for (uint32_t k = 1; k < ctas; ++k) total = __fadd2_rn(total, of_cta[turn][k]);
+        return total;
+    }
+};
+
 // Column i of dweight, or i - dim of dbias.
 template <int W> __device__ __forceinline__ void store_sum(void* dweight, void* dbias, uint64_t dim, uint64_t i, double sum, int add)
 {
@@ -70,7 +106,8 @@ template <int W> __device__ __forceinline__ void store_sum(void* dweight, void* 
 template <int E> constexpr bool kSums = E <= 16;
 
 // E elements to a thread, V to a vector.  FULL: rows of E times the threads of a group, without a condition on any vector.
-template <int X, int Y, int V, int E, bool WIDE, bool FULL>
+// SPLIT: rows whose columns are shared out among the CTAs of a cluster, a group to a CTA.
+template <int X, int Y, int V, int E, bool WIDE, bool FULL, bool SPLIT = false>
 __global__ void __launch_bounds__(kRowThreads, (kResident<X, Y, V, E>)) grad_rows_kernel(const GradArgs a, uint32_t threads, int sums)
 {
     using R = Ring<X, Y, V, E>;
@@ -79,19 +116,23 @@ __global__ void __launch_bounds__(kRowThreads, (kResident<X, Y, V, E>)) grad_row
     auto& ring = *reinterpret_cast<R*>(memory);
     __shared__ RowSums row_sums;
     const uint32_t place = threadIdx.x % threads, group = threadIdx.x / threads, groups = blockDim.x / threads;
-    const RowPlace<V, K, WIDE, FULL> at(a.dim, place, threads);
+    __shared__ ClusterSums cluster_sums;
+    const uint32_t ctas = SPLIT ? cluster_ctas() : 1, rank = SPLIT ? cluster_rank() : 0;
+    const uint64_t share = SPLIT ? (a.dim + ctas * V - 1) / (ctas * V) * V : a.dim, first_column = rank * share;
+    const RowPlace<V, K, WIDE, FULL> at(SPLIT ? min(share, a.dim - first_column) : a.dim, place, threads);
     // the first thread of this one's group in its warp
     const uint32_t first = threads >= 32 ? threadIdx.x & ~31u : threadIdx.x - place;
-    const uint64_t stride = (uint64_t)gridDim.x * groups;
+    const uint64_t stride = (uint64_t)(gridDim.x / ctas) * groups, first_row = (uint64_t)(blockIdx.x / ctas) * groups + group;
     const float per_element = __fdiv_rn(1.0f, (float)a.dim);
+    if (SPLIT) cluster_arrive();                        // (all CTAs of the cluster are there before one writes to another)
     grid_dependency_wait();
-    const auto* x = static_cast<const typename Element<X>::type*>(a.x);
-    const auto* dy = static_cast<const typename Element<Y>::type*>(a.dy);
-    auto* dx = static_cast<typename Element<X>::type*>(a.dx);
+    const auto* x = static_cast<const typename Element<X>::type*>(a.x) + first_column;
+    const auto* dy = static_cast<const typename Element<Y>::type*>(a.dy) + first_column;
+    auto* dx = static_cast<typename Element<X>::type*>(a.dx) + first_column;
     // Where this thread's elements of the row are that is fetched next, and of the one that is written next: kept where registers are
     // left for it (65,536 rows of 4096 in bf16 at the power limit: 284 us, 303 with two products for every row).
     constexpr bool kKept = R::kAsync && E > 8;
-    const uint64_t row_step = stride * a.dim, from = ((uint64_t)blockIdx.x * groups + group) * a.dim + at.element(0);
+    const uint64_t row_step = stride * a.dim, from = first_row * a.dim + at.element(0);
     const auto* next_of_x = x + from;
     const auto* next_of_dy = dy + from;
     auto* next_of_dx = dx + from;
@@ -121,7 +162,7 @@ __global__ void __launch_bounds__(kRowThreads, (kResident<X, Y, V, E>)) grad_row
         float wk[V];
 #pragma unroll
         for (int e = 0; e < V; ++e) wk[e] = 0.0f;
-        if (at.has(k)) weights_at<V>(a.weight, a.w_dtype, at.element(k), 1.0f, wk);
+        if (at.has(k)) weights_at<V>(a.weight, a.w_dtype, (uint32_t)first_column + at.element(k), 1.0f, wk);
 #pragma unroll
         for (int e = 0; e < V; ++e) w[k * V + e] = wk[e];
     }
@@ -140,7 +181,7 @@ __global__ void __launch_bounds__(kRowThreads, (kResident<X, Y, V, E>)) grad_row
                         ring.dy[s][k][threadIdx.x].set(e, 0.0f);
                     }
 #pragma unroll
-        for (int s = 0; s < R::kStages - 1; ++s) fetch((uint64_t)blockIdx.x * groups + group + s * stride, s);
+        for (int s = 0; s < R::kStages - 1; ++s) fetch(first_row + s * stride, s);
     }
     // single elements: the next row, where registers hold one more
     constexpr bool kAhead = !R::kAsync && E <= 12;
@@ -159,10 +200,11 @@ __global__ void __launch_bounds__(kRowThreads, (kResident<X, Y, V, E>)) grad_row
         }
         if (row < a.rows) next_stats = make_float2(__ldg(a.stats + 2 * row), __ldg(a.stats + 2 * row + 1));
     };
-    if constexpr (kAhead) load_next((uint64_t)blockIdx.x * groups + group);
+    if constexpr (kAhead) load_next(first_row);
     int slot = 0, turn = 0;
+    if (SPLIT) cluster_wait();
     // Every group of a CTA takes as many turns: the barriers of its warps are its own, but the lanes of one warp stay together.
-    for (uint64_t base = (uint64_t)blockIdx.x * groups; base < a.rows; base += stride) {
+    for (uint64_t base = first_row - group; base < a.rows; base += stride) {
         const uint64_t row = base + group;
         const bool has = row < a.rows;
         float vx[E], vd[E];
@@ -209,8 +251,9 @@ __global__ void __launch_bounds__(kRowThreads, (kResident<X, Y, V, E>)) grad_row
                 vd[e + 1] = g.y;
             }
         }
-        if (dx == nullptr) continue;
-        const float2 both = row_sums.two(make_float2(sum.x + sum.y, along.x + along.y), threads, group, turn);
+        if (a.dx == nullptr) continue;
+        float2 both = row_sums.two(make_float2(sum.x + sum.y, along.x + along.y), threads, group, turn);
+        if constexpr (SPLIT) both = cluster_sums(both, ctas, rank, turn);
         turn ^= 1;
         auto* row_dx = kKept ? next_of_dx : dx + row * a.dim + at.element(0);
         next_of_dx += row_step;
@@ -241,7 +284,7 @@ __global__ void __launch_bounds__(kRowThreads, (kResident<X, Y, V, E>)) grad_row
     // one of several stripes, and then one the stripes.
     if constexpr (R::kAsync) wait_copies<0>();
     __syncthreads();
-    const uint32_t dim = (uint32_t)a.dim, columns = 2 * dim;        // of dweight and of dbias
+    const uint32_t dim = (uint32_t)(SPLIT ? min(share, a.dim - first_column) : a.dim), columns = 2 * dim;        // of dweight and of dbias
     float* all = reinterpret_cast<float*>(memory);      // [2][groups][dim]
     float* totals = all + 2 * kRowThreads * E;          // [stripes][2][dim]
 #pragma unroll
@@ -252,13 +295,13 @@ __global__ void __launch_bounds__(kRowThreads, (kResident<X, Y, V, E>)) grad_row
             to[groups * dim] = e % 2 ? db[e / 2].y : db[e / 2].x;
         }
     __syncthreads();
-    float* left = a.partial != nullptr ? a.partial + (uint64_t)blockIdx.x * columns : totals;
+    float* left = a.partial != nullptr ? a.partial + (uint64_t)(blockIdx.x / ctas) * 2 * a.dim + first_column : totals;
     if (columns >= blockDim.x) {
         for (uint32_t i = threadIdx.x; i < columns; i += blockDim.x) {
             const float* from = all + (i < dim ? i : groups * dim + i - dim);
             float total = from[0];
             for (uint32_t g = 1; g < groups; ++g) total += from[g * dim];
-            left[i] = total;
+            left[SPLIT && i >= dim ? a.dim + i - dim : i] = total;
         }
     } else {
         const uint32_t stripes = blockDim.x / columns, stripe = threadIdx.x / columns, column = threadIdx.x - stripe * columns;
@@ -429,19 +472,19 @@ uint32_t long_parts(uint64_t rows, uint64_t dim)
     return (uint32_t)(most < want ? (most < 1 ? 1 : most) : want);
 }
 
-template <int X, int Y, int V, int E, bool WIDE, bool FULL>
-cudaError_t launch_groups(const GradArgs& a, const RowGroups& g, uint32_t cluster, int sums, cudaStream_t stream)
+// Shared memory: the ring, then the sums.
+template <int X, int Y, int V, int E>
+constexpr size_t kGroupBytes = std::max<size_t>(Ring<X, Y, V, E>::kAsync ? sizeof(Ring<X, Y, V, E>) : 0,
+                                                kSums<E> ? 3 * kRowThreads * E * sizeof(float) : 16);
+
+template <typename Kernel>
+cudaError_t launch_clusters(Kernel kernel, uint32_t ctas, uint32_t cluster, uint32_t block, size_t bytes, cudaStream_t stream, const GradArgs& a,
+                            uint32_t threads, int sums)
 {
-    using R = Ring<X, Y, V, E>;
-    static std::atomic<bool> ready[64];
-    const auto kernel = grad_rows_kernel<X, Y, V, E, WIDE, FULL>;
-    constexpr size_t kAll = kSums<E> ? 3 * kRowThreads * E * sizeof(float) : 16, kBytes = R::kAsync && sizeof(R) > kAll ? sizeof(R) : kAll;
-    if (const cudaError_t err = allow_shared(kernel, kBytes, ready)) return err;
-    if (cluster == 0) return launch_pdl_smem(kernel, g.ctas, g.block, kBytes, stream, a, g.threads, sums);
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(cluster);
-    cfg.blockDim = dim3(g.block);
-    cfg.dynamicSmemBytes = kBytes;
+    cfg.gridDim = dim3(ctas);
+    cfg.blockDim = dim3(block);
+    cfg.dynamicSmemBytes = bytes;
     cfg.stream = stream;
     cudaLaunchAttribute attr[2];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
@@ -451,7 +494,18 @@ cudaError_t launch_groups(const GradArgs& a, const RowGroups& g, uint32_t cluste
     attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
     cfg.attrs = attr;
     cfg.numAttrs = 2;
-    return cudaLaunchKernelEx(&cfg, kernel, a, g.threads, sums);
+    return cudaLaunchKernelEx(&cfg, kernel, a, threads, sums);
+}
+
+template <int X, int Y, int V, int E, bool WIDE, bool FULL>
+cudaError_t launch_groups(const GradArgs& a, const RowGroups& g, uint32_t cluster, int sums, cudaStream_t stream)
+{
+    static std::atomic<bool> ready[64];
+    const auto kernel = grad_rows_kernel<X, Y, V, E, WIDE, FULL>;
+    constexpr size_t kBytes = kGroupBytes<X, Y, V, E>;
+    if (const cudaError_t err = allow_shared(kernel, kBytes, ready)) return err;
+    if (cluster == 0) return launch_pdl_smem(kernel, g.ctas, g.block, kBytes, stream, a, g.threads, sums);
+    return launch_clusters(kernel, cluster, cluster, g.block, kBytes, stream, a, g.threads, sums);
 }
 
 template <int X, int Y, int V, int E> cudaError_t launch_elements(GradArgs a, int sums, uint32_t* parts, cudaStream_t stream)
@@ -473,6 +527,32 @@ template <int X, int Y, int V, int E> cudaError_t launch_elements(GradArgs a, in
         if (g.threads < 32) return launch_groups<X, Y, V, E, false, false>(a, g, cluster, sums, stream);
     }
     return launch_groups<X, Y, V, E, true, false>(a, g, cluster, sums, stream);
+}
+
+// Rows longer than kSumsDim by two CTAs, on an SM each: the sums over the rows stay in registers and x and dy are read once, but the CTAs
+// wait for one another in every row, 2 us for a pair.  Single elements (12 to a thread) where they fit: 2926 rows of 8201 in bf16 75 us,
+// 109 by two kernels, 8 of 10,001 9.7 and 11.4.  Vectors where a row has bytes for that time, and rows enough to be worth it: 24 million
+// elements in rows of 12,288 71 us and 94 in fp32, 60 and 64 of two types, of 9000 91 and 102, 66 and 66; in bf16 of 16,000 63 and 50;
+// 300 of 16,000 in fp32 27.6 and 25.7, 74 16.2 and 13.2.
+constexpr uint32_t kSplitCtas = 2;
+template <int V> constexpr int kSplitE = V == 1 ? 12 : 16;
+template <int X, int Y, int V> bool split(uint64_t rows, uint64_t dim)
+{
+    return dim > kSumsDim && dim <= kSplitCtas * kSplitE<V> * kRowThreads &&
+           (V == 1 || (dim * (kElemBytes<X> + kElemBytes<Y>) >= 72000 && rows * dim >= 8000000));
+}
+uint32_t split_parts(uint64_t rows) { return (uint32_t)(rows < 148 / kSplitCtas ? (rows < 1 ? 1 : rows) : 148 / kSplitCtas); }
+
+template <int X, int Y, int V> cudaError_t launch_split(const GradArgs& a, int sums, uint32_t* parts, cudaStream_t stream)
+{
+    constexpr int E = kSplitE<V>;
+    static std::atomic<bool> ready[64];
+    const auto kernel = grad_rows_kernel<X, Y, V, E, true, false, true>;
+    constexpr size_t kBytes = kGroupBytes<X, Y, V, E>;
+    if (const cudaError_t err = allow_shared(kernel, kBytes, ready)) return err;
+    const uint32_t threads = (uint32_t)ceil_div(ceil_div(ceil_div(a.dim, kSplitCtas * V) * V, E), 32) * 32;
+    *parts = split_parts(a.rows);
+    return launch_clusters(kernel, *parts * kSplitCtas, kSplitCtas, threads, kBytes, stream, a, threads, sums);
 }
 
 // Elements to a thread.  More of them cost fewer shuffles and barriers to a row: with 8 / 16 65,536 rows of 4096 in bf16 take 326 / 270 us,
@@ -504,6 +584,8 @@ template <int X, int Y, int V> cudaError_t launch_vectors(const GradArgs& a, int
             if (e == 12) return launch_elements<X, Y, V, 12>(a, sums, parts, stream);
         return e == 8 ? launch_elements<X, Y, V, 8>(a, sums, parts, stream) : launch_elements<X, Y, V, 16>(a, sums, parts, stream);
     }
+    if constexpr (V == 1 || X == kF32 || Y == kF32)
+        if (split<X, Y, V>(a.rows, a.dim)) return launch_split<X, Y, V>(a, sums, parts, stream);
     cudaError_t err = cudaSuccess;
     if (a.dx != nullptr && a.rows != 0) {
         if (a.dim <= 32 * kRowThreads) err = launch_elements<X, Y, V, 32>(a, 0, parts, stream);
@@ -534,7 +616,8 @@ template <int X, int Y> cudaError_t launch(const GradArgs& a, const NormGrads& o
 // (8 elements to a thread, two CTAs to an SM leave the most parts)
 size_t layer_norm_workspace_floats(uint64_t rows, uint64_t dim)
 {
-    const uint64_t parts = dim > kSumsDim ? long_parts(rows, dim) : row_groups(rows, dim, dim <= 8 * kRowThreads ? 8 : 16, 2 * kRowThreads).ctas;
+    uint64_t parts = dim > kSumsDim ? long_parts(rows, dim) : row_groups(rows, dim, dim <= 8 * kRowThreads ? 8 : 16, 2 * kRowThreads).ctas;
+    if (dim > kSumsDim && dim <= kSplitCtas * kSplitE<4> * kRowThreads) parts = std::max<uint64_t>(parts, split_parts(rows));
     return (size_t)(parts * 2 * dim);
 }
 

@@ -98,7 +98,10 @@ def test_forward_of_many_rows(rows, dim, types):
 # enough elements for several turns, where the elements to a thread follow from how rows of that length fill the device
 TURNS = [(16_000, 264, (BF16, BF16)), (5_500, 768, (BF16, F32)), (2_000, 2304, (F32, BF16)), (1_000, 4104, (F32, F32)), (60_000, 72, (F32, F32)),
          (24_000, 515, (F32, F32)), (8_000, 643, (BF16, F32)), (500, 8200, (BF16, BF16)), (400, 12_288, (F32, F32)), (12_000, 385, (BF16, BF16)),
-         (2_000, 2050, (F32, BF16)), (2_000, 2056, (F32, F32)), (8_000, 2001, (BF16, BF16)), (600, 9001, (F32, BF16))]
+         (700, 12_296, (F32, F32)), (600, 14_000, (F32, BF16)), (500, 16_384, (BF16, F32)), (300, 12_296, (BF16, BF16)), (75, 10_001, (F32, F32)),
+         (800, 12_287, (BF16, BF16)), (600, 9001, (F32, BF16)), (90, 16_400, (F32, BF16)), (200, 24_577, (BF16, F32)), (60, 49_152, (F32, F32)),
+         (70, 49_153, (BF16, BF16)), (1, 65_536, (F32, F32)), (77, 65_544, (BF16, BF16)), (0, 9_001, (F32, F32)), (2_000, 2050, (F32, BF16)),
+         (2_000, 2056, (F32, F32)), (8_000, 2001, (BF16, BF16))]
 
 
 @pytest.mark.parametrize("rows,dim,types", TURNS, ids=str)
@@ -224,6 +227,19 @@ def test_any_of_the_gradients_may_be_left_out():
         grad_check(*c[:4], None, *c[5:])
         if dim < 17000:
             mqg.mqg_layer_norm_grad(c[0].view, c[1].view, 50, dim, None, c[5].view, c[6].view, None, None, None)
+
+
+@pytest.mark.parametrize("rows,dim,types", [(50, 9001, (F32, F32)), (600, 14_000, (F32, F32)), (700, 12_288, (F32, BF16)), (50, 16_384, (BF16, BF16))], ids=str)
+def test_any_of_the_gradients_of_long_rows_may_be_left_out(rows, dim, types):
+    full = grad_case(rows, dim, types)
+    grad(*full)
+    for keep in (1, 2, 3, 4, 6):
+        c = grad_case(rows, dim, types)
+        out = [d if keep >> i & 1 else None for i, d in enumerate(c[6:])]
+        grad(*c[:6], *out)
+        for d, whole in zip(out, full[6:]):
+            if d is not None:
+                assert torch.equal(d.cpu(), whole.cpu())
 
 
 @pytest.mark.parametrize("rows", [1, 2, 63, 64, 65, 129, 1000, 4097])
