@@ -301,6 +301,29 @@ def test_captured_and_replayed():
         grad_check(c[0], c[1], 300, 515, c[4], stats, *c[6:])
 
 
+@pytest.mark.parametrize("rows,dim", [(90, 9001), (700, 12_288), (40, 16_400)])
+def test_long_rows_captured_and_replayed_on_two_streams(rows, dim):
+    cases = [grad_case(rows, dim, (F32, F32), seed=k) for k in range(2)]
+    alone, graphs, streams = [], [], [torch.cuda.Stream() for _ in cases]
+    for c, s in zip(cases, streams):
+        grad(*c)
+        alone.append([d.cpu() for d in c[6:]])
+        work = torch.empty(mqg.mqg_layer_norm_workspace_floats(rows, dim), device="cuda")
+        graphs.append((torch.cuda.CUDAGraph(), work))
+        with torch.cuda.graph(graphs[-1][0], stream=s):
+            mqg.mqg_layer_norm_grad(c[0].view, c[1].view, rows, dim, c[4].view, c[5].view, c[6].view, c[7].view, c[8].view, work)
+        for d in c[6:]:
+            d.view.zero_()
+    torch.cuda.synchronize()
+    for _ in range(20):
+        for (graph, _), s in zip(graphs, streams):
+            with torch.cuda.stream(s):
+                graph.replay()
+    torch.cuda.synchronize()
+    for c, want in zip(cases, alone):
+        assert all(torch.equal(d.cpu(), w) for d, w in zip(c[6:], want))
+
+
 def test_on_two_streams_at_once_behind_what_they_still_write():
     cases = [grad_case(2000, dim, (F32, F32)) for dim in (64, 1024)]
     alone = []
@@ -323,7 +346,7 @@ def test_on_two_streams_at_once_behind_what_they_still_write():
         assert all(torch.equal(d.cpu(), w) for d, w in zip(c[6:], want))
 
 
-@pytest.mark.parametrize("dim", [1024, 515, 17000])
+@pytest.mark.parametrize("dim", [1024, 515, 9001, 17000])
 def test_offsets_beyond_32_bits(dim):
     rows = (1 << 32) // dim + 70
     n = rows * dim
