@@ -5,8 +5,8 @@
 //   v' = b2 * v + (w2 * g) * g                      w2 = 1 - b2
 //   p' = p - (rate * p + a * (m' / d))              d = sqrt(v') * r2 + eps,  rate = lr * decay,  a = lr / c1,  r2 = 1 / sqrt(c2)
 //
-// (the root and the quotient within two units in the last place).  m' and v' are sums of products that are rounded one by one, not
-// fused, so that states held in 8 bits are the same bits for everybody who follows the formulas.
+// (the root and the quotient within two units in the last place, for every v' and d).  m' and v' are sums of products that are rounded
+// one by one, not fused, so that states held in 8 bits are the same bits for everybody who follows the formulas.
 //
 // States in 8 bits, in blocks of 256 elements: m is e4m3 times the block's scale max|m'| / 448, v is e5m2 times max v' / 57344.  A
 // step moves v by about (1 - b2) v, far less than half the distance of two neighbours on any grid of 8 bits, so rounding to the
@@ -97,7 +97,7 @@ struct FromDevice {
 struct Step {
     float k, a, r2, lr;
     uint32_t t;
-    bool skip;
+    bool skip, any;          // any: the root or the quotient of any number (see root, reciprocal)
     __device__ __forceinline__ Step(const Scalars& s, const FromDevice& d) : k(s.grad_scale), a(s.a), r2(s.r2), lr(s.lr), t(s.step), skip(false)
     {
         if (s.factor != nullptr) {
@@ -110,21 +110,37 @@ struct Step {
             r2 = reciprocal_root(d.schedule[2]);
             t = (uint32_t)d.schedule[3];
         }
+        any = !(s.eps >= 0x1p-38f * r2 && s.eps <= 0x1p60f && r2 <= 0x1p15f);
     }
 };
 
-// sqrt(x), x >= 0, within two roundings; zero below 2^-126.
+// sqrt(x), x >= 0, within two units in the last place; zero below 2^-126, which takes 2^-63 r2 from d at most: below a quarter of d's last
+// place where eps is 2^-38 r2 or more.
 __device__ __forceinline__ float root(float x)
 {
     float r;
     asm("sqrt.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
     return r;
 }
-// 1 / d within two roundings, 2^-50 <= d < 2^77.
+// 1 / d within one unit in the last place, d < 2^126 or infinite (d is sqrt(v') * r2 + eps, below 2^80 with eps up to 2^60 and r2 up to 2^15).
 __device__ __forceinline__ float reciprocal(float d)
 {
     float r;
     asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(d));
+    return r;
+}
+
+// The same without those limits, and the quotient (its reciprocal would leave fp32's normal numbers).
+__device__ __forceinline__ float root_of_any(float x)
+{
+    float r;
+    asm("sqrt.approx.f32 %0, %1;" : "=f"(r) : "f"(x));
+    return r;
+}
+__device__ __forceinline__ float quotient_of_any(float m, float d)
+{
+    float r;
+    asm("div.full.f32 %0, %1, %2;" : "=f"(r) : "f"(m), "f"(d));
     return r;
 }
 
@@ -147,6 +163,18 @@ __device__ __forceinline__ void update2(float* p, const float* g_in, float* m, f
     p[0] = old.x - less.x, p[1] = old.y - less.y;
     m[0] = m2.x, m[1] = m2.y;
     v[0] = v2.x, v[1] = v2.y;
+}
+
+// The new parameters again, of any v' and d, from the old ones and the new averages.  (For steps whose scalars ask for it: by itself and with
+// the old parameters read again, since the registers do not hold both forms side by side.)
+__device__ __forceinline__ void parameters_of_any(float (&p)[kPerLane], const float (&m)[kPerLane], const float (&v)[kPerLane], const Scalars& s,
+                                                  const Step& st, float rate)
+{
+#pragma unroll
+    for (int i = 0; i < kPerLane; ++i) {
+        const float u = quotient_of_any(m[i], fmaf(root_of_any(v[i]), st.r2, s.eps));
+        p[i] -= fmaf(st.a, u, __fmul_rn(rate, p[i]));
+    }
 }
 
 // A float of 8 bits: the bits of an fp32 times 2^EXP2, cut off behind bit SHIFT.  The power of two takes the grid's smallest normal
@@ -389,6 +417,14 @@ __device__ __forceinline__ void step_vectors(const Place<P, G, EIGHT>& at, uint6
             most_v = largest(most_v, v[i], v[i + 1]);
         }
     }
+    if (st.any) {
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            in.p[k].load(at.p + 128 * k);
+            widen_to<P, 4>(in.p[k], p + 4 * k);
+        }
+        parameters_of_any(p, m, v, s, st, rate);
+    }
 #pragma unroll
     for (int k = 0; k < 2; ++k) {
 #pragma unroll
@@ -463,6 +499,11 @@ __device__ __forceinline__ void step_elements(const Block& b, const Scalars& s, 
             most_m = largest(most_m, m[i], m[i + 1]);  // (places without elements stay zeros)
             most_v = largest(most_v, v[i], v[i + 1]);
         }
+    }
+    if (st.any) {
+#pragma unroll
+        for (int i = 0; i < kPerLane; ++i) p[i] = has(i) ? widen(__ldcg(at_p + 32 * i)) : 0.0f;
+        parameters_of_any(p, m, v, s, st, rate);
     }
 #pragma unroll
     for (int i = 0; i < kPerLane; ++i) {
