@@ -473,6 +473,7 @@ mqg_status mqg_adamw(void* const* params, const mqg_dtype* param_dtypes, const v
  * The same with m and v in 8 bits each: every block of 256 elements of a tensor, from its first on, has a scale for each.
  *   m       [in/out] a byte an element, a float of 1 + 4 + 3 bits (e4m3, largest 448): its value is e4m3 * scales[2 b]
  *   v       [in/out] a byte an element, a float of 1 + 5 + 2 bits (e5m2, largest 57344), never negative: e5m2 * scales[2 b + 1]
+ *           (codes that are infinities or NaN in these formats are that)
  *   scales  [in/out] HOST array of pointers to mqg_adamw8_scale_floats(size) floats per tensor (two to a block), 4-byte aligned
  * All three are zeros before the first step.  The parameter's step is computed from m and v before they are rounded.  Then
  * scales[2 b] = max|m| / 448, scales[2 b + 1] = max v / 57344 of the block (0, and all its codes 0, where that maximum is below

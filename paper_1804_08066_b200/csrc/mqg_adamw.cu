@@ -180,33 +180,22 @@ __device__ __forceinline__ void parameters_of_any(float (&p)[kPerLane], const fl
 // A float of 8 bits: the bits of an fp32 times 2^EXP2, cut off behind bit SHIFT.  The power of two takes the grid's smallest normal
 // number to fp32's, so that both have their subnormal numbers in the same place and a code is a shift of fp32's bits.
 template <int SHIFT, int EXP2> struct Format {
-    // the value of a code's magnitude
-    static __device__ __forceinline__ float value(uint32_t code) { return __uint_as_float(code << SHIFT) * exp2f_const(-EXP2); }
     // x >= 0, at most the grid's largest, rounded up if what is cut off and the draw h in 0 .. 2^16 - 1, (h + 1/2) / 2^16 of a
     // step, make a step.  (The largest element of a block comes within two units in the last place of the grid's largest
     // number, from where no draw carries it further, nor leaves it below.)
-    static __device__ __forceinline__ uint32_t bits(float x) { return __float_as_uint(x * exp2f_const(EXP2)); }
+    static __device__ __forceinline__ uint32_t bits(float x) { return __float_as_uint(x * (EXP2 == -120 ? 0x1p-120f : 0x1p-112f)); }
     static __device__ __forceinline__ uint32_t code(uint32_t bits, uint32_t h)
     {
         return (bits + (h << (SHIFT - 16) | 1u << (SHIFT - 17))) >> SHIFT;
-    }
-    static __device__ __forceinline__ constexpr float exp2f_const(int e)
-    {
-        return e == 120 ? 0x1p120f : e == -120 ? 0x1p-120f : e == 112 ? 0x1p112f : 0x1p-112f;
     }
 };
 using FormatM = Format<20, -120>;
 using FormatV = Format<21, -112>;
 
-__device__ __forceinline__ float decode_m(uint32_t code, float scale)
-{
-    return __fmul_rn(__uint_as_float(__float_as_uint(FormatM::value(code & 0x7F)) | (code & 0x80) << 24), scale);
-}
-__device__ __forceinline__ float decode_v(uint32_t code, float scale) { return __fmul_rn(FormatV::value(code), scale); }
-
+// (an infinite m times its block's inverse, 0, is a NaN, of which nothing reaches the sign)
 __device__ __forceinline__ uint32_t encode_m(float m, float inverse, uint32_t h)
 {
-    return FormatM::code(FormatM::bits(__fmul_rn(fabsf(m), inverse)), h) | (__float_as_uint(m) >> 24 & 0x80u);
+    return FormatM::code(FormatM::bits(__fmul_rn(fabsf(m), inverse)), h) & 0x7Fu | (__float_as_uint(m) >> 24 & 0x80u);
 }
 // (a v of 2^-128 or more never becomes zero, also where `inverse` takes it below fp32's range)
 __device__ __forceinline__ uint32_t encode_v(float v, float inverse, uint32_t h)
@@ -237,19 +226,23 @@ __device__ __forceinline__ void new_scales(float most_m, float most_v, float* sc
     inverse_v = __shfl_sync(0xFFFFFFFFu, q, 3);
 }
 
-// Four codes in a word, and back; all of one block.  fp16 holds the values of both formats: e5m2 is its upper byte.
+// The values of two codes of each; all of one block.  fp16 holds the values of both formats, infinities and NaN among them: e5m2 is
+// its upper byte.
+__device__ __forceinline__ void decode2(uint16_t m, uint32_t half_v, float scale_m, float scale_v, float* to_m, float* to_v)
+{
+    uint32_t half_m;
+    asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(half_m) : "h"(m));
+    const float2 x = __fmul2_rn(__half22float2(*reinterpret_cast<const __half2*>(&half_m)), both(scale_m));
+    const float2 y = __fmul2_rn(__half22float2(*reinterpret_cast<const __half2*>(&half_v)), both(scale_v));
+    to_m[0] = x.x, to_m[1] = x.y;
+    to_v[0] = y.x, to_v[1] = y.y;
+}
+
+// Four codes in a word, and back.
 __device__ __forceinline__ void decode4(uint32_t m, uint32_t v, float scale_m, float scale_v, float* to_m, float* to_v)
 {
-#pragma unroll
-    for (int j = 0; j < 4; j += 2) {
-        uint32_t half_m;
-        asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(half_m) : "h"((uint16_t)(j ? m >> 16 : m)));
-        const uint32_t half_v = __byte_perm(v, 0, j ? 0x3424 : 0x1404);
-        const float2 x = __fmul2_rn(__half22float2(*reinterpret_cast<const __half2*>(&half_m)), both(scale_m));
-        const float2 y = __fmul2_rn(__half22float2(*reinterpret_cast<const __half2*>(&half_v)), both(scale_v));
-        to_m[j] = x.x, to_m[j + 1] = x.y;
-        to_v[j] = y.x, to_v[j + 1] = y.y;
-    }
+    decode2((uint16_t)m, __byte_perm(v, 0, 0x1404), scale_m, scale_v, to_m, to_v);
+    decode2((uint16_t)(m >> 16), __byte_perm(v, 0, 0x3424), scale_m, scale_v, to_m + 2, to_v + 2);
 }
 
 // One half of a word of draws, times 2^p, plus x; `half`: 2^p in the byte that meets that half in a two-way dot product.
@@ -484,12 +477,11 @@ __device__ __forceinline__ void step_elements(const Block& b, const Scalars& s, 
     for (int i = 0; i < kPerLane; ++i) {
         p[i] = widen(in_p[i]);
         g[i] = widen(in_g[i]);
-        if constexpr (EIGHT) {
-            m[i] = decode_m(in_m[i], scale_m);
-            v[i] = decode_v(in_v[i], scale_v);
-        } else {
+        if constexpr (!EIGHT) {
             m[i] = in_m[i];
             v[i] = in_v[i];
+        } else if (i % 2 == 0) {
+            decode2((uint16_t)(in_m[i] | in_m[i + 1] << 8), (uint32_t)in_v[i] << 8 | (uint32_t)in_v[i + 1] << 24, scale_m, scale_v, m + i, v + i);
         }
     }
 #pragma unroll
