@@ -92,6 +92,13 @@ struct ClusterSums {
     }
 };
 
+// x rounded towards zero, its last bit set where that left something out: rounded to a bf16 then, it is x rounded once.
+__device__ __forceinline__ float round_to_odd(double x)
+{
+    const float r = __double2float_rz(x);
+    return (double)r == x ? r : __uint_as_float(__float_as_uint(r) | 1u);
+}
+
 // Column i of dweight, or i - dim of dbias.
 template <int W> __device__ __forceinline__ void store_sum(void* dweight, void* dbias, uint64_t dim, uint64_t i, double sum, int add)
 {
@@ -99,7 +106,7 @@ template <int W> __device__ __forceinline__ void store_sum(void* dweight, void* 
     if (to == nullptr) return;
     const uint64_t col = i < dim ? i : i - dim;
     if (add) sum += (double)widen(to[col]);
-    narrow((float)sum, to[col]);
+    narrow(W == kF32 ? (float)sum : round_to_odd(sum), to[col]);
 }
 
 // Rows of more elements leave the sums over the rows to a kernel of their own: registers hold no more.
