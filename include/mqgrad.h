@@ -512,8 +512,9 @@ mqg_status mqg_layer_norm(const void* x, mqg_dtype x_dtype, uint64_t rows, uint6
 /*
  * Its gradient.  With h = (x - mu) * r and a = weight * dy:
  *     dx = r * (a - mean(a) - h * mean(a h))    dweight = sum over rows of dy * h    dbias = sum over rows of dy
- * Sums over rows are formed in fp32 within a part of the rows and in 64 bits over the parts, in an order that rows, dim and the
- * arguments' types and addresses modulo 16 fix: the result is reproducible bit for bit on one device model.
+ * Sums over rows are formed in fp32 over the rows that a thread takes, in 64 bits over the threads of a part of the rows, rounded to
+ * fp32, and in 64 bits over the parts, in an order that rows, dim and the arguments' types and addresses modulo 16 fix: the result
+ * is reproducible bit for bit on one device model.
  *   dy             [in] rows x dim elements;  x, weight, stats [in] as mqg_layer_norm took and wrote them
  *   dx             [out] rows x dim elements of x_dtype, or NULL
  *   dweight, dbias [out] dim elements of dweight_dtype each, or NULL; with add_into_grads the sum over rows is added to what is

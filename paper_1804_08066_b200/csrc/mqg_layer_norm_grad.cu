@@ -287,13 +287,14 @@ __global__ void __launch_bounds__(kRowThreads, (kResident<X, Y, V, E>)) grad_row
         }
     }
     if (!kSums<E> || !sums) return;
-    // The groups' sums through shared memory, in a fixed order: where there are more threads than columns, each adds up the groups of
-    // one of several stripes, and then one the stripes.
+    // The groups' sums through shared memory, in 64 bits and a fixed order: where there are more threads than columns, each adds up the
+    // groups of one of several stripes, and then one the stripes.
     if constexpr (R::kAsync) wait_copies<0>();
     __syncthreads();
     const uint32_t dim = (uint32_t)(SPLIT ? min(share, a.dim - first_column) : a.dim), columns = 2 * dim;        // of dweight and of dbias
     float* all = reinterpret_cast<float*>(memory);      // [2][groups][dim]
-    float* totals = all + 2 * kRowThreads * E;          // [stripes][2][dim]
+    float* totals = all + 2 * kRowThreads * E;          // [2][dim]; behind one for each thread, [stripes][2][dim]
+    double* of_stripes = reinterpret_cast<double*>(totals + kRowThreads);
 #pragma unroll
     for (int e = 0; e < E; ++e)
         if (at.has(e / V)) {
@@ -306,23 +307,23 @@ __global__ void __launch_bounds__(kRowThreads, (kResident<X, Y, V, E>)) grad_row
     if (columns >= blockDim.x) {
         for (uint32_t i = threadIdx.x; i < columns; i += blockDim.x) {
             const float* from = all + (i < dim ? i : groups * dim + i - dim);
-            float total = from[0];
-            for (uint32_t g = 1; g < groups; ++g) total += from[g * dim];
-            left[SPLIT && i >= dim ? a.dim + i - dim : i] = total;
+            double total = (double)from[0];
+            for (uint32_t g = 1; g < groups; ++g) total += (double)from[g * dim];
+            left[SPLIT && i >= dim ? a.dim + i - dim : i] = (float)total;
         }
     } else {
         const uint32_t stripes = blockDim.x / columns, stripe = threadIdx.x / columns, column = threadIdx.x - stripe * columns;
-        float total = 0.0f;
+        double total = 0.0;
         if (stripe < stripes) {
             const float* from = all + (column < dim ? column : groups * dim + column - dim);
 #pragma unroll 4
-            for (uint32_t g = stripe; g < groups; g += stripes) total += from[g * dim];
-            totals[threadIdx.x] = total;
+            for (uint32_t g = stripe; g < groups; g += stripes) total += (double)from[g * dim];
+            of_stripes[threadIdx.x] = total;
         }
         __syncthreads();
         if (stripe == 0) {
-            for (uint32_t k = 1; k < stripes; ++k) total += totals[k * columns + column];
-            left[column] = total;                       // (where that is in `totals`: what this thread alone has read)
+            for (uint32_t k = 1; k < stripes; ++k) total += of_stripes[k * columns + column];
+            left[column] = (float)total;
         }
     }
     if (a.partial != nullptr) return;
@@ -428,11 +429,15 @@ __global__ void __launch_bounds__(kColumnLanes* kStripes) columns_kernel(const G
 #pragma unroll
     for (int e = 0; e < C * V; ++e) {
         if (!has(e / V)) continue;
+        double dw = (double)sum[e].x, db = (double)sum[e].y;
 #pragma unroll
-        for (int k = 1; k < kStripes; ++k) sum[e] = __fadd2_rn(sum[e], sums[k][e][lane]);
+        for (int k = 1; k < kStripes; ++k) {
+            dw += (double)sums[k][e][lane].x;
+            db += (double)sums[k][e][lane].y;
+        }
         const uint64_t i = col + e / V * kColumnLanes * V + e % V;
-        a.partial[(blockIdx.y * 2ull + 0) * a.dim + i] = sum[e].x;
-        a.partial[(blockIdx.y * 2ull + 1) * a.dim + i] = sum[e].y;
+        a.partial[(blockIdx.y * 2ull + 0) * a.dim + i] = (float)dw;
+        a.partial[(blockIdx.y * 2ull + 1) * a.dim + i] = (float)db;
     }
 }
 

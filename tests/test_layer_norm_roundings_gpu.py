@@ -46,3 +46,23 @@ def test_sums_rounded_to_bf16_of_every_kind():
                          2.0 ** -130 + 2.0 ** -133, 0.0, 1.0, 1.0, 2.0])
     _, _, db = gradients(torch.ones(1, 16), dy[None], torch.tensor([[0.0, 1.0]]), BF16, start.to(BF16))
     assert torch.equal(db.float().isnan(), want.isnan()) and torch.equal(db.float().nan_to_num(9.0), want.nan_to_num(9.0)), (db, want)
+
+
+# rows, elements, rows that a thread takes
+SHAPES = [(512, 64, 1), (64, 64, 1), (250, 256, 2), (64, 1000, 2), (4736, 256, 1), (592, 1024, 1), (9472, 128, 1), (4736, 129, 2),
+          (20_000, 33, 3), (8, 17_000, 1), (8, 16_400, 1), (300, 9001, 5)]
+
+
+@pytest.mark.parametrize("rows,dim,own", SHAPES)
+@pytest.mark.parametrize("kind", [F32, BF16], ids=str)
+def test_sums_of_a_ctas_rows_beside_one_large_row(rows, dim, own, kind):
+    """One row of 2^24 among ones, which fp32 loses where it adds them one by one.  A thread's own rows are added in fp32, 1 lost with each
+    of them at most; what follows in 64 bits, with one rounding for each part and one at the end, of 1 at most each."""
+    for large in (0, rows // 2, rows - 1):
+        dy = torch.ones(rows, dim)
+        dy[large] = 2.0 ** 24
+        stats = torch.tensor([0.0, 1.0]).repeat(rows, 1)
+        _, dw, db = gradients(torch.ones(rows, dim, dtype=kind), dy.to(kind), stats)
+        want = 2.0 ** 24 + rows - 1
+        for got in (dw, db):
+            assert ((got.double() - want).abs() <= 2 * U * want + own - 1).all(), (got.double() - want).abs().max()
