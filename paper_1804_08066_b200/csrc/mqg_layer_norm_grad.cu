@@ -304,12 +304,14 @@ __global__ void __launch_bounds__(kRowThreads, (kResident<X, Y, V, E>)) grad_row
         }
     __syncthreads();
     float* left = a.partial != nullptr ? a.partial + (uint64_t)(blockIdx.x / ctas) * 2 * a.dim + first_column : totals;
-    if (columns >= blockDim.x) {
+    if constexpr (SPLIT) {                              // (one group)
+        for (uint32_t i = threadIdx.x; i < columns; i += blockDim.x) left[i < dim ? i : a.dim + i - dim] = all[i];
+    } else if (columns >= blockDim.x) {
         for (uint32_t i = threadIdx.x; i < columns; i += blockDim.x) {
             const float* from = all + (i < dim ? i : groups * dim + i - dim);
             double total = (double)from[0];
             for (uint32_t g = 1; g < groups; ++g) total += (double)from[g * dim];
-            left[SPLIT && i >= dim ? a.dim + i - dim : i] = (float)total;
+            left[i] = (float)total;
         }
     } else {
         const uint32_t stripes = blockDim.x / columns, stripe = threadIdx.x / columns, column = threadIdx.x - stripe * columns;
