@@ -257,6 +257,13 @@ __global__ void __launch_bounds__(kRowThreads, (kResident<X, Y, V, E>)) grad_row
                 vd[e] = g.x;
                 vd[e + 1] = g.y;
             }
+            // (places without elements have x = dy = 0, and so h = -mu r: where that is infinite, its product with zero is left out)
+            if (!FULL && !(fabsf(stats.x * stats.y) < INFINITY)) {
+                along = make_float2(0.0f, 0.0f);
+#pragma unroll
+                for (int e = 0; e < E; ++e)
+                    if (at.has(e / V)) along.x = fmaf(vd[e], vx[e], along.x);
+            }
         }
         if (a.dx == nullptr) continue;
         float2 both = row_sums.two(make_float2(sum.x + sum.y, along.x + along.y), threads, group, turn);
