@@ -434,20 +434,17 @@ __global__ void __launch_bounds__(kColumnLanes* kStripes) columns_kernel(const G
 #pragma unroll
     for (int e = 0; e < C * V; ++e) sums[stripe][e][lane] = sum[e];
     __syncthreads();
-    if (stripe != 0) return;
+    static_assert(C * V <= kStripes, "a warp to each of a lane's columns");
+    if (stripe >= C * V || !has(stripe / V)) return;
+    double dw = 0.0, db = 0.0;
 #pragma unroll
-    for (int e = 0; e < C * V; ++e) {
-        if (!has(e / V)) continue;
-        double dw = (double)sum[e].x, db = (double)sum[e].y;
-#pragma unroll
-        for (int k = 1; k < kStripes; ++k) {
-            dw += (double)sums[k][e][lane].x;
-            db += (double)sums[k][e][lane].y;
-        }
-        const uint64_t i = col + e / V * kColumnLanes * V + e % V;
-        a.partial[(blockIdx.y * 2ull + 0) * a.dim + i] = (float)dw;
-        a.partial[(blockIdx.y * 2ull + 1) * a.dim + i] = (float)db;
+    for (int k = 0; k < kStripes; ++k) {
+        dw += (double)sums[k][stripe][lane].x;
+        db += (double)sums[k][stripe][lane].y;
     }
+    const uint64_t i = col + stripe / V * kColumnLanes * V + stripe % V;
+    a.partial[(blockIdx.y * 2ull + 0) * a.dim + i] = (float)dw;
+    a.partial[(blockIdx.y * 2ull + 1) * a.dim + i] = (float)db;
 }
 
 // The parts' sums, in 64 bits: stripes of the parts side by side, then the stripes in order.
