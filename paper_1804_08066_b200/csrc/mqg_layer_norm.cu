@@ -187,13 +187,15 @@ template <int X, int Y, int V, int E, bool WIDE, bool FULL> cudaError_t launch_g
 template <int X, int Y, int V, int E> cudaError_t launch_elements(const NormArgs& a, cudaStream_t stream)
 {
     const RowGroups g = row_groups(a.rows, a.dim, E, kResident<E> * kRowThreads);
-    if constexpr (V > 1) {
-        if (a.dim == (uint64_t)g.threads * E)
-            return g.threads < 32 ? launch_groups<X, Y, V, E, false, true>(a, g, stream) : launch_groups<X, Y, V, E, true, true>(a, g, stream);
-    }
-    if constexpr (V > 1 || E <= 8) {
-        if (g.threads < 32) return launch_groups<X, Y, V, E, false, false>(a, g, stream);
-    }
+    const bool full = V > 1 && a.dim == (uint64_t)g.threads * E;
+    if constexpr (V > 1 ? E < 32 : E <= 8)              // (rows that 32 elements to a thread are chosen for take whole warps)
+        if (g.threads < 32) {
+            if constexpr (V > 1)
+                if (full) return launch_groups<X, Y, V, E, false, true>(a, g, stream);
+            return launch_groups<X, Y, V, E, false, false>(a, g, stream);
+        }
+    if constexpr (V > 1)
+        if (full) return launch_groups<X, Y, V, E, true, true>(a, g, stream);
     return launch_groups<X, Y, V, E, true, false>(a, g, stream);
 }
 

@@ -536,14 +536,15 @@ template <int X, int Y, int V, int E> cudaError_t launch_elements(GradArgs a, in
         a.partial = nullptr;
         *parts = 0;
     }
-    if constexpr (V > 1) {
-        if (a.dim == (uint64_t)g.threads * E)
-            return g.threads < 32 ? launch_groups<X, Y, V, E, false, true>(a, g, cluster, sums, stream)
-                                  : launch_groups<X, Y, V, E, true, true>(a, g, cluster, sums, stream);
-    }
-    if constexpr (V > 1 || E <= 8) {
-        if (g.threads < 32) return launch_groups<X, Y, V, E, false, false>(a, g, cluster, sums, stream);
-    }
+    const bool full = V > 1 && a.dim == (uint64_t)g.threads * E;
+    if constexpr (V > 1 ? E < 32 : E <= 8)              // (rows that 32 elements to a thread are chosen for take whole warps)
+        if (g.threads < 32) {
+            if constexpr (V > 1 && !(E == 16 && X == kF32 && Y == kF32))        // (16 in fp32: where 8 leave threads of such groups idle)
+                if (full) return launch_groups<X, Y, V, E, false, true>(a, g, cluster, sums, stream);
+            return launch_groups<X, Y, V, E, false, false>(a, g, cluster, sums, stream);
+        }
+    if constexpr (V > 1)
+        if (full) return launch_groups<X, Y, V, E, true, true>(a, g, cluster, sums, stream);
     return launch_groups<X, Y, V, E, true, false>(a, g, cluster, sums, stream);
 }
 
