@@ -264,7 +264,6 @@ __device__ __forceinline__ void encode4(const float* m, const float* v, float in
             const uint32_t bits_m = add_draw(h, i ? 16u << 8 : 16u, __float_as_uint(i ? x.y : x.x));   // (27 bits below the sign)
             const uint32_t bits_v = add_draw(turned, i ? 32u << 8 : 32u, __float_as_uint(i ? y.y : y.x));
             at_top_m[j + i] = __float_as_uint(m[j + i]) & 0x80000000u | bits_m * 16u + 8u * 16u & 0x7FFFFFFFu;
-            // (shifted before the maximum, the code of every second element came out three bits too low, with nvcc 12.9)
             at_top_v[j + i] = max(bits_v + 16u, min(__float_as_uint(v[j + i]), least)) * 8u;
         }
     }
