@@ -53,9 +53,9 @@ template <int CAP, bool EIGHT> struct AdamwTable {
 };
 template <bool EIGHT> constexpr int kLargeTable = EIGHT ? 448 : 640;
 
-// Turns of a warp, where there are blocks for four times the warps that the device holds.  (100 M elements with states in 8 bits by 2 / 4 / 8 /
-// 16 turns: 263 / 251 / 257 / 267 us.)
-constexpr uint32_t kTurns = 4, kManyBlocks = 148 * 4 * kWarps * 4;
+// Turns of a warp, where there are more than 128 blocks to an SM, five to each of the 24 warps that it holds.  (100 M elements with states in
+// 8 bits by 2 / 4 / 8 / 16 turns: 263 / 251 / 257 / 267 us.)
+constexpr uint32_t kTurns = 4, kManyBlocks = 148 * 128;
 
 struct Scalars {
     float b1, w1, b2, w2, eps, lr, a, r2, grad_scale, minus_zero;
