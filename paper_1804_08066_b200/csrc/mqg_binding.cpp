@@ -134,8 +134,17 @@ mqg_dtype grad_dtype(PyObject* o)
     throw PythonError();
 }
 
+// The items of a list, a tuple or any iterable, which live as long as what is returned: a list could be changed by another thread while
+// the call runs without the interpreter lock.
+PyObject* hold_items(PyObject* o, const char* expected)
+{
+    PyObject* items = PyList_CheckExact(o) ? PyList_AsTuple(o) : PySequence_Fast(o, expected);
+    if (!items) throw PythonError();
+    return items;
+}
+
 // A list (or tuple, or any iterable) of W tensors as a table of device pointers.  Everything that is wanted of the
-// items is read at once: later arguments may run Python code that changes the list.
+// items is read at once: later arguments may run Python code that changes the list.  They live as long as this.
 struct PointerTable {
     void* ptr[MQG_MAX_WORKERS];
     PyObject* items = nullptr;
@@ -145,8 +154,7 @@ struct PointerTable {
     // `exact`: the list has to hold exactly W tensors; otherwise at least W.
     void read(PyObject* o, const char* what, int W, bool exact)
     {
-        items = PySequence_Fast(o, "a list of tensors is expected");
-        if (!items) throw PythonError();
+        items = hold_items(o, "a list of tensors is expected");
         count = PySequence_Fast_GET_SIZE(items);
         // a worker count outside the library's range is the C ABI's to reject: it reads no table then
         if (exact ? count != W : count < W && W <= MQG_MAX_WORKERS) {
@@ -621,8 +629,8 @@ uint64_t area(uint64_t a, uint64_t b)
 }
 
 // A list (or tuple, or any iterable) of gradient tensors of any sizes.  Everything that is wanted of the items is read at once,
-// and no Python code runs meanwhile.  The items live as long as this: tensors that an iterable made for the call alone are
-// not freed before the launch.
+// and no Python code runs meanwhile.  The items live as long as this: tensors that an iterable made for the call alone, or that
+// another thread takes out of the list, are not freed before the launch.
 struct TensorTable {
     static constexpr size_t kInline = 64;
     void* inline_ptr[kInline];
@@ -638,8 +646,7 @@ struct TensorTable {
 
     void read(PyObject* o, Operands& on)
     {
-        items.object = PySequence_Fast(o, "a list of tensors is expected");
-        if (!items.object) throw PythonError();
+        items.object = hold_items(o, "a list of tensors is expected");
         n = (size_t)PySequence_Fast_GET_SIZE(items.object);
         if (n > kInline) {
             store.resize(n * (sizeof(void*) + sizeof(uint64_t) + sizeof(mqg_dtype)));
@@ -802,10 +809,7 @@ struct AdamwLists {
 
     AdamwLists(PyObject* const* lists, int count, PyObject* decays, PyObject* factor, PyObject* schedule) : nlists(count)
     {
-        for (int k = 0; k < count; ++k) {
-            items[k].object = PySequence_Fast(lists[k], "lists of tensors are expected");
-            if (!items[k].object) throw PythonError();
-        }
+        for (int k = 0; k < count; ++k) items[k].object = hold_items(lists[k], "lists of tensors are expected");
         n = (size_t)PySequence_Fast_GET_SIZE(items[0].object);
         const bool several = !absent(decays) && (PySequence_Check(decays) || PyIter_Check(decays)), one = !absent(decays) && !several;
         const Reference numbers = {several ? PySequence_Tuple(decays) : nullptr};
