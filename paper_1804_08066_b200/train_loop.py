@@ -186,6 +186,8 @@ LEARNING_RATES = {"sgd": 0.05, "adamw": 2e-3, "adamw8": 2e-3}
 
 def run(iters=60, workers=4, batch=128, lr=None, selector="window", seed=0, model="cnn", clip=None, clip_at="worker", norm=False,
         optimizer="sgd"):
+    if norm and model != "tokens":
+        raise ValueError("norm: only the model over tokens has rows to normalise")
     lr = LEARNING_RATES[optimizer] if lr is None else lr
     torch.manual_seed(seed)
     kind, model = model, (SmallCnn() if model == "cnn" else TokenClassifier(norm)).cuda()
@@ -274,5 +276,7 @@ if __name__ == "__main__":
     ap.add_argument("--optimizer", default="sgd", choices=["sgd", "adamw", "adamw8"])
     ap.add_argument("--lr", type=float, default=None)
     a = ap.parse_args()
+    if a.norm and a.model != "tokens":
+        ap.error("--norm needs --model tokens")
     print(json.dumps(run(a.iters, a.workers, lr=a.lr, selector=a.selector, model=a.model, clip=a.clip, clip_at=a.clip_at, norm=a.norm,
                          optimizer=a.optimizer)))
