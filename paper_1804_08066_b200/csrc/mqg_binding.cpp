@@ -14,6 +14,7 @@
 
 #include <algorithm>
 #include <cstring>
+#include <memory>
 #include <vector>
 
 #include "../../include/mqgrad.h"
@@ -134,19 +135,26 @@ mqg_dtype grad_dtype(PyObject* o)
     throw PythonError();
 }
 
-// The items of a list, a tuple or any iterable, which live as long as what is returned: a list could be changed by another thread while
-// the call runs without the interpreter lock.
-PyObject* hold_items(PyObject* o, const char* expected)
-{
-    PyObject* items = PyList_CheckExact(o) ? PyList_AsTuple(o) : PySequence_Fast(o, expected);
-    if (!items) throw PythonError();
-    return items;
-}
+// Tensors of a list that live as long as this: while the call runs without the interpreter lock, another thread could take them out of
+// the list.
+struct HeldItems {
+    PyObject** at;                                      // room for them
+    size_t count = 0;
+    void hold(PyObject* o) { at[count++] = Py_NewRef(o); }
+    explicit HeldItems(PyObject** room = nullptr) : at(room) {}
+    HeldItems(const HeldItems&) = delete;
+    ~HeldItems()
+    {
+        while (count != 0) Py_DECREF(at[--count]);
+    }
+};
 
 // A list (or tuple, or any iterable) of W tensors as a table of device pointers.  Everything that is wanted of the
 // items is read at once: later arguments may run Python code that changes the list.  They live as long as this.
 struct PointerTable {
     void* ptr[MQG_MAX_WORKERS];
+    PyObject* item[MQG_MAX_WORKERS];
+    HeldItems kept{item};
     PyObject* items = nullptr;
     Py_ssize_t count = 0;
     ~PointerTable() { Py_XDECREF(items); }
@@ -154,7 +162,8 @@ struct PointerTable {
     // `exact`: the list has to hold exactly W tensors; otherwise at least W.
     void read(PyObject* o, const char* what, int W, bool exact)
     {
-        items = hold_items(o, "a list of tensors is expected");
+        items = PySequence_Fast(o, "a list of tensors is expected");
+        if (!items) throw PythonError();
         count = PySequence_Fast_GET_SIZE(items);
         // a worker count outside the library's range is the C ABI's to reject: it reads no table then
         if (exact ? count != W : count < W && W <= MQG_MAX_WORKERS) {
@@ -162,7 +171,10 @@ struct PointerTable {
             throw PythonError();
         }
         const Py_ssize_t n = count < MQG_MAX_WORKERS ? count : MQG_MAX_WORKERS;
-        for (Py_ssize_t i = 0; i < n; ++i) ptr[i] = device_ptr(PySequence_Fast_GET_ITEM(items, i), what, i);
+        for (Py_ssize_t i = 0; i < n; ++i) {
+            ptr[i] = device_ptr(PySequence_Fast_GET_ITEM(items, i), what, i);
+            kept.hold(PySequence_Fast_GET_ITEM(items, i));
+        }
     }
     template <typename T> T* const* as() const { return reinterpret_cast<T* const*>(ptr); }
 };
@@ -636,7 +648,9 @@ struct TensorTable {
     void* inline_ptr[kInline];
     uint64_t inline_size[kInline];
     mqg_dtype inline_dtype[kInline];
-    std::vector<char> store;
+    PyObject* inline_item[kInline];
+    std::unique_ptr<char[]> store;                      // (not filled with zeros first)
+    HeldItems kept{inline_item};
     void** ptr = inline_ptr;
     uint64_t* size = inline_size;
     mqg_dtype* dtype = inline_dtype;
@@ -646,18 +660,21 @@ struct TensorTable {
 
     void read(PyObject* o, Operands& on)
     {
-        items.object = hold_items(o, "a list of tensors is expected");
+        items.object = PySequence_Fast(o, "a list of tensors is expected");
+        if (!items.object) throw PythonError();
         n = (size_t)PySequence_Fast_GET_SIZE(items.object);
         if (n > kInline) {
-            store.resize(n * (sizeof(void*) + sizeof(uint64_t) + sizeof(mqg_dtype)));
-            ptr = reinterpret_cast<void**>(store.data());
-            size = reinterpret_cast<uint64_t*>(ptr + n);
+            store.reset(new char[n * (2 * sizeof(void*) + sizeof(uint64_t) + sizeof(mqg_dtype))]);
+            ptr = reinterpret_cast<void**>(store.get());
+            kept.at = reinterpret_cast<PyObject**>(ptr + n);
+            size = reinterpret_cast<uint64_t*>(kept.at + n);
             dtype = reinterpret_cast<mqg_dtype*>(size + n);
         }
         PyObject** item = PySequence_Fast_ITEMS(items.object);
         for (size_t i = 0; i < n; ++i) {
             ptr[i] = on.values(item[i], "grads", 0, &dtype[i], (Py_ssize_t)i, &size[i]);
             total += size[i];
+            kept.hold(item[i]);
         }
     }
     const char* end(size_t i) const { return static_cast<const char*>(ptr[i]) + size[i] * (dtype[i] == MQG_F32 ? 4 : 2); }
@@ -796,8 +813,10 @@ struct AdamwLists {
     Reference items[kMost] = {};
     int nlists = 0;
     size_t n = 0;
-    std::vector<char> store;
-    alignas(8) char inline_store[kInline * (kMost * sizeof(void*) + sizeof(uint64_t) + 2 * sizeof(mqg_dtype) + sizeof(float))];
+    std::unique_ptr<char[]> store;                      // (not filled with zeros first)
+    static constexpr size_t kPer = 2 * kMost * sizeof(void*) + sizeof(uint64_t) + 2 * sizeof(mqg_dtype) + sizeof(float);
+    alignas(8) char inline_store[kInline * kPer];
+    HeldItems kept;
     void** ptr[kMost];
     uint64_t* size;
     mqg_dtype* dtype[2];
@@ -809,18 +828,21 @@ struct AdamwLists {
 
     AdamwLists(PyObject* const* lists, int count, PyObject* decays, PyObject* factor, PyObject* schedule) : nlists(count)
     {
-        for (int k = 0; k < count; ++k) items[k].object = hold_items(lists[k], "lists of tensors are expected");
+        for (int k = 0; k < count; ++k) {
+            items[k].object = PySequence_Fast(lists[k], "lists of tensors are expected");
+            if (!items[k].object) throw PythonError();
+        }
         n = (size_t)PySequence_Fast_GET_SIZE(items[0].object);
         const bool several = !absent(decays) && (PySequence_Check(decays) || PyIter_Check(decays)), one = !absent(decays) && !several;
         const Reference numbers = {several ? PySequence_Tuple(decays) : nullptr};
         if (several && !numbers.object) throw PythonError();
         const double all = one ? to_double(decays) : 0.0;
         has_decay = !absent(decays);
-        const size_t per = kMost * sizeof(void*) + sizeof(uint64_t) + 2 * sizeof(mqg_dtype) + sizeof(float);
-        if (n > kInline) store.resize(n * per);
-        char* at = n > kInline ? store.data() : inline_store;
+        if (n > kInline) store.reset(new char[n * kPer]);
+        char* at = n > kInline ? store.get() : inline_store;
         for (int k = 0; k < kMost; ++k, at += n * sizeof(void*)) ptr[k] = reinterpret_cast<void**>(at);
-        size = reinterpret_cast<uint64_t*>(at);
+        kept.at = reinterpret_cast<PyObject**>(at);
+        size = reinterpret_cast<uint64_t*>(at + kMost * n * sizeof(void*));
         dtype[0] = reinterpret_cast<mqg_dtype*>(size + n);
         dtype[1] = dtype[0] + n;
         decay = reinterpret_cast<float*>(dtype[1] + n);
@@ -835,10 +857,11 @@ struct AdamwLists {
                 PyErr_Format(PyExc_ValueError, "%s holds %zd tensors, params %zu", name(k), PySequence_Fast_GET_SIZE(items[k].object), n);
                 throw PythonError();
             }
-        for (int k = 0; k < count; ++k) {
-            PyObject** item = PySequence_Fast_ITEMS(items[k].object);
-            for (size_t j = 0; j < n; ++j) read(k, j, item[j]);
-        }
+        read_list<0>();
+        read_list<1>();
+        read_list<2>();
+        read_list<3>();
+        if (count == kMost) read_list<4>();
         this->factor = absent(factor) ? nullptr : on.floats(factor, "factor", 1);
         this->schedule = absent(schedule) ? nullptr : on.floats(schedule, "schedule", 4);
     }
@@ -846,7 +869,11 @@ struct AdamwLists {
 
     const float *factor, *schedule;
 
-    static const char* name(int k) { return (const char* const[]){"params", "grads", "m", "v", "scales"}[k]; }
+    static const char* name(int k)
+    {
+        static constexpr const char* kNames[kMost] = {"params", "grads", "m", "v", "scales"};
+        return kNames[k];
+    }
 
     // A tensor's address.  Of tensors one after the other that are slices of one vector, only the first one's is asked for, which takes
     // as long as everything else that is wanted of a tensor.
@@ -862,12 +889,21 @@ struct AdamwLists {
         }
         return p;
     }
-    void read(int k, size_t j, PyObject* o)
+    // (a template: what differs from list to list is not asked for every tensor, which makes up for half of what holding it costs)
+    template <int k> void read_list()
+    {
+        PyObject** item = PySequence_Fast_ITEMS(items[k].object);
+        for (size_t j = 0; j < n; ++j) {
+            read<k>(j, item[j]);
+            kept.hold(item[j]);
+        }
+    }
+    template <int k> void read(size_t j, PyObject* o)
     {
         const at::Tensor& t = on.tensor(o, name(k), 0, (Py_ssize_t)j);
         const at::ScalarType s = t.scalar_type();
         const uint64_t held = (uint64_t)t.numel();
-        if (k < 2) {
+        if constexpr (k < 2) {
             if (s != at::kFloat && s != at::kBFloat16) wrong_type(k, j, "float32 or bfloat16", s);
             dtype[k][j] = s == at::kFloat ? MQG_F32 : MQG_BF16;
             if (k == 0) size[j] = held;
