@@ -476,11 +476,11 @@ mqg_status mqg_adamw(void* const* params, const mqg_dtype* param_dtypes, const v
  *           (codes that are infinities or NaN in these formats are that)
  *   scales  [in/out] HOST array of pointers to mqg_adamw8_scale_floats(size) floats per tensor (two to a block), 4-byte aligned
  * All three are zeros before the first step.  The parameter's step is computed from m and v before they are rounded.  Then
- * scales[2 b] = max|m| / 448, scales[2 b + 1] = max v / 57344 of the block (0, and all its codes 0, where that maximum is below
- * 2^-110), and m * (448 / max|m|), v * (57344 / max v) are rounded to one of their two neighbours at random, up where the share
- * above the lower neighbour plus (h + 1/2) / 2^16 reaches 1: without bias, while rounding to nearest would not move an average whose
- * steps are small beside the distance of two codes.  A v of 2^-128 or more never
- * gets code 0.
+ * scales[2 b] = max|m| / 448, scales[2 b + 1] = max v / 57344 of the block, and m * (448 / max|m|), v * (57344 / max v) are rounded to
+ * one of their two neighbours at random, up where the share above the lower neighbour plus (h + 1/2) / 2^16 reaches 1: without
+ * bias, while rounding to nearest would not move an average whose steps are small beside the distance of two codes.  Only a v of
+ * 2^-128 or more that would get code 0 gets code 1 instead.  Where that maximum is below 2^-110, the scale is 0 and the codes are
+ * zeros (m's of the sign of m); where it is infinite or a NaN, the scale is that, and the block's values are infinite or NaN.
  *   seed    keys the draws: h has 16 bits of the Philox4x32-10 block with key = seed and counter = (q, 0xFFFFFFFF, step).  q = 32 B +
  *           l, B = blocks before this one in the whole list of the call, draws for the block's elements 4 l .. 4 l + 3 (words 0
  *           and 1, low half first) and 128 + 4 l .. 128 + 4 l + 3 (words 2 and 3); v takes h with its two bytes swapped.  The
