@@ -501,7 +501,7 @@ mqg_status mqg_adamw8(void* const* params, const mqg_dtype* param_dtypes, const 
  *   x             [in] rows x dim elements, row after row;  y [out] the same, of y_dtype
  *   weight, bias  [in] dim elements of weight_dtype each; NULL = ones, zeros
  *   stats         [out] NULL, or 2 floats to a row: mu, r, as the gradient takes them
- *   eps           above 0.  The rows' deviations and their squares' mean must be in fp32's range.
+ *   eps           above 0.  The rows' sums, their deviations and their squares' sum must be in fp32's range.
  * All buffers need their types' own alignment only; rows whose bytes are a multiple of 16 on 16-byte boundaries are fastest.  What
  * is written must not share memory with anything else (MQG_ERR_INVALID).  A row without elements, or no rows: nothing is done.
  * Errors: MQG_ERR_INVALID (null pointers, unknown types, eps; rows above 2^31 - 1, dim above 2^22), MQG_ERR_ALIGN.

@@ -137,7 +137,7 @@ __global__ void __launch_bounds__(kRowThreads, (kResident<X, Y, V, E>)) grad_row
     const auto* dy = static_cast<const typename Element<Y>::type*>(a.dy) + first_column;
     auto* dx = static_cast<typename Element<X>::type*>(a.dx) + first_column;
     // Where this thread's elements of the row are that is fetched next, and of the one that is written next: kept where registers are
-    // left for it (65,536 rows of 4096 in bf16 at the power limit: 284 us, 303 with two products for every row).
+    // left for it (65,536 rows of 4096 in bf16 at the power limit: 7 % longer with two products for every row).
     constexpr bool kKept = R::kAsync && E > 8;
     const uint64_t row_step = stride * a.dim, from = first_row * a.dim + at.element(0);
     const auto* next_of_x = x + from;
@@ -574,10 +574,10 @@ template <int X, int Y, int V> cudaError_t launch_split(const GradArgs& a, int s
     return launch_clusters(kernel, *parts * kSplitCtas, kSplitCtas, threads, kBytes, stream, a, threads, sums);
 }
 
-// Elements to a thread.  More of them cost fewer shuffles and barriers to a row: with 8 / 16 65,536 rows of 4096 in bf16 take 326 / 270 us,
-// 16,384 of 1024 27.7 / 24.0, but 64 of 4096 7.6 / 9.5; 4096 of 4096 in fp32 39.3 / 40.3; a million rows of 16 27 / 40.  In fp32 16 where 8 leave
-// much of an SM's threads idle and 16 have as many rows on it: 24 million in rows of 264 61.5 / 51.4, of 2056 59.5 / 53.5, of 520 55.5 / 54.0, of 392
-// 52.2 / 52.1, of 904 51.5 / 52.5.
+// Elements to a thread.  More of them cost fewer shuffles and barriers to a row: 65,536 rows of 4096 in bf16 take a fifth longer with 8 than with
+// 16 (then 263 to 285 us at the power limit, 252 after an idle moment); with 8 / 16 16,384 of 1024 27.7 / 24.0, but 64 of 4096 7.6 / 9.5; 4096 of
+// 4096 in fp32 39.3 / 40.3; a million rows of 16 27 / 40.  In fp32 16 where 8 leave much of an SM's threads idle and 16 have as many rows on it:
+// 24 million in rows of 264 61.5 / 51.4, of 2056 59.5 / 53.5, of 520 55.5 / 54.0, of 392 52.2 / 52.1, of 904 51.5 / 52.5.
 // Single elements take 12 where that puts more rows on an SM: 24 million in rows of 515 with 8 / 12 in fp32 65.4 / 57.1, of 2050 75.4 / 57.7, of
 // 3201 (one row either way) 62.4 / 63.1; 16 where these are a warp's, and 12 are more: of 385 with 8 / 12 / 16 60.9 / 63.9 / 54.9.
 template <int X, int Y, int V> int elements_of(uint64_t rows, uint64_t dim)
