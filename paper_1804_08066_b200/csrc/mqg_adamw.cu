@@ -16,7 +16,7 @@
 // under the root.
 //
 // In 32 bits bound by memory, 28 bytes an element in fp32: 25 M elements in 106 us, 1.02 of the copy rate.  In 8 bits, 14 bytes with
-// bf16 gradients, by instructions, 60 an element: 100 M in 250 us after an idle moment (0.87 of the copy rate), 266 to 275 at the power
+// bf16 gradients, by instructions, 60 an element: 100 M in 250 us after an idle moment (0.87 of the copy rate), 264 to 275 at the power
 // limit.  A block's inputs come by way of shared memory while the one before is computed, which took 288 us to 267.
 #include <cuda_fp16.h>
 

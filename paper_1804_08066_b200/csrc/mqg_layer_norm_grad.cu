@@ -575,7 +575,7 @@ template <int X, int Y, int V> cudaError_t launch_split(const GradArgs& a, int s
 }
 
 // Elements to a thread.  More of them cost fewer shuffles and barriers to a row: 65,536 rows of 4096 in bf16 take a fifth longer with 8 than with
-// 16 (then 263 to 285 us at the power limit, 252 after an idle moment); with 8 / 16 16,384 of 1024 27.7 / 24.0, but 64 of 4096 7.6 / 9.5; 4096 of
+// 16 (then 260 to 285 us at the power limit, 252 after an idle moment); with 8 / 16 16,384 of 1024 27.7 / 24.0, but 64 of 4096 7.6 / 9.5; 4096 of
 // 4096 in fp32 39.3 / 40.3; a million rows of 16 27 / 40.  In fp32 16 where 8 leave much of an SM's threads idle and 16 have as many rows on it:
 // 24 million in rows of 264 61.5 / 51.4, of 2056 59.5 / 53.5, of 520 55.5 / 54.0, of 392 52.2 / 52.1, of 904 51.5 / 52.5.
 // Single elements take 12 where that puts more rows on an SM: 24 million in rows of 515 with 8 / 12 in fp32 65.4 / 57.1, of 2050 75.4 / 57.7, of
